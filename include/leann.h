@@ -36,7 +36,7 @@ enum {
     LEANN_ECAPACITY = -5  /* a per-query queue outgrew its capacity */
 };
 
-enum { LEANN_F32 = 0, LEANN_BF16 = 1 };
+enum { LEANN_F32 = 0, LEANN_BF16 = 1, LEANN_F16 = 2 };
 
 typedef struct leann_ctx leann_ctx;
 typedef struct leann_pq leann_pq;
@@ -337,6 +337,53 @@ int leann_bench_gather(leann_ctx *ctx, const uint8_t *table_dev, int64_t table_r
  * bytes_per_s_host receives the rate over `launches` timed launches after one warm-up launch.  Synchronises.
  */
 int leann_bench_l1pull(leann_ctx *ctx, int64_t panel_rows, int32_t launches, double *bytes_per_s_host, double *ms_host);
+
+/*
+ * Operators for adapting an encoder to a collection: dropout, LayerNorm with its gradient, and projections with low-rank
+ * adapters.  They need a context for its device, stream and workspaces only (an encoder of no layers is enough).  What
+ * holds for all of them:
+ *   - Matrices are rows of unit stride, `ld` elements apart (ld >= the row's length; rows need no alignment unless a call
+ *     says so).  Element offsets are 64-bit.
+ *   - Everything is enqueued on the context's stream and nothing synchronises, except that a workspace which has to grow is
+ *     allocated in the call; a buffer that another stream writes or reads has to be ordered with it by the caller.
+ *   - Sums and statistics are fp32; every output is rounded once, to nearest.  No atomics: the bits repeat from call to call.
+ *   - Zero rows are no error.  leann_profile_begin does not bracket their kernels.
+ */
+
+/* Dropout: element (row, col) of a matrix is dropped where 16 bits, a function of seed, offset, row and col, are below
+ * rint(p * 65536); what stays is multiplied by 65536 / (65536 - rint(p * 65536)).  The bits are halves of the words of
+ * Philox4x32-10 under the key `seed` (low word first) and the counter (col / 8, row, offset low, offset high): half
+ * number col % 8, the low half of a word first.  No mask is stored: the gradient takes the same seed and offset. */
+typedef struct {
+    float p; /* in [0, 1] */
+    uint64_t seed, offset;
+} leann_dropout_desc;
+
+/* out = dropout(x) (+ residual, NULL for none); the gradient with respect to x is the same call on the gradient of out,
+ * without a residual.  Dropped infinities and NaN are 0.  x, residual and out have the type `dtype` (LEANN_F32, LEANN_BF16 or
+ * LEANN_F16); out may be x or residual itself.
+ * Errors: p outside [0, 1], null pointers, negative row count -> LEANN_EINVAL; ld < cols, 2^31 rows or columns -> LEANN_ESHAPE. */
+int leann_dropout(leann_ctx *ctx, const void *x_dev, int64_t ldx, const void *residual_dev, int64_t ldr, int64_t rows, int64_t cols, int dtype,
+                  const leann_dropout_desc *drop, void *out_dev, int64_t ldo);
+
+/* t = dropout(x) (+ residual); out = (t - mean(t)) / sqrt(var(t) + eps) * gamma + beta over each row, biased variance.
+ * drop and residual may be NULL.  For a backward pass total_dev (may be NULL) receives t rounded to dtype, mean_dev and
+ * rstd_dev (both or neither; fp32[rows]) the statistics, taken before that rounding.  gamma, beta: fp32[cols].  out may be x or residual
+ * itself, total may be the other one.
+ * Errors: as leann_dropout; eps not positive -> LEANN_EINVAL; more than 8192 columns -> LEANN_ESHAPE. */
+int leann_layernorm(leann_ctx *ctx, const void *x_dev, int64_t ldx, const void *residual_dev, int64_t ldr, int64_t rows, int32_t cols, int dtype,
+                    const leann_dropout_desc *drop, const float *gamma_dev, const float *beta_dev, float eps, void *out_dev, int64_t ldo,
+                    void *total_dev, int64_t ldt, float *mean_dev, float *rstd_dev);
+
+/* Gradients of leann_layernorm from dout, the gradient of out.  total is t (x itself where there was neither dropout nor a
+ * residual).  dtotal (NULL for none) is what reaches t besides, where t is used elsewhere, too (pre-LN blocks).
+ *   dresidual = gradient of t, which is the residual's; dx = dropout's gradient of it (drop as in the forward call; without
+ *   dropout dx is dresidual and dx_dev is not used); dgamma, dbeta: fp32[cols], the sums over the rows (written, not added to).
+ * dresidual and dx may be dout or dtotal itself.  Errors: as leann_layernorm. */
+int leann_layernorm_backward(leann_ctx *ctx, const void *dout_dev, int64_t ldd, const void *total_dev, int64_t ldt, int64_t rows, int32_t cols,
+                             int dtype, const float *gamma_dev, const float *mean_dev, const float *rstd_dev, const void *dtotal_dev, int64_t lde,
+                             const leann_dropout_desc *drop, void *dresidual_dev, int64_t ldr, void *dx_dev, int64_t ldx, float *dgamma_dev,
+                             float *dbeta_dev);
 
 #ifdef __cplusplus
 }

@@ -15,13 +15,14 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libleann.so")
 _lib = None
 
-LEANN_F32, LEANN_BF16 = 0, 1
+LEANN_F32, LEANN_BF16, LEANN_F16 = 0, 1, 2
 STATUS = {0: "LEANN_OK", -1: "LEANN_EINVAL", -2: "LEANN_ENOMEM", -3: "LEANN_EDEVICE", -4: "LEANN_ESHAPE",
           -5: "LEANN_ECAPACITY"}
 EXPORTS = ["leann_last_error", "leann_create", "leann_destroy", "leann_embed", "leann_build_pq", "leann_pq_export",
            "leann_pq_import", "leann_pq_wrap", "leann_pq_info", "leann_pq_free", "leann_adc", "leann_adc_noalloc", "leann_search",
            "leann_search_updates", "leann_build_graph", "leann_top_degree",
-           "leann_set_limits", "leann_set_call_memo", "leann_set_gemm_tiles", "leann_profile_begin", "leann_profile_end", "leann_bench_mfma", "leann_bench_gather", "leann_bench_l1pull"]
+           "leann_set_limits", "leann_set_call_memo", "leann_set_gemm_tiles", "leann_profile_begin", "leann_profile_end", "leann_bench_mfma", "leann_bench_gather", "leann_bench_l1pull",
+           "leann_dropout", "leann_layernorm", "leann_layernorm_backward"]
 PROF_KINDS = ["gemm_qkv", "gemm_o", "gemm_ffn1", "gemm_ffn2", "attention", "layernorm", "enc_other", "traverse",
               "collect", "score_insert", "lut", "adc"]
 
@@ -78,6 +79,12 @@ def load_library(path=LIB_PATH):
             getattr(lib, name)
         lib.leann_destroy.restype = None
         lib.leann_pq_free.restype = None
+        V, I, N, F = C.c_void_p, C.c_int32, C.c_int64, C.c_float
+        for name, args in {  # argument types: plain numbers are converted by ctypes, which small calls are faster with
+                "leann_dropout": [V, V, N, V, N, N, N, I, V, V, N],
+                "leann_layernorm": [V, V, N, V, N, N, I, I, V, V, V, F, V, N, V, N, V, V],
+                "leann_layernorm_backward": [V, V, N, V, N, N, I, I, V, V, V, V, N, V, V, N, V, N, V, V]}.items():
+            getattr(lib, name).argtypes = args
         _lib = lib
     return _lib
 
@@ -346,3 +353,79 @@ def leann_bench_l1pull(ctx, panel_rows, launches=5):
     bps, ms = C.c_double(), C.c_double()
     _check(load_library().leann_bench_l1pull(ctx, C.c_int64(panel_rows), C.c_int32(launches), C.byref(bps), C.byref(ms)))
     return bps.value, ms.value
+
+
+# ---- operators for adapting an encoder
+class DropoutDesc(C.Structure):
+    _fields_ = [("p", C.c_float), ("seed", C.c_uint64), ("offset", C.c_uint64)]
+
+
+_DTYPES = {torch.float32: LEANN_F32, torch.bfloat16: LEANN_BF16, torch.float16: LEANN_F16}
+
+
+def _rows(t, what, like=None):
+    """(pointer, distance of rows) of a 2-D CUDA tensor with unit column stride, (None, 0) for None."""
+    if t is None:
+        return None, 0
+    assert t.is_cuda and t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] <= 1), f"{what}: need a 2-D CUDA tensor with unit column stride"
+    assert like is None or (t.shape == like.shape and t.dtype == like.dtype), f"{what}: shape or type differs"
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _drop(drop):
+    return None if drop is None else C.byref(DropoutDesc(*drop))
+
+
+def _vector(t, n, what):
+    assert t.is_cuda and t.dtype == torch.float32 and t.is_contiguous() and t.numel() == n, f"{what}: need {n} contiguous float32 values"
+    return t.data_ptr()
+
+
+def _dtype(t):
+    assert t.dtype in _DTYPES, "need float32, bfloat16 or float16"
+    return _DTYPES[t.dtype]
+
+
+def leann_dropout(ctx, x, drop, residual=None, out=None):
+    """dropout(x) (+ residual) of a 2-D tensor; drop = (p, seed, offset).  The gradient is the same call on the gradient."""
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    (xp, ldx), (rp, ldr), (op, ldo) = _rows(x, "x"), _rows(residual, "residual", x), _rows(out, "out", x)
+    _check(load_library().leann_dropout(ctx, xp, ldx, rp, ldr, x.shape[0], x.shape[1], _dtype(x), _drop(drop), op, ldo))
+    return out
+
+
+def leann_layernorm(ctx, x, gamma, beta, eps, residual=None, drop=None, keep=False, out=None):
+    """LayerNorm of dropout(x) (+ residual) over the rows of a 2-D tensor; drop = (p, seed, offset) or None.
+    keep: returns (out, total, mean, rstd), what the backward pass needs (total is x where it would hold the same); else out."""
+    rows, cols = x.shape
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    total = mean = rstd = None
+    if keep:
+        if residual is not None or drop is not None:
+            total = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=x.device)
+    (xp, ldx), (rp, ldr), (op, ldo), (tp, ldt) = (_rows(x, "x"), _rows(residual, "residual", x), _rows(out, "out", x),
+                                                  _rows(total, "total", x))
+    _check(load_library().leann_layernorm(ctx, xp, ldx, rp, ldr, rows, cols, _dtype(x), _drop(drop), _vector(gamma, cols, "gamma"),
+                                          _vector(beta, cols, "beta"), eps, op, ldo, tp, ldt,
+                                          mean.data_ptr() if keep else None, rstd.data_ptr() if keep else None))
+    return (out, x if total is None else total, mean, rstd) if keep else out
+
+
+def leann_layernorm_backward(ctx, dout, total, mean, rstd, gamma, drop=None, dtotal=None):
+    """(dresidual, dx, dgamma, dbeta) from the gradient of leann_layernorm's output and what it kept; dtotal: the gradient that
+    reaches the kept total besides.  Without dropout dx is dresidual."""
+    rows, cols = dout.shape
+    dres = torch.empty(dout.shape, dtype=dout.dtype, device=dout.device)
+    dx = dres if drop is None else torch.empty_like(dres)
+    dgamma, dbeta = torch.empty((2, cols), dtype=torch.float32, device=dout.device)
+    (dp, ldd), (tp, ldt), (ep, lde), (rp, ldr), (xp, ldx) = (_rows(dout, "dout"), _rows(total, "total", dout), _rows(dtotal, "dtotal", dout),
+                                                             _rows(dres, "dresidual"), _rows(dx, "dx"))
+    _check(load_library().leann_layernorm_backward(ctx, dp, ldd, tp, ldt, rows, cols, _dtype(dout), _vector(gamma, cols, "gamma"),
+                                                   _vector(mean, rows, "mean"), _vector(rstd, rows, "rstd"), ep, lde, _drop(drop), rp, ldr,
+                                                   xp, ldx, dgamma.data_ptr(), dbeta.data_ptr()))
+    if drop is not None and round(DropoutDesc(*drop).p * 65536) == 0:
+        dx = dres
+    return dres, dx, dgamma, dbeta

@@ -81,6 +81,7 @@ struct leann_ctx {
     int *host_flags = nullptr;           // pinned host memory: what kernels report, see clear_host_flags
     hipEvent_t pass_event = nullptr;     // recorded behind the kernel that counts an encoder pass's tokens
     double clock_khz = 1e5;              // of the kernels' wall_clock64()
+    DevBuf op_work;  // partial sums and intermediate matrices of the operators for adapting an encoder
     int64_t memo_rows = 0;  // rows of the per-call embedding memo (leann_set_call_memo), 0 = off
     // optional per-kernel timing (leann_profile_begin / leann_profile_end)
     bool prof_on = false;
