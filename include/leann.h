@@ -40,6 +40,8 @@ enum { LEANN_F32 = 0, LEANN_BF16 = 1, LEANN_F16 = 2 };
 
 typedef struct leann_ctx leann_ctx;
 typedef struct leann_pq leann_pq;
+typedef struct leann_projection leann_projection;
+typedef struct leann_adapter_rows leann_adapter_rows;
 
 /* Encoder shape.  The paper fixes a BERT-style encoder of 110 M parameters with
  * 768-d output over 256-token chunks (Sec. 7 set-up); the layer equations are the
@@ -384,6 +386,41 @@ int leann_layernorm_backward(leann_ctx *ctx, const void *dout_dev, int64_t ldd, 
                              int dtype, const float *gamma_dev, const float *mean_dev, const float *rstd_dev, const void *dtotal_dev, int64_t lde,
                              const leann_dropout_desc *drop, void *dresidual_dev, int64_t ldr, void *dx_dev, int64_t ldx, float *dgamma_dev,
                              float *dbeta_dev);
+
+/* Projections with low-rank adapters: out_t = W x_t + bias + scale_a up_a (down_a x_t), where a is the adapter of the request that
+ * row t belongs to: many requests, each with its own adapter or none, in one call beside the weight that all of them share.
+ * The adapters lie in two pools, down[n_adapters][max_rank][n_in] and up[n_adapters][n_out][max_rank], of which adapter a uses the
+ * first rank[a] ranks; what the pools hold beyond may be anything.  Activations, W and pools have one type, LEANN_BF16 or LEANN_F16, and
+ * 16-byte alignment (rows: a multiple of 8 elements apart). */
+
+/* The shared weight W[n_out][n_in] (rows without gaps) and bias fp32[n_out] (NULL for none), copied in the order that the kernels read; with_gradient: a
+ * second time, transposed, for leann_adapter_project_backward's dx.  W stays as it is for the handle's life (adapters are
+ * what is trained).  n_out and n_in: multiples of 8 up to 65536, else LEANN_ESHAPE.  Synchronises the stream. */
+int leann_projection_create(leann_ctx *ctx, const void *w_dev, const float *bias_dev, int32_t n_out, int32_t n_in, int dtype, int with_gradient,
+                            leann_projection **out);
+void leann_projection_free(leann_projection *proj);
+
+/* The rows of a batch: request i has the next rows_of_request[i] rows (0 is allowed) and adapter adapter_of_request[i], -1 for none.  rank[a] in
+ * [0, max_rank] and scale[a], finite, of the n_adapters (1 to 65535) adapters; max_rank: the pools' room, a multiple of 8 from 8 to 128.  Host arrays,
+ * copied.  One handle serves every projection that the batch goes through.  Synchronises the stream.
+ * Errors: a negative row count, adapter, rank or scale outside what is said here -> LEANN_EINVAL; 2^31 - 256 rows or more, max_rank,
+ * n_adapters -> LEANN_ESHAPE. */
+int leann_adapter_rows_create(leann_ctx *ctx, const int32_t *rows_of_request_host, const int32_t *adapter_of_request_host, int32_t n_requests,
+                              const int32_t *rank_host, const float *scale_host, int32_t n_adapters, int32_t max_rank, leann_adapter_rows **out);
+void leann_adapter_rows_free(leann_adapter_rows *rows);
+
+/* The forward pass over x[T][n_in], T the rows of the handle.  low_dev (NULL, or fp32[T][max_rank]) receives down_a x_t, which the backward pass
+ * needs; zeros beyond the adapter's rank and for rows without one.  out must not overlap x.  A row's values do not depend on other rows; its bits
+ * may depend on their number, as products of different sizes add up in different orders. */
+int leann_adapter_project(leann_ctx *ctx, const leann_projection *proj, const leann_adapter_rows *rows, const void *x_dev, int64_t ldx,
+                          const void *down_dev, const void *up_dev, void *out_dev, int64_t ldo, float *low_dev);
+
+/* Gradients from dout[T][n_out]: dx[T][n_in] = W^T dout + scale_a down_a^T (up_a^T dout) (NULL: not wanted; else the projection needs with_gradient), and
+ * ddown[n_adapters][max_rank][n_in], dup[n_adapters][n_out][max_rank] in fp32 (both or neither; written, not added to; zeros for adapters without
+ * rows and beyond their rank), which need x and the forward pass's low.  dx must not overlap dout or x. */
+int leann_adapter_project_backward(leann_ctx *ctx, const leann_projection *proj, const leann_adapter_rows *rows, const void *dout_dev, int64_t ldd,
+                                   const void *x_dev, int64_t ldx, const float *low_dev, const void *down_dev, const void *up_dev, void *dx_dev,
+                                   int64_t lddx, float *ddown_dev, float *dup_dev);
 
 #ifdef __cplusplus
 }

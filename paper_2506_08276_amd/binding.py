@@ -22,7 +22,9 @@ EXPORTS = ["leann_last_error", "leann_create", "leann_destroy", "leann_embed", "
            "leann_pq_import", "leann_pq_wrap", "leann_pq_info", "leann_pq_free", "leann_adc", "leann_adc_noalloc", "leann_search",
            "leann_search_updates", "leann_build_graph", "leann_top_degree",
            "leann_set_limits", "leann_set_call_memo", "leann_set_gemm_tiles", "leann_profile_begin", "leann_profile_end", "leann_bench_mfma", "leann_bench_gather", "leann_bench_l1pull",
-           "leann_dropout", "leann_layernorm", "leann_layernorm_backward"]
+           "leann_dropout", "leann_layernorm", "leann_layernorm_backward",
+           "leann_projection_create", "leann_projection_free", "leann_adapter_rows_create", "leann_adapter_rows_free",
+           "leann_adapter_project", "leann_adapter_project_backward"]
 PROF_KINDS = ["gemm_qkv", "gemm_o", "gemm_ffn1", "gemm_ffn2", "attention", "layernorm", "enc_other", "traverse",
               "collect", "score_insert", "lut", "adc"]
 
@@ -78,12 +80,17 @@ def load_library(path=LIB_PATH):
         for name in EXPORTS:
             getattr(lib, name)
         lib.leann_destroy.restype = None
-        lib.leann_pq_free.restype = None
+        for name in ("leann_pq_free", "leann_projection_free", "leann_adapter_rows_free"):
+            getattr(lib, name).restype = None
         V, I, N, F = C.c_void_p, C.c_int32, C.c_int64, C.c_float
         for name, args in {  # argument types: plain numbers are converted by ctypes, which small calls are faster with
                 "leann_dropout": [V, V, N, V, N, N, N, I, V, V, N],
                 "leann_layernorm": [V, V, N, V, N, N, I, I, V, V, V, F, V, N, V, N, V, V],
-                "leann_layernorm_backward": [V, V, N, V, N, N, I, I, V, V, V, V, N, V, V, N, V, N, V, V]}.items():
+                "leann_layernorm_backward": [V, V, N, V, N, N, I, I, V, V, V, V, N, V, V, N, V, N, V, V],
+                "leann_projection_create": [V, V, V, I, I, I, I, V], "leann_projection_free": [V],
+                "leann_adapter_rows_create": [V, V, V, I, V, V, I, I, V], "leann_adapter_rows_free": [V],
+                "leann_adapter_project": [V, V, V, V, N, V, V, V, N, V],
+                "leann_adapter_project_backward": [V, V, V, V, N, V, N, V, V, V, V, N, V, V]}.items():
             getattr(lib, name).argtypes = args
         _lib = lib
     return _lib
@@ -429,3 +436,76 @@ def leann_layernorm_backward(ctx, dout, total, mean, rstd, gamma, drop=None, dto
     if drop is not None and round(DropoutDesc(*drop).p * 65536) == 0:
         dx = dres
     return dres, dx, dgamma, dbeta
+
+
+class _Handle(C.c_void_p):
+    """A handle of the library with the sizes that its calls' tensors have to have."""
+
+
+def leann_projection_create(ctx, w, bias=None, gradient=False):
+    """A projection's shared weight [n_out][n_in] (bfloat16 or float16, contiguous) and bias; gradient: also for the backward pass."""
+    assert w.is_cuda and w.dim() == 2 and w.is_contiguous() and w.dtype in (torch.bfloat16, torch.float16), "w: need a contiguous 16-bit matrix"
+    h = _Handle()
+    _check(load_library().leann_projection_create(ctx, w.data_ptr(), None if bias is None else _vector(bias, w.shape[0], "bias"), w.shape[0],
+                                                  w.shape[1], _dtype(w), int(gradient), C.byref(h)))
+    h.n_out, h.n_in, h.dtype = w.shape[0], w.shape[1], w.dtype
+    return h
+
+
+def leann_projection_free(proj):
+    load_library().leann_projection_free(proj)
+
+
+def _int32(values):
+    a = np.asarray(values, dtype=None if len(values) else np.int32)
+    assert a.dtype.kind in "iu" and (a.size == 0 or -2**31 <= int(a.min()) and int(a.max()) < 2**31), "need whole numbers of 32 bits"
+    return np.ascontiguousarray(a, dtype=np.int32)
+
+
+def leann_adapter_rows_create(ctx, rows_of_request, adapter_of_request, rank, scale, max_rank):
+    """Which rows go through which adapter: row counts and adapters (-1: none) of the requests, ranks and scales of the adapters."""
+    n, of, rank = _int32(rows_of_request), _int32(adapter_of_request), _int32(rank)
+    scale = np.ascontiguousarray(scale, dtype=np.float32)
+    assert n.ndim == of.ndim == rank.ndim == scale.ndim == 1 and len(n) == len(of) and len(rank) == len(scale)
+    h = _Handle()
+    _check(load_library().leann_adapter_rows_create(ctx, n.ctypes.data, of.ctypes.data, len(n), rank.ctypes.data, scale.ctypes.data, len(rank),
+                                                    max_rank, C.byref(h)))
+    h.T, h.n_adapters, h.max_rank = int(n.sum(dtype=np.int64)), len(rank), max_rank
+    return h
+
+
+def leann_adapter_rows_free(rows):
+    load_library().leann_adapter_rows_free(rows)
+
+
+def _pools(proj, rows, down, up):
+    assert down.is_cuda and up.is_cuda and down.is_contiguous() and up.is_contiguous() and down.dtype == up.dtype == proj.dtype
+    assert down.shape == (rows.n_adapters, rows.max_rank, proj.n_in) and up.shape == (rows.n_adapters, proj.n_out, rows.max_rank)
+    return down.data_ptr(), up.data_ptr()
+
+
+def leann_adapter_project(ctx, proj, rows, x, down, up, keep=False, out=None):
+    """x W^T + bias + each request's adapter's part, x [T][n_in]; keep: returns (out, low), what the backward pass needs; else out."""
+    if out is None:
+        out = torch.empty((rows.T, proj.n_out), dtype=proj.dtype, device=x.device)
+    assert x.shape == (rows.T, proj.n_in) and out.shape == (rows.T, proj.n_out) and x.dtype == out.dtype == proj.dtype
+    low = torch.empty((rows.T, rows.max_rank), dtype=torch.float32, device=x.device) if keep else None
+    (xp, ldx), (op, ldo), (dp, up) = _rows(x, "x"), _rows(out, "out"), _pools(proj, rows, down, up)
+    _check(load_library().leann_adapter_project(ctx, proj, rows, xp, ldx, dp, up, op, ldo, low.data_ptr() if keep else None))
+    return (out, low) if keep else out
+
+
+def leann_adapter_project_backward(ctx, proj, rows, dout, x, low, down, up, need_dx=True, need_adapters=True):
+    """(dx, ddown, dup) from the gradient of leann_adapter_project's output, its input and what it kept; None for what is not needed
+    (x and low may be None without need_adapters)."""
+    assert dout.shape == (rows.T, proj.n_out) and dout.dtype == proj.dtype
+    dx = torch.empty((rows.T, proj.n_in), dtype=proj.dtype, device=dout.device) if need_dx else None
+    ddown = torch.empty(down.shape, dtype=torch.float32, device=dout.device) if need_adapters else None
+    dup = torch.empty(up.shape, dtype=torch.float32, device=dout.device) if need_adapters else None
+    if need_adapters:
+        assert x.shape == (rows.T, proj.n_in) and x.dtype == proj.dtype
+        assert low.is_cuda and low.is_contiguous() and low.shape == (rows.T, rows.max_rank) and low.dtype == torch.float32
+    (gp, ldd), (xp, ldx), (op, lddx), (dp, up) = _rows(dout, "dout"), _rows(x, "x"), _rows(dx, "dx"), _pools(proj, rows, down, up)
+    _check(load_library().leann_adapter_project_backward(ctx, proj, rows, gp, ldd, xp, ldx, None if low is None else low.data_ptr(), dp, up, op, lddx,
+                                                         ddown.data_ptr() if need_adapters else None, dup.data_ptr() if need_adapters else None))
+    return dx, ddown, dup

@@ -1,0 +1,667 @@
+// Projections with low-rank adapters beside a shared weight, and their gradients (gfx950).
+#include <math.h>
+#include <string.h>
+
+#include <algorithm>
+#include <exception>
+#include <new>
+#include <vector>
+
+#include "adapter.h"
+
+namespace {
+
+// ------------------------------------------------------------------ layouts
+// W[N][K] (or, transposed, W[K][N] read by columns) in the MFMA's operand order: [N / 32][K / 16][lane][8], lane l holding column l & 31 and the K
+// of 8 (l >> 5) on.  Zeros beyond N and K.
+template <class T>
+__global__ __launch_bounds__(256) void pack_kernel(const T *w, int N, int K, int transposed, T *out)
+{
+    const int ksteps = (K + 15) >> 4;
+    const size_t pieces = (size_t)((N + 31) >> 5) * ksteps * 64;
+    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < pieces; i += (size_t)gridDim.x * 256) {
+        const int lane = (int)(i & 63), step = (int)((i >> 6) % ksteps), ct = (int)((i >> 6) / ksteps);
+        const int n = ct * 32 + (lane & 31), k = step * 16 + (lane >> 5) * 8;
+        Raw8<T> v;
+        for (int j = 0; j < 8; ++j)
+            v.v[j] = n < N && k + j < K ? (transposed ? w[(size_t)(k + j) * N + n] : w[(size_t)n * K + k + j]) : (T)0.f;
+        v.store(out + i * 8, 8);
+    }
+}
+
+// The used adapters' matrices transposed: down[r][k] -> down_t[k][r], up[n][r] -> up_t[r][n], tiles of 32 x 32.
+template <class T>
+__global__ __launch_bounds__(256) void transpose_kernel(const T *down, const T *up, const int32_t *used, int R, int K, int N, T *down_t, T *up_t)
+{
+    __shared__ T tile[32][34];
+    const int a = used[blockIdx.z], tiles_k = (K + 31) / 32;
+    const bool is_down = (int)blockIdx.x < tiles_k;
+    const int c = (is_down ? blockIdx.x : blockIdx.x - tiles_k) * 32, r = blockIdx.y * 32;  // long side, rank
+    const T *from = is_down ? down + (size_t)a * R * K : up + (size_t)a * N * R;
+    T *to = is_down ? down_t + (size_t)blockIdx.z * R * K : up_t + (size_t)blockIdx.z * N * R;
+    const int C = is_down ? K : N;
+    const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
+    for (int j = ty; j < 32; j += 8) {  // rows of the source
+        const int row = (is_down ? r : c) + j, col = (is_down ? c : r) + tx;
+        const bool in = is_down ? row < R && col < C : row < C && col < R;
+        if (in) tile[j][tx] = from[(size_t)row * (is_down ? C : R) + col];
+    }
+    __syncthreads();
+    for (int j = ty; j < 32; j += 8) {
+        const int row = (is_down ? c : r) + j, col = (is_down ? r : c) + tx;
+        const bool in = is_down ? row < C && col < R : row < R && col < C;
+        if (in) to[(size_t)row * (is_down ? R : C) + col] = tile[tx][j];
+    }
+}
+
+// ------------------------------------------------------------------ low-rank activations
+// low[row][r] = sum over k of x[row][k] down[a][r][k] for 16 slots of one adapter, in MFMA 16x16x32: a lane ends with four ranks of one row.
+// SPLIT: a block per tile, whose four wavefronts share K; else a wavefront per tile.
+template <class T, int NT, bool SPLIT>
+__global__ __launch_bounds__(256) void low_kernel(const T *x, int64_t ldx, const T *down, int R, int K, const int32_t *row_of, const int4 *tiles,
+                                                  int n_tiles, int compact, float *low)
+{
+    typedef typename Frag<T>::type F;
+    __shared__ f32x4 part[SPLIT ? 4 : 1][SPLIT ? NT : 1][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane & 15, q = lane >> 4;
+    const int index = SPLIT ? blockIdx.x : blockIdx.x * 4 + wave;
+    if (index >= n_tiles) return;
+    const int4 tile = tiles[index];
+    const int n = tile.z & 0xffff, rank = tile.z >> 16, groups = (rank + 15) >> 4;
+    const int64_t row = row_of[tile.y + min(j, n - 1)];
+    f32x4 acc[NT];
+#pragma unroll
+    for (int g = 0; g < NT; ++g) acc[g] = f32x4{};
+    if (rank) {
+        const T *xp = x + row * ldx + q * 8;
+        const T *ap[NT];
+#pragma unroll
+        for (int g = 0; g < NT; ++g) ap[g] = down + ((size_t)(compact ? tile.w : tile.x) * R + min(g * 16 + j, rank - 1)) * K + q * 8;
+        const int steps = (K + 31) >> 5, per = SPLIT ? (steps + 3) >> 2 : steps;
+        const int from = SPLIT ? wave * per : 0, to = min(steps, from + per);
+#pragma unroll 4
+        for (int s = from; s < to; ++s) {
+            const bool in = s * 32 + q * 8 < K;  // K is a multiple of 8
+            const int k = in ? s * 32 : 0;
+            F xf = *reinterpret_cast<const F *>(xp + k);
+            if (!in) xf = F{};
+#pragma unroll
+            for (int g = 0; g < NT; ++g)
+                if (g < groups) {
+                    F af = *reinterpret_cast<const F *>(ap[g] + k);
+                    if (!in) af = F{};
+                    acc[g] = mfma16(af, xf, acc[g]);
+                }
+        }
+        if constexpr (SPLIT) {
+#pragma unroll
+            for (int g = 0; g < NT; ++g) part[wave][g][lane] = acc[g];
+            __syncthreads();
+#pragma unroll
+            for (int g = 0; g < NT; ++g) acc[g] = (part[0][g][lane] + part[1][g][lane]) + (part[2][g][lane] + part[3][g][lane]);
+        }
+    }
+    if (j >= n) return;
+#pragma unroll
+    for (int g = 0; g < NT; ++g) {
+        const int r = g * 16 + q * 4;
+        if (r < R && (!SPLIT || (g & 3) == wave)) {
+            f32x4 v = acc[g];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = r + i < rank ? v[i] : 0.f;
+            *reinterpret_cast<f32x4 *>(low + row * R + r) = v;
+        }
+    }
+}
+
+// ------------------------------------------------------------------ the projection
+// out[row][n] = sum over k of x[row][k] W[n][k] + bias[n] + the adapter's part, tiles of 32 TM x 32 TN slots and columns.  Four wavefronts share K, operands from
+// memory to registers; their sums meet in LDS.
+template <class T, int TM, int TN>
+__global__ __launch_bounds__(256) void project_kernel(const T *x, int64_t ldx, const T *w, const float *bias, int N, int K, const int32_t *row_of,
+                                                      int rows, const int32_t *run_ptr, const int4 *runs, int compact, const float *low, int R,
+                                                      const T *up, T *out, int64_t ldo)
+{
+    typedef typename Frag<T>::type F;
+    constexpr int BM = 32 * TM, BN = 32 * TN, PITCH = BN + 4;
+    __shared__ float sums[4][BM][PITCH];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, l32 = lane & 31;
+    const int tiles_n = (N + BN - 1) / BN, tile_n = blockIdx.x % tiles_n, tile_m = blockIdx.x / tiles_n;
+    const int ksteps = (K + 15) >> 4, per = (ksteps + 3) >> 2, from = wave * per, to = min(ksteps, from + per);
+    int64_t row[TM];
+    const T *xp[TM], *wp[TN];
+#pragma unroll
+    for (int mi = 0; mi < TM; ++mi) {
+        row[mi] = row_of[tile_m * BM + mi * 32 + l32];
+        xp[mi] = x + row[mi] * ldx + half * 8;
+    }
+    const int last_ct = (N - 1) >> 5;
+#pragma unroll
+    for (int ni = 0; ni < TN; ++ni) wp[ni] = w + ((size_t)min(tile_n * TN + ni, last_ct) * ksteps * 64 + lane) * 8;
+    f32x16 acc[TM][TN];
+#pragma unroll
+    for (int mi = 0; mi < TM; ++mi)
+#pragma unroll
+        for (int ni = 0; ni < TN; ++ni) acc[mi][ni] = f32x16{};
+#pragma unroll 4
+    for (int s = from; s < to; ++s) {
+        const bool in = s * 16 + half * 8 < K;
+        const int k = in ? s * 16 : 0;
+        F xf[TM], wf[TN];
+#pragma unroll
+        for (int ni = 0; ni < TN; ++ni) wf[ni] = *reinterpret_cast<const F *>(wp[ni] + (size_t)s * 512);
+#pragma unroll
+        for (int mi = 0; mi < TM; ++mi) {
+            xf[mi] = *reinterpret_cast<const F *>(xp[mi] + k);
+            if (!in) xf[mi] = F{};
+        }
+#pragma unroll
+        for (int mi = 0; mi < TM; ++mi)
+#pragma unroll
+            for (int ni = 0; ni < TN; ++ni) acc[mi][ni] = mfma32(wf[ni], xf[mi], acc[mi][ni]);
+    }
+#pragma unroll
+    for (int mi = 0; mi < TM; ++mi)
+        if (tile_m * BM + mi * 32 < rows)
+            add_adapters<T, TN>(acc[mi], run_ptr, runs, tile_m * TM + mi, wave, 4, low + row[mi] * R, up, R, N, tile_n * BN, compact);
+#pragma unroll
+    for (int mi = 0; mi < TM; ++mi)
+#pragma unroll
+        for (int ni = 0; ni < TN; ++ni)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const f32x4 v = {acc[mi][ni][4 * g], acc[mi][ni][4 * g + 1], acc[mi][ni][4 * g + 2], acc[mi][ni][4 * g + 3]};
+                *reinterpret_cast<f32x4 *>(&sums[wave][mi * 32 + l32][ni * 32 + 8 * g + 4 * half]) = v;
+            }
+    __syncthreads();
+    for (int i = threadIdx.x; i < BM * BN / 8; i += 256) {
+        const int m = i / (BN / 8), c = i % (BN / 8) * 8, col = tile_n * BN + c, slot = tile_m * BM + m;
+        if (col >= N || slot >= rows) continue;  // N is a multiple of 8
+        f32x8 v = {};
+        if (bias) __builtin_memcpy(&v, bias + col, sizeof(v));
+#pragma unroll
+        for (int p = 0; p < 4; ++p) v += *reinterpret_cast<const f32x8 *>(&sums[p][m][c]);
+        Raw8<T> o;
+        o.round(v);
+        *reinterpret_cast<typename Vec8<T>::type *>(out + (int64_t)row_of[slot] * ldo + col) = o.v;
+    }
+}
+
+// ------------------------------------------------------------------ the adapters' gradients
+// Eight rows of eight 16-bit elements, transposed: out[f] holds element f of the rows in order.
+__device__ inline void transpose8(const u32x4 (&in)[8], u32x4 (&out)[8])
+{
+#pragma unroll
+    for (int f = 0; f < 8; ++f)
+#pragma unroll
+        for (int p = 0; p < 4; ++p)  // rows 2p and 2p + 1
+            out[f][p] = __builtin_amdgcn_perm(in[2 * p + 1][f >> 1], in[2 * p][f >> 1], f & 1 ? 0x07060302 : 0x05040100);
+}
+
+// Sixteen rows' share of sum over rows of h[row][r] p[row][c], to 24 bits of h: three pieces of it; fp16 elements are two bf16 pieces exactly.
+__device__ inline f32x16 outer_step(const bf16x8 (&h)[3], const bf16x8 &p, f32x16 c)
+{
+    c = mfma32(h[2], p, c);
+    c = mfma32(h[1], p, c);
+    return mfma32(h[0], p, c);
+}
+__device__ inline f32x16 outer_step(const bf16x8 (&h)[3], const f16x8 &p, f32x16 c)
+{
+    f32x8 v = __builtin_convertvector(p, f32x8);
+    const bf16x8 p1 = take_piece(v), p2 = take_piece(v);
+    c = mfma32(h[2], p1, c);
+    c = mfma32(h[1], p2, c);
+    c = mfma32(h[1], p1, c);
+    c = mfma32(h[0], p2, c);
+    return mfma32(h[0], p1, c);
+}
+
+// partial[chunk][r][c] = sum over the chunk's rows of low[row][r] p[row][c]: c < K from x and the low-rank gradients (down's), then N from dout and the
+// low-rank activations (up's).  A block takes 256 columns and 32 ranks; a lane reads 16 bytes of a row and turns eight rows of them, in registers,
+// into the MFMA operands of its eight columns.
+template <class T>
+__global__ __launch_bounds__(256) void outer_kernel(const T *x, int64_t ldx, const T *dout, int64_t ldd, const float *grad_low, const float *low, int R,
+                                                    int K, int N, const int32_t *row_of, const int4 *chunks, float *partial)
+{
+    __shared__ float sums[32][256];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, l32 = lane & 31;
+    const int strips_k = (K + 255) / 256, strips = strips_k + (N + 255) / 256, strip = blockIdx.x % strips;
+    const int4 chunk = chunks[blockIdx.x / strips];
+    const int n = chunk.z & 0xffff, rank = chunk.z >> 16, r0 = blockIdx.y * 32;
+    if (r0 >= rank) return;
+    const bool of_x = strip < strips_k;
+    const T *p = of_x ? x : dout;
+    const int64_t ld = of_x ? ldx : ldd;
+    const float *h = of_x ? grad_low : low;
+    const int C = of_x ? K : N, c0 = (of_x ? strip : strip - strips_k) * 256, col = c0 + l32 * 8;
+    const bool has_col = col < C, has_rank = r0 + l32 < rank;
+    f32x16 acc[8];
+#pragma unroll
+    for (int f = 0; f < 8; ++f) acc[f] = f32x16{};
+    for (int base = wave * 16; base < n; base += 64) {
+        u32x4 d[8], t[8];
+        f32x8 hv;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int at = base + half * 8 + i;
+            const int64_t row = row_of[chunk.y + min(at, n - 1)];
+            d[i] = at < n && has_col ? *reinterpret_cast<const u32x4 *>(p + row * ld + col) : u32x4{};
+            hv[i] = at < n && has_rank ? h[row * R + r0 + l32] : 0.f;
+        }
+        bf16x8 piece[3];
+#pragma unroll
+        for (int i = 0; i < 3; ++i) piece[i] = take_piece(hv);
+        transpose8(d, t);
+#pragma unroll
+        for (int f = 0; f < 8; ++f) acc[f] = outer_step(piece, __builtin_bit_cast(typename Frag<T>::type, t[f]), acc[f]);
+    }
+    for (int w = 0; w < 4; ++w) {
+        if (wave == w)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                f32x8 v;
+#pragma unroll
+                for (int f = 0; f < 8; ++f) v[f] = acc[f][e];
+                f32x8 *to = reinterpret_cast<f32x8 *>(&sums[8 * (e >> 2) + 4 * half + (e & 3)][l32 * 8]);
+                *to = w ? *to + v : v;
+            }
+        __syncthreads();
+    }
+    float *to = partial + (size_t)(blockIdx.x / strips) * R * (K + N) + (of_x ? 0 : K) + c0;
+    for (int i = threadIdx.x; i < 32 * 64; i += 256) {
+        const int r = i >> 6, c = (i & 63) * 4;
+        if (r0 + r < rank && c0 + c < C) *reinterpret_cast<f32x4 *>(to + (size_t)(r0 + r) * (K + N) + c) = *reinterpret_cast<const f32x4 *>(&sums[r][c]);
+    }
+}
+
+// ddown[a][r][k] and dup[a][n][r] from the chunks' sums, in their order; 0 where an adapter has no rows, and beyond its rank.
+__global__ __launch_bounds__(256) void outer_sum_kernel(const float *partial, const int4 *adapters, int R, int K, int N, float *ddown, float *dup)
+{
+    __shared__ float tile[32][33];
+    const int4 a = adapters[blockIdx.z];
+    const int c0 = blockIdx.x * 32, r0 = blockIdx.y * 32, tx = threadIdx.x & 31, ty = threadIdx.x >> 5, c = c0 + tx;
+    const float scale = __int_as_float(a.w);
+    float s[4] = {};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int r = r0 + ty + 8 * j;
+        if (r < a.z && c < K + N)
+            for (int i = 0; i < a.y; ++i) s[j] += partial[((size_t)(a.x + i) * R + r) * (K + N) + c];
+        s[j] *= scale;
+        if (r < R && c < K) ddown[((size_t)blockIdx.z * R + r) * K + c] = s[j];
+        tile[ty + 8 * j][tx] = s[j];
+    }
+    if (c0 + 32 <= K) return;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int n = c0 + ty + 8 * j - K;
+        if (n >= 0 && n < N && r0 + tx < R) dup[((size_t)blockIdx.z * N + n) * R + r0 + tx] = tile[tx][ty + 8 * j];
+    }
+}
+
+template <class F>
+int with_half_type(int dtype, F f)
+{
+    if (dtype == LEANN_BF16) return f((bf16_t *)nullptr);
+    return f((f16_t *)nullptr);
+}
+
+int launched(const char *call)
+{
+    const hipError_t e = hipGetLastError();
+    if (e == hipSuccess) return LEANN_OK;
+    leann_set_error("%s: launch failed: %s", call, hipGetErrorString(e));
+    return LEANN_EDEVICE;
+}
+
+size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
+bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
+
+int check_half_rows(const char *call, const char *what, const void *p, int64_t ld, int64_t cols)
+{
+    if (!p || !aligned16(p)) {
+        leann_set_error("%s: %s is null or not aligned to 16 bytes", call, what);
+        return LEANN_EINVAL;
+    }
+    if (ld < cols || ld % 8) {
+        leann_set_error("%s: rows of %s are %lld elements apart, need at least %lld and a multiple of 8", call, what, (long long)ld, (long long)cols);
+        return LEANN_ESHAPE;
+    }
+    return LEANN_OK;
+}
+
+// low = x down^T for the adapted rows; with_zeros: zeros for the others, too.
+template <class T>
+void enqueue_low(leann_ctx *ctx, const leann_adapter_rows *rows, const T *x, int64_t ldx, int K, const T *down, int compact, float *low, bool with_zeros)
+{
+    const int n = with_zeros ? rows->n_tiles : rows->n_adapted_tiles, R = rows->max_rank;
+    if (!n) return;
+    const bool split = n < ctx->num_cus * 4;
+    auto go = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3(split ? n : (n + 3) / 4), dim3(256), 0, ctx->stream, x, ldx, down, R, K, rows->row_of, rows->tiles, n, compact,
+                           low);
+    };
+    if (R <= 16) split ? go(low_kernel<T, 1, true>) : go(low_kernel<T, 1, false>);
+    else if (R <= 32) split ? go(low_kernel<T, 2, true>) : go(low_kernel<T, 2, false>);
+    else if (R <= 64) split ? go(low_kernel<T, 4, true>) : go(low_kernel<T, 4, false>);
+    else split ? go(low_kernel<T, 8, true>) : go(low_kernel<T, 8, false>);
+}
+
+// out = x w^T + bias + the adapters' part
+template <class T>
+void enqueue_project(leann_ctx *ctx, const leann_adapter_rows *rows, const T *x, int64_t ldx, const T *w, const float *bias, int N, int K,
+                     const float *low, const T *up, int compact, T *out, int64_t ldo)
+{
+    const int T32 = (int)((rows->T + 31) / 32), T64 = (int)((rows->T + 63) / 64);
+    const int64_t tiles64 = (int64_t)T64 * ((N + 63) / 64);
+    auto go = [&](auto kernel, int64_t blocks) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, ctx->stream, x, ldx, w, bias, N, K, rows->row_of, (int)rows->T, rows->run_ptr,
+                           rows->runs, compact, low, rows->max_rank, up, out, ldo);
+    };
+    if (tiles64 < ctx->num_cus) go(project_kernel<T, 1, 1>, (int64_t)T32 * ((N + 31) / 32));
+    else go(project_kernel<T, 2, 2>, tiles64);
+}
+
+int check_pair(const char *call, const leann_ctx *ctx, const leann_projection *proj, const leann_adapter_rows *rows)
+{
+    if (!ctx || !proj || !rows) {
+        leann_set_error("%s: null context, projection or rows", call);
+        return LEANN_EINVAL;
+    }
+    if (proj->device != ctx->device || rows->device != ctx->device) {
+        leann_set_error("%s: the projection or the rows belong to another device", call);
+        return LEANN_EINVAL;
+    }
+    return LEANN_OK;
+}
+
+int make_rows(leann_ctx *ctx, const int32_t *rows_of_request, const int32_t *adapter_of_request, int32_t n_requests, const int32_t *rank,
+              const float *scale, int32_t n_adapters, int32_t max_rank, leann_adapter_rows *out)
+{
+    int64_t T = 0;
+    std::vector<int64_t> start(n_requests + 1, 0);
+    for (int i = 0; i < n_requests; ++i) start[i + 1] = T += rows_of_request[i];
+    auto of = [&](int i) { return adapter_of_request[i] >= 0 && rank[adapter_of_request[i]] > 0 ? adapter_of_request[i] : n_adapters; };
+    // requests by adapter (those without one, or with one of rank 0, last), in their order
+    std::vector<int32_t> first(n_adapters + 2, 0), order(n_requests);
+    for (int i = 0; i < n_requests; ++i) ++first[of(i) + 1];
+    for (int a = 0; a <= n_adapters; ++a) first[a + 1] += first[a];
+    {
+        std::vector<int32_t> next(first.begin(), first.end() - 1);
+        for (int i = 0; i < n_requests; ++i) order[next[of(i)]++] = i;
+    }
+    std::vector<int32_t> row_of;
+    row_of.reserve(T + 256);
+    std::vector<int64_t> slot_of(n_adapters + 2, 0);  // an adapter's first slot
+    for (int a = 0; a <= n_adapters; ++a) {
+        for (int j = first[a]; j < first[a + 1]; ++j)
+            for (int64_t r = start[order[j]]; r < start[order[j] + 1]; ++r) row_of.push_back((int32_t)r);
+        slot_of[a + 1] = (int64_t)row_of.size();
+    }
+    while (row_of.size() % 256) row_of.push_back(row_of[T - 1]);
+
+    const int64_t adapted = slot_of[n_adapters];
+    // Rows of a chunk: as many as leave some four blocks for each CU (a block takes 256 columns of one), 64 at least, 1024 at most.
+    const int chunk_rows = (int)std::min<int64_t>(1024, std::max<int64_t>(64, (adapted / (ctx->num_cus * 2 / 3) + 63) / 64 * 64));
+    std::vector<int4> tiles, chunks, runs, adapters(n_adapters);
+    std::vector<int32_t> used, run_ptr((T + 31) / 32 + 1, 0);
+    auto bits = [](float f) {
+        int32_t i;
+        memcpy(&i, &f, sizeof(i));
+        return i;
+    };
+    for (int a = 0; a <= n_adapters; ++a) {
+        const int64_t from = slot_of[a], to = slot_of[a + 1];
+        const int r = a < n_adapters ? rank[a] : 0, number = (int)used.size();
+        if (a == n_adapters) out->n_adapted_tiles = (int)tiles.size();
+        for (int64_t s = from; s < to; s += 16) tiles.push_back(int4{a < n_adapters ? a : -1, (int)s, (int)std::min<int64_t>(16, to - s) | r << 16, number});
+        if (a == n_adapters) break;
+        adapters[a] = int4{(int)chunks.size(), 0, r, bits(scale[a])};
+        for (int64_t s = from; s < to; s += chunk_rows) chunks.push_back(int4{a, (int)s, (int)std::min<int64_t>(chunk_rows, to - s) | r << 16, number});
+        adapters[a].y = (int)chunks.size() - adapters[a].x;
+        for (int64_t s = from; s < to;) {
+            const int64_t group = s / 32, end = std::min<int64_t>(to, (group + 1) * 32);
+            runs.push_back(int4{a, (int)(s - group * 32) | (int)(end - group * 32) << 8 | r << 16, bits(scale[a]), number});
+            ++run_ptr[group + 1];
+            s = end;
+        }
+        if (to > from) used.push_back(a);
+    }
+    for (size_t g = 1; g < run_ptr.size(); ++g) run_ptr[g] += run_ptr[g - 1];
+
+    out->device = ctx->device;
+    out->T = T;
+    out->n_adapters = n_adapters;
+    out->max_rank = max_rank;
+    out->n_used = (int)used.size();
+    out->n_tiles = (int)tiles.size();
+    out->n_chunks = (int)chunks.size();
+    std::vector<char> image;
+    auto put = [&](const auto &v) {
+        const size_t at = up256(image.size()), bytes = v.size() * sizeof(v[0]);
+        image.resize(at + bytes);
+        if (bytes) memcpy(image.data() + at, v.data(), bytes);
+        return at;
+    };
+    const size_t at[7] = {put(row_of), put(run_ptr), put(runs), put(tiles), put(chunks), put(adapters), put(used)};
+    LEANN_TRY(ctx->reserve(out->mem, std::max<size_t>(image.size(), 1)));
+    LEANN_HIP(hipMemcpyAsync(out->mem.p, image.data(), image.size(), hipMemcpyHostToDevice, ctx->stream));
+    LEANN_HIP(hipStreamSynchronize(ctx->stream));
+    const char *base = (const char *)out->mem.p;
+    out->row_of = (const int32_t *)(base + at[0]);
+    out->run_ptr = (const int32_t *)(base + at[1]);
+    out->runs = (const int4 *)(base + at[2]);
+    out->tiles = (const int4 *)(base + at[3]);
+    out->chunks = (const int4 *)(base + at[4]);
+    out->adapters = (const int4 *)(base + at[5]);
+    out->used = (const int32_t *)(base + at[6]);
+    return LEANN_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+void leann_projection_free(leann_projection *p)
+{
+    if (!p) return;
+    (void)hipSetDevice(p->device);
+    for (DevBuf *b : {&p->w, &p->wt, &p->bias}) b->release();
+    delete p;
+}
+
+void leann_adapter_rows_free(leann_adapter_rows *p)
+{
+    if (!p) return;
+    (void)hipSetDevice(p->device);
+    p->mem.release();
+    delete p;
+}
+
+int leann_projection_create(leann_ctx *ctx, const void *w_dev, const float *bias_dev, int32_t n_out, int32_t n_in, int dtype, int with_gradient,
+                            leann_projection **out)
+{
+    static const char *call = "leann_projection_create";
+    if (!ctx || !w_dev || !out || n_out < 1 || n_in < 1 || (dtype != LEANN_BF16 && dtype != LEANN_F16)) {
+        leann_set_error("%s: null argument, no rows or columns, or a type other than bf16 and f16", call);
+        return LEANN_EINVAL;
+    }
+    if (n_out % 8 || n_in % 8 || n_out > 65536 || n_in > 65536) {
+        leann_set_error("%s: %d x %d is not covered (multiples of 8, at most 65536)", call, n_out, n_in);
+        return LEANN_ESHAPE;
+    }
+    LEANN_HIP(hipSetDevice(ctx->device));
+    leann_projection *p = new (std::nothrow) leann_projection();
+    if (!p) {
+        leann_set_error("%s: no host memory", call);
+        return LEANN_ENOMEM;
+    }
+    p->device = ctx->device;
+    p->dtype = dtype;
+    p->n_out = n_out;
+    p->n_in = n_in;
+    auto packed = [&](int N, int K) { return (size_t)((N + 31) / 32) * ((K + 15) / 16) * 1024; };
+    int rc = ctx->reserve(p->w, packed(n_out, n_in));
+    if (rc == LEANN_OK && with_gradient) rc = ctx->reserve(p->wt, packed(n_in, n_out));
+    if (rc == LEANN_OK && bias_dev) rc = ctx->reserve(p->bias, n_out * sizeof(float));
+    if (rc == LEANN_OK)
+        rc = with_half_type(dtype, [&](auto *type) {
+            typedef std::remove_pointer_t<decltype(type)> T;
+            hipLaunchKernelGGL(pack_kernel<T>, dim3(1024), dim3(256), 0, ctx->stream, (const T *)w_dev, n_out, n_in, 0, (T *)p->w.p);
+            if (with_gradient) hipLaunchKernelGGL(pack_kernel<T>, dim3(1024), dim3(256), 0, ctx->stream, (const T *)w_dev, n_in, n_out, 1, (T *)p->wt.p);
+            return launched(call);
+        });
+    if (rc == LEANN_OK && bias_dev) {
+        const hipError_t e = hipMemcpyAsync(p->bias.p, bias_dev, n_out * sizeof(float), hipMemcpyDeviceToDevice, ctx->stream);
+        if (e != hipSuccess) {
+            leann_set_error("%s: copying the bias failed: %s", call, hipGetErrorString(e));
+            rc = LEANN_EDEVICE;
+        }
+    }
+    if (rc == LEANN_OK) {
+        const hipError_t e = hipStreamSynchronize(ctx->stream);  // the caller may free the weight
+        if (e != hipSuccess) {
+            leann_set_error("%s: %s", call, hipGetErrorString(e));
+            rc = LEANN_EDEVICE;
+        }
+    }
+    if (rc != LEANN_OK) {
+        leann_projection_free(p);
+        return rc;
+    }
+    *out = p;
+    return LEANN_OK;
+}
+
+int leann_adapter_rows_create(leann_ctx *ctx, const int32_t *rows_of_request_host, const int32_t *adapter_of_request_host, int32_t n_requests,
+                              const int32_t *rank_host, const float *scale_host, int32_t n_adapters, int32_t max_rank, leann_adapter_rows **out)
+{
+    static const char *call = "leann_adapter_rows_create";
+    if (!ctx || !out || n_requests < 0 || n_adapters < 1 || !rank_host || !scale_host ||
+        (n_requests > 0 && (!rows_of_request_host || !adapter_of_request_host))) {
+        leann_set_error("%s: null argument, negative request count or no adapters", call);
+        return LEANN_EINVAL;
+    }
+    if (max_rank < 8 || max_rank > 128 || max_rank % 8) {
+        leann_set_error("%s: room for %d ranks is not covered (a multiple of 8, at most 128)", call, max_rank);
+        return LEANN_ESHAPE;
+    }
+    int64_t T = 0;
+    for (int i = 0; i < n_requests; ++i) {
+        if (rows_of_request_host[i] < 0 || adapter_of_request_host[i] < -1 || adapter_of_request_host[i] >= n_adapters) {
+            leann_set_error("%s: request %d has a negative row count or an adapter outside [-1, %d)", call, i, n_adapters);
+            return LEANN_EINVAL;
+        }
+        T += rows_of_request_host[i];
+    }
+    for (int a = 0; a < n_adapters; ++a)
+        if (rank_host[a] < 0 || rank_host[a] > max_rank || !std::isfinite(scale_host[a])) {
+            leann_set_error("%s: adapter %d has a rank outside [0, %d] or a scale that is not finite", call, a, max_rank);
+            return LEANN_EINVAL;
+        }
+    if (T > 0x7fffffffll - 256) {
+        leann_set_error("%s: %lld rows are not covered (below 2^31 - 256)", call, (long long)T);
+        return LEANN_ESHAPE;
+    }
+    if (n_adapters > 65535) {
+        leann_set_error("%s: %d adapters are not covered (at most 65535)", call, n_adapters);
+        return LEANN_ESHAPE;
+    }
+    LEANN_HIP(hipSetDevice(ctx->device));
+    leann_adapter_rows *p = nullptr;
+    int rc;
+    try {
+        p = new leann_adapter_rows();
+        rc = make_rows(ctx, rows_of_request_host, adapter_of_request_host, n_requests, rank_host, scale_host, n_adapters, max_rank, p);
+    } catch (const std::exception &) {
+        leann_set_error("%s: no host memory", call);
+        rc = LEANN_ENOMEM;
+    }
+    if (rc != LEANN_OK) {
+        leann_adapter_rows_free(p);
+        return rc;
+    }
+    *out = p;
+    return LEANN_OK;
+}
+
+int leann_adapter_project(leann_ctx *ctx, const leann_projection *proj, const leann_adapter_rows *rows, const void *x_dev, int64_t ldx,
+                          const void *down_dev, const void *up_dev, void *out_dev, int64_t ldo, float *low_dev)
+{
+    static const char *call = "leann_adapter_project";
+    LEANN_TRY(check_pair(call, ctx, proj, rows));
+    if (rows->T == 0) return LEANN_OK;
+    LEANN_TRY(check_half_rows(call, "x", x_dev, ldx, proj->n_in));
+    LEANN_TRY(check_half_rows(call, "out", out_dev, ldo, proj->n_out));
+    if (!down_dev || !up_dev || !aligned16(down_dev) || !aligned16(up_dev) || !aligned16(low_dev)) {
+        leann_set_error("%s: the adapters' matrices are null, or they or low are not aligned to 16 bytes", call);
+        return LEANN_EINVAL;
+    }
+    LEANN_HIP(hipSetDevice(ctx->device));
+    float *low = low_dev;
+    if (!low) {
+        LEANN_TRY(ctx->reserve(ctx->op_work, (size_t)rows->T * rows->max_rank * sizeof(float)));
+        low = (float *)ctx->op_work.p;
+    }
+    return with_half_type(proj->dtype, [&](auto *type) {
+        typedef std::remove_pointer_t<decltype(type)> T;
+        enqueue_low<T>(ctx, rows, (const T *)x_dev, ldx, proj->n_in, (const T *)down_dev, 0, low, low_dev != nullptr);
+        enqueue_project<T>(ctx, rows, (const T *)x_dev, ldx, (const T *)proj->w.p, (const float *)proj->bias.p, proj->n_out, proj->n_in, low,
+                           (const T *)up_dev, 0, (T *)out_dev, ldo);
+        return launched(call);
+    });
+}
+
+int leann_adapter_project_backward(leann_ctx *ctx, const leann_projection *proj, const leann_adapter_rows *rows, const void *dout_dev, int64_t ldd,
+                                   const void *x_dev, int64_t ldx, const float *low_dev, const void *down_dev, const void *up_dev, void *dx_dev,
+                                   int64_t lddx, float *ddown_dev, float *dup_dev)
+{
+    static const char *call = "leann_adapter_project_backward";
+    LEANN_TRY(check_pair(call, ctx, proj, rows));
+    if ((rows->T > 0 && !dx_dev && !ddown_dev) || !ddown_dev != !dup_dev) {
+        leann_set_error("%s: no output, or only one of ddown and dup", call);
+        return LEANN_EINVAL;
+    }
+    if (dx_dev && !proj->wt.p) {
+        leann_set_error("%s: the projection was created without gradient", call);
+        return LEANN_EINVAL;
+    }
+    const int N = proj->n_out, K = proj->n_in, R = rows->max_rank;
+    if (rows->T > 0) {
+        LEANN_TRY(check_half_rows(call, "dout", dout_dev, ldd, N));
+        if (dx_dev) LEANN_TRY(check_half_rows(call, "dx", dx_dev, lddx, K));
+        if (ddown_dev) LEANN_TRY(check_half_rows(call, "x", x_dev, ldx, K));
+        if (!down_dev || !up_dev || (ddown_dev && !low_dev) || !aligned16(down_dev) || !aligned16(up_dev) || !aligned16(low_dev)) {
+            leann_set_error("%s: the adapters' matrices or low are null or not aligned to 16 bytes", call);
+            return LEANN_EINVAL;
+        }
+    }
+    LEANN_HIP(hipSetDevice(ctx->device));
+    const size_t low_bytes = up256((size_t)rows->T * R * sizeof(float)), down_bytes = up256((size_t)rows->n_used * R * K * 2),
+                 up_bytes = up256((size_t)rows->n_used * R * N * 2), partial_bytes = ddown_dev ? (size_t)rows->n_chunks * R * (K + N) * sizeof(float) : 0;
+    LEANN_TRY(ctx->reserve(ctx->op_work, std::max<size_t>(1, low_bytes + down_bytes + up_bytes + partial_bytes)));
+    char *work = (char *)ctx->op_work.p;
+    float *grad_low = (float *)work, *partial = (float *)(work + low_bytes + down_bytes + up_bytes);
+    return with_half_type(proj->dtype, [&](auto *type) {
+        typedef std::remove_pointer_t<decltype(type)> T;
+        T *down_t = (T *)(work + low_bytes), *up_t = (T *)(work + low_bytes + down_bytes);
+        if (rows->n_used) {
+            hipLaunchKernelGGL(transpose_kernel<T>, dim3((K + 31) / 32 + (N + 31) / 32, (R + 31) / 32, rows->n_used), dim3(256), 0, ctx->stream,
+                               (const T *)down_dev, (const T *)up_dev, rows->used, R, K, N, down_t, up_t);
+            enqueue_low<T>(ctx, rows, (const T *)dout_dev, ldd, N, up_t, 1, grad_low, false);
+        }
+        if (dx_dev && rows->T)
+            enqueue_project<T>(ctx, rows, (const T *)dout_dev, ldd, (const T *)proj->wt.p, nullptr, K, N, grad_low, down_t, 1, (T *)dx_dev, lddx);
+        if (ddown_dev) {
+            if (rows->n_chunks)
+                hipLaunchKernelGGL(outer_kernel<T>, dim3(((K + 255) / 256 + (N + 255) / 256) * rows->n_chunks, (R + 31) / 32), dim3(256), 0, ctx->stream,
+                                   (const T *)x_dev, ldx, (const T *)dout_dev, ldd, grad_low, low_dev, R, K, N, rows->row_of, rows->chunks, partial);
+            hipLaunchKernelGGL(outer_sum_kernel, dim3((K + N + 31) / 32, (R + 31) / 32, rows->n_adapters), dim3(256), 0, ctx->stream, partial,
+                               rows->adapters, R, K, N, ddown_dev, dup_dev);
+        }
+        return launched(call);
+    });
+}
+
+}  // extern "C"

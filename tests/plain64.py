@@ -50,3 +50,33 @@ def layernorm_backward(dout, t, mean, rstd, gamma):
     gy = dout * gamma
     dt = rstd[:, None] * (gy - gy.mean(1, keepdims=True) - xhat * (gy * xhat).mean(1, keepdims=True))
     return dt, (dout * xhat).sum(0), dout.sum(0)
+
+
+def request_rows(lengths, of):
+    """[(adapter or -1, slice of its rows)] of the requests."""
+    starts = np.concatenate([[0], np.cumsum(lengths)]).astype(np.int64)
+    return [(a, slice(int(starts[i]), int(starts[i + 1]))) for i, a in enumerate(of)]
+
+
+def project(x, w, bias, down, up, lengths, of, ranks, scales):
+    """(out, low)."""
+    out, low = x @ w.T + bias, np.zeros((x.shape[0], down.shape[1]))
+    for a, rows in request_rows(lengths, of):
+        if a >= 0:
+            r = ranks[a]
+            low[rows, :r] = x[rows] @ down[a, :r].T
+            out[rows] += scales[a] * (low[rows, :r] @ up[a, :, :r].T)
+    return out, low
+
+
+def project_backward(dout, x, low, w, down, up, lengths, of, ranks, scales):
+    """(dx, ddown, dup)."""
+    dx, ddown, dup = dout @ w, np.zeros(down.shape), np.zeros(up.shape)
+    for a, rows in request_rows(lengths, of):
+        if a >= 0:
+            r = ranks[a]
+            g = scales[a] * (dout[rows] @ up[a, :, :r])
+            dx[rows] += g @ down[a, :r]
+            ddown[a, :r] += g.T @ x[rows]
+            dup[a, :, :r] += scales[a] * (dout[rows].T @ low[rows, :r])
+    return dx, ddown, dup

@@ -46,3 +46,19 @@ def test_layernorm_gradient_against_differences():
                 up, down = list(args), list(args)
                 up[i], down[i] = v + d, v - d
                 assert abs((loss(*up) - loss(*down)) / 2e-6 - g[j]) < 1e-6 * (1 + abs(g[j])) * 100
+
+
+def test_project_gradient_against_differences():
+    rng = np.random.default_rng(2)
+    lengths, of, ranks, scales = [2, 0, 3, 1], [1, 0, -1, 1], [2, 3], [0.5, 2.0]
+    x, w, bias, down, up, dout = (rng.normal(size=s) for s in [(6, 4), (5, 4), (5,), (2, 3, 4), (2, 5, 3), (6, 5)])
+    loss = lambda x, down, up: (plain64.project(x, w, bias, down, up, lengths, of, ranks, scales)[0] * dout).sum()
+    low = plain64.project(x, w, bias, down, up, lengths, of, ranks, scales)[1]
+    grads = plain64.project_backward(dout, x, low, w, down, up, lengths, of, ranks, scales)
+    for i, (g, v) in enumerate(zip(grads, (x, down, up))):
+        for j in np.ndindex(v.shape):
+            a, b = [[x, down, up] for _ in range(2)]
+            a[i], b[i] = v.copy(), v.copy()
+            a[i][j] += 1e-6
+            b[i][j] -= 1e-6
+            assert abs((loss(*a) - loss(*b)) / 2e-6 - g[j]) < 1e-7 * (1 + abs(g[j]))
