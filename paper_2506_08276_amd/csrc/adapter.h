@@ -20,7 +20,7 @@ struct leann_adapter_rows {
     DevBuf mem;
     const int32_t *row_of = nullptr;     // [T, up to a multiple of 256: the last row again]
     const int32_t *run_ptr = nullptr;    // [32-slot groups + 1]
-    const int4 *runs = nullptr;          // adapter, begin | end << 8 | rank << 16 (slots of the group), scale, number among the used adapters
+    const int4 *runs = nullptr;          // adapter, first slot, slots | rank << 8 | number among the used adapters << 16, scale
     const int4 *tiles = nullptr;         // adapter, first slot, slots | rank << 16, number among the used adapters
     const int4 *chunks = nullptr;        // likewise, by adapter
     const int4 *adapters = nullptr;      // [n_adapters] first chunk, chunks, rank, scale
@@ -29,15 +29,20 @@ struct leann_adapter_rows {
 
 namespace {
 
+// Steps of 16 of K in a packed weight: whole numbers of four slabs of 32, zeros beyond K.
+__host__ __device__ inline int project_ksteps(int K) { return (K + 127) / 128 * 8; }
+
 template <class T>
 struct Frag;
 template <>
 struct Frag<bf16_t> {
     typedef bf16x8 type;
+    typedef bf16x4 four;
 };
 template <>
 struct Frag<f16_t> {
     typedef f16x8 type;
+    typedef f16x4 four;
 };
 
 __device__ inline f32x16 mfma32(const bf16x8 &a, const bf16x8 &b, const f32x16 &c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
@@ -81,10 +86,10 @@ __device__ inline void add_adapters(f32x16 (&acc)[TN], const int32_t *run_ptr, c
     const int begin = run_ptr[group], count = run_ptr[group + 1] - begin;
     for (int i = first; i < count; i += step) {
         const int4 run = runs[begin + i];
-        const int rank = (uint32_t)run.y >> 16, from = run.y & 255, to = run.y >> 8 & 255;
-        const float scale = __int_as_float(run.z);
+        const int rank = run.z >> 8 & 255, from = run.y - group * 32, to = from + (run.z & 255);
+        const float scale = __int_as_float(run.w);
         const bool own = l32 >= from && l32 < to;
-        const T *u = up + (size_t)(compact ? run.w : run.x) * N * R;
+        const T *u = up + (size_t)(compact ? (uint32_t)run.z >> 16 : (uint32_t)run.x) * N * R;
         f32x16 sum[TN];
 #pragma unroll
         for (int ni = 0; ni < TN; ++ni) sum[ni] = acc[ni];

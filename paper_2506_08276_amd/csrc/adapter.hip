@@ -7,17 +7,17 @@
 #include <new>
 #include <vector>
 
-#include "adapter.h"
+#include "adapter_gemm.h"
 
 namespace {
 
 // ------------------------------------------------------------------ layouts
 // W[N][K] (or, transposed, W[K][N] read by columns) in the MFMA's operand order: [N / 32][K / 16][lane][8], lane l holding column l & 31 and the K
-// of 8 (l >> 5) on.  Zeros beyond N and K.
+// of 8 (l >> 5) on.  Zeros beyond N and K, up to a multiple of 32 and of 128.
 template <class T>
 __global__ __launch_bounds__(256) void pack_kernel(const T *w, int N, int K, int transposed, T *out)
 {
-    const int ksteps = (K + 15) >> 4;
+    const int ksteps = project_ksteps(K);
     const size_t pieces = (size_t)((N + 31) >> 5) * ksteps * 64;
     for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < pieces; i += (size_t)gridDim.x * 256) {
         const int lane = (int)(i & 63), step = (int)((i >> 6) % ksteps), ct = (int)((i >> 6) / ksteps);
@@ -79,19 +79,27 @@ __global__ __launch_bounds__(256) void low_kernel(const T *x, int64_t ldx, const
         for (int g = 0; g < NT; ++g) ap[g] = down + ((size_t)(compact ? tile.w : tile.x) * R + min(g * 16 + j, rank - 1)) * K + q * 8;
         const int steps = (K + 31) >> 5, per = SPLIT ? (steps + 3) >> 2 : steps;
         const int from = SPLIT ? wave * per : 0, to = min(steps, from + per);
-#pragma unroll 4
-        for (int s = from; s < to; ++s) {
-            const bool in = s * 32 + q * 8 < K;  // K is a multiple of 8
-            const int k = in ? s * 32 : 0;
-            F xf = *reinterpret_cast<const F *>(xp + k);
-            if (!in) xf = F{};
+        constexpr int U = NT > 2 ? 2 : 4;  // steps whose operands are on their way together
+        for (int s = from; s < to; s += U) {
+            F xf[U], af[U][NT];
 #pragma unroll
-            for (int g = 0; g < NT; ++g)
-                if (g < groups) {
-                    F af = *reinterpret_cast<const F *>(ap[g] + k);
-                    if (!in) af = F{};
-                    acc[g] = mfma16(af, xf, acc[g]);
-                }
+            for (int i = 0; i < U; ++i) {
+                const bool in = s + i < to && (s + i) * 32 + q * 8 < K;  // K is a multiple of 8
+                const int k = in ? (s + i) * 32 : 0;
+                xf[i] = *reinterpret_cast<const F *>(xp + k);
+                if (!in) xf[i] = F{};
+#pragma unroll
+                for (int g = 0; g < NT; ++g)
+                    if (g < groups) {
+                        af[i][g] = *reinterpret_cast<const F *>(ap[g] + k);
+                        if (!in) af[i][g] = F{};
+                    }
+            }
+#pragma unroll
+            for (int i = 0; i < U; ++i)
+#pragma unroll
+                for (int g = 0; g < NT; ++g)
+                    if (g < groups) acc[g] = mfma16(af[i][g], xf[i], acc[g]);
         }
         if constexpr (SPLIT) {
 #pragma unroll
@@ -127,7 +135,7 @@ __global__ __launch_bounds__(256) void project_kernel(const T *x, int64_t ldx, c
     __shared__ float sums[4][BM][PITCH];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, l32 = lane & 31;
     const int tiles_n = (N + BN - 1) / BN, tile_n = blockIdx.x % tiles_n, tile_m = blockIdx.x / tiles_n;
-    const int ksteps = (K + 15) >> 4, per = (ksteps + 3) >> 2, from = wave * per, to = min(ksteps, from + per);
+    const int ksteps = project_ksteps(K), used = (K + 15) >> 4, per = (used + 3) >> 2, from = wave * per, to = min(used, from + per);
     int64_t row[TM];
     const T *xp[TM], *wp[TN];
 #pragma unroll
@@ -143,22 +151,27 @@ __global__ __launch_bounds__(256) void project_kernel(const T *x, int64_t ldx, c
     for (int mi = 0; mi < TM; ++mi)
 #pragma unroll
         for (int ni = 0; ni < TN; ++ni) acc[mi][ni] = f32x16{};
-#pragma unroll 4
-    for (int s = from; s < to; ++s) {
-        const bool in = s * 16 + half * 8 < K;
-        const int k = in ? s * 16 : 0;
-        F xf[TM], wf[TN];
+    constexpr int U = TM * TN > 1 ? 4 : 6;  // steps whose operands are on their way together
+    for (int s = from; s < to; s += U) {
+        F xf[U][TM], wf[U][TN];
 #pragma unroll
-        for (int ni = 0; ni < TN; ++ni) wf[ni] = *reinterpret_cast<const F *>(wp[ni] + (size_t)s * 512);
+        for (int i = 0; i < U; ++i) {
+            const bool in = s + i < to && (s + i) * 16 + half * 8 < K;
+            const int k = in ? (s + i) * 16 : 0;
 #pragma unroll
-        for (int mi = 0; mi < TM; ++mi) {
-            xf[mi] = *reinterpret_cast<const F *>(xp[mi] + k);
-            if (!in) xf[mi] = F{};
+            for (int ni = 0; ni < TN; ++ni) wf[i][ni] = *reinterpret_cast<const F *>(wp[ni] + (size_t)min(s + i, to - 1) * 512);
+#pragma unroll
+            for (int mi = 0; mi < TM; ++mi) {
+                xf[i][mi] = *reinterpret_cast<const F *>(xp[mi] + k);
+                if (!in) xf[i][mi] = F{};
+            }
         }
 #pragma unroll
-        for (int mi = 0; mi < TM; ++mi)
+        for (int i = 0; i < U; ++i)
 #pragma unroll
-            for (int ni = 0; ni < TN; ++ni) acc[mi][ni] = mfma32(wf[ni], xf[mi], acc[mi][ni]);
+            for (int mi = 0; mi < TM; ++mi)
+#pragma unroll
+                for (int ni = 0; ni < TN; ++ni) acc[mi][ni] = mfma32(wf[i][ni], xf[i][mi], acc[mi][ni]);
     }
 #pragma unroll
     for (int mi = 0; mi < TM; ++mi)
@@ -300,6 +313,13 @@ __global__ __launch_bounds__(256) void outer_sum_kernel(const float *partial, co
     }
 }
 
+template <class K>
+int allow_lds(K kernel, int bytes)
+{
+    LEANN_HIP(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes));
+    return LEANN_OK;
+}
+
 template <class F>
 int with_half_type(int dtype, F f)
 {
@@ -359,6 +379,15 @@ void enqueue_project(leann_ctx *ctx, const leann_adapter_rows *rows, const T *x,
         hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, ctx->stream, x, ldx, w, bias, N, K, rows->row_of, (int)rows->T, rows->run_ptr,
                            rows->runs, compact, low, rows->max_rank, up, out, ldo);
     };
+    if (K >= 256 && tiles64 >= ctx->num_cus * 8) {
+        typedef ProjectCfg<2, 4, 2> Cfg;
+        const int tiles_n = (N + Cfg::BN - 1) / Cfg::BN;
+        const int64_t tiles = (rows->T + Cfg::BM - 1) / Cfg::BM * tiles_n;
+        hipLaunchKernelGGL((project_large_kernel<T, 2, 4, 2>), dim3((unsigned)std::min<int64_t>((tiles + 7) / 8 * 8, ctx->num_cus)), dim3(512), Cfg::SMEM,
+                           ctx->stream, x, ldx, w, bias, N, K, rows->row_of, (int)rows->T, rows->run_ptr, rows->runs, compact, low, rows->max_rank, up,
+                           out, ldo, tiles_n, tiles_n);
+        return;
+    }
     if (tiles64 < ctx->num_cus) go(project_kernel<T, 1, 1>, (int64_t)T32 * ((N + 31) / 32));
     else go(project_kernel<T, 2, 2>, tiles64);
 }
@@ -422,7 +451,7 @@ int make_rows(leann_ctx *ctx, const int32_t *rows_of_request, const int32_t *ada
         adapters[a].y = (int)chunks.size() - adapters[a].x;
         for (int64_t s = from; s < to;) {
             const int64_t group = s / 32, end = std::min<int64_t>(to, (group + 1) * 32);
-            runs.push_back(int4{a, (int)(s - group * 32) | (int)(end - group * 32) << 8 | r << 16, bits(scale[a]), number});
+            runs.push_back(int4{a, (int)s, (int)(end - s) | r << 8 | (int)((uint32_t)number << 16), bits(scale[a])});
             ++run_ptr[group + 1];
             s = end;
         }
@@ -460,6 +489,12 @@ int make_rows(leann_ctx *ctx, const int32_t *rows_of_request, const int32_t *ada
 }
 
 }  // namespace
+
+int adapter_init_device()
+{
+    LEANN_TRY(allow_lds(project_large_kernel<bf16_t, 2, 4, 2>, ProjectCfg<2, 4, 2>::SMEM));
+    return allow_lds(project_large_kernel<f16_t, 2, 4, 2>, ProjectCfg<2, 4, 2>::SMEM);
+}
 
 extern "C" {
 
@@ -501,7 +536,7 @@ int leann_projection_create(leann_ctx *ctx, const void *w_dev, const float *bias
     p->dtype = dtype;
     p->n_out = n_out;
     p->n_in = n_in;
-    auto packed = [&](int N, int K) { return (size_t)((N + 31) / 32) * ((K + 15) / 16) * 1024; };
+    auto packed = [&](int N, int K) { return (size_t)((N + 31) / 32) * project_ksteps(K) * 1024; };
     int rc = ctx->reserve(p->w, packed(n_out, n_in));
     if (rc == LEANN_OK && with_gradient) rc = ctx->reserve(p->wt, packed(n_in, n_out));
     if (rc == LEANN_OK && bias_dev) rc = ctx->reserve(p->bias, n_out * sizeof(float));

@@ -127,6 +127,7 @@ int enc_pack_weights(leann_ctx *ctx, const bf16_t *W, int N, int K, bf16_t *pack
 int enc_ln_blocks_per_cu(int d, int *out);  // resident blocks of the LayerNorm kernel for rows of d elements per CU on the current device
 int pq_init_device();
 int search_init_device();
+int adapter_init_device();
 
 // ---- encoder.hip
 // Embeds the chunks named by ids_dev[0..n) (NULL: first_id .. first_id+n) into out[n][d] (fp32), in passes of at

@@ -6,6 +6,7 @@ namespace {
 
 typedef _Float16 f16_t;
 typedef __attribute__((__vector_size__(8 * sizeof(_Float16)))) _Float16 f16x8;
+typedef __attribute__((__vector_size__(4 * sizeof(_Float16)))) _Float16 f16x4;
 typedef __attribute__((__vector_size__(8 * sizeof(float)))) float f32x8;
 
 template <class T>

@@ -273,3 +273,46 @@ def test_refusals(ctx):
     L.leann_adapter_rows_free(rows)
     L.leann_projection_free(None)
     L.leann_adapter_rows_free(None)
+
+
+LARGE = {
+    # one adapter; runs that end inside every tile; single rows among long requests; rows beyond the last tile
+    "one adapter": ([11000], [0], [16]),
+    "many runs": ([70, 1, 33, 400, 129, 64] * 18, [(5 * i) % 13 - 1 for i in range(108)], [16, 3, 40, 128, 64, 1, 24, 17, 8, 100, 32, 9]),
+    "few adapted": ([9000, 5, 2500, 300], [-1, 0, -1, 1], [8, 33]),
+}
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("batch", LARGE)
+@pytest.mark.parametrize("n_in,n_out", [(256, 1000), (776, 768), (768, 1160)])
+def test_large_batches(ctx, batch, n_in, n_out, dtype):
+    """Tiles of 256 rows, several per block."""
+    import torch
+    say("large batch", batch, n_in, n_out, dtype)
+    BATCHES[batch] = LARGE[batch]
+    p = Problem(ctx, batch, n_in, n_out, dtype, pad=8)
+    del BATCHES[batch]
+    bias = p.bias.double().cpu().numpy()
+    want, low64 = plain64.project(p.x64, p.w64, bias, p.down64, p.up64, *p.plan)
+    _, mag, mag_low = sizes(p)
+    out, low = p.forward(keep=True)
+    close(low, low64, "float32", steps(n_in) * mag_low, "low")
+    close(out, want, dtype, (steps(n_in) + steps(p.R) + 2.0 ** -16) * mag, "out")
+    a = np.abs
+    low64 = low.double().cpu().numpy()
+    want = plain64.project_backward(p.dout64, p.x64, low64, p.w64, p.down64, p.up64, *p.plan)
+    mag = plain64.project_backward(a(p.dout64), a(p.x64), a(low64), a(p.w64), a(p.down64), a(p.up64), p.lengths, p.of, p.ranks, a(p.plan[3]))
+    dx, ddown, dup = p.backward(low)
+    close(dx, want[0], dtype, (steps(n_out) + steps(p.R) + 2.0 ** -16) * mag[0], "dx")
+    close(ddown, want[1], "float32", (steps(n_out) + steps(p.T) + 2.0 ** -22) * mag[1], "ddown")
+    close(dup, want[2], "float32", (steps(p.T) + 2.0 ** -22) * mag[2], "dup")
+    # another request's infinities
+    sick = p.of[0] if p.of[0] >= 0 else p.of[1]
+    rest = torch.ones(p.T, dtype=torch.bool, device="cuda:0")
+    for o, rows in plain64.request_rows(p.lengths, p.of):
+        if o == sick:
+            rest[rows] = False
+    p.up[sick], p.down[sick] = float("inf"), float("nan")
+    assert bool((p.forward()[rest] == out[rest]).all())
+    p.close()
