@@ -211,106 +211,129 @@ __device__ inline void transpose8(const u32x4 (&in)[8], u32x4 (&out)[8])
             out[f][p] = __builtin_amdgcn_perm(in[2 * p + 1][f >> 1], in[2 * p][f >> 1], f & 1 ? 0x07060302 : 0x05040100);
 }
 
-// Sixteen rows' share of sum over rows of h[row][r] p[row][c], to 24 bits of h: three pieces of it; fp16 elements are two bf16 pieces exactly.
-__device__ inline f32x16 outer_step(const bf16x8 (&h)[3], const bf16x8 &p, f32x16 c)
+// 32 rows' share of sum over rows of h[row][r] p[row][c], to 24 bits of h: three pieces of it; fp16 elements are two bf16 pieces exactly.
+__device__ inline f32x4 outer_step(const bf16x8 (&h)[3], const bf16x8 &p, f32x4 c)
 {
-    c = mfma32(h[2], p, c);
-    c = mfma32(h[1], p, c);
-    return mfma32(h[0], p, c);
+    c = mfma16(h[2], p, c);
+    c = mfma16(h[1], p, c);
+    return mfma16(h[0], p, c);
 }
-__device__ inline f32x16 outer_step(const bf16x8 (&h)[3], const f16x8 &p, f32x16 c)
+__device__ inline f32x4 outer_step(const bf16x8 (&h)[3], const f16x8 &p, f32x4 c)
 {
     f32x8 v = __builtin_convertvector(p, f32x8);
     const bf16x8 p1 = take_piece(v), p2 = take_piece(v);
-    c = mfma32(h[2], p1, c);
-    c = mfma32(h[1], p2, c);
-    c = mfma32(h[1], p1, c);
-    c = mfma32(h[0], p2, c);
-    return mfma32(h[0], p1, c);
+    c = mfma16(h[2], p1, c);
+    c = mfma16(h[1], p2, c);
+    c = mfma16(h[1], p1, c);
+    c = mfma16(h[0], p2, c);
+    return mfma16(h[0], p1, c);
 }
 
 // partial[chunk][r][c] = sum over the chunk's rows of low[row][r] p[row][c]: c < K from x and the low-rank gradients (down's), then N from dout and the
-// low-rank activations (up's).  A block takes 256 columns and 32 ranks; a lane reads 16 bytes of a row and turns eight rows of them, in registers,
-// into the MFMA operands of its eight columns.
-template <class T>
+// low-rank activations (up's).  A block takes 128 columns and 16 NR ranks, its wavefronts 32 rows each in turn; a lane reads 16 bytes of a row and turns
+// eight rows of them, in registers, into the MFMA operands of its eight columns.  The next rows are on their way while these are multiplied, and the
+// numbers of those after them.
+template <class T, int NR>
 __global__ __launch_bounds__(256) void outer_kernel(const T *x, int64_t ldx, const T *dout, int64_t ldd, const float *grad_low, const float *low, int R,
                                                     int K, int N, const int32_t *row_of, const int4 *chunks, float *partial)
 {
-    __shared__ float sums[32][256];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, l32 = lane & 31;
-    const int strips_k = (K + 255) / 256, strips = strips_k + (N + 255) / 256, strip = blockIdx.x % strips;
+    __shared__ float sums[16 * NR][128];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, j = lane & 15;
+    const int strips_k = (K + 127) / 128, strips = strips_k + (N + 127) / 128, strip = blockIdx.x % strips;
     const int4 chunk = chunks[blockIdx.x / strips];
-    const int n = chunk.z & 0xffff, rank = chunk.z >> 16, r0 = blockIdx.y * 32;
+    const int n = chunk.z & 0xffff, rank = chunk.z >> 16, r0 = blockIdx.y * 16 * NR;
     if (r0 >= rank) return;
     const bool of_x = strip < strips_k;
     const T *p = of_x ? x : dout;
     const int64_t ld = of_x ? ldx : ldd;
     const float *h = of_x ? grad_low : low;
-    const int C = of_x ? K : N, c0 = (of_x ? strip : strip - strips_k) * 256, col = c0 + l32 * 8;
-    const bool has_col = col < C, has_rank = r0 + l32 < rank;
-    f32x16 acc[8];
+    const int C = of_x ? K : N, c0 = (of_x ? strip : strip - strips_k) * 128, col = c0 + j * 8;
+    const bool has_col = col < C;
+    f32x4 acc[NR][8];
 #pragma unroll
-    for (int f = 0; f < 8; ++f) acc[f] = f32x16{};
-    for (int base = wave * 16; base < n; base += 64) {
-        u32x4 d[8], t[8];
-        f32x8 hv;
+    for (int g = 0; g < NR; ++g)
+#pragma unroll
+        for (int f = 0; f < 8; ++f) acc[g][f] = f32x4{};
+    int row[8];
+    u32x4 d[8];
+    f32x8 hv[NR];
+    auto number = [&](int base) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) row[i] = row_of[chunk.y + min(base + q * 8 + i, n - 1)];
+    };
+    auto request = [&](int base) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const int at = base + half * 8 + i;
-            const int64_t row = row_of[chunk.y + min(at, n - 1)];
-            d[i] = at < n && has_col ? *reinterpret_cast<const u32x4 *>(p + row * ld + col) : u32x4{};
-            hv[i] = at < n && has_rank ? h[row * R + r0 + l32] : 0.f;
+            const bool in = base + q * 8 + i < n;
+            d[i] = in && has_col ? *reinterpret_cast<const u32x4 *>(p + row[i] * ld + col) : u32x4{};
+#pragma unroll
+            for (int g = 0; g < NR; ++g) hv[g][i] = in && r0 + g * 16 + j < rank ? h[(int64_t)row[i] * R + r0 + g * 16 + j] : 0.f;
         }
-        bf16x8 piece[3];
+    };
+    number(wave * 32);
+    request(wave * 32);
+    number(wave * 32 + 128);
+    for (int base = wave * 32; base < n; base += 128) {
+        u32x4 t[8];
+        bf16x8 piece[NR][3];
 #pragma unroll
-        for (int i = 0; i < 3; ++i) piece[i] = take_piece(hv);
+        for (int g = 0; g < NR; ++g)
+#pragma unroll
+            for (int i = 0; i < 3; ++i) piece[g][i] = take_piece(hv[g]);
         transpose8(d, t);
+        request(base + 128);
+        number(base + 256);
 #pragma unroll
-        for (int f = 0; f < 8; ++f) acc[f] = outer_step(piece, __builtin_bit_cast(typename Frag<T>::type, t[f]), acc[f]);
+        for (int f = 0; f < 8; ++f)
+#pragma unroll
+            for (int g = 0; g < NR; ++g) acc[g][f] = outer_step(piece[g], __builtin_bit_cast(typename Frag<T>::type, t[f]), acc[g][f]);
     }
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < 4; ++w) {  // the wavefronts' sums, in order
         if (wave == w)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                f32x8 v;
+            for (int g = 0; g < NR; ++g)
 #pragma unroll
-                for (int f = 0; f < 8; ++f) v[f] = acc[f][e];
-                f32x8 *to = reinterpret_cast<f32x8 *>(&sums[8 * (e >> 2) + 4 * half + (e & 3)][l32 * 8]);
-                *to = w ? *to + v : v;
-            }
+                for (int e = 0; e < 4; ++e) {
+                    f32x8 v;
+#pragma unroll
+                    for (int f = 0; f < 8; ++f) v[f] = acc[g][f][e];
+                    f32x8 *to = reinterpret_cast<f32x8 *>(&sums[g * 16 + q * 4 + e][j * 8]);
+                    *to = w ? *to + v : v;
+                }
         __syncthreads();
     }
     float *to = partial + (size_t)(blockIdx.x / strips) * R * (K + N) + (of_x ? 0 : K) + c0;
-    for (int i = threadIdx.x; i < 32 * 64; i += 256) {
-        const int r = i >> 6, c = (i & 63) * 4;
+    for (int i = threadIdx.x; i < 16 * NR * 32; i += 256) {
+        const int r = i >> 5, c = (i & 31) * 4;
         if (r0 + r < rank && c0 + c < C) *reinterpret_cast<f32x4 *>(to + (size_t)(r0 + r) * (K + N) + c) = *reinterpret_cast<const f32x4 *>(&sums[r][c]);
     }
 }
 
 // ddown[a][r][k] and dup[a][n][r] from the chunks' sums, in their order; 0 where an adapter has no rows, and beyond its rank.
-__global__ __launch_bounds__(256) void outer_sum_kernel(const float *partial, const int4 *adapters, int R, int K, int N, float *ddown, float *dup)
+__global__ __launch_bounds__(1024) void outer_sum_kernel(const float *partial, const int4 *adapters, int R, int K, int N, float *ddown, float *dup)
 {
     __shared__ float tile[32][33];
     const int4 a = adapters[blockIdx.z];
-    const int c0 = blockIdx.x * 32, r0 = blockIdx.y * 32, tx = threadIdx.x & 31, ty = threadIdx.x >> 5, c = c0 + tx;
-    const float scale = __int_as_float(a.w);
-    float s[4] = {};
+    const int c0 = blockIdx.x * 32, r0 = blockIdx.y * 32, tx = threadIdx.x & 31, ty = threadIdx.x >> 5, c = c0 + tx, r = r0 + ty;
+    float s = 0.f;
+    if (r < a.z && c < K + N) {
+        const float *from = partial + ((size_t)a.x * R + r) * (K + N) + c;
+        const size_t step = (size_t)R * (K + N);
+        for (int i = 0; i < a.y; i += 8) {
+            float v[8];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int r = r0 + ty + 8 * j;
-        if (r < a.z && c < K + N)
-            for (int i = 0; i < a.y; ++i) s[j] += partial[((size_t)(a.x + i) * R + r) * (K + N) + c];
-        s[j] *= scale;
-        if (r < R && c < K) ddown[((size_t)blockIdx.z * R + r) * K + c] = s[j];
-        tile[ty + 8 * j][tx] = s[j];
+            for (int j = 0; j < 8; ++j) v[j] = i + j < a.y ? from[(i + j) * step] : 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s += v[j];
+        }
     }
+    s *= __int_as_float(a.w);
+    if (r < R && c < K) ddown[((size_t)blockIdx.z * R + r) * K + c] = s;
     if (c0 + 32 <= K) return;
+    tile[ty][tx] = s;
     __syncthreads();
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int n = c0 + ty + 8 * j - K;
-        if (n >= 0 && n < N && r0 + tx < R) dup[((size_t)blockIdx.z * N + n) * R + r0 + tx] = tile[tx][ty + 8 * j];
-    }
+    const int n = c0 + ty - K;
+    if (n >= 0 && n < N && r0 + tx < R) dup[((size_t)blockIdx.z * N + n) * R + r0 + tx] = tile[tx][ty];
 }
 
 template <class K>
@@ -390,6 +413,19 @@ void enqueue_project(leann_ctx *ctx, const leann_adapter_rows *rows, const T *x,
     }
     if (tiles64 < ctx->num_cus) go(project_kernel<T, 1, 1>, (int64_t)T32 * ((N + 31) / 32));
     else go(project_kernel<T, 2, 2>, tiles64);
+}
+
+template <class T>
+void enqueue_outer(leann_ctx *ctx, const leann_adapter_rows *rows, const T *x, int64_t ldx, const T *dout, int64_t ldd, const float *grad_low,
+                   const float *low, int K, int N, float *partial)
+{
+    const int R = rows->max_rank, strips = (K + 127) / 128 + (N + 127) / 128;
+    auto go = [&](auto kernel, int ranks) {
+        hipLaunchKernelGGL(kernel, dim3(strips * rows->n_chunks, (R + ranks - 1) / ranks), dim3(256), 0, ctx->stream, x, ldx, dout, ldd, grad_low, low, R,
+                           K, N, rows->row_of, rows->chunks, partial);
+    };
+    if (R <= 16) go(outer_kernel<T, 1>, 16);
+    else go(outer_kernel<T, 2>, 32);
 }
 
 int check_pair(const char *call, const leann_ctx *ctx, const leann_projection *proj, const leann_adapter_rows *rows)
@@ -690,9 +726,8 @@ int leann_adapter_project_backward(leann_ctx *ctx, const leann_projection *proj,
             enqueue_project<T>(ctx, rows, (const T *)dout_dev, ldd, (const T *)proj->wt.p, nullptr, K, N, grad_low, down_t, 1, (T *)dx_dev, lddx);
         if (ddown_dev) {
             if (rows->n_chunks)
-                hipLaunchKernelGGL(outer_kernel<T>, dim3(((K + 255) / 256 + (N + 255) / 256) * rows->n_chunks, (R + 31) / 32), dim3(256), 0, ctx->stream,
-                                   (const T *)x_dev, ldx, (const T *)dout_dev, ldd, grad_low, low_dev, R, K, N, rows->row_of, rows->chunks, partial);
-            hipLaunchKernelGGL(outer_sum_kernel, dim3((K + N + 31) / 32, (R + 31) / 32, rows->n_adapters), dim3(256), 0, ctx->stream, partial,
+                enqueue_outer<T>(ctx, rows, (const T *)x_dev, ldx, (const T *)dout_dev, ldd, grad_low, low_dev, K, N, partial);
+            hipLaunchKernelGGL(outer_sum_kernel, dim3((K + N + 31) / 32, (R + 31) / 32, rows->n_adapters), dim3(1024), 0, ctx->stream, partial,
                                rows->adapters, R, K, N, ddown_dev, dup_dev);
         }
         return launched(call);

@@ -251,20 +251,33 @@ __global__ __launch_bounds__(WPR == 1 ? 256 : WPR * 64) void layernorm_grad_kern
     }
 }
 
-// dgamma and dbeta from the blocks' sums: 32 columns per block, 32 threads per column, always in the same order.
+// dgamma and dbeta from the blocks' sums: 16 columns per block, four lanes to a row of them, 256 rows at a time.  Always in the same order.
 __global__ __launch_bounds__(1024) void column_sum_kernel(const float *partial, int blocks, int cols, float *dgamma, float *dbeta)
 {
-    __shared__ float sums[32][33];
-    const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5, c = blockIdx.x * 32 + tx;
-    float s = 0.f;
-    if (c < 2 * cols)
-        for (int i = ty; i < blocks; i += 32) s += partial[(size_t)i * 2 * cols + c];
-    sums[ty][tx] = s;
+    __shared__ float sums[256][17];
+    const int tx = threadIdx.x & 3, ty = threadIdx.x >> 2, c = blockIdx.x * 16 + tx * 4, width = 2 * cols;
+    f32x4 s = {};
+    for (int i = ty; i < blocks; i += 256) {
+        f32x4 v = {};
+        if (c + 4 <= width) {
+            __builtin_memcpy(&v, partial + (size_t)i * width + c, sizeof(v));
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = c + e < width ? partial[(size_t)i * width + c + e] : 0.f;
+        }
+        s += v;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sums[ty][tx * 4 + e] = s[e];
+    for (int half = 128; half >= 1; half >>= 1) {
+        __syncthreads();
+        for (int i = threadIdx.x; i < half * 16; i += 1024) sums[i >> 4][i & 15] += sums[(i >> 4) + half][i & 15];
+    }
     __syncthreads();
-    if (ty == 0 && c < 2 * cols) {
-        s = 0.f;
-        for (int i = 0; i < 32; ++i) s += sums[i][tx];
-        (c < cols ? dgamma[c] : dbeta[c - cols]) = s;
+    if (threadIdx.x < 16) {
+        const int to = blockIdx.x * 16 + threadIdx.x;
+        if (to < cols) dgamma[to] = sums[0][threadIdx.x];
+        else if (to < width) dbeta[to - cols] = sums[0][threadIdx.x];
     }
 }
 
@@ -451,7 +464,7 @@ int leann_layernorm_backward(leann_ctx *ctx, const void *dout_dev, int64_t ldd, 
         return with_row_shape(cols, [&](auto wpr, auto nc) {
             constexpr int WPR = decltype(wpr)::value, NC = decltype(nc)::value;
             const int64_t wanted = WPR == 1 ? (rows + 3) / 4 : rows;
-            const unsigned grid = (unsigned)std::min<int64_t>(wanted, (int64_t)ctx->num_cus * 4);
+            const unsigned grid = (unsigned)std::min<int64_t>(wanted, (int64_t)ctx->num_cus * 2);
             LEANN_TRY(ctx->reserve(ctx->op_work, std::max<size_t>(1, (size_t)grid * 2 * cols * sizeof(float))));
             float *partial = (float *)ctx->op_work.p;
             if (grid) {
@@ -463,7 +476,7 @@ int leann_layernorm_backward(leann_ctx *ctx, const void *dout_dev, int64_t ldd, 
                 if (d.below) go(layernorm_grad_kernel<T, WPR, NC, true>);
                 else go(layernorm_grad_kernel<T, WPR, NC, false>);
             }
-            hipLaunchKernelGGL(column_sum_kernel, dim3((2 * cols + 31) / 32), dim3(1024), 0, ctx->stream, partial, (int)grid, (int)cols, dgamma_dev,
+            hipLaunchKernelGGL(column_sum_kernel, dim3((2 * cols + 15) / 16), dim3(1024), 0, ctx->stream, partial, (int)grid, (int)cols, dgamma_dev,
                                dbeta_dev);
             return launched(call);
         });
