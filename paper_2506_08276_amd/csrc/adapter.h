@@ -21,6 +21,8 @@ struct leann_adapter_rows {
     const int32_t *row_of = nullptr;     // [T, up to a multiple of 256: the last row again]
     const int32_t *run_ptr = nullptr;    // [32-slot groups + 1]
     const int4 *runs = nullptr;          // adapter, first slot, slots | rank << 8 | number among the used adapters << 16, scale
+    const int32_t *seg_ptr = nullptr;    // [256-slot tiles + 1]
+    const int4 *segs = nullptr;          // a tile's adapters: first slot, slot behind the last, rank, number among the used adapters
     const int4 *tiles = nullptr;         // adapter, first slot, slots | rank << 16, number among the used adapters
     const int4 *chunks = nullptr;        // likewise, by adapter
     const int4 *adapters = nullptr;      // [n_adapters] first chunk, chunks, rank, scale
@@ -38,11 +40,13 @@ template <>
 struct Frag<bf16_t> {
     typedef bf16x8 type;
     typedef bf16x4 four;
+    static constexpr int PIECES = 1;  // bf16 numbers that hold one exactly
 };
 template <>
 struct Frag<f16_t> {
     typedef f16x8 type;
     typedef f16x4 four;
+    static constexpr int PIECES = 2;
 };
 
 __device__ inline f32x16 mfma32(const bf16x8 &a, const bf16x8 &b, const f32x16 &c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
@@ -58,57 +62,39 @@ __device__ inline bf16x8 take_piece(f32x8 &v)
     return p;
 }
 
-// One step of 16 ranks of an adapter's part, acc += up low^T, on bf16 MFMAs for both types: the low-rank activations are fp32 and may leave
-// fp16's range.  They go in as two pieces of 8 bits (2^-17 of each term, where the output's own rounding is 2^-8 or 2^-11); fp16 weights are
-// two pieces exactly, of whose four products the smallest is left out.
-__device__ inline f32x16 adapter_step(const bf16x8 &up, const bf16x8 &h1, const bf16x8 &h2, f32x16 c)
-{
-    c = mfma32(up, h2, c);
-    return mfma32(up, h1, c);
-}
-__device__ inline f32x16 adapter_step(const f16x8 &up, const bf16x8 &h1, const bf16x8 &h2, f32x16 c)
-{
-    f32x8 u = __builtin_convertvector(up, f32x8);
-    const bf16x8 u1 = take_piece(u), u2 = take_piece(u);
-    c = mfma32(u1, h2, c);
-    c = mfma32(u2, h1, c);
-    return mfma32(u1, h1, c);
-}
+// Low-rank activations go into the matrix instructions as two pieces of 8 bits, 16 ranks of a row as 32 numbers, first pieces first: [slot][ranks / 16][32],
+// times the adapter's scale.  On bf16 MFMAs for both types: they are sums in fp32 and may leave fp16's range.  What is left out is 2^-17 of each term, where the
+// output's own rounding is 2^-9 or 2^-12.  `up` is laid out anew in each call, as its values change from step to step in training: in operand order
+// [used adapter][columns / 32][ranks / 16][piece][lane][8], zeros beyond rank and columns; fp16 numbers are two pieces exactly.
+__host__ __device__ inline int rank_groups(int R) { return (R + 15) >> 4; }
 
-// The adapters' part of one 32-slot group's tiles: acc[ni] += scale * up[columns of tile ni] low[slots]^T for every run of the group that is
-// number `first`, `first + step`, ...  A lane holds one slot of the output, so a run that is not the whole group changes only the lanes that are its own:
-// another request's infinities stay with it.
-template <class T, int TN>
-__device__ inline void add_adapters(f32x16 (&acc)[TN], const int32_t *run_ptr, const int4 *runs, int group, int first, int step, const float *low_row,
-                                    const T *up, int R, int N, int col, bool compact)
+// The adapters' part of one 32-slot group's tiles: acc[ni] += up[columns of tile ni] pieces[slots]^T for every run of the group that is number `first`,
+// `first + step`, ...  A lane holds one slot of the output, so a run that is not the whole group changes only the lanes that are its own: another request's
+// infinities stay with it.
+template <int TN, int UP>
+__device__ inline void add_adapters(f32x16 (&acc)[TN], const int32_t *run_ptr, const int4 *runs, int group, int first, int step, const bf16_t *pieces,
+                                    const bf16_t *up, int R16, int column_tiles, int column_tile)
 {
     const int lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31;
     const int begin = run_ptr[group], count = run_ptr[group + 1] - begin;
     for (int i = first; i < count; i += step) {
         const int4 run = runs[begin + i];
-        const int rank = run.z >> 8 & 255, from = run.y - group * 32, to = from + (run.z & 255);
-        const float scale = __int_as_float(run.w);
+        const int steps = rank_groups(run.z >> 8 & 255), from = run.y - group * 32, to = from + (run.z & 255);
         const bool own = l32 >= from && l32 < to;
-        const T *u = up + (size_t)(compact ? (uint32_t)run.z >> 16 : (uint32_t)run.x) * N * R;
+        const bf16_t *u = up + ((size_t)((uint32_t)run.z >> 16) * column_tiles * R16 * UP * 64 + lane) * 8;
         f32x16 sum[TN];
 #pragma unroll
         for (int ni = 0; ni < TN; ++ni) sum[ni] = acc[ni];
-        for (int k = 0; k < rank; k += 16) {
-            const int at = k + half * 8, n = rank - at;  // n: of this lane's eight ranks those that exist
-            f32x8 h = {};
-            if (n > 0) __builtin_memcpy(&h, low_row + at, sizeof(h));  // zeros beyond the rank
-            h *= scale;
-            const bf16x8 h1 = take_piece(h), h2 = take_piece(h);
+        for (int k = 0; k < steps; ++k) {
+            const bf16x8 h1 = *reinterpret_cast<const bf16x8 *>(pieces + k * 32 + half * 8), h2 = *reinterpret_cast<const bf16x8 *>(pieces + k * 32 + 16 + half * 8);
 #pragma unroll
-            for (int ni = 0; ni < TN; ++ni) {
-                typename Frag<T>::type f = {};
-                if (n > 0) {
-                    f = *reinterpret_cast<const typename Frag<T>::type *>(u + (size_t)min(col + ni * 32 + l32, N - 1) * R + at);
+            for (int ni = 0; ni < TN; ++ni)
 #pragma unroll
-                    for (int j = 1; j < 8; ++j) f[j] = j < n ? f[j] : (T)0.f;  // what lies beyond the rank may be anything
+                for (int e = 0; e < UP; ++e) {
+                    const bf16x8 f = *reinterpret_cast<const bf16x8 *>(u + (((size_t)min(column_tile + ni, column_tiles - 1) * R16 + k) * UP + e) * 512);
+                    sum[ni] = mfma32(f, h2, sum[ni]);
+                    sum[ni] = mfma32(f, h1, sum[ni]);
                 }
-                sum[ni] = adapter_step(f, h1, h2, sum[ni]);
-            }
         }
 #pragma unroll
         for (int ni = 0; ni < TN; ++ni)

@@ -29,38 +29,68 @@ __global__ __launch_bounds__(256) void pack_kernel(const T *w, int N, int K, int
     }
 }
 
-// The used adapters' matrices transposed: down[r][k] -> down_t[k][r], up[n][r] -> up_t[r][n], tiles of 32 x 32.
-template <class T>
-__global__ __launch_bounds__(256) void transpose_kernel(const T *down, const T *up, const int32_t *used, int R, int K, int N, T *down_t, T *up_t)
+// up[n][r] (IS_UP) or down[r][n] of the used adapters in the order that the products read, see adapter.h: one piece of 8 ranks of a column per thread and step.
+template <class T, bool IS_UP>
+__device__ inline void lay_out(const T *from, const int32_t *used, const int4 *adapters, int n_used, int R, int N, bf16_t *to, int block, int blocks)
 {
+    constexpr int UP = Frag<T>::PIECES;
+    const int R16 = rank_groups(R), column_tiles = (N + 31) >> 5;
+    const size_t items = (size_t)n_used * column_tiles * R16 * 64;
+    for (size_t i = (size_t)block * 256 + threadIdx.x; i < items; i += (size_t)blocks * 256) {
+        const int lane = (int)(i & 63), k = (int)((i >> 6) % R16), a = used[(i >> 6) / R16 / column_tiles];
+        const int n = (int)((i >> 6) / R16 % column_tiles) * 32 + (lane & 31), r = k * 16 + (lane >> 5) * 8, left = adapters[a].z - r;
+        Raw8<T> v;
+        v.v = typename Vec8<T>::type{};
+        if (n < N && left > 0) {
+            if constexpr (IS_UP) {
+                v.load(from + ((size_t)a * N + n) * R + r, min(left, 8));
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (j < left) v.v[j] = from[((size_t)a * R + r + j) * N + n];
+            }
+        }
+        f32x8 f = v.wide();
+#pragma unroll
+        for (int e = 0; e < UP; ++e) *reinterpret_cast<bf16x8 *>(to + ((i >> 6) * UP * 64 + e * 64 + lane) * 8) = take_piece(f);
+    }
+}
+
+// Before the gradients: `up` of the used adapters transposed (up[n][r] -> up_t[r][n], blocks of 32 x 32), and `down` laid out for the product.
+template <class T>
+__global__ __launch_bounds__(256) void lay_out_kernel(const T *down, const T *up, const int32_t *used, const int4 *adapters, int n_used, int R, int K,
+                                                      int N, T *up_t, bf16_t *down_packed, int transposing)
+{
+    if ((int)blockIdx.x >= transposing) {
+        lay_out<T, false>(down, used, adapters, n_used, R, K, down_packed, blockIdx.x - transposing, gridDim.x - transposing);
+        return;
+    }
     __shared__ T tile[32][34];
-    const int a = used[blockIdx.z], tiles_k = (K + 31) / 32;
-    const bool is_down = (int)blockIdx.x < tiles_k;
-    const int c = (is_down ? blockIdx.x : blockIdx.x - tiles_k) * 32, r = blockIdx.y * 32;  // long side, rank
-    const T *from = is_down ? down + (size_t)a * R * K : up + (size_t)a * N * R;
-    T *to = is_down ? down_t + (size_t)blockIdx.z * R * K : up_t + (size_t)blockIdx.z * N * R;
-    const int C = is_down ? K : N;
+    const int tiles_n = (N + 31) / 32, tiles_r = (R + 31) / 32;
+    const int n0 = blockIdx.x % tiles_n * 32, r0 = blockIdx.x / tiles_n % tiles_r * 32, number = blockIdx.x / tiles_n / tiles_r;
+    const T *from = up + (size_t)used[number] * N * R;
+    T *to = up_t + (size_t)number * N * R;
     const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
-    for (int j = ty; j < 32; j += 8) {  // rows of the source
-        const int row = (is_down ? r : c) + j, col = (is_down ? c : r) + tx;
-        const bool in = is_down ? row < R && col < C : row < C && col < R;
-        if (in) tile[j][tx] = from[(size_t)row * (is_down ? C : R) + col];
-    }
+    for (int j = ty; j < 32; j += 8)
+        if (n0 + j < N && r0 + tx < R) tile[j][tx] = from[(size_t)(n0 + j) * R + r0 + tx];
     __syncthreads();
-    for (int j = ty; j < 32; j += 8) {
-        const int row = (is_down ? c : r) + j, col = (is_down ? r : c) + tx;
-        const bool in = is_down ? row < C && col < R : row < R && col < C;
-        if (in) to[(size_t)row * (is_down ? R : C) + col] = tile[tx][j];
-    }
+    for (int j = ty; j < 32; j += 8)
+        if (r0 + j < R && n0 + tx < N) to[(size_t)(r0 + j) * N + n0 + tx] = tile[tx][j];
 }
 
 // ------------------------------------------------------------------ low-rank activations
 // low[row][r] = sum over k of x[row][k] down[a][r][k] for 16 slots of one adapter, in MFMA 16x16x32: a lane ends with four ranks of one row.
-// SPLIT: a block per tile, whose four wavefronts share K; else a wavefront per tile.
+// They go out as they are, by row (`low`, if wanted), and times the adapter's scale in the pieces that the product reads, by slot.
+// SPLIT: a block per tile, whose four wavefronts share K; else a wavefront per tile.  Blocks from `low_blocks` on lay out `up`.
 template <class T, int NT, bool SPLIT>
 __global__ __launch_bounds__(256) void low_kernel(const T *x, int64_t ldx, const T *down, int R, int K, const int32_t *row_of, const int4 *tiles,
-                                                  int n_tiles, int compact, float *low)
+                                                  int n_tiles, int low_blocks, int compact, float *low, bf16_t *pieces, const int4 *adapters, const T *up,
+                                                  int N, const int32_t *used, int n_used, bf16_t *up_packed)
 {
+    if ((int)blockIdx.x >= low_blocks) {
+        lay_out<T, true>(up, used, adapters, n_used, R, N, up_packed, blockIdx.x - low_blocks, gridDim.x - low_blocks);
+        return;
+    }
     typedef typename Frag<T>::type F;
     __shared__ f32x4 part[SPLIT ? 4 : 1][SPLIT ? NT : 1][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane & 15, q = lane >> 4;
@@ -110,14 +140,25 @@ __global__ __launch_bounds__(256) void low_kernel(const T *x, int64_t ldx, const
         }
     }
     if (j >= n) return;
+    const float scale = rank ? __int_as_float(adapters[tile.x].w) : 0.f;
+    bf16_t *to = pieces + (int64_t)(tile.y + j) * rank_groups(R) * 32;
 #pragma unroll
     for (int g = 0; g < NT; ++g) {
         const int r = g * 16 + q * 4;
-        if (r < R && (!SPLIT || (g & 3) == wave)) {
-            f32x4 v = acc[g];
+        if (SPLIT && (g & 3) != wave) continue;
+        f32x4 v = acc[g];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = r + i < rank ? v[i] : 0.f;
-            *reinterpret_cast<f32x4 *>(low + row * R + r) = v;
+        for (int i = 0; i < 4; ++i) v[i] = r + i < rank ? v[i] : 0.f;
+        if (low && r < R) *reinterpret_cast<f32x4 *>(low + row * R + r) = v;
+        if (r < rank) {
+            v *= scale;
+            const bf16x4 first = __builtin_convertvector(v, bf16x4);
+            v -= __builtin_convertvector(first, f32x4);
+            *reinterpret_cast<bf16x4 *>(to + g * 32 + q * 4) = first;
+            *reinterpret_cast<bf16x4 *>(to + g * 32 + 16 + q * 4) = __builtin_convertvector(v, bf16x4);
+        } else if (g < groups) {
+            *reinterpret_cast<bf16x4 *>(to + g * 32 + q * 4) = bf16x4{};
+            *reinterpret_cast<bf16x4 *>(to + g * 32 + 16 + q * 4) = bf16x4{};
         }
     }
 }
@@ -127,8 +168,8 @@ __global__ __launch_bounds__(256) void low_kernel(const T *x, int64_t ldx, const
 // memory to registers; their sums meet in LDS.
 template <class T, int TM, int TN>
 __global__ __launch_bounds__(256) void project_kernel(const T *x, int64_t ldx, const T *w, const float *bias, int N, int K, const int32_t *row_of,
-                                                      int rows, const int32_t *run_ptr, const int4 *runs, int compact, const float *low, int R,
-                                                      const T *up, T *out, int64_t ldo)
+                                                      int rows, const int32_t *run_ptr, const int4 *runs, const bf16_t *pieces, int R16,
+                                                      const bf16_t *up, T *out, int64_t ldo)
 {
     typedef typename Frag<T>::type F;
     constexpr int BM = 32 * TM, BN = 32 * TN, PITCH = BN + 4;
@@ -176,7 +217,8 @@ __global__ __launch_bounds__(256) void project_kernel(const T *x, int64_t ldx, c
 #pragma unroll
     for (int mi = 0; mi < TM; ++mi)
         if (tile_m * BM + mi * 32 < rows)
-            add_adapters<T, TN>(acc[mi], run_ptr, runs, tile_m * TM + mi, wave, 4, low + row[mi] * R, up, R, N, tile_n * BN, compact);
+            add_adapters<TN, Frag<T>::PIECES>(acc[mi], run_ptr, runs, tile_m * TM + mi, wave, 4,
+                                              pieces + (int64_t)min(tile_m * BM + mi * 32 + l32, rows - 1) * R16 * 32, up, R16, last_ct + 1, tile_n * TN);
 #pragma unroll
     for (int mi = 0; mi < TM; ++mi)
 #pragma unroll
@@ -374,16 +416,20 @@ int check_half_rows(const char *call, const char *what, const void *p, int64_t l
     return LEANN_OK;
 }
 
-// low = x down^T for the adapted rows; with_zeros: zeros for the others, too.
+// What a product's adapters need: the low-rank activations in pieces (and as they are, if wanted; with_zeros: zeros for rows without adapter, too), `up` laid
+// out (up: from here, in the same launch; null: it is there already).
 template <class T>
-void enqueue_low(leann_ctx *ctx, const leann_adapter_rows *rows, const T *x, int64_t ldx, int K, const T *down, int compact, float *low, bool with_zeros)
+void enqueue_low(leann_ctx *ctx, const leann_adapter_rows *rows, const T *x, int64_t ldx, int K, const T *down, int compact, float *low, bool with_zeros,
+                 bf16_t *pieces, const T *up, int N, bf16_t *up_packed)
 {
     const int n = with_zeros ? rows->n_tiles : rows->n_adapted_tiles, R = rows->max_rank;
     if (!n) return;
     const bool split = n < ctx->num_cus * 4;
+    const int low_blocks = split ? n : (n + 3) / 4;
+    const int64_t laying = up ? ((int64_t)rows->n_used * ((N + 31) / 32) * rank_groups(R) * 64 + 255) / 256 : 0;
     auto go = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3(split ? n : (n + 3) / 4), dim3(256), 0, ctx->stream, x, ldx, down, R, K, rows->row_of, rows->tiles, n, compact,
-                           low);
+        hipLaunchKernelGGL(kernel, dim3(low_blocks + (unsigned)std::min<int64_t>(laying, ctx->num_cus * 4)), dim3(256), 0, ctx->stream, x, ldx, down, R,
+                           K, rows->row_of, rows->tiles, n, low_blocks, compact, low, pieces, rows->adapters, up, N, rows->used, rows->n_used, up_packed);
     };
     if (R <= 16) split ? go(low_kernel<T, 1, true>) : go(low_kernel<T, 1, false>);
     else if (R <= 32) split ? go(low_kernel<T, 2, true>) : go(low_kernel<T, 2, false>);
@@ -394,25 +440,31 @@ void enqueue_low(leann_ctx *ctx, const leann_adapter_rows *rows, const T *x, int
 // out = x w^T + bias + the adapters' part
 template <class T>
 void enqueue_project(leann_ctx *ctx, const leann_adapter_rows *rows, const T *x, int64_t ldx, const T *w, const float *bias, int N, int K,
-                     const float *low, const T *up, int compact, T *out, int64_t ldo)
+                     const bf16_t *pieces, const bf16_t *up, T *out, int64_t ldo)
 {
-    const int T32 = (int)((rows->T + 31) / 32), T64 = (int)((rows->T + 63) / 64);
+    const int T32 = (int)((rows->T + 31) / 32), T64 = (int)((rows->T + 63) / 64), R16 = rank_groups(rows->max_rank);
     const int64_t tiles64 = (int64_t)T64 * ((N + 63) / 64);
-    auto go = [&](auto kernel, int64_t blocks) {
-        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, ctx->stream, x, ldx, w, bias, N, K, rows->row_of, (int)rows->T, rows->run_ptr,
-                           rows->runs, compact, low, rows->max_rank, up, out, ldo);
-    };
     if (K >= 256 && tiles64 >= ctx->num_cus * 8) {
         typedef ProjectCfg<2, 4, 2> Cfg;
         const int tiles_n = (N + Cfg::BN - 1) / Cfg::BN;
         const int64_t tiles = (rows->T + Cfg::BM - 1) / Cfg::BM * tiles_n;
         hipLaunchKernelGGL((project_large_kernel<T, 2, 4, 2>), dim3((unsigned)std::min<int64_t>((tiles + 7) / 8 * 8, ctx->num_cus)), dim3(512), Cfg::SMEM,
-                           ctx->stream, x, ldx, w, bias, N, K, rows->row_of, (int)rows->T, rows->run_ptr, rows->runs, compact, low, rows->max_rank, up,
-                           out, ldo, tiles_n, tiles_n);
+                           ctx->stream, x, ldx, w, bias, N, K, rows->row_of, (int)rows->T, rows->seg_ptr, rows->segs, pieces, R16, up, out, ldo, tiles_n,
+                           tiles_n);
         return;
     }
+    auto go = [&](auto kernel, int64_t blocks) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, ctx->stream, x, ldx, w, bias, N, K, rows->row_of, (int)rows->T, rows->run_ptr,
+                           rows->runs, pieces, R16, up, out, ldo);
+    };
     if (tiles64 < ctx->num_cus) go(project_kernel<T, 1, 1>, (int64_t)T32 * ((N + 31) / 32));
     else go(project_kernel<T, 2, 2>, tiles64);
+}
+
+size_t pieces_bytes(const leann_adapter_rows *rows) { return up256((size_t)rows->T * rank_groups(rows->max_rank) * 64 + 64); }  // 64: read past the last one's, see request_pieces
+size_t packed_bytes(const leann_adapter_rows *rows, int N)  // room for fp16's two pieces
+{
+    return up256((size_t)rows->n_used * ((N + 31) / 32) * rank_groups(rows->max_rank) * 2048);
 }
 
 template <class T>
@@ -470,7 +522,8 @@ int make_rows(leann_ctx *ctx, const int32_t *rows_of_request, const int32_t *ada
     // Rows of a chunk: as many as leave some four blocks for each CU (a block takes 256 columns of one), 64 at least, 1024 at most.
     const int chunk_rows = (int)std::min<int64_t>(1024, std::max<int64_t>(64, (adapted / (ctx->num_cus * 2 / 3) + 63) / 64 * 64));
     std::vector<int4> tiles, chunks, runs, adapters(n_adapters);
-    std::vector<int32_t> used, run_ptr((T + 31) / 32 + 1, 0);
+    std::vector<int4> segs;
+    std::vector<int32_t> used, run_ptr((T + 31) / 32 + 1, 0), seg_ptr((T + 255) / 256 + 1, 0);
     auto bits = [](float f) {
         int32_t i;
         memcpy(&i, &f, sizeof(i));
@@ -491,8 +544,15 @@ int make_rows(leann_ctx *ctx, const int32_t *rows_of_request, const int32_t *ada
             ++run_ptr[group + 1];
             s = end;
         }
+        for (int64_t s = from; s < to;) {
+            const int64_t tile = s / 256, end = std::min<int64_t>(to, (tile + 1) * 256);
+            segs.push_back(int4{(int)s, (int)end, r, number});
+            ++seg_ptr[tile + 1];
+            s = end;
+        }
         if (to > from) used.push_back(a);
     }
+    for (size_t g = 1; g < seg_ptr.size(); ++g) seg_ptr[g] += seg_ptr[g - 1];
     for (size_t g = 1; g < run_ptr.size(); ++g) run_ptr[g] += run_ptr[g - 1];
 
     out->device = ctx->device;
@@ -509,7 +569,7 @@ int make_rows(leann_ctx *ctx, const int32_t *rows_of_request, const int32_t *ada
         if (bytes) memcpy(image.data() + at, v.data(), bytes);
         return at;
     };
-    const size_t at[7] = {put(row_of), put(run_ptr), put(runs), put(tiles), put(chunks), put(adapters), put(used)};
+    const size_t at[9] = {put(row_of), put(run_ptr), put(runs), put(tiles), put(chunks), put(adapters), put(used), put(seg_ptr), put(segs)};
     LEANN_TRY(ctx->reserve(out->mem, std::max<size_t>(image.size(), 1)));
     LEANN_HIP(hipMemcpyAsync(out->mem.p, image.data(), image.size(), hipMemcpyHostToDevice, ctx->stream));
     LEANN_HIP(hipStreamSynchronize(ctx->stream));
@@ -521,6 +581,8 @@ int make_rows(leann_ctx *ctx, const int32_t *rows_of_request, const int32_t *ada
     out->chunks = (const int4 *)(base + at[4]);
     out->adapters = (const int4 *)(base + at[5]);
     out->used = (const int32_t *)(base + at[6]);
+    out->seg_ptr = (const int32_t *)(base + at[7]);
+    out->segs = (const int4 *)(base + at[8]);
     return LEANN_OK;
 }
 
@@ -670,16 +732,13 @@ int leann_adapter_project(leann_ctx *ctx, const leann_projection *proj, const le
         return LEANN_EINVAL;
     }
     LEANN_HIP(hipSetDevice(ctx->device));
-    float *low = low_dev;
-    if (!low) {
-        LEANN_TRY(ctx->reserve(ctx->op_work, (size_t)rows->T * rows->max_rank * sizeof(float)));
-        low = (float *)ctx->op_work.p;
-    }
+    const int N = proj->n_out, K = proj->n_in;
+    LEANN_TRY(ctx->reserve(ctx->op_work, pieces_bytes(rows) + packed_bytes(rows, N)));
+    bf16_t *pieces = (bf16_t *)ctx->op_work.p, *packed = (bf16_t *)((char *)ctx->op_work.p + pieces_bytes(rows));
     return with_half_type(proj->dtype, [&](auto *type) {
         typedef std::remove_pointer_t<decltype(type)> T;
-        enqueue_low<T>(ctx, rows, (const T *)x_dev, ldx, proj->n_in, (const T *)down_dev, 0, low, low_dev != nullptr);
-        enqueue_project<T>(ctx, rows, (const T *)x_dev, ldx, (const T *)proj->w.p, (const float *)proj->bias.p, proj->n_out, proj->n_in, low,
-                           (const T *)up_dev, 0, (T *)out_dev, ldo);
+        enqueue_low<T>(ctx, rows, (const T *)x_dev, ldx, K, (const T *)down_dev, 0, low_dev, low_dev != nullptr, pieces, (const T *)up_dev, N, packed);
+        enqueue_project<T>(ctx, rows, (const T *)x_dev, ldx, (const T *)proj->w.p, (const float *)proj->bias.p, N, K, pieces, packed, (T *)out_dev, ldo);
         return launched(call);
     });
 }
@@ -709,21 +768,34 @@ int leann_adapter_project_backward(leann_ctx *ctx, const leann_projection *proj,
         }
     }
     LEANN_HIP(hipSetDevice(ctx->device));
-    const size_t low_bytes = up256((size_t)rows->T * R * sizeof(float)), down_bytes = up256((size_t)rows->n_used * R * K * 2),
-                 up_bytes = up256((size_t)rows->n_used * R * N * 2), partial_bytes = ddown_dev ? (size_t)rows->n_chunks * R * (K + N) * sizeof(float) : 0;
-    LEANN_TRY(ctx->reserve(ctx->op_work, std::max<size_t>(1, low_bytes + down_bytes + up_bytes + partial_bytes)));
+    const size_t low_bytes = up256((size_t)rows->T * R * sizeof(float)), up_bytes = up256((size_t)rows->n_used * R * N * 2),
+                 partial_bytes = ddown_dev ? (size_t)rows->n_chunks * R * (K + N) * sizeof(float) : 0;
+    LEANN_TRY(ctx->reserve(ctx->op_work,
+                           std::max<size_t>(1, pieces_bytes(rows) + packed_bytes(rows, K) + low_bytes + up_bytes + partial_bytes)));
     char *work = (char *)ctx->op_work.p;
-    float *grad_low = (float *)work, *partial = (float *)(work + low_bytes + down_bytes + up_bytes);
+    auto take = [&](size_t bytes) {
+        char *p = work;
+        work += bytes;
+        return p;
+    };
+    bf16_t *pieces = (bf16_t *)take(pieces_bytes(rows)), *packed = (bf16_t *)take(packed_bytes(rows, K));
+    float *grad_low = (float *)take(low_bytes);
+    char *up_at = take(up_bytes);
+    float *partial = (float *)take(partial_bytes);
     return with_half_type(proj->dtype, [&](auto *type) {
         typedef std::remove_pointer_t<decltype(type)> T;
-        T *down_t = (T *)(work + low_bytes), *up_t = (T *)(work + low_bytes + down_bytes);
+        T *up_t = (T *)up_at;
         if (rows->n_used) {
-            hipLaunchKernelGGL(transpose_kernel<T>, dim3((K + 31) / 32 + (N + 31) / 32, (R + 31) / 32, rows->n_used), dim3(256), 0, ctx->stream,
-                               (const T *)down_dev, (const T *)up_dev, rows->used, R, K, N, down_t, up_t);
-            enqueue_low<T>(ctx, rows, (const T *)dout_dev, ldd, N, up_t, 1, grad_low, false);
+            const int64_t transposing = (int64_t)rows->n_used * ((N + 31) / 32) * ((R + 31) / 32);
+            const int64_t laying = dx_dev ? ((int64_t)rows->n_used * ((K + 31) / 32) * rank_groups(R) * 64 + 255) / 256 : 0;
+            hipLaunchKernelGGL(lay_out_kernel<T>, dim3((unsigned)(transposing + std::min<int64_t>(laying, ctx->num_cus * 4))), dim3(256), 0, ctx->stream,
+                               (const T *)down_dev, (const T *)up_dev, rows->used, rows->adapters, rows->n_used, R, K, N, up_t, packed,
+                               (int)transposing);
+            enqueue_low<T>(ctx, rows, (const T *)dout_dev, ldd, N, up_t, 1, ddown_dev ? grad_low : nullptr, false, pieces, (const T *)nullptr, 0,
+                           (bf16_t *)nullptr);
         }
         if (dx_dev && rows->T)
-            enqueue_project<T>(ctx, rows, (const T *)dout_dev, ldd, (const T *)proj->wt.p, nullptr, K, N, grad_low, down_t, 1, (T *)dx_dev, lddx);
+            enqueue_project<T>(ctx, rows, (const T *)dout_dev, ldd, (const T *)proj->wt.p, nullptr, K, N, pieces, packed, (T *)dx_dev, lddx);
         if (ddown_dev) {
             if (rows->n_chunks)
                 enqueue_outer<T>(ctx, rows, (const T *)x_dev, ldx, (const T *)dout_dev, ldd, grad_low, low_dev, K, N, partial);

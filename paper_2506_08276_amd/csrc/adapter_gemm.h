@@ -8,16 +8,20 @@ typedef __attribute__((address_space(3))) void lds_t;
 typedef const __attribute__((address_space(1))) void global_t;
 
 __device__ const uint32_t zero_piece[4] = {0, 0, 0, 0};  // what rows hold beyond K
+__device__ u32x4 nowhere[64];                            // where lanes without an output store; never read
 
-// A tile: WM x (8 / WM) wavefronts of TM x TN 32x32 MFMA tiles.
+// A tile: WM x (8 / WM) wavefronts of TM x TN 32x32 MFMA tiles.  K goes by pairs of slabs of 32, 128 bytes of a row of x.
 template <int WM, int TM, int TN>
 struct ProjectCfg {
     static constexpr int WN = 8 / WM, BM = WM * TM * 32, BN = WN * TN * 32;
-    static constexpr int A_BYTES = BM * 64, STAGE = (BM + BN) * 64;  // of a slab of 32 columns of K
-    static constexpr int SMEM = 4 * STAGE + 8 * (2048 + 512);        // four stages; per wavefront 16 rows of outputs on their way, and the bias of its columns
-    static constexpr int A_LOADS = BM / 128;                         // requests of 1 KB per wavefront and slab
-    static constexpr int LOADS = A_LOADS + BN / 128;                 // at least
-    static constexpr int STORES = TM * TN * 2;                       // per wavefront and tile
+    static constexpr int A_BYTES = BM * 128, W_BYTES = BN * 64, STAGE = A_BYTES + 2 * W_BYTES;  // of a pair, of a slab, of a pair
+    static constexpr int ROWS_AT = 2 * STAGE, OWN_AT = ROWS_AT + 3 * BM * 4;
+    static constexpr int OWN = 2048 + 512;            // per wavefront: 16 rows of outputs on their way, the bias of its columns
+    static constexpr int SMEM = OWN_AT + 8 * OWN;     // two stages, the row numbers of three tiles
+    static constexpr int A_LOADS = BM / 64;           // requests of 1 KB per wavefront and pair
+    static constexpr int W_LOADS = BN / 128;          // per wavefront and slab
+    static constexpr int STORES = TM * ((TN + 1) / 2) * 4; // per tile
+    static_assert(BN % 128 == 0 && BM % 128 == 0, "every wavefront has as many requests");
 };
 
 template <int VM>
@@ -57,12 +61,13 @@ __device__ inline void load_word_to_lds(__amdgpu_buffer_rsrc_t b, int offset, un
 
 template <class T, int WM, int TM, int TN>
 __global__ __launch_bounds__(512, 1) void project_large_kernel(const T *x, int64_t ldx, const T *w, const float *bias, int N, int K,
-                                                               const int32_t *row_of, int rows, const int32_t *run_ptr, const int4 *runs, int compact,
-                                                               const float *low, int R, const T *up, T *out, int64_t ldo, int tiles_n, int gcols)
+                                                               const int32_t *row_of, int rows, const int32_t *seg_ptr, const int4 *segs,
+                                                               const bf16_t *pieces, int R16, const bf16_t *up, T *out, int64_t ldo, int tiles_n,
+                                                               int gcols)
 {
     typedef ProjectCfg<WM, TM, TN> Cfg;
     typedef typename Frag<T>::type F;
-    constexpr int BM = Cfg::BM, BN = Cfg::BN;
+    constexpr int BM = Cfg::BM, BN = Cfg::BN, UP = Frag<T>::PIECES;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, l32 = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -82,62 +87,63 @@ __global__ __launch_bounds__(512, 1) void project_large_kernel(const T *x, int64
     };
     int tile_m = 0, tile_n = 0;
     if (!tile_at(0, tile_m, tile_n)) return;
-    const int ksteps = project_ksteps(K), KT = ksteps >> 1;  // slabs: a multiple of 4; the host sees to it that there are 8
-    const int whole = K >> 5, last_ct = (N - 1) >> 5;
+    const int ksteps = project_ksteps(K), KP = (K + 63) >> 6;  // pairs: the host sees to it that there are 4
+    const int whole = K >> 6, last_ct = (N - 1) >> 5;
 
-    // Requests.  A: 16 rows of 64 bytes each, the lanes' pieces permuted so that piece c of row r lands at c ^ ((r >> 2) & 3).
-    const int a_row = lane >> 2, a_piece = (lane & 3) ^ ((lane >> 4) & 3);
-    int a_next[Cfg::A_LOADS];  // rows of the lanes' pieces in the tile after this one
-    const T *p[Cfg::A_LOADS];
-    auto rows_at = [&](int tm) {
-#pragma unroll
-        for (int i = 0; i < Cfg::A_LOADS; ++i) a_next[i] = row_of[tm * BM + (wave * Cfg::A_LOADS + i) * 16 + a_row];
+    // The row numbers of the tile before, this one and the next, in LDS; `which`: of the three places.
+    unsigned char *row_table = smem + Cfg::ROWS_AT;
+    auto request_rows = [&](int tm, int which) {
+        if (wave < BM / 64) load_word_to_lds(buffer_of(row_of + (size_t)tm * BM, BM * 4), (wave * 64 + lane) * 4, row_table + which * BM * 4 + wave * 256);
     };
-    auto advance = [&] {
+    auto row_number = [&](int which, int at) { return (int64_t) * reinterpret_cast<const int *>(row_table + (which * BM + at) * 4); };
+
+    // Requests.  A: 8 rows of 128 bytes each, whole lines, the lanes' pieces permuted so that piece c of row r lands at c ^ (r & 7).
+    const int a_at = wave * Cfg::A_LOADS * 8 + (lane >> 3), a_piece = (lane & 7) ^ (lane >> 3);
+    const T *p[Cfg::A_LOADS];
+    auto take_rows = [&](int which) {
 #pragma unroll
-        for (int i = 0; i < Cfg::A_LOADS; ++i) p[i] = x + (int64_t)a_next[i] * ldx + a_piece * 8;
+        for (int i = 0; i < Cfg::A_LOADS; ++i) p[i] = x + row_number(which, a_at + i * 8) * ldx + a_piece * 8;
+    };
+    auto request_a = [&](int pair, int stage) {
+        unsigned char *to = smem + stage * Cfg::STAGE + wave * Cfg::A_LOADS * 1024;
+        const bool in = pair < whole || pair * 64 + a_piece * 8 < K;
+#pragma unroll
+        for (int i = 0; i < Cfg::A_LOADS; ++i) load_to_lds(in ? p[i] + pair * 64 : reinterpret_cast<const T *>(zero_piece), to + i * 1024);
+    };
+    // An adapter's pair: the pieces of 32 ranks of the rows' low-rank activations (what follows them where there are fewer).
+    auto request_pieces = [&](int tm, int group, int stage) {
+        unsigned char *to = smem + stage * Cfg::STAGE + wave * Cfg::A_LOADS * 1024;
+#pragma unroll
+        for (int i = 0; i < Cfg::A_LOADS; ++i)
+            load_to_lds(pieces + ((int64_t)min(tm * BM + a_at + i * 8, rows - 1) * R16 + group) * 32 + a_piece * 8, to + i * 1024);
     };
     // W: 32 columns and 16 of K each, operand order in LDS too.  Offsets behind the last column: zeros.
-    constexpr int W_PIECES = BN / 16, W_LOADS = (W_PIECES + 7) / 8;
-    int w_off[W_LOADS];
+    auto request_w = [&](__amdgpu_buffer_rsrc_t b, int column_bytes, int step_bytes, int at, int slab, int stage) {
+        unsigned char *to = smem + stage * Cfg::STAGE + Cfg::A_BYTES + slab * Cfg::W_BYTES + wave * 1024;
 #pragma unroll
-    for (int i = 0; i < W_LOADS; ++i) w_off[i] = lane * 16 + (wave & 1) * 1024 + ((wave >> 1) + 4 * i) * ksteps * 1024;
-    auto request = [&](int tn, int slab, int stage) {
-        unsigned char *to = smem + stage * Cfg::STAGE;
-#pragma unroll
-        for (int i = 0; i < Cfg::A_LOADS; ++i) {
-            const T *from = p[i] + slab * 32;
-            if (slab >= whole && slab * 32 + a_piece * 8 >= K) from = reinterpret_cast<const T *>(zero_piece);
-            load_to_lds(from, to + (wave * Cfg::A_LOADS + i) * 1024);
-        }
-        const auto wr = buffer_of(w + (size_t)tn * (BN / 32) * ksteps * 512, min(last_ct + 1 - tn * (BN / 32), BN / 32) * ksteps * 1024);
-#pragma unroll
-        for (int i = 0; i < W_LOADS; ++i)
-            if (i * 8 + 8 <= W_PIECES || i * 8 + wave < W_PIECES)
-                load_to_lds(wr, w_off[i], slab * 2048, to + Cfg::A_BYTES + (i * 8 + wave) * 1024);
+        for (int i = 0; i < Cfg::W_LOADS; ++i)
+            load_to_lds(b, lane * 16 + (wave & 1) * step_bytes + ((wave >> 1) + 4 * i) * column_bytes, at, to + i * 8192);
     };
-    unsigned char *own = smem + 4 * Cfg::STAGE + wave * (2048 + 512), *own_bias = own + 2048;
+    auto columns = [&](int tn) { return min(last_ct + 1 - tn * (BN / 32), BN / 32); };
+    unsigned char *own = smem + Cfg::OWN_AT + wave * Cfg::OWN, *own_bias = own + 2048;
     const auto bias_buffer = buffer_of(bias, bias ? N * 4 : 0);
     auto request_bias = [&](int tn) {
 #pragma unroll
-        for (int i = 0; i < TN * 32; i += 64)
-            load_word_to_lds(bias_buffer, (tn * BN + wn * TN * 32 + i + lane) * 4, own_bias + i * 4);
+        for (int i = 0; i < TN * 32; i += 64) load_word_to_lds(bias_buffer, (tn * BN + wn * TN * 32 + i + lane) * 4, own_bias + i * 4);
     };
 
-    int foff[2];
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks) foff[ks] = l32 * 64 + (((ks * 2 + half) ^ ((lane >> 2) & 3)) << 4);
+    const int a_read = wm * TM * 4096 + l32 * 128 + ((half ^ (l32 & 7)) << 4), w_read = Cfg::A_BYTES + wn * TN * 2048 + lane * 16;
     F af[2][TM], bf[2][TN];
     f32x16 acc[TM][TN];
-    auto read = [&](int stage) {
+    auto read = [&](int a_slab, int w_slab, int stage) {
         const unsigned char *at = smem + stage * Cfg::STAGE;
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
+            const unsigned char *a = at + (a_read ^ (a_slab * 64 + ks * 32)), *w = at + w_read + w_slab * Cfg::W_BYTES + ks * 1024;
 #pragma unroll
-            for (int ni = 0; ni < TN; ++ni)
-                bf[ks][ni] = *reinterpret_cast<const F *>(at + Cfg::A_BYTES + (wn * TN + ni) * 2048 + ks * 1024 + lane * 16);
+            for (int ni = 0; ni < TN; ++ni) bf[ks][ni] = *reinterpret_cast<const F *>(w + ni * 2048);
 #pragma unroll
-            for (int mi = 0; mi < TM; ++mi) af[ks][mi] = *reinterpret_cast<const F *>(at + (wm * TM + mi) * 2048 + foff[ks]);
+            for (int mi = 0; mi < TM; ++mi) af[ks][mi] = *reinterpret_cast<const F *>(a + mi * 4096);
         }
     };
     auto multiply = [&](int ks) {
@@ -155,22 +161,112 @@ __global__ __launch_bounds__(512, 1) void project_large_kernel(const T *x, int64
         barrier();
     };
 
-    rows_at(tile_m);
-    advance();
+    // Out: 16 rows of 64 columns at a time through the wavefront's own 2 KB (piece c of row r at c ^ (r & 7)), in whole lines of 128 bytes.  Every lane issues
+    // every store, as waits count them.
+    typedef typename Frag<T>::four Four;
+    auto write_out = [&](int which) {
+        int l = lane;
+        asm volatile("" : "+v"(l));  // what follows from it is worked out here, not held in registers over the whole tile
+        const int l32 = l & 31, half = l >> 5;
+#pragma unroll
+        for (int mi = 0; mi < TM; ++mi)
+#pragma unroll
+            for (int hi = 0; hi < 2; ++hi)
+#pragma unroll
+                for (int n2 = 0; n2 < TN; n2 += 2) {
+                    __builtin_amdgcn_wave_barrier();  // LDS serves a wavefront's accesses in order
+                    if ((l32 >> 4) == hi) {
+#pragma unroll
+                        for (int c2 = 0; c2 < 2 && n2 + c2 < TN; ++c2)
+#pragma unroll
+                            for (int g = 0; g < 4; ++g) {
+                                Four v;
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) v[i] = (T)acc[mi][n2 + c2][4 * g + i];
+                                *reinterpret_cast<Four *>(own + (l32 & 15) * 128 + (((c2 * 4 + g) ^ (l32 & 7)) << 4) + half * 8) = v;
+                            }
+                    }
+                    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const int r = j * 8 + (l >> 3), c = l & 7, at = wm * TM * 32 + mi * 32 + hi * 16 + r;
+                        const int col = tile_n * BN + (wn * TN + n2) * 32 + c * 8;
+                        const u32x4 v = *reinterpret_cast<const u32x4 *>(own + r * 128 + ((c ^ (r & 7)) << 4));
+                        const int64_t row = row_number(which, at);
+                        const bool has = tile_m * BM + at < rows && col < N && (n2 + 1 < TN || c < 4);
+                        *(has ? reinterpret_cast<u32x4 *>(out + row * ldo + col) : nowhere + l) = v;
+                    }
+                }
+    };
+
+    // What comes: pairs of K of this tile, pairs of its adapters, pairs of the next tile.  Pair d is multiplied while A of pair d + 1 and W's second slab of
+    // it are requested, then W's first slab of pair d + 2.  (Its first two pairs again where there is no tile after this one: in bounds, unused.)
+    struct Pair {
+        int tile;   // 0: this one, 1: the next
+        int seg;    // of the adapters, -1: K
+        int group;  // pair of K, or first group of 16 ranks
+    };
+    constexpr int GROUPS = 2 / UP;  // of 16 ranks in a pair: fp16's `up` takes two slabs for one
+    int next_m, next_n, seg_end;
+    auto after = [&](const Pair &a, int rank, int first_seg) {  // rank: of a's segment
+        Pair b = a;
+        if (a.seg < 0) {
+            if (++b.group == KP && a.tile == 0) {
+                b.group = 0;
+                if (first_seg < seg_end) b.seg = first_seg;
+                else b.tile = 1;
+            }
+        } else if ((b.group += GROUPS) >= ((rank + 15) >> 4)) {
+            b.group = 0;
+            if (++b.seg == seg_end) {
+                b.seg = -1;
+                b.tile = 1;
+            }
+        }
+        return b;
+    };
+    auto ask_w = [&](const Pair &a, int number, int slab, int stage) {
+        const int tn = a.tile ? next_n : tile_n;
+        if (a.seg < 0) {
+            request_w(buffer_of(w + (size_t)tn * (BN / 32) * ksteps * 512, columns(tn) * ksteps * 1024), ksteps * 1024, 1024, a.group * 4096 + slab * 2048,
+                      slab, stage);
+        } else {  // both pieces of the low-rank activations times one piece of `up`
+            const int per_column = R16 * UP * 1024, step = min(a.group * UP + slab, R16 * UP - 1);
+            request_w(buffer_of(up + ((size_t)number * (last_ct + 1) + tn * (BN / 32)) * R16 * UP * 512, columns(tn) * per_column), per_column, 0,
+                      step * 1024, slab, stage);
+        }
+    };
+    auto ask_a = [&](const Pair &a, int which, int stage) {
+        if (a.seg >= 0) {
+            request_pieces(tile_m, a.group, stage);
+        } else {
+            if (a.tile && a.group == 0) take_rows(which);
+            request_a(a.group, stage);
+        }
+    };
+
+    request_rows(tile_m, 0);
+    wait_memory_and_lds<0>();
+    barrier();
+    next_m = tile_m;
+    next_n = tile_n;
     request_bias(tile_n);
-    request(tile_n, 0, 0);
-    request(tile_n, 1, 1);
-    request(tile_n, 2, 2);
-    wait_memory_and_lds<2 * Cfg::LOADS>();
+    take_rows(0);
+    request_a(0, 0);
+    ask_w(Pair{0, -1, 0}, 0, 0, 0);
+    ask_w(Pair{0, -1, 0}, 0, 1, 0);
+    ask_w(Pair{0, -1, 1}, 0, 0, 1);
+    wait_memory_and_lds<2 * Cfg::W_LOADS>();
     barrier();
     if (second) barrier();  // a phase behind
-    for (int step = 0;; ++step) {
-        // without a tile after this one its first slabs are requested again (in bounds, unused)
-        int next_m = tile_m, next_n = tile_n;
+    int stage = 0;          // of the pair at hand
+    for (int which = 0, step = 0;; ++step) {
+        const int next_which = which == 2 ? 0 : which + 1;
+        next_m = tile_m;
+        next_n = tile_n;
         const bool have_next = tile_at(step + 1, next_m, next_n);
-        const int s0 = tile_m * BM + wm * TM * 32, col0 = tile_n * BN + wn * TN * 32;  // the wavefront's first slot and column
-        int own_row[TM];  // of slot s0 + 32 mi + l32
-        {  // slab 0: the sums start at the bias
+        // The first pair: the sums start at the bias.
+        {
             f32x16 start[TN];
 #pragma unroll
             for (int ni = 0; ni < TN; ++ni)
@@ -180,9 +276,10 @@ __global__ __launch_bounds__(512, 1) void project_large_kernel(const T *x, int64
 #pragma unroll
                     for (int i = 0; i < 4; ++i) start[ni][4 * g + i] = b[i];
                 }
-            read(0);
-            request(tile_n, 3, 3);
-            wait_memory_and_lds<2 * Cfg::LOADS>();
+            read(0, 0, stage);
+            request_a(1, stage ^ 1);
+            ask_w(Pair{0, -1, 1}, 0, 1, stage ^ 1);
+            wait_memory_and_lds<2 * Cfg::W_LOADS + Cfg::A_LOADS + Cfg::STORES>();
             barrier();
             __builtin_amdgcn_s_setprio(1);
 #pragma unroll
@@ -193,136 +290,88 @@ __global__ __launch_bounds__(512, 1) void project_large_kernel(const T *x, int64
             __builtin_amdgcn_s_setprio(0);
             barrier();
         }
-#pragma unroll
-        for (int u = 1; u < 4; ++u) {
-            read(u);
-            if (u == 1) {
-                rows_at(next_m);
-#pragma unroll
-                for (int mi = 0; mi < TM; ++mi) own_row[mi] = row_of[s0 + mi * 32 + l32];
-            }
-            request(tile_n, u + 3, (u + 3) & 3);
-            wait_memory_and_lds<2 * Cfg::LOADS>();
+        read(1, 1, stage);
+        ask_w(Pair{0, -1, 2}, 0, 0, stage);
+        request_rows(next_m, next_which);  // held the rows of two tiles ago, which are out
+        wait_memory_and_lds<2 * Cfg::W_LOADS>();
+        compute_phase();
+        stage ^= 1;
+        const int first_seg = seg_ptr[tile_m];
+        seg_end = seg_ptr[tile_m + 1];
+        int d = 1;
+        for (; d < KP - 2; ++d, stage ^= 1) {
+            read(0, 0, stage);
+            request_a(d + 1, stage ^ 1);
+            ask_w(Pair{0, -1, d + 1}, 0, 1, stage ^ 1);
+            wait_memory_and_lds<2 * Cfg::W_LOADS + Cfg::A_LOADS>();
             compute_phase();
-        }
-        for (int s = 4; s < KT - 4; s += 4) {
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                read(u);
-                request(tile_n, s + u + 3, (u + 3) & 3);
-                wait_memory_and_lds<2 * Cfg::LOADS>();
-                compute_phase();
-            }
+            read(1, 1, stage);
+            ask_w(Pair{0, -1, d + 2}, 0, 0, stage);
+            wait_memory_and_lds<2 * Cfg::W_LOADS>();
+            compute_phase();
         }
         request_bias(next_n);
-        // The wavefront's adapters: their runs, and what the first 16 ranks of the first one need, on its way during the last slabs.
-        const int groups = (rows + 31) >> 5, g0 = s0 >> 5;
-        int run = __builtin_amdgcn_readfirstlane(run_ptr[min(g0, groups)]);
-        const int runs_end = __builtin_amdgcn_readfirstlane(run_ptr[min(g0 + TM, groups)]);
-        int from = 0, to = 0, rank = 0, k = 0;
-        float scale = 0.f;
-        const T *u = up;
-        auto next_adapter = [&] {  // the next runs of one adapter
-            const int4 r = runs[run];
-            from = r.y;
-            rank = r.z >> 8 & 255;
-            scale = __int_as_float(r.w);
-            u = up + (size_t)(compact ? (uint32_t)r.z >> 16 : (uint32_t)r.x) * N * R;
-            to = r.y + (r.z & 255);
-            while (++run < runs_end && runs[run].x == r.x) to += runs[run].z & 255;
-            k = 0;
+        // The last two pairs of K, then the adapters'.
+        Pair now = {0, -1, KP - 2}, ask1 = {0, -1, KP - 1}, ask2;
+        int4 now_seg = {}, ask1_seg = {}, ask2_seg = {};
+        auto first_half = [&] {
+            ask2 = after(ask1, ask1_seg.z, first_seg);
+            ask2_seg = ask2.seg == ask1.seg ? ask1_seg : ask2.seg >= 0 ? segs[ask2.seg] : int4{};
+            ask_a(ask1, next_which, stage ^ 1);
+            ask_w(ask1, ask1_seg.w, 1, stage ^ 1);
+            wait_memory_and_lds<2 * Cfg::W_LOADS + Cfg::A_LOADS>();
         };
-        f32x8 h[TM];
-        F uf[TN];
-        auto fetch = [&] {
-            const bool in = k + half * 8 < rank;
-#pragma unroll
-            for (int mi = 0; mi < TM; ++mi) {
-                h[mi] = f32x8{};
-                if (in) __builtin_memcpy(&h[mi], low + (int64_t)own_row[mi] * R + k + half * 8, sizeof(h[mi]));
-            }
-#pragma unroll
-            for (int ni = 0; ni < TN; ++ni) {
-                uf[ni] = F{};
-                if (in) uf[ni] = *reinterpret_cast<const F *>(u + (size_t)min(col0 + ni * 32 + l32, N - 1) * R + k + half * 8);
-            }
+        auto second_half = [&] {
+            ask_w(ask2, ask2_seg.w, 0, stage);
+            wait_memory_and_lds<2 * Cfg::W_LOADS>();
         };
-        const bool adapted = run < runs_end;
-        if (adapted) {
-            next_adapter();
-            fetch();
-        }
-#pragma unroll
-        for (int v = 0; v < 4; ++v) {
-            read(v);
-            if (v == 1) advance();
-            if (v == 0) request(tile_n, KT - 1, 3);
-            else request(next_n, v - 1, v - 1);
-            wait_memory_and_lds<2 * Cfg::LOADS>();
+        auto shift = [&] {
+            stage ^= 1;
+            now = ask1;
+            now_seg = ask1_seg;
+            ask1 = ask2;
+            ask1_seg = ask2_seg;
+        };
+        for (int i = 0; i < 2; ++i) {
+            read(0, 0, stage);
+            first_half();
             compute_phase();
+            read(1, 1, stage);
+            second_half();
+            compute_phase();
+            shift();
         }
-        if (adapted)
-            for (;;) {
-                const int left = rank - k - half * 8;
-#pragma unroll
-                for (int ni = 0; ni < TN; ++ni)
-#pragma unroll
-                    for (int j = 1; j < 8; ++j) uf[ni][j] = j < left ? uf[ni][j] : (T)0.f;  // what lies beyond the rank may be anything
+        // A lane holds one slot of the output; the lanes that are not the adapter's keep what they have: another request's infinities stay with it.
+        auto adapter_phase = [&](int slab) {
+            barrier();
+            if (now.group * UP + slab < ((now_seg.z + 15) >> 4) * UP) {
 #pragma unroll
                 for (int mi = 0; mi < TM; ++mi) {
-                    const int slot = s0 + mi * 32;
-                    if (from < slot + 32 && to > slot) {
-                        f32x8 v = h[mi] * scale;
-                        const bf16x8 h1 = take_piece(v), h2 = take_piece(v);
-                        const bool whole_group = from <= slot && to >= slot + 32, mine = slot + l32 >= from && slot + l32 < to;
+                    const int first = tile_m * BM + (wm * TM + mi) * 32;
+                    const bool mine = first + l32 >= now_seg.x && first + l32 < now_seg.y;
 #pragma unroll
-                        for (int ni = 0; ni < TN; ++ni) {
-                            const f32x16 sum = adapter_step(uf[ni], h1, h2, acc[mi][ni]);
-                            if (whole_group) {
-                                acc[mi][ni] = sum;
-                            } else {
+                    for (int ni = 0; ni < TN; ++ni) {
+                        const bf16x8 u = __builtin_bit_cast(bf16x8, bf[0][ni]);
+                        f32x16 sum = mfma32(u, __builtin_bit_cast(bf16x8, af[1][mi]), acc[mi][ni]);
+                        sum = mfma32(u, __builtin_bit_cast(bf16x8, af[0][mi]), sum);
 #pragma unroll
-                                for (int j = 0; j < 16; ++j) acc[mi][ni][j] = mine ? sum[j] : acc[mi][ni][j];
-                            }
-                        }
+                        for (int j = 0; j < 16; ++j) acc[mi][ni][j] = mine ? sum[j] : acc[mi][ni][j];
                     }
                 }
-                k += 16;
-                if (k >= rank) {
-                    if (run >= runs_end) break;
-                    next_adapter();
-                }
-                fetch();
             }
-        // Out: 16 rows of 64 columns at a time through the wavefront's own 2 KB (piece c of row r at c ^ (r & 7)), whole lines of 128 bytes.  96 columns: 32 at a time.
-#pragma unroll
-        for (int mi = 0; mi < TM; ++mi)
-#pragma unroll
-            for (int hi = 0; hi < 2; ++hi)
-#pragma unroll
-                for (int n2 = 0; n2 < TN; n2 += 2) {
-                    constexpr int PAIR = 2;
-                    __builtin_amdgcn_wave_barrier();  // LDS serves a wavefront's accesses in order
-                    if ((l32 >> 4) == hi) {
-#pragma unroll
-                        for (int c2 = 0; c2 < PAIR && n2 + c2 < TN; ++c2)
-#pragma unroll
-                            for (int g = 0; g < 4; ++g) {
-                                typename Frag<T>::four v;
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) v[i] = (T)acc[mi][n2 + c2][4 * g + i];
-                                *reinterpret_cast<typename Frag<T>::four *>(own + (l32 & 15) * 128 + (((c2 * 4 + g) ^ (l32 & 7)) << 4) + half * 8) = v;
-                            }
-                    }
-                    __builtin_amdgcn_wave_barrier();
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        const int r = j * 8 + (lane >> 3), c = lane & 7, slot = s0 + mi * 32 + hi * 16 + r, col = col0 + n2 * 32 + c * 8;
-                        const u32x4 v = *reinterpret_cast<const u32x4 *>(own + r * 128 + ((c ^ (r & 7)) << 4));
-                        const int row = __builtin_amdgcn_ds_bpermute((hi * 16 + r) << 2, own_row[mi]);
-                        if (slot < rows && col < N && (n2 + 1 < TN || c < 4)) *reinterpret_cast<u32x4 *>(out + (int64_t)row * ldo + col) = v;
-                    }
-                }
+            barrier();
+        };
+        while (!now.tile) {
+            read(0, 0, stage);
+            first_half();
+            adapter_phase(0);
+            read(UP == 2 ? 0 : 1, 1, stage);
+            second_half();
+            adapter_phase(1);
+            shift();
+        }
+        write_out(which);
+        which = next_which;
         if (!have_next) break;
         tile_m = next_m;
         tile_n = next_n;
