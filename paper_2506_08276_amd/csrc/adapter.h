@@ -9,6 +9,8 @@ struct leann_projection {
     DevBuf w, wt, bias;
 };
 
+constexpr int WIDE_ROWS = 32;
+
 // Which rows of a batch go through which adapter.  Rows are put in an order, their slots, in which an adapter's rows are adjacent (those without one
 // last), so that a tile of rows meets few adapters.  All tables lie in one allocation.
 struct leann_adapter_rows {
@@ -16,14 +18,16 @@ struct leann_adapter_rows {
     int64_t T = 0;
     int32_t n_adapters = 0, max_rank = 0, n_used = 0;
     int32_t n_tiles = 0, n_adapted_tiles = 0;  // of 16 slots of one adapter; tiles of rows without one come last
+    int32_t n_wide_tiles = 0, n_adapted_wide_tiles = 0;  // likewise, of 32
     int32_t n_chunks = 0;                      // of up to chunk_rows slots of one adapter
     DevBuf mem;
-    const int32_t *row_of = nullptr;     // [T, up to a multiple of 256: the last row again]
+    const int32_t *row_of = nullptr;     // [T, up to a multiple of 256: the last row again, 8 more]
     const int32_t *run_ptr = nullptr;    // [32-slot groups + 1]
     const int4 *runs = nullptr;          // adapter, first slot, slots | rank << 8 | number among the used adapters << 16, scale
     const int32_t *seg_ptr = nullptr;    // [256-slot tiles + 1]
     const int4 *segs = nullptr;          // a tile's adapters: first slot, slot behind the last, rank, number among the used adapters
     const int4 *tiles = nullptr;         // adapter, first slot, slots | rank << 16, number among the used adapters
+    const int4 *wide_tiles = nullptr;    // likewise
     const int4 *chunks = nullptr;        // likewise, by adapter
     const int4 *adapters = nullptr;      // [n_adapters] first chunk, chunks, rank, scale
     const int32_t *used = nullptr;       // [n_used] adapters that have rows

@@ -79,10 +79,11 @@ __global__ __launch_bounds__(256) void lay_out_kernel(const T *down, const T *up
 }
 
 // ------------------------------------------------------------------ low-rank activations
-// low[row][r] = sum over k of x[row][k] down[a][r][k] for 16 slots of one adapter, in MFMA 16x16x32: a lane ends with four ranks of one row.
+// low[row][r] = sum over k of x[row][k] down[a][r][k] for 16 RT slots of one adapter, in MFMA 16x16x32: a lane ends with four ranks of a row.
 // They go out as they are, by row (`low`, if wanted), and times the adapter's scale in the pieces that the product reads, by slot.
-// SPLIT: a block per tile, whose four wavefronts share K; else a wavefront per tile.  Blocks from `low_blocks` on lay out `up`.
-template <class T, int NT, bool SPLIT>
+// SPLIT: a block per tile, whose four wavefronts share K; else a wavefront per tile, of 32 rows, as reading `down` again for every 16 of them would
+// cost as much as reading x.  Blocks from `low_blocks` on lay out `up`.
+template <class T, int NT, int RT, bool SPLIT>
 __global__ __launch_bounds__(256) void low_kernel(const T *x, int64_t ldx, const T *down, int R, int K, const int32_t *row_of, const int4 *tiles,
                                                   int n_tiles, int low_blocks, int compact, float *low, bf16_t *pieces, const int4 *adapters, const T *up,
                                                   int N, const int32_t *used, int n_used, bf16_t *up_packed)
@@ -92,73 +93,85 @@ __global__ __launch_bounds__(256) void low_kernel(const T *x, int64_t ldx, const
         return;
     }
     typedef typename Frag<T>::type F;
+    static_assert(!SPLIT || RT == 1, "");
     __shared__ f32x4 part[SPLIT ? 4 : 1][SPLIT ? NT : 1][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane & 15, q = lane >> 4;
     const int index = SPLIT ? blockIdx.x : blockIdx.x * 4 + wave;
     if (index >= n_tiles) return;
     const int4 tile = tiles[index];
     const int n = tile.z & 0xffff, rank = tile.z >> 16, groups = (rank + 15) >> 4;
-    const int64_t row = row_of[tile.y + min(j, n - 1)];
-    f32x4 acc[NT];
+    int64_t row[RT];
 #pragma unroll
-    for (int g = 0; g < NT; ++g) acc[g] = f32x4{};
+    for (int t = 0; t < RT; ++t) row[t] = row_of[tile.y + min(t * 16 + j, n - 1)];
+    f32x4 acc[RT][NT];
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+#pragma unroll
+        for (int g = 0; g < NT; ++g) acc[t][g] = f32x4{};
     if (rank) {
-        const T *xp = x + row * ldx + q * 8;
-        const T *ap[NT];
+        const T *xp[RT], *ap[NT];
+#pragma unroll
+        for (int t = 0; t < RT; ++t) xp[t] = x + row[t] * ldx + q * 8;
 #pragma unroll
         for (int g = 0; g < NT; ++g) ap[g] = down + ((size_t)(compact ? tile.w : tile.x) * R + min(g * 16 + j, rank - 1)) * K + q * 8;
         const int steps = (K + 31) >> 5, per = SPLIT ? (steps + 3) >> 2 : steps;
         const int from = SPLIT ? wave * per : 0, to = min(steps, from + per);
-        constexpr int U = NT > 2 ? 2 : 4;  // steps whose operands are on their way together
+        constexpr int U = RT > 1 || NT > 2 ? 2 : 4;  // steps whose operands are on their way together
         for (int s = from; s < to; s += U) {
-            F xf[U], af[U][NT];
+            F xf[U][RT], af[U][NT];
 #pragma unroll
-            for (int i = 0; i < U; ++i) {
-                const bool in = s + i < to && (s + i) * 32 + q * 8 < K;  // K is a multiple of 8
-                const int k = in ? (s + i) * 32 : 0;
-                xf[i] = *reinterpret_cast<const F *>(xp + k);
-                if (!in) xf[i] = F{};
+            for (int t = 0; t < RT; ++t)
 #pragma unroll
-                for (int g = 0; g < NT; ++g)
-                    if (g < groups) {
-                        af[i][g] = *reinterpret_cast<const F *>(ap[g] + k);
+                for (int i = 0; i < U; ++i) {
+                    const bool in = s + i < to && (s + i) * 32 + q * 8 < K;  // K is a multiple of 8
+                    xf[i][t] = *reinterpret_cast<const F *>(xp[t] + (in ? (s + i) * 32 : 0));
+                    if (!in) xf[i][t] = F{};
+                }
+#pragma unroll
+            for (int g = 0; g < NT; ++g)
+                if (g < groups)
+#pragma unroll
+                    for (int i = 0; i < U; ++i) {
+                        const bool in = s + i < to && (s + i) * 32 + q * 8 < K;
+                        af[i][g] = *reinterpret_cast<const F *>(ap[g] + (in ? (s + i) * 32 : 0));
                         if (!in) af[i][g] = F{};
                     }
-            }
 #pragma unroll
             for (int i = 0; i < U; ++i)
 #pragma unroll
                 for (int g = 0; g < NT; ++g)
-                    if (g < groups) acc[g] = mfma16(af[i][g], xf[i], acc[g]);
+                    if (g < groups)
+#pragma unroll
+                        for (int t = 0; t < RT; ++t) acc[t][g] = mfma16(af[i][g], xf[i][t], acc[t][g]);
         }
         if constexpr (SPLIT) {
 #pragma unroll
-            for (int g = 0; g < NT; ++g) part[wave][g][lane] = acc[g];
+            for (int g = 0; g < NT; ++g) part[wave][g][lane] = acc[0][g];
             __syncthreads();
 #pragma unroll
-            for (int g = 0; g < NT; ++g) acc[g] = (part[0][g][lane] + part[1][g][lane]) + (part[2][g][lane] + part[3][g][lane]);
+            for (int g = 0; g < NT; ++g) acc[0][g] = (part[0][g][lane] + part[1][g][lane]) + (part[2][g][lane] + part[3][g][lane]);
         }
     }
-    if (j >= n) return;
     const float scale = rank ? __int_as_float(adapters[tile.x].w) : 0.f;
-    bf16_t *to = pieces + (int64_t)(tile.y + j) * rank_groups(R) * 32;
 #pragma unroll
-    for (int g = 0; g < NT; ++g) {
-        const int r = g * 16 + q * 4;
-        if (SPLIT && (g & 3) != wave) continue;
-        f32x4 v = acc[g];
+    for (int t = 0; t < RT; ++t) {
+        if (t * 16 + j >= n) continue;
+        bf16_t *to = pieces + (int64_t)(tile.y + t * 16 + j) * rank_groups(R) * 32;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = r + i < rank ? v[i] : 0.f;
-        if (low && r < R) *reinterpret_cast<f32x4 *>(low + row * R + r) = v;
-        if (r < rank) {
-            v *= scale;
-            const bf16x4 first = __builtin_convertvector(v, bf16x4);
-            v -= __builtin_convertvector(first, f32x4);
-            *reinterpret_cast<bf16x4 *>(to + g * 32 + q * 4) = first;
-            *reinterpret_cast<bf16x4 *>(to + g * 32 + 16 + q * 4) = __builtin_convertvector(v, bf16x4);
-        } else if (g < groups) {
-            *reinterpret_cast<bf16x4 *>(to + g * 32 + q * 4) = bf16x4{};
-            *reinterpret_cast<bf16x4 *>(to + g * 32 + 16 + q * 4) = bf16x4{};
+        for (int g = 0; g < NT; ++g) {
+            const int r = g * 16 + q * 4;
+            if (SPLIT && (g & 3) != wave) continue;
+            f32x4 v = acc[t][g];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = r + i < rank ? v[i] : 0.f;
+            if (low && r < R) *reinterpret_cast<f32x4 *>(low + row[t] * R + r) = v;
+            if (g < groups) {
+                v *= scale;
+                const bf16x4 first = __builtin_convertvector(v, bf16x4);
+                v -= __builtin_convertvector(first, f32x4);
+                *reinterpret_cast<bf16x4 *>(to + g * 32 + q * 4) = first;
+                *reinterpret_cast<bf16x4 *>(to + g * 32 + 16 + q * 4) = __builtin_convertvector(v, bf16x4);
+            }
         }
     }
 }
@@ -273,13 +286,15 @@ __device__ inline f32x4 outer_step(const bf16x8 (&h)[3], const f16x8 &p, f32x4 c
 
 // partial[chunk][r][c] = sum over the chunk's rows of low[row][r] p[row][c]: c < K from x and the low-rank gradients (down's), then N from dout and the
 // low-rank activations (up's).  A block takes 128 columns and 16 NR ranks, its wavefronts 32 rows each in turn; a lane reads 16 bytes of a row and turns
-// eight rows of them, in registers, into the MFMA operands of its eight columns.  The next rows are on their way while these are multiplied, and the
-// numbers of those after them.
+// eight rows of them, in registers, into the MFMA operands of its eight columns; low goes through LDS, 16 bytes of a row per lane on the way in.  The next
+// rows are on their way while these are multiplied, and the numbers of those after them.
 template <class T, int NR>
 __global__ __launch_bounds__(256) void outer_kernel(const T *x, int64_t ldx, const T *dout, int64_t ldd, const float *grad_low, const float *low, int R,
-                                                    int K, int N, const int32_t *row_of, const int4 *chunks, float *partial)
+                                                    int K, int N, const int32_t *row_of, const int4 *chunks, int last_slots, float *partial)
 {
-    __shared__ float sums[16 * NR][128];
+    constexpr int PITCH = 36;  // rows of a rank's 32, in steps of 16 bytes, and all banks by ranks
+    __shared__ __attribute__((aligned(16))) float sums[16 * NR][128];
+    __shared__ __attribute__((aligned(16))) float turned[4][16 * NR][PITCH];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, j = lane & 15;
     const int strips_k = (K + 127) / 128, strips = strips_k + (N + 127) / 128, strip = blockIdx.x % strips;
     const int4 chunk = chunks[blockIdx.x / strips];
@@ -288,7 +303,7 @@ __global__ __launch_bounds__(256) void outer_kernel(const T *x, int64_t ldx, con
     const bool of_x = strip < strips_k;
     const T *p = of_x ? x : dout;
     const int64_t ld = of_x ? ldx : ldd;
-    const float *h = of_x ? grad_low : low;
+    const float *h = (of_x ? grad_low : low) + r0 + (lane & 3) * 4;
     const int C = of_x ? K : N, c0 = (of_x ? strip : strip - strips_k) * 128, col = c0 + j * 8;
     const bool has_col = col < C;
     f32x4 acc[NR][8];
@@ -296,21 +311,24 @@ __global__ __launch_bounds__(256) void outer_kernel(const T *x, int64_t ldx, con
     for (int g = 0; g < NR; ++g)
 #pragma unroll
         for (int f = 0; f < 8; ++f) acc[g][f] = f32x4{};
-    int row[8];
+    int row[8], h_row[2];
     u32x4 d[8];
-    f32x8 hv[NR];
-    auto number = [&](int base) {
+    f32x4 hv[NR][2];
+    auto number = [&](int base) {  // the table goes on behind the last slot: what is read there is not used
+        __builtin_memcpy(row, row_of + min(chunk.y + base + q * 8, last_slots), sizeof(row));
 #pragma unroll
-        for (int i = 0; i < 8; ++i) row[i] = row_of[chunk.y + min(base + q * 8 + i, n - 1)];
+        for (int i = 0; i < 2; ++i) h_row[i] = row_of[min(chunk.y + base + i * 16 + (lane >> 2), last_slots)];
     };
     auto request = [&](int base) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const bool in = base + q * 8 + i < n;
-            d[i] = in && has_col ? *reinterpret_cast<const u32x4 *>(p + row[i] * ld + col) : u32x4{};
+        for (int i = 0; i < 8; ++i)
+            d[i] = base + q * 8 + i < n && has_col ? *reinterpret_cast<const u32x4 *>(p + row[i] * ld + col) : u32x4{};
 #pragma unroll
-            for (int g = 0; g < NR; ++g) hv[g][i] = in && r0 + g * 16 + j < rank ? h[(int64_t)row[i] * R + r0 + g * 16 + j] : 0.f;
-        }
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int g = 0; g < NR; ++g)
+                hv[g][i] = base + i * 16 + (lane >> 2) < n && r0 + g * 16 + (lane & 3) * 4 < R
+                               ? *reinterpret_cast<const f32x4 *>(h + (int64_t)h_row[i] * R + g * 16) : f32x4{};
     };
     number(wave * 32);
     request(wave * 32);
@@ -318,10 +336,21 @@ __global__ __launch_bounds__(256) void outer_kernel(const T *x, int64_t ldx, con
     for (int base = wave * 32; base < n; base += 128) {
         u32x4 t[8];
         bf16x8 piece[NR][3];
+        __builtin_amdgcn_wave_barrier();  // LDS serves a wavefront's accesses in order
 #pragma unroll
         for (int g = 0; g < NR; ++g)
 #pragma unroll
-            for (int i = 0; i < 3; ++i) piece[g][i] = take_piece(hv[g]);
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) turned[wave][g * 16 + (lane & 3) * 4 + e][i * 16 + (lane >> 2)] = hv[g][i][e];
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int g = 0; g < NR; ++g) {
+            f32x8 v;
+            __builtin_memcpy(&v, __builtin_assume_aligned(&turned[wave][g * 16 + j][q * 8], 16), sizeof(v));
+#pragma unroll
+            for (int i = 0; i < 3; ++i) piece[g][i] = take_piece(v);
+        }
         transpose8(d, t);
         request(base + 128);
         number(base + 256);
@@ -422,19 +451,22 @@ template <class T>
 void enqueue_low(leann_ctx *ctx, const leann_adapter_rows *rows, const T *x, int64_t ldx, int K, const T *down, int compact, float *low, bool with_zeros,
                  bf16_t *pieces, const T *up, int N, bf16_t *up_packed)
 {
-    const int n = with_zeros ? rows->n_tiles : rows->n_adapted_tiles, R = rows->max_rank;
+    const int R = rows->max_rank;
+    const bool split = rows->n_tiles < ctx->num_cus * 4;
+    const int n = split ? (with_zeros ? rows->n_tiles : rows->n_adapted_tiles) : with_zeros ? rows->n_wide_tiles : rows->n_adapted_wide_tiles;
     if (!n) return;
-    const bool split = n < ctx->num_cus * 4;
     const int low_blocks = split ? n : (n + 3) / 4;
     const int64_t laying = up ? ((int64_t)rows->n_used * ((N + 31) / 32) * rank_groups(R) * 64 + 255) / 256 : 0;
     auto go = [&](auto kernel) {
         hipLaunchKernelGGL(kernel, dim3(low_blocks + (unsigned)std::min<int64_t>(laying, ctx->num_cus * 4)), dim3(256), 0, ctx->stream, x, ldx, down, R,
-                           K, rows->row_of, rows->tiles, n, low_blocks, compact, low, pieces, rows->adapters, up, N, rows->used, rows->n_used, up_packed);
+                           K, rows->row_of, split ? rows->tiles : rows->wide_tiles, n, low_blocks, compact, low, pieces, rows->adapters, up, N, rows->used,
+                           rows->n_used, up_packed);
     };
-    if (R <= 16) split ? go(low_kernel<T, 1, true>) : go(low_kernel<T, 1, false>);
-    else if (R <= 32) split ? go(low_kernel<T, 2, true>) : go(low_kernel<T, 2, false>);
-    else if (R <= 64) split ? go(low_kernel<T, 4, true>) : go(low_kernel<T, 4, false>);
-    else split ? go(low_kernel<T, 8, true>) : go(low_kernel<T, 8, false>);
+    static_assert(WIDE_ROWS == 32, "two tiles of 16");
+    if (R <= 16) split ? go(low_kernel<T, 1, 1, true>) : go(low_kernel<T, 1, 2, false>);
+    else if (R <= 32) split ? go(low_kernel<T, 2, 1, true>) : go(low_kernel<T, 2, 2, false>);
+    else if (R <= 64) split ? go(low_kernel<T, 4, 1, true>) : go(low_kernel<T, 4, 2, false>);
+    else split ? go(low_kernel<T, 8, 1, true>) : go(low_kernel<T, 8, 2, false>);
 }
 
 // out = x w^T + bias + the adapters' part
@@ -444,7 +476,7 @@ void enqueue_project(leann_ctx *ctx, const leann_adapter_rows *rows, const T *x,
 {
     const int T32 = (int)((rows->T + 31) / 32), T64 = (int)((rows->T + 63) / 64), R16 = rank_groups(rows->max_rank);
     const int64_t tiles64 = (int64_t)T64 * ((N + 63) / 64);
-    if (K >= 256 && tiles64 >= ctx->num_cus * 8) {
+    if (K >= 256 && tiles64 >= ctx->num_cus * 8 && rows->T * ldx / 8 < 0xffffff00ll) {
         typedef ProjectCfg<2, 4, 2> Cfg;
         const int tiles_n = (N + Cfg::BN - 1) / Cfg::BN;
         const int64_t tiles = (rows->T + Cfg::BM - 1) / Cfg::BM * tiles_n;
@@ -474,7 +506,7 @@ void enqueue_outer(leann_ctx *ctx, const leann_adapter_rows *rows, const T *x, i
     const int R = rows->max_rank, strips = (K + 127) / 128 + (N + 127) / 128;
     auto go = [&](auto kernel, int ranks) {
         hipLaunchKernelGGL(kernel, dim3(strips * rows->n_chunks, (R + ranks - 1) / ranks), dim3(256), 0, ctx->stream, x, ldx, dout, ldd, grad_low, low, R,
-                           K, N, rows->row_of, rows->chunks, partial);
+                           K, N, rows->row_of, rows->chunks, (int)((rows->T + 255) / 256 * 256), partial);
     };
     if (R <= 16) go(outer_kernel<T, 1>, 16);
     else go(outer_kernel<T, 2>, 32);
@@ -509,7 +541,7 @@ int make_rows(leann_ctx *ctx, const int32_t *rows_of_request, const int32_t *ada
         for (int i = 0; i < n_requests; ++i) order[next[of(i)]++] = i;
     }
     std::vector<int32_t> row_of;
-    row_of.reserve(T + 256);
+    row_of.reserve(T + 256 + 8);
     std::vector<int64_t> slot_of(n_adapters + 2, 0);  // an adapter's first slot
     for (int a = 0; a <= n_adapters; ++a) {
         for (int j = first[a]; j < first[a + 1]; ++j)
@@ -517,11 +549,12 @@ int make_rows(leann_ctx *ctx, const int32_t *rows_of_request, const int32_t *ada
         slot_of[a + 1] = (int64_t)row_of.size();
     }
     while (row_of.size() % 256) row_of.push_back(row_of[T - 1]);
+    row_of.insert(row_of.end(), 8, 0);  // outer_kernel reads eight at a time
 
     const int64_t adapted = slot_of[n_adapters];
     // Rows of a chunk: as many as leave some four blocks for each CU (a block takes 256 columns of one), 64 at least, 1024 at most.
     const int chunk_rows = (int)std::min<int64_t>(1024, std::max<int64_t>(64, (adapted / (ctx->num_cus * 2 / 3) + 63) / 64 * 64));
-    std::vector<int4> tiles, chunks, runs, adapters(n_adapters);
+    std::vector<int4> tiles, wide, chunks, runs, adapters(n_adapters);
     std::vector<int4> segs;
     std::vector<int32_t> used, run_ptr((T + 31) / 32 + 1, 0), seg_ptr((T + 255) / 256 + 1, 0);
     auto bits = [](float f) {
@@ -532,7 +565,12 @@ int make_rows(leann_ctx *ctx, const int32_t *rows_of_request, const int32_t *ada
     for (int a = 0; a <= n_adapters; ++a) {
         const int64_t from = slot_of[a], to = slot_of[a + 1];
         const int r = a < n_adapters ? rank[a] : 0, number = (int)used.size();
-        if (a == n_adapters) out->n_adapted_tiles = (int)tiles.size();
+        if (a == n_adapters) {
+            out->n_adapted_tiles = (int)tiles.size();
+            out->n_adapted_wide_tiles = (int)wide.size();
+        }
+        for (int64_t s = from; s < to; s += WIDE_ROWS)
+            wide.push_back(int4{a < n_adapters ? a : -1, (int)s, (int)std::min<int64_t>(WIDE_ROWS, to - s) | r << 16, number});
         for (int64_t s = from; s < to; s += 16) tiles.push_back(int4{a < n_adapters ? a : -1, (int)s, (int)std::min<int64_t>(16, to - s) | r << 16, number});
         if (a == n_adapters) break;
         adapters[a] = int4{(int)chunks.size(), 0, r, bits(scale[a])};
@@ -561,6 +599,7 @@ int make_rows(leann_ctx *ctx, const int32_t *rows_of_request, const int32_t *ada
     out->max_rank = max_rank;
     out->n_used = (int)used.size();
     out->n_tiles = (int)tiles.size();
+    out->n_wide_tiles = (int)wide.size();
     out->n_chunks = (int)chunks.size();
     std::vector<char> image;
     auto put = [&](const auto &v) {
@@ -569,7 +608,7 @@ int make_rows(leann_ctx *ctx, const int32_t *rows_of_request, const int32_t *ada
         if (bytes) memcpy(image.data() + at, v.data(), bytes);
         return at;
     };
-    const size_t at[9] = {put(row_of), put(run_ptr), put(runs), put(tiles), put(chunks), put(adapters), put(used), put(seg_ptr), put(segs)};
+    const size_t at[10] = {put(row_of), put(run_ptr), put(runs), put(tiles), put(chunks), put(adapters), put(used), put(seg_ptr), put(segs), put(wide)};
     LEANN_TRY(ctx->reserve(out->mem, std::max<size_t>(image.size(), 1)));
     LEANN_HIP(hipMemcpyAsync(out->mem.p, image.data(), image.size(), hipMemcpyHostToDevice, ctx->stream));
     LEANN_HIP(hipStreamSynchronize(ctx->stream));
@@ -583,6 +622,7 @@ int make_rows(leann_ctx *ctx, const int32_t *rows_of_request, const int32_t *ada
     out->used = (const int32_t *)(base + at[6]);
     out->seg_ptr = (const int32_t *)(base + at[7]);
     out->segs = (const int4 *)(base + at[8]);
+    out->wide_tiles = (const int4 *)(base + at[9]);
     return LEANN_OK;
 }
 

@@ -99,16 +99,27 @@ __global__ __launch_bounds__(512, 1) void project_large_kernel(const T *x, int64
 
     // Requests.  A: 8 rows of 128 bytes each, whole lines, the lanes' pieces permuted so that piece c of row r lands at c ^ (r & 7).
     const int a_at = wave * Cfg::A_LOADS * 8 + (lane >> 3), a_piece = (lane & 7) ^ (lane >> 3);
-    const T *p[Cfg::A_LOADS];
+    // Where x ends below 4 GB, offsets of 32 bits from its start (K of 768, 83 229 rows: 320 us, with addresses of 64 bits 336), else addresses; in units of 16 bytes, of
+    // which the host sees to it that there are fewer than 2^32.
+    const uint64_t x_bytes = ((uint64_t)(rows - 1) * ldx + K) * sizeof(T);
+    const bool narrow = x_bytes < 0xffffff00u;
+    const auto x_buffer = buffer_of(x, (int)(uint32_t)x_bytes);
+    uint32_t p[Cfg::A_LOADS];
     auto take_rows = [&](int which) {
 #pragma unroll
-        for (int i = 0; i < Cfg::A_LOADS; ++i) p[i] = x + row_number(which, a_at + i * 8) * ldx + a_piece * 8;
+        for (int i = 0; i < Cfg::A_LOADS; ++i) p[i] = (uint32_t)(row_number(which, a_at + i * 8) * ldx >> 3) + a_piece;
     };
     auto request_a = [&](int pair, int stage) {
         unsigned char *to = smem + stage * Cfg::STAGE + wave * Cfg::A_LOADS * 1024;
         const bool in = pair < whole || pair * 64 + a_piece * 8 < K;
+        if (narrow) {  // beyond x: zeros
 #pragma unroll
-        for (int i = 0; i < Cfg::A_LOADS; ++i) load_to_lds(in ? p[i] + pair * 64 : reinterpret_cast<const T *>(zero_piece), to + i * 1024);
+            for (int i = 0; i < Cfg::A_LOADS; ++i) load_to_lds(x_buffer, in ? (int)((p[i] + pair * 8) * 16) : -256, 0, to + i * 1024);
+        } else {
+#pragma unroll
+            for (int i = 0; i < Cfg::A_LOADS; ++i)
+                load_to_lds(in ? (const void *)(reinterpret_cast<const char *>(x) + ((uint64_t)p[i] + pair * 8) * 16) : zero_piece, to + i * 1024);
+        }
     };
     // An adapter's pair: the pieces of 32 ranks of the rows' low-rank activations (what follows them where there are fewer).
     auto request_pieces = [&](int tm, int group, int stage) {
@@ -194,7 +205,7 @@ __global__ __launch_bounds__(512, 1) void project_large_kernel(const T *x, int64
                         const u32x4 v = *reinterpret_cast<const u32x4 *>(own + r * 128 + ((c ^ (r & 7)) << 4));
                         const int64_t row = row_number(which, at);
                         const bool has = tile_m * BM + at < rows && col < N && (n2 + 1 < TN || c < 4);
-                        *(has ? reinterpret_cast<u32x4 *>(out + row * ldo + col) : nowhere + l) = v;
+                        __builtin_nontemporal_store(v, has ? reinterpret_cast<u32x4 *>(out + row * ldo + col) : nowhere + l);  // W and x stay in L2
                     }
                 }
     };

@@ -316,3 +316,26 @@ def test_large_batches(ctx, batch, n_in, n_out, dtype):
     p.up[sick], p.down[sick] = float("inf"), float("nan")
     assert bool((p.forward()[rest] == out[rest]).all())
     p.close()
+
+
+def test_rows_far_apart_in_large_batches(ctx):
+    """x of more than 4 GB through the tiles of large batches."""
+    import torch
+    import paper_2506_08276_amd as L
+    T, ld, n = 66000, 40960, 256
+    wide = torch.empty((T, ld), dtype=torch.bfloat16, device="cuda:0")  # 5.4 GB
+    g = torch.Generator(device="cuda:0").manual_seed(2)
+    rand = lambda *s: torch.randn(s, generator=g, device="cuda:0").bfloat16()
+    x, out = wide[:, 128:128 + n], wide[:, 1024:1024 + n]
+    x.copy_(rand(T, n))
+    w, down, up = rand(n, n), rand(2, 24, n), rand(2, n, 24)
+    proj = L.leann_projection_create(ctx, w, gradient=True)
+    rows = L.leann_adapter_rows_create(ctx, [30000, 20000, 16000], [1, -1, 0], [24, 9], [0.5, 1.0], 24)
+    y, low = L.leann_adapter_project(ctx, proj, rows, x.contiguous(), down, up, keep=True)
+    L.leann_adapter_project(ctx, proj, rows, x, down, up, out=out)
+    assert bool((out == y).all())
+    a = L.leann_adapter_project_backward(ctx, proj, rows, out, x, low, down, up)
+    b = L.leann_adapter_project_backward(ctx, proj, rows, y, x.contiguous(), low, down, up)
+    assert all(bool((u == v).all()) for u, v in zip(a, b))
+    L.leann_projection_free(proj)
+    L.leann_adapter_rows_free(rows)
