@@ -396,7 +396,7 @@ def _dtype(t):
 def leann_dropout(ctx, x, drop, residual=None, out=None):
     """dropout(x) (+ residual) of a 2-D tensor; drop = (p, seed, offset).  The gradient is the same call on the gradient."""
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        out = torch.empty_like(x)
     (xp, ldx), (rp, ldr), (op, ldo) = _rows(x, "x"), _rows(residual, "residual", x), _rows(out, "out", x)
     _check(load_library().leann_dropout(ctx, xp, ldx, rp, ldr, x.shape[0], x.shape[1], _dtype(x), _drop(drop), op, ldo))
     return out
@@ -407,12 +407,12 @@ def leann_layernorm(ctx, x, gamma, beta, eps, residual=None, drop=None, keep=Fal
     keep: returns (out, total, mean, rstd), what the backward pass needs (total is x where it would hold the same); else out."""
     rows, cols = x.shape
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        out = torch.empty_like(x)
     total = mean = rstd = None
     if keep:
         if residual is not None or drop is not None:
-            total = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=x.device)
+            total = torch.empty_like(x)
+        mean, rstd = gamma.new_empty(rows), gamma.new_empty(rows)
     (xp, ldx), (rp, ldr), (op, ldo), (tp, ldt) = (_rows(x, "x"), _rows(residual, "residual", x), _rows(out, "out", x),
                                                   _rows(total, "total", x))
     _check(load_library().leann_layernorm(ctx, xp, ldx, rp, ldr, rows, cols, _dtype(x), _drop(drop), _vector(gamma, cols, "gamma"),
@@ -425,9 +425,9 @@ def leann_layernorm_backward(ctx, dout, total, mean, rstd, gamma, drop=None, dto
     """(dresidual, dx, dgamma, dbeta) from the gradient of leann_layernorm's output and what it kept; dtotal: the gradient that
     reaches the kept total besides.  Without dropout dx is dresidual."""
     rows, cols = dout.shape
-    dres = torch.empty(dout.shape, dtype=dout.dtype, device=dout.device)
+    dres = torch.empty_like(dout)
     dx = dres if drop is None else torch.empty_like(dres)
-    dgamma, dbeta = torch.empty((2, cols), dtype=torch.float32, device=dout.device)
+    dgamma, dbeta = torch.empty_like(gamma), torch.empty_like(gamma)
     (dp, ldd), (tp, ldt), (ep, lde), (rp, ldr), (xp, ldx) = (_rows(dout, "dout"), _rows(total, "total", dout), _rows(dtotal, "dtotal", dout),
                                                              _rows(dres, "dresidual"), _rows(dx, "dx"))
     _check(load_library().leann_layernorm_backward(ctx, dp, ldd, tp, ldt, rows, cols, _dtype(dout), _vector(gamma, cols, "gamma"),
@@ -487,7 +487,7 @@ def _pools(proj, rows, down, up):
 def leann_adapter_project(ctx, proj, rows, x, down, up, keep=False, out=None):
     """x W^T + bias + each request's adapter's part, x [T][n_in]; keep: returns (out, low), what the backward pass needs; else out."""
     if out is None:
-        out = torch.empty((rows.T, proj.n_out), dtype=proj.dtype, device=x.device)
+        out = x.new_empty((rows.T, proj.n_out))
     assert x.shape == (rows.T, proj.n_in) and out.shape == (rows.T, proj.n_out) and x.dtype == out.dtype == proj.dtype
     low = torch.empty((rows.T, rows.max_rank), dtype=torch.float32, device=x.device) if keep else None
     (xp, ldx), (op, ldo), (dp, up) = _rows(x, "x"), _rows(out, "out"), _pools(proj, rows, down, up)
@@ -499,9 +499,9 @@ def leann_adapter_project_backward(ctx, proj, rows, dout, x, low, down, up, need
     """(dx, ddown, dup) from the gradient of leann_adapter_project's output, its input and what it kept; None for what is not needed
     (x and low may be None without need_adapters)."""
     assert dout.shape == (rows.T, proj.n_out) and dout.dtype == proj.dtype
-    dx = torch.empty((rows.T, proj.n_in), dtype=proj.dtype, device=dout.device) if need_dx else None
-    ddown = torch.empty(down.shape, dtype=torch.float32, device=dout.device) if need_adapters else None
-    dup = torch.empty(up.shape, dtype=torch.float32, device=dout.device) if need_adapters else None
+    dx = dout.new_empty((rows.T, proj.n_in)) if need_dx else None
+    ddown = torch.empty_like(down, dtype=torch.float32) if need_adapters else None
+    dup = torch.empty_like(up, dtype=torch.float32) if need_adapters else None
     if need_adapters:
         assert x.shape == (rows.T, proj.n_in) and x.dtype == proj.dtype
         assert low.is_cuda and low.is_contiguous() and low.shape == (rows.T, rows.max_rank) and low.dtype == torch.float32

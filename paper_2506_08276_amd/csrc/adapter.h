@@ -38,6 +38,8 @@ namespace {
 // Steps of 16 of K in a packed weight: whole numbers of four slabs of 32, zeros beyond K.
 __host__ __device__ inline int project_ksteps(int K) { return (K + 127) / 128 * 8; }
 
+__device__ u32x4 zero_piece;  // zeros, read instead of what rows hold beyond K (not a constant: the compiler would make a branch of the choice, and a wait)
+
 template <class T>
 struct Frag;
 template <>
@@ -74,36 +76,66 @@ __host__ __device__ inline int rank_groups(int R) { return (R + 15) >> 4; }
 
 // The adapters' part of one 32-slot group's tiles: acc[ni] += up[columns of tile ni] pieces[slots]^T for every run of the group that is number `first`,
 // `first + step`, ...  A lane holds one slot of the output, so a run that is not the whole group changes only the lanes that are its own: another request's
-// infinities stay with it.
+// infinities stay with it.  Lane l holds run l of the group's `count`; with an adapter per row, what bounds it is the runs' latency, so B of them have
+// their first 16 ranks on the way together.
 template <int TN, int UP>
-__device__ inline void add_adapters(f32x16 (&acc)[TN], const int32_t *run_ptr, const int4 *runs, int group, int first, int step, const bf16_t *pieces,
+__device__ inline void add_adapters(f32x16 (&acc)[TN], const int4 &my_run, int count, int group, int first, int step, const bf16_t *pieces,
                                     const bf16_t *up, int R16, int column_tiles, int column_tile)
 {
     const int lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31;
-    const int begin = run_ptr[group], count = run_ptr[group + 1] - begin;
-    for (int i = first; i < count; i += step) {
-        const int4 run = runs[begin + i];
-        const int steps = rank_groups(run.z >> 8 & 255), from = run.y - group * 32, to = from + (run.z & 255);
-        const bool own = l32 >= from && l32 < to;
-        const bf16_t *u = up + ((size_t)((uint32_t)run.z >> 16) * column_tiles * R16 * UP * 64 + lane) * 8;
-        f32x16 sum[TN];
+    constexpr int B = TN * UP == 1 ? 4 : 2;
+    if (first >= count) return;
+    auto piece = [&](int k, int which) { return *reinterpret_cast<const bf16x8 *>(pieces + k * 32 + which * 16 + half * 8); };
+    const bf16x8 h1 = piece(0, 0), h2 = piece(0, 1);
+    size_t at[TN];  // of the lane's piece of a column tile; behind the last one: the last one's, for nothing
 #pragma unroll
-        for (int ni = 0; ni < TN; ++ni) sum[ni] = acc[ni];
-        for (int k = 0; k < steps; ++k) {
-            const bf16x8 h1 = *reinterpret_cast<const bf16x8 *>(pieces + k * 32 + half * 8), h2 = *reinterpret_cast<const bf16x8 *>(pieces + k * 32 + 16 + half * 8);
+    for (int ni = 0; ni < TN; ++ni) at[ni] = (size_t)min(column_tile + ni, column_tiles - 1) * R16 * UP * 512 + lane * 8;
+    for (int i = first; i < count; i += B * step) {
+        bf16x8 f[B][TN][UP];
+        int z[B], slot[B];
+#pragma unroll
+        for (int r = 0; r < B; ++r) {
+            const int from = min(i + r * step, count - 1);
+            slot[r] = __builtin_amdgcn_readlane(my_run.y, from) - group * 32;
+            z[r] = __builtin_amdgcn_readlane(my_run.z, from);
+            const bf16_t *u = up + (size_t)((uint32_t)z[r] >> 16) * column_tiles * R16 * UP * 512;
 #pragma unroll
             for (int ni = 0; ni < TN; ++ni)
 #pragma unroll
-                for (int e = 0; e < UP; ++e) {
-                    const bf16x8 f = *reinterpret_cast<const bf16x8 *>(u + (((size_t)min(column_tile + ni, column_tiles - 1) * R16 + k) * UP + e) * 512);
-                    sum[ni] = mfma32(f, h2, sum[ni]);
-                    sum[ni] = mfma32(f, h1, sum[ni]);
-                }
+                for (int e = 0; e < UP; ++e) f[r][ni][e] = *reinterpret_cast<const bf16x8 *>(u + at[ni] + e * 512);
         }
 #pragma unroll
-        for (int ni = 0; ni < TN; ++ni)
+        for (int r = 0; r < B; ++r) {
+            if (i + r * step >= count) break;
+            const int steps = rank_groups(z[r] >> 8 & 255);
+            const bool own = l32 >= slot[r] && l32 < slot[r] + (z[r] & 255);
+            const bf16_t *u = up + (size_t)((uint32_t)z[r] >> 16) * column_tiles * R16 * UP * 512;
+            f32x16 sum[TN];
 #pragma unroll
-            for (int j = 0; j < 16; ++j) acc[ni][j] = own ? sum[ni][j] : acc[ni][j];
+            for (int ni = 0; ni < TN; ++ni) {
+                sum[ni] = acc[ni];
+#pragma unroll
+                for (int e = 0; e < UP; ++e) {
+                    sum[ni] = mfma32(f[r][ni][e], h2, sum[ni]);
+                    sum[ni] = mfma32(f[r][ni][e], h1, sum[ni]);
+                }
+            }
+            for (int k = 1; k < steps; ++k) {
+                const bf16x8 k1 = piece(k, 0), k2 = piece(k, 1);
+#pragma unroll
+                for (int ni = 0; ni < TN; ++ni)
+#pragma unroll
+                    for (int e = 0; e < UP; ++e) {
+                        const bf16x8 g = *reinterpret_cast<const bf16x8 *>(u + at[ni] + (k * UP + e) * 512);
+                        sum[ni] = mfma32(g, k2, sum[ni]);
+                        sum[ni] = mfma32(g, k1, sum[ni]);
+                    }
+            }
+#pragma unroll
+            for (int ni = 0; ni < TN; ++ni)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) acc[ni][j] = own ? sum[ni][j] : acc[ni][j];
+        }
     }
 }
 

@@ -124,8 +124,7 @@ __global__ __launch_bounds__(256) void low_kernel(const T *x, int64_t ldx, const
 #pragma unroll
                 for (int i = 0; i < U; ++i) {
                     const bool in = s + i < to && (s + i) * 32 + q * 8 < K;  // K is a multiple of 8
-                    xf[i][t] = *reinterpret_cast<const F *>(xp[t] + (in ? (s + i) * 32 : 0));
-                    if (!in) xf[i][t] = F{};
+                    xf[i][t] = *(in ? reinterpret_cast<const F *>(xp[t] + (s + i) * 32) : reinterpret_cast<const F *>(&zero_piece));
                 }
 #pragma unroll
             for (int g = 0; g < NT; ++g)
@@ -133,8 +132,7 @@ __global__ __launch_bounds__(256) void low_kernel(const T *x, int64_t ldx, const
 #pragma unroll
                     for (int i = 0; i < U; ++i) {
                         const bool in = s + i < to && (s + i) * 32 + q * 8 < K;
-                        af[i][g] = *reinterpret_cast<const F *>(ap[g] + (in ? (s + i) * 32 : 0));
-                        if (!in) af[i][g] = F{};
+                        af[i][g] = *(in ? reinterpret_cast<const F *>(ap[g] + (s + i) * 32) : reinterpret_cast<const F *>(&zero_piece));
                     }
 #pragma unroll
             for (int i = 0; i < U; ++i)
@@ -178,9 +176,9 @@ __global__ __launch_bounds__(256) void low_kernel(const T *x, int64_t ldx, const
 
 // ------------------------------------------------------------------ the projection
 // out[row][n] = sum over k of x[row][k] W[n][k] + bias[n] + the adapter's part, tiles of 32 TM x 32 TN slots and columns.  Four wavefronts share K, operands from
-// memory to registers; their sums meet in LDS.
-template <class T, int TM, int TN>
-__global__ __launch_bounds__(256) void project_kernel(const T *x, int64_t ldx, const T *w, const float *bias, int N, int K, const int32_t *row_of,
+// memory to registers, U steps of 16 ahead; their sums meet in LDS.  The adapters come first, while the first operands are on their way.
+template <class T, int TM, int TN, int U>
+__global__ __launch_bounds__(256, 2) void project_kernel(const T *x, int64_t ldx, const T *w, const float *bias, int N, int K, const int32_t *row_of,
                                                       int rows, const int32_t *run_ptr, const int4 *runs, const bf16_t *pieces, int R16,
                                                       const bf16_t *up, T *out, int64_t ldo)
 {
@@ -188,14 +186,22 @@ __global__ __launch_bounds__(256) void project_kernel(const T *x, int64_t ldx, c
     constexpr int BM = 32 * TM, BN = 32 * TN, PITCH = BN + 4;
     __shared__ float sums[4][BM][PITCH];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, l32 = lane & 31;
-    const int tiles_n = (N + BN - 1) / BN, tile_n = blockIdx.x % tiles_n, tile_m = blockIdx.x / tiles_n;
+    // Blocks go round-robin to the 8 XCDs: those of one take a run of tiles, all columns of a few rows (3391 x 384 x 1536: 18 us, with columns apart 24).
+    const int tiles_n = (N + BN - 1) / BN, tile = (int)((blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3));
+    const int tile_n = tile % tiles_n, tile_m = tile / tiles_n;
+    if (tile_m * BM >= rows) return;
     const int ksteps = project_ksteps(K), used = (K + 15) >> 4, per = (used + 3) >> 2, from = wave * per, to = min(used, from + per);
-    int64_t row[TM];
     const T *xp[TM], *wp[TN];
+    int4 my_run[TM];
+    int count[TM];
+#pragma unroll
+    for (int mi = 0; mi < TM; ++mi) xp[mi] = x + (int64_t)row_of[tile_m * BM + mi * 32 + l32] * ldx + half * 8;
 #pragma unroll
     for (int mi = 0; mi < TM; ++mi) {
-        row[mi] = row_of[tile_m * BM + mi * 32 + l32];
-        xp[mi] = x + row[mi] * ldx + half * 8;
+        const int group = tile_m * TM + mi, begin = group * 32 < rows ? run_ptr[group] : 0;
+        count[mi] = group * 32 < rows ? run_ptr[group + 1] - begin : 0;
+        my_run[mi] = int4{};
+        if (lane < count[mi]) my_run[mi] = runs[begin + lane];
     }
     const int last_ct = (N - 1) >> 5;
 #pragma unroll
@@ -205,33 +211,31 @@ __global__ __launch_bounds__(256) void project_kernel(const T *x, int64_t ldx, c
     for (int mi = 0; mi < TM; ++mi)
 #pragma unroll
         for (int ni = 0; ni < TN; ++ni) acc[mi][ni] = f32x16{};
-    constexpr int U = TM * TN > 1 ? 4 : 6;  // steps whose operands are on their way together
+    F xf[U][TM], wf[U][TN];
+    auto fetch = [&](int i, int s) {  // behind the share's end: zeros of x
+        const bool in = s < to && s * 16 + half * 8 < K;
+        const int ws = max(min(s, to - 1), 0);
+#pragma unroll
+        for (int ni = 0; ni < TN; ++ni) wf[i][ni] = *reinterpret_cast<const F *>(wp[ni] + (size_t)ws * 512);
+#pragma unroll
+        for (int mi = 0; mi < TM; ++mi) xf[i][mi] = *(in ? reinterpret_cast<const F *>(xp[mi] + s * 16) : reinterpret_cast<const F *>(&zero_piece));
+    };
+#pragma unroll
+    for (int i = 0; i < U; ++i) fetch(i, from + i);
+#pragma unroll
+    for (int mi = 0; mi < TM; ++mi)
+        add_adapters<TN, Frag<T>::PIECES>(acc[mi], my_run[mi], count[mi], tile_m * TM + mi, wave, 4,
+                                          pieces + (int64_t)min(tile_m * BM + mi * 32 + l32, rows - 1) * R16 * 32, up, R16, last_ct + 1, tile_n * TN);
     for (int s = from; s < to; s += U) {
-        F xf[U][TM], wf[U][TN];
 #pragma unroll
         for (int i = 0; i < U; ++i) {
-            const bool in = s + i < to && (s + i) * 16 + half * 8 < K;
-            const int k = in ? (s + i) * 16 : 0;
-#pragma unroll
-            for (int ni = 0; ni < TN; ++ni) wf[i][ni] = *reinterpret_cast<const F *>(wp[ni] + (size_t)min(s + i, to - 1) * 512);
-#pragma unroll
-            for (int mi = 0; mi < TM; ++mi) {
-                xf[i][mi] = *reinterpret_cast<const F *>(xp[mi] + k);
-                if (!in) xf[i][mi] = F{};
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < U; ++i)
 #pragma unroll
             for (int mi = 0; mi < TM; ++mi)
 #pragma unroll
                 for (int ni = 0; ni < TN; ++ni) acc[mi][ni] = mfma32(wf[i][ni], xf[i][mi], acc[mi][ni]);
+            fetch(i, s + U + i);
+        }
     }
-#pragma unroll
-    for (int mi = 0; mi < TM; ++mi)
-        if (tile_m * BM + mi * 32 < rows)
-            add_adapters<TN, Frag<T>::PIECES>(acc[mi], run_ptr, runs, tile_m * TM + mi, wave, 4,
-                                              pieces + (int64_t)min(tile_m * BM + mi * 32 + l32, rows - 1) * R16 * 32, up, R16, last_ct + 1, tile_n * TN);
 #pragma unroll
     for (int mi = 0; mi < TM; ++mi)
 #pragma unroll
@@ -486,11 +490,11 @@ void enqueue_project(leann_ctx *ctx, const leann_adapter_rows *rows, const T *x,
         return;
     }
     auto go = [&](auto kernel, int64_t blocks) {
-        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, ctx->stream, x, ldx, w, bias, N, K, rows->row_of, (int)rows->T, rows->run_ptr,
+        hipLaunchKernelGGL(kernel, dim3((unsigned)((blocks + 7) / 8 * 8)), dim3(256), 0, ctx->stream, x, ldx, w, bias, N, K, rows->row_of, (int)rows->T, rows->run_ptr,
                            rows->runs, pieces, R16, up, out, ldo);
     };
-    if (tiles64 < ctx->num_cus) go(project_kernel<T, 1, 1>, (int64_t)T32 * ((N + 31) / 32));
-    else go(project_kernel<T, 2, 2>, tiles64);
+    if (tiles64 < ctx->num_cus) go(project_kernel<T, 1, 1, 8>, (int64_t)T32 * ((N + 31) / 32));
+    else go(project_kernel<T, 2, 2, 4>, tiles64);
 }
 
 size_t pieces_bytes(const leann_adapter_rows *rows) { return up256((size_t)rows->T * rank_groups(rows->max_rank) * 64 + 64); }  // 64: read past the last one's, see request_pieces

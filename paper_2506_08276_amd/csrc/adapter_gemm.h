@@ -7,7 +7,6 @@ namespace {
 typedef __attribute__((address_space(3))) void lds_t;
 typedef const __attribute__((address_space(1))) void global_t;
 
-__device__ const uint32_t zero_piece[4] = {0, 0, 0, 0};  // what rows hold beyond K
 __device__ u32x4 nowhere[64];                            // where lanes without an output store; never read
 
 // A tile: WM x (8 / WM) wavefronts of TM x TN 32x32 MFMA tiles.  K goes by pairs of slabs of 32, 128 bytes of a row of x.
@@ -118,7 +117,7 @@ __global__ __launch_bounds__(512, 1) void project_large_kernel(const T *x, int64
         } else {
 #pragma unroll
             for (int i = 0; i < Cfg::A_LOADS; ++i)
-                load_to_lds(in ? (const void *)(reinterpret_cast<const char *>(x) + ((uint64_t)p[i] + pair * 8) * 16) : zero_piece, to + i * 1024);
+                load_to_lds(in ? (const void *)(reinterpret_cast<const char *>(x) + ((uint64_t)p[i] + pair * 8) * 16) : (const void *)&zero_piece, to + i * 1024);
         }
     };
     // An adapter's pair: the pieces of 32 ranks of the rows' low-rank activations (what follows them where there are fewer).
@@ -267,7 +266,7 @@ __global__ __launch_bounds__(512, 1) void project_large_kernel(const T *x, int64
     ask_w(Pair{0, -1, 0}, 0, 0, 0);
     ask_w(Pair{0, -1, 0}, 0, 1, 0);
     ask_w(Pair{0, -1, 1}, 0, 0, 1);
-    wait_memory_and_lds<2 * Cfg::W_LOADS>();
+    wait_memory_and_lds<Cfg::W_LOADS>();  // W's first two slabs: the first phase's wait counts on stores, which the first tile has not issued
     barrier();
     if (second) barrier();  // a phase behind
     int stage = 0;          // of the pair at hand
