@@ -556,8 +556,9 @@ int make_rows(leann_ctx *ctx, const int32_t *rows_of_request, const int32_t *ada
     row_of.insert(row_of.end(), 8, 0);  // outer_kernel reads eight at a time
 
     const int64_t adapted = slot_of[n_adapters];
-    // Rows of a chunk: as many as leave some four blocks for each CU (a block takes 256 columns of one), 64 at least, 1024 at most.
-    const int chunk_rows = (int)std::min<int64_t>(1024, std::max<int64_t>(64, (adapted / (ctx->num_cus * 2 / 3) + 63) / 64 * 64));
+    // Rows of a chunk of outer_kernel: as many as leave one chunk for every third CU (times the blocks of 128 columns, twelve at 768 + 768), 64 at least, 2048 at most.
+    // 82 953 rows 768 -> 768, ranks up to 32: 229 us for the whole gradient, with chunks half as long 239 (their sums are written and read again).
+    const int chunk_rows = (int)std::min<int64_t>(2048, std::max<int64_t>(64, (adapted / std::max(1, ctx->num_cus / 3) + 63) / 64 * 64));
     std::vector<int4> tiles, wide, chunks, runs, adapters(n_adapters);
     std::vector<int4> segs;
     std::vector<int32_t> used, run_ptr((T + 31) / 32 + 1, 0), seg_ptr((T + 255) / 256 + 1, 0);

@@ -41,9 +41,13 @@ struct Raw8 {
     }
     __device__ inline f32x8 wide() const { return __builtin_convertvector(v, f32x8); }
     __device__ inline void round(const f32x8 &f) { v = __builtin_convertvector(f, typename Vec8<T>::type); }  // to nearest, ties to even
-    __device__ inline void store(T *p, int n) const
+    __device__ inline void store(T *p, int n, bool streaming = false) const
     {
-        if (n >= 8) {
+        if (n >= 8 && streaming) {
+            typedef typename Vec8<T>::type V;
+            typedef V Anywhere __attribute__((aligned(sizeof(T))));
+            __builtin_nontemporal_store(v, reinterpret_cast<Anywhere *>(p));
+        } else if (n >= 8) {
             __builtin_memcpy(p, &v, sizeof(v));
         } else {
 #pragma unroll
