@@ -8,6 +8,7 @@
 #include <vector>
 
 #include "adapter_gemm.h"
+#include "adapter_plan.h"
 
 namespace {
 
@@ -166,7 +167,9 @@ __global__ __launch_bounds__(256) void low_kernel(const T *x, int64_t ldx, const
             if (g < groups) {
                 v *= scale;
                 const bf16x4 first = __builtin_convertvector(v, bf16x4);
-                v -= __builtin_convertvector(first, f32x4);
+                const f32x4 taken = __builtin_convertvector(first, f32x4);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] = __builtin_isfinite(taken[i]) ? v[i] - taken[i] : 0.f;  // an infinity is its first piece
                 *reinterpret_cast<bf16x4 *>(to + g * 32 + q * 4) = first;
                 *reinterpret_cast<bf16x4 *>(to + g * 32 + 16 + q * 4) = __builtin_convertvector(v, bf16x4);
             }
@@ -478,9 +481,10 @@ template <class T>
 void enqueue_project(leann_ctx *ctx, const leann_adapter_rows *rows, const T *x, int64_t ldx, const T *w, const float *bias, int N, int K,
                      const bf16_t *pieces, const bf16_t *up, T *out, int64_t ldo)
 {
-    const int T32 = (int)((rows->T + 31) / 32), T64 = (int)((rows->T + 63) / 64), R16 = rank_groups(rows->max_rank);
-    const int64_t tiles64 = (int64_t)T64 * ((N + 63) / 64);
-    if (K >= 256 && tiles64 >= ctx->num_cus * 8 && rows->T * ldx / 8 < 0xffffff00ll) {
+    const int R16 = rank_groups(rows->max_rank);
+    ProjectTile tile = choose_project(ctx->num_cus, rows->T, N, K);
+    if (tile == PROJECT_256 && rows->T * ldx / 8 >= 0xffffff00ll) tile = PROJECT_64;  // beyond the large tiles' offsets
+    if (tile == PROJECT_256) {
         typedef ProjectCfg<2, 4, 2> Cfg;
         const int tiles_n = (N + Cfg::BN - 1) / Cfg::BN;
         const int64_t tiles = (rows->T + Cfg::BM - 1) / Cfg::BM * tiles_n;
@@ -489,12 +493,14 @@ void enqueue_project(leann_ctx *ctx, const leann_adapter_rows *rows, const T *x,
                            tiles_n);
         return;
     }
-    auto go = [&](auto kernel, int64_t blocks) {
-        hipLaunchKernelGGL(kernel, dim3((unsigned)((blocks + 7) / 8 * 8)), dim3(256), 0, ctx->stream, x, ldx, w, bias, N, K, rows->row_of, (int)rows->T, rows->run_ptr,
-                           rows->runs, pieces, R16, up, out, ldo);
+    const int size = tile == PROJECT_32 ? 32 : 64;
+    const int64_t blocks = (rows->T + size - 1) / size * ((N + size - 1) / size);
+    auto go = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)((blocks + 7) / 8 * 8)), dim3(256), 0, ctx->stream, x, ldx, w, bias, N, K, rows->row_of, (int)rows->T,
+                           rows->run_ptr, rows->runs, pieces, R16, up, out, ldo);
     };
-    if (tiles64 < ctx->num_cus) go(project_kernel<T, 1, 1, 8>, (int64_t)T32 * ((N + 31) / 32));
-    else go(project_kernel<T, 2, 2, 4>, tiles64);
+    if (tile == PROJECT_32) go(project_kernel<T, 1, 1, 8>);
+    else go(project_kernel<T, 2, 2, 4>);
 }
 
 size_t pieces_bytes(const leann_adapter_rows *rows) { return up256((size_t)rows->T * rank_groups(rows->max_rank) * 64 + 64); }  // 64: read past the last one's, see request_pieces
