@@ -361,11 +361,22 @@ __global__ __launch_bounds__(512, 1) void project_large_kernel(const T *x, int64
         // A lane holds one slot of the output; the lanes that are not the adapter's keep what they have: another request's infinities stay with it.
         auto adapter_phase = [&](int slab) {
             barrier();
-            if (now.group * UP + slab < ((now_seg.z + 15) >> 4) * UP) {
+            const int first = tile_m * BM + wm * TM * 32;  // the wavefront's slots: all the adapter's, some or none
+            const bool has_ranks = now.group * UP + slab < ((now_seg.z + 15) >> 4) * UP;
+            if (has_ranks && now_seg.x <= first && now_seg.y >= first + TM * 32) {
+#pragma unroll
+                for (int ks = 1; ks >= 0; --ks)
+#pragma unroll
+                    for (int mi = 0; mi < TM; ++mi)
+#pragma unroll
+                        for (int ni = 0; ni < TN; ++ni)
+                            acc[mi][ni] = mfma32(__builtin_bit_cast(bf16x8, bf[0][ni]), __builtin_bit_cast(bf16x8, af[ks][mi]), acc[mi][ni]);
+            }
+            if (has_ranks && now_seg.x < first + TM * 32 && now_seg.y > first && (now_seg.x > first || now_seg.y < first + TM * 32)) {
 #pragma unroll
                 for (int mi = 0; mi < TM; ++mi) {
-                    const int first = tile_m * BM + (wm * TM + mi) * 32;
-                    const bool mine = first + l32 >= now_seg.x && first + l32 < now_seg.y;
+                    const int slot = first + mi * 32 + l32;
+                    const bool mine = slot >= now_seg.x && slot < now_seg.y;
 #pragma unroll
                     for (int ni = 0; ni < TN; ++ni) {
                         const bf16x8 u = __builtin_bit_cast(bf16x8, bf[0][ni]);
@@ -382,7 +393,7 @@ __global__ __launch_bounds__(512, 1) void project_large_kernel(const T *x, int64
             read(0, 0, stage);
             first_half();
             adapter_phase(0);
-            read(UP == 2 ? 0 : 1, 1, stage);
+            if (now.group * UP + 1 < ((now_seg.z + 15) >> 4) * UP) read(UP == 2 ? 0 : 1, 1, stage);
             second_half();
             adapter_phase(1);
             shift();
