@@ -101,6 +101,7 @@ __global__ __launch_bounds__(256) void low_kernel(const T *x, int64_t ldx, const
     if (index >= n_tiles) return;
     const int4 tile = tiles[index];
     const int n = tile.z & 0xffff, rank = tile.z >> 16, groups = (rank + 15) >> 4;
+    const float scale = rank ? __int_as_float(adapters[tile.x].w) : 0.f;
     int64_t row[RT];
 #pragma unroll
     for (int t = 0; t < RT; ++t) row[t] = row_of[tile.y + min(t * 16 + j, n - 1)];
@@ -151,7 +152,6 @@ __global__ __launch_bounds__(256) void low_kernel(const T *x, int64_t ldx, const
             for (int g = 0; g < NT; ++g) acc[0][g] = (part[0][g][lane] + part[1][g][lane]) + (part[2][g][lane] + part[3][g][lane]);
         }
     }
-    const float scale = rank ? __int_as_float(adapters[tile.x].w) : 0.f;
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
         if (t * 16 + j >= n) continue;

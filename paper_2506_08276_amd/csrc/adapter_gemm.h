@@ -98,8 +98,11 @@ __global__ __launch_bounds__(512, 1) void project_large_kernel(const T *x, int64
     };
     auto row_number = [&](int which, int at) { return (int64_t) * reinterpret_cast<const int *>(row_table + (which * BM + at) * 4); };
 
-    // Requests.  A: 8 rows of 128 bytes each, whole lines, the lanes' pieces permuted so that piece c of row r lands at c ^ (r & 7).
-    const int a_at = wave * Cfg::A_LOADS * 8 + (lane >> 3), a_piece = (lane & 7) ^ (lane >> 3);
+    // Requests.  A: 8 rows of 128 bytes each, whole lines, the lanes' pieces permuted so that piece c of row r lands at c ^ ((r >> 1) & 7): 16 rows'
+    // reads of one piece reach all 64 banks.
+    const int a_at = wave * Cfg::A_LOADS * 8 + (lane >> 3);
+    static_assert(Cfg::A_LOADS % 2 == 0, "a wavefront's first row is a multiple of 16");
+    auto a_piece = [&](int i) { return (lane & 7) ^ ((lane >> 4) + (i & 1) * 4); };  // of request i
     // Where x ends below 4 GB, offsets of 32 bits from its start (K of 768, 83 229 rows: 320 us, with addresses of 64 bits 336), else addresses; in units of 16 bytes, of
     // which the host sees to it that there are fewer than 2^32.
     const uint64_t x_bytes = ((uint64_t)(rows - 1) * ldx + K) * sizeof(T);
@@ -108,18 +111,18 @@ __global__ __launch_bounds__(512, 1) void project_large_kernel(const T *x, int64
     uint32_t p[Cfg::A_LOADS];
     auto take_rows = [&](int which) {
 #pragma unroll
-        for (int i = 0; i < Cfg::A_LOADS; ++i) p[i] = (uint32_t)(row_number(which, a_at + i * 8) * ldx >> 3) + a_piece;
+        for (int i = 0; i < Cfg::A_LOADS; ++i) p[i] = (uint32_t)(row_number(which, a_at + i * 8) * ldx >> 3) + a_piece(i);
     };
     auto request_a = [&](int pair, int stage) {
         unsigned char *to = smem + stage * Cfg::STAGE + wave * Cfg::A_LOADS * 1024;
-        const bool in = pair < whole || pair * 64 + a_piece * 8 < K;
+        auto in = [&](int i) { return pair < whole || pair * 64 + a_piece(i) * 8 < K; };
         if (narrow) {  // beyond x: zeros
 #pragma unroll
-            for (int i = 0; i < Cfg::A_LOADS; ++i) load_to_lds(x_buffer, in ? (int)((p[i] + pair * 8) * 16) : -256, 0, to + i * 1024);
+            for (int i = 0; i < Cfg::A_LOADS; ++i) load_to_lds(x_buffer, in(i) ? (int)((p[i] + pair * 8) * 16) : -256, 0, to + i * 1024);
         } else {
 #pragma unroll
             for (int i = 0; i < Cfg::A_LOADS; ++i)
-                load_to_lds(in ? (const void *)(reinterpret_cast<const char *>(x) + ((uint64_t)p[i] + pair * 8) * 16) : (const void *)&zero_piece, to + i * 1024);
+                load_to_lds(in(i) ? (const void *)(reinterpret_cast<const char *>(x) + ((uint64_t)p[i] + pair * 8) * 16) : (const void *)&zero_piece, to + i * 1024);
         }
     };
     // An adapter's pair: the pieces of 32 ranks of the rows' low-rank activations (what follows them where there are fewer).
@@ -127,7 +130,7 @@ __global__ __launch_bounds__(512, 1) void project_large_kernel(const T *x, int64
         unsigned char *to = smem + stage * Cfg::STAGE + wave * Cfg::A_LOADS * 1024;
 #pragma unroll
         for (int i = 0; i < Cfg::A_LOADS; ++i)
-            load_to_lds(pieces + ((int64_t)min(tm * BM + a_at + i * 8, rows - 1) * R16 + group) * 32 + a_piece * 8, to + i * 1024);
+            load_to_lds(pieces + ((int64_t)min(tm * BM + a_at + i * 8, rows - 1) * R16 + group) * 32 + a_piece(i) * 8, to + i * 1024);
     };
     // W: 32 columns and 16 of K each, operand order in LDS too.  Offsets behind the last column: zeros.
     auto request_w = [&](__amdgpu_buffer_rsrc_t b, int column_bytes, int step_bytes, int at, int slab, int stage) {
@@ -144,7 +147,7 @@ __global__ __launch_bounds__(512, 1) void project_large_kernel(const T *x, int64
         for (int i = 0; i < TN * 32; i += 64) load_word_to_lds(bias_buffer, (tn * BN + wn * TN * 32 + i + lane) * 4, own_bias + i * 4);
     };
 
-    const int a_read = wm * TM * 4096 + l32 * 128 + ((half ^ (l32 & 7)) << 4), w_read = Cfg::A_BYTES + wn * TN * 2048 + lane * 16;
+    const int a_read = wm * TM * 4096 + l32 * 128 + ((half ^ ((l32 >> 1) & 7)) << 4), w_read = Cfg::A_BYTES + wn * TN * 2048 + lane * 16;
     F af[2][TM], bf[2][TN];
     f32x16 acc[TM][TN];
     auto read = [&](int a_slab, int w_slab, int stage) {
@@ -173,7 +176,7 @@ __global__ __launch_bounds__(512, 1) void project_large_kernel(const T *x, int64
         barrier();
     };
 
-    // Out: 16 rows of 64 columns at a time through the wavefront's own 2 KB (piece c of row r at c ^ (r & 7)), in whole lines of 128 bytes.  Every lane issues
+    // Out: 16 rows of 64 columns at a time through the wavefront's own 2 KB (piece c of row r at c ^ ((r >> 1) & 7)), in whole lines of 128 bytes.  Every lane issues
     // every store, as waits count them.
     typedef typename Frag<T>::four Four;
     const uint64_t out_bytes = ((uint64_t)(rows - 1) * ldo + N) * sizeof(T);
@@ -198,7 +201,7 @@ __global__ __launch_bounds__(512, 1) void project_large_kernel(const T *x, int64
                                 Four v;
 #pragma unroll
                                 for (int i = 0; i < 4; ++i) v[i] = (T)acc[mi][n2 + c2][4 * g + i];
-                                *reinterpret_cast<Four *>(own + (l32 & 15) * 128 + (((c2 * 4 + g) ^ (l32 & 7)) << 4) + half * 8) = v;
+                                *reinterpret_cast<Four *>(own + (l32 & 15) * 128 + (((c2 * 4 + g) ^ ((l32 >> 1) & 7)) << 4) + half * 8) = v;
                             }
                     }
                     __builtin_amdgcn_wave_barrier();
@@ -206,7 +209,7 @@ __global__ __launch_bounds__(512, 1) void project_large_kernel(const T *x, int64
                     for (int j = 0; j < 2; ++j) {
                         const int r = j * 8 + (l >> 3), c = l & 7, at = wm * TM * 32 + mi * 32 + hi * 16 + r;
                         const int col = tile_n * BN + (wn * TN + n2) * 32 + c * 8;
-                        const u32x4 v = *reinterpret_cast<const u32x4 *>(own + r * 128 + ((c ^ (r & 7)) << 4));
+                        const u32x4 v = *reinterpret_cast<const u32x4 *>(own + r * 128 + ((c ^ ((r >> 1) & 7)) << 4));
                         const int64_t row = row_number(which, at);
                         const bool has = tile_m * BM + at < rows && col < N && (n2 + 1 < TN || c < 4);
                         // Past L2, where W and x stay (83 229 x 2304 x 768: 318 us, through it 350).  Below 4 GB an offset behind the end is no access at all.
