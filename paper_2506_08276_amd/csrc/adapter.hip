@@ -31,6 +31,7 @@ __global__ __launch_bounds__(256) void pack_kernel(const T *w, int N, int K, int
 }
 
 // up[n][r] (IS_UP) or down[r][n] of the used adapters in the order that the products read, see adapter.h: one piece of 8 ranks of a column per thread and step.
+// In the low-rank activations' launch, beside them.
 template <class T, bool IS_UP>
 __device__ inline void lay_out(const T *from, const int32_t *used, const int4 *adapters, int n_used, int R, int N, bf16_t *to, int block, int blocks)
 {
@@ -57,7 +58,8 @@ __device__ inline void lay_out(const T *from, const int32_t *used, const int4 *a
     }
 }
 
-// Before the gradients: `up` of the used adapters transposed (up[n][r] -> up_t[r][n], blocks of 32 x 32), and `down` laid out for the product.
+// Before the gradients: `up` of the used adapters transposed (up[n][r] -> up_t[r][n], blocks of 32 x 32, so that the low-rank activations' kernel reads rows of it as it
+// reads `down`), and `down` laid out for the product.  A few hundred KB: a launch, 5 to 6 us.
 template <class T>
 __global__ __launch_bounds__(256) void lay_out_kernel(const T *down, const T *up, const int32_t *used, const int4 *adapters, int n_used, int R, int K,
                                                       int N, T *up_t, bf16_t *down_packed, int transposing)
@@ -83,7 +85,8 @@ __global__ __launch_bounds__(256) void lay_out_kernel(const T *down, const T *up
 // low[row][r] = sum over k of x[row][k] down[a][r][k] for 16 RT slots of one adapter, in MFMA 16x16x32: a lane ends with four ranks of a row.
 // They go out as they are, by row (`low`, if wanted), and times the adapter's scale in the pieces that the product reads, by slot.
 // SPLIT: a block per tile, whose four wavefronts share K; else a wavefront per tile, of 32 rows, as reading `down` again for every 16 of them would
-// cost as much as reading x.  Blocks from `low_blocks` on lay out `up`.
+// cost as much as reading x.  Blocks from `low_blocks` on lay out `up`.  Bound by memory and the way there: 83 229 rows of 768, rank 16, take 29 us (4.8 TB/s with what
+// it writes), with 16 rows per wavefront 31.5; rank 32 38 and 46, K of 2304 82 and 106.  48 rows of 768: 4.2 us, a launch and two dependent reads.
 template <class T, int NT, int RT, bool SPLIT>
 __global__ __launch_bounds__(256) void low_kernel(const T *x, int64_t ldx, const T *down, int R, int K, const int32_t *row_of, const int4 *tiles,
                                                   int n_tiles, int low_blocks, int compact, float *low, bf16_t *pieces, const int4 *adapters, const T *up,
@@ -179,7 +182,9 @@ __global__ __launch_bounds__(256) void low_kernel(const T *x, int64_t ldx, const
 
 // ------------------------------------------------------------------ the projection
 // out[row][n] = sum over k of x[row][k] W[n][k] + bias[n] + the adapter's part, tiles of 32 TM x 32 TN slots and columns.  Four wavefronts share K, operands from
-// memory to registers, U steps of 16 ahead; their sums meet in LDS.  The adapters come first, while the first operands are on their way.
+// memory to registers, U steps of 16 ahead; their sums meet in LDS.  The adapters come first, while the first operands are on their way.  For few rows, where the time
+// of one tile is what counts: 48 x 768 x 768 5.8 us, bound by the reads that wait for each other (row number, x; runs, pieces, `up`); 3391 x 384 x 1536 in tiles of
+// 64 x 64 21 us.  Beyond that the larger tile reads less.
 template <class T, int TM, int TN, int U>
 __global__ __launch_bounds__(256, 2) void project_kernel(const T *x, int64_t ldx, const T *w, const float *bias, int N, int K, const int32_t *row_of,
                                                       int rows, const int32_t *run_ptr, const int4 *runs, const bf16_t *pieces, int R16,
@@ -294,7 +299,8 @@ __device__ inline f32x4 outer_step(const bf16x8 (&h)[3], const f16x8 &p, f32x4 c
 // partial[chunk][r][c] = sum over the chunk's rows of low[row][r] p[row][c]: c < K from x and the low-rank gradients (down's), then N from dout and the
 // low-rank activations (up's).  A block takes 128 columns and 16 NR ranks, its wavefronts 32 rows each in turn; a lane reads 16 bytes of a row and turns
 // eight rows of them, in registers, into the MFMA operands of its eight columns; low goes through LDS, 16 bytes of a row per lane on the way in.  The next
-// rows are on their way while these are multiplied, and the numbers of those after them.
+// rows are on their way while these are multiplied, and the numbers of those after them.  Bound by the bytes in flight (208 registers, two wavefronts per SIMD):
+// 82 953 rows, 768 + 768 columns, rank up to 32: 72 us, 3.5 TB/s.
 template <class T, int NR>
 __global__ __launch_bounds__(256) void outer_kernel(const T *x, int64_t ldx, const T *dout, int64_t ldd, const float *grad_low, const float *low, int R,
                                                     int K, int N, const int32_t *row_of, const int4 *chunks, int last_slots, float *partial)
@@ -387,7 +393,7 @@ __global__ __launch_bounds__(256) void outer_kernel(const T *x, int64_t ldx, con
     }
 }
 
-// ddown[a][r][k] and dup[a][n][r] from the chunks' sums, in their order; 0 where an adapter has no rows, and beyond its rank.
+// ddown[a][r][k] and dup[a][n][r] from the chunks' sums, in their order; 0 where an adapter has no rows, and beyond its rank.  13.5 MB of sums: 4.9 us.
 __global__ __launch_bounds__(1024) void outer_sum_kernel(const float *partial, const int4 *adapters, int R, int K, int N, float *ddown, float *dup)
 {
     __shared__ float tile[32][33];

@@ -60,6 +60,12 @@ __device__ inline void load_word_to_lds(__amdgpu_buffer_rsrc_t b, int offset, un
 
 __device__ inline void store_past_l2(const u32x4 &v, __amdgpu_buffer_rsrc_t b, int offset) { __builtin_amdgcn_raw_buffer_store_b128(v, b, offset, 0, 2); }
 
+// out[row][n] = sum over k of x[row][k] W[n][k] + bias[n] + the adapter's part, for many rows.  Persistent blocks of eight wavefronts, one per compute unit, a tile after the
+// other; two groups of four take turns, one multiplying a slab while the other reads operands and requests, so that every SIMD has one of each.  An adapter of the
+// tile is one more pair of slabs: pieces of the low-rank activations against `up`.
+// 83 229 x 2304 x 768 with six adapters of rank 16: 300 us, 1.0 PFLOP/s, matrix pipes 49 % busy.  Bound by the memory phase: 48 KB of LDS reads per slab and the bytes
+// of x in flight (two pairs, all that LDS holds) against the cache's latency; the write-out is 8 us per tile.  In turn: 256 x 192 tiles 421 us, two blocks
+// of 128 x 192 per unit 356, three pairs of x and three slabs of W 343, at the times when this one took 372, 318 and 328 with all else of the call.
 template <class T, int WM, int TM, int TN>
 __global__ __launch_bounds__(512, 1) void project_large_kernel(const T *x, int64_t ldx, const T *w, const float *bias, int N, int K,
                                                                const int32_t *row_of, int rows, const int32_t *seg_ptr, const int4 *segs,

@@ -6,7 +6,8 @@
 
 namespace {
 
-// out = residual + dropout(x).  One access of eight elements per thread and step.
+// out = residual + dropout(x).  One access of eight elements per thread and step: one generator call makes the eight's numbers, and no row length leaves lanes idle.
+// Bound by memory: 131 072 x 768 bf16 with residual 112 us, 5.4 TB/s; a dozen rows take a launch, 7.6 us.
 template <class T, bool DROP, bool RES>
 __global__ __launch_bounds__(256) void dropout_kernel(const T *x, int64_t ldx, const T *res, int64_t ldr, T *out, int64_t ldo, int rows, int cols,
                                                       int streaming, Drop drop)
@@ -36,12 +37,25 @@ __global__ __launch_bounds__(256) void dropout_kernel(const T *x, int64_t ldx, c
     }
 }
 
-// Sum over the WPR wavefronts of a row, in all of them; `slot` is one of two alternating places, so that one barrier per sum is enough.
-template <int WPR>
+// Sum over the LPR lanes of a row, in all of them: part of a wavefront (of neighbouring lanes), one, or several; for those `slot` is one of two alternating
+// places, so that one barrier per sum is enough.
+template <int LPR>
 __device__ inline float row_sum(float v, float *shared, int slot)
 {
-    v = wave_sum(v);
-    if constexpr (WPR > 1) {
+    if constexpr (LPR < 64) {
+        if constexpr (LPR == 32) {
+            const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+            v = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+        }
+        v += __uint_as_float(dpp_mov<DPP_ROW_ROR8>(__float_as_uint(v)));
+        v += __uint_as_float(dpp_mov<DPP_ROW_ROR4>(__float_as_uint(v)));
+        v += __uint_as_float(dpp_mov<DPP_ROW_ROR2>(__float_as_uint(v)));
+        v += __uint_as_float(dpp_mov<DPP_QUAD_XOR1>(__float_as_uint(v)));
+    } else {
+        v = wave_sum(v);
+    }
+    if constexpr (LPR > 64) {
+        constexpr int WPR = LPR / 64;
         float *s = shared + slot * WPR;
         if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
         __syncthreads();
@@ -52,22 +66,36 @@ __device__ inline float row_sum(float v, float *shared, int slot)
     return v;
 }
 
+// Which rows a thread works on: LPR lanes per row, blocks of 256 threads.
+template <int LPR>
+struct RowsOf {
+    static constexpr int PER_BLOCK = 256 / LPR;
+    static __device__ inline int at() { return threadIdx.x % LPR; }  // the thread's first access of a row
+    static __device__ inline int64_t first()
+    {
+        // the same in a whole wavefront or block: a scalar
+        if constexpr (LPR == 256) return blockIdx.x;
+        else if constexpr (LPR == 64) return (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        else return (int64_t)blockIdx.x * PER_BLOCK + threadIdx.x / LPR;
+    }
+};
+
 __device__ inline float sum8(const f32x8 &v) { return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7])); }
 
-// t = residual + dropout(x); out = (t - mean) rstd gamma + beta.  WPR wavefronts per row (1: four rows per block), NC accesses of eight elements per lane.
-// Mean first, then the squares of what is left, both from registers in 32 bits: rows whose mean is large lose nothing.
-template <class T, int WPR, int NC, bool DROP>
-__global__ __launch_bounds__(WPR == 1 ? 256 : WPR * 64) void layernorm_kernel(const T *x, int64_t ldx, const T *res, int64_t ldr, int rows, int cols,
-                                                                              const float *gamma, const float *beta, float eps, T *out, int64_t ldo,
-                                                                              T *total, int64_t ldt, float *mean_out, float *rstd_out, int streaming, Drop drop)
+// t = residual + dropout(x); out = (t - mean) rstd gamma + beta.  LPR lanes per row, NC accesses of eight elements per lane.
+// Mean first, then the squares of what is left, both from registers in 32 bits: rows whose mean is large lose nothing, and x is read once.  The next row is on its
+// way while this one is added up.  Bound by memory: 131 072 x 768 bf16 with dropout, residual, total and statistics 149 us, 5.4 TB/s; a dozen rows 9.2 us.
+template <class T, int LPR, int NC, bool DROP>
+__global__ __launch_bounds__(256) void layernorm_kernel(const T *x, int64_t ldx, const T *res, int64_t ldr, int rows, int cols,
+                                                        const float *gamma, const float *beta, float eps, T *out, int64_t ldo, T *total,
+                                                        int64_t ldt, float *mean_out, float *rstd_out, int streaming, Drop drop)
 {
-    __shared__ float shared[2 * 2 * WPR];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int at = WPR == 1 ? lane : threadIdx.x;  // this thread's first access of a row
-    constexpr int STRIDE = WPR * 64;
-    int64_t row = WPR == 1 ? (int64_t)blockIdx.x * 4 + wave : blockIdx.x;
-    const int64_t step = WPR == 1 ? (int64_t)gridDim.x * 4 : gridDim.x;
-    if (row >= rows) return;
+    __shared__ float shared[2 * 2 * 4];
+    constexpr int STRIDE = LPR;
+    const int at = RowsOf<LPR>::at();
+    int64_t row = RowsOf<LPR>::first();
+    const int64_t step = (int64_t)gridDim.x * RowsOf<LPR>::PER_BLOCK;
+    if (row >= rows) return;  // all lanes of the row
 
     int n[NC];
     f32x8 g[NC], b[NC];
@@ -110,7 +138,7 @@ __global__ __launch_bounds__(WPR == 1 ? 256 : WPR * 64) void layernorm_kernel(co
         }
         const int64_t next = row + step;
         if (next < rows) request(next);
-        const float mean = row_sum<WPR>(s, shared, slot) * inv;
+        const float mean = row_sum<LPR>(s, shared, slot) * inv;
         float q = 0.f;
 #pragma unroll
         for (int i = 0; i < NC; ++i)
@@ -126,7 +154,7 @@ __global__ __launch_bounds__(WPR == 1 ? 256 : WPR * 64) void layernorm_kernel(co
                     q += j < n[i] ? t[i][j] * t[i][j] : 0.f;
                 }
             }
-        const float rstd = rsqrtf(row_sum<WPR>(q, shared, slot + 1) * inv + eps);
+        const float rstd = rsqrtf(row_sum<LPR>(q, shared, slot + 1) * inv + eps);
 #pragma unroll
         for (int i = 0; i < NC; ++i)
             if (n[i] > 0) {
@@ -144,20 +172,20 @@ __global__ __launch_bounds__(WPR == 1 ? 256 : WPR * 64) void layernorm_kernel(co
 }
 
 // dt = rstd (gy - mean(gy) - xhat mean(gy xhat)) + dtotal with gy = dout gamma, xhat = (t - mean) rstd; dx = dropout's gradient of dt.  Every block adds up
-// dout xhat and dout over its rows in registers and writes one row of `partial` [blocks][2][cols].
-template <class T, int WPR, int NC, bool DROP>
-__global__ __launch_bounds__(WPR == 1 ? 256 : WPR * 64) void layernorm_grad_kernel(const T *dout, int64_t ldd, const T *total, int64_t ldt, int rows,
-                                                                                   int cols, const float *gamma, const float *mean_in,
-                                                                                   const float *rstd_in, const T *dtotal, int64_t lde, T *dres,
-                                                                                   int64_t ldr, T *dx, int64_t ldx, float *partial, int streaming, Drop drop)
+// dout xhat and dout over its rows in registers and writes one row of `partial` [blocks][2][cols]: no atomics, the same order in every call.  Two blocks per compute
+// unit: each more adds a row to sum (131 072 x 768 bf16: 162 us, with four 170).  Bound by memory: with dropout, without dtotal 153 to 162 us by card, 5.0 to 5.3 TB/s.
+template <class T, int LPR, int NC, bool DROP>
+__global__ __launch_bounds__(256) void layernorm_grad_kernel(const T *dout, int64_t ldd, const T *total, int64_t ldt, int rows, int cols,
+                                                             const float *gamma, const float *mean_in, const float *rstd_in, const T *dtotal,
+                                                             int64_t lde, T *dres, int64_t ldr, T *dx, int64_t ldx, float *partial,
+                                                             int streaming, Drop drop)
 {
-    __shared__ float shared[2 * 2 * WPR];
-    extern __shared__ float column[];  // WPR 1: [2][NC * 64 * 8]
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int at = WPR == 1 ? lane : threadIdx.x;
-    constexpr int STRIDE = WPR * 64;
-    int64_t row = WPR == 1 ? (int64_t)blockIdx.x * 4 + wave : blockIdx.x;
-    const int64_t step = WPR == 1 ? (int64_t)gridDim.x * 4 : gridDim.x;
+    __shared__ float shared[2 * 2 * 4];
+    extern __shared__ float column[];  // more than one row per block: [2][NC * LPR * 8]
+    constexpr int STRIDE = LPR;
+    const int at = RowsOf<LPR>::at();
+    int64_t row = RowsOf<LPR>::first();
+    const int64_t step = (int64_t)gridDim.x * RowsOf<LPR>::PER_BLOCK;
 
     int n[NC];
     f32x8 g[NC], dg[NC], db[NC];
@@ -206,8 +234,8 @@ __global__ __launch_bounds__(WPR == 1 ? 256 : WPR * 64) void layernorm_grad_kern
                 if (dtotal) e[i] = es[i].wide();
             }
         if (row + step < rows) request(row + step);
-        s = row_sum<WPR>(s, shared, slot) * inv;
-        q = row_sum<WPR>(q, shared, slot + 1) * inv;
+        s = row_sum<LPR>(s, shared, slot) * inv;
+        q = row_sum<LPR>(q, shared, slot + 1) * inv;
 #pragma unroll
         for (int i = 0; i < NC; ++i)
             if (n[i] > 0) {
@@ -223,20 +251,21 @@ __global__ __launch_bounds__(WPR == 1 ? 256 : WPR * 64) void layernorm_grad_kern
             }
     }
     float *mine = partial + (size_t)blockIdx.x * 2 * cols;
-    if constexpr (WPR == 1) {  // the four wavefronts' sums, in order
-        for (int w = 0; w < 4; ++w) {
-            if (wave == w)
+    if constexpr (LPR <= 64) {  // the sums of the block's rows, in order
+        const int mine_of = threadIdx.x / LPR;
+        for (int w = 0; w < 256 / LPR; ++w) {
+            if (mine_of == w)
 #pragma unroll
                 for (int i = 0; i < NC; ++i) {
-                    f32x8 *to = reinterpret_cast<f32x8 *>(column) + (lane + i * 64);
+                    f32x8 *to = reinterpret_cast<f32x8 *>(column) + (at + i * LPR);
                     to[0] = w ? to[0] + dg[i] : dg[i];
-                    to[NC * 64] = w ? to[NC * 64] + db[i] : db[i];
+                    to[NC * LPR] = w ? to[NC * LPR] + db[i] : db[i];
                 }
             __syncthreads();
         }
         for (int c = threadIdx.x; c < cols; c += 256) {
             mine[c] = column[c];
-            mine[cols + c] = column[NC * 512 + c];
+            mine[cols + c] = column[NC * LPR * 8 + c];
         }
     } else {
 #pragma unroll
@@ -251,7 +280,8 @@ __global__ __launch_bounds__(WPR == 1 ? 256 : WPR * 64) void layernorm_grad_kern
     }
 }
 
-// dgamma and dbeta from the blocks' sums: 16 columns per block, four lanes to a row of them, 256 rows at a time.  Always in the same order.
+// dgamma and dbeta from the blocks' sums: 16 columns per block, four lanes to a row of them, 256 rows at a time.  Always in the same order.  512 sums of 768 columns
+// (3 MB, in the caches): 5.1 us, most of it the launch and the sums' way through LDS.
 __global__ __launch_bounds__(1024) void column_sum_kernel(const float *partial, int blocks, int cols, float *dgamma, float *dbeta)
 {
     __shared__ float sums[256][17];
@@ -283,22 +313,21 @@ __global__ __launch_bounds__(1024) void column_sum_kernel(const float *partial, 
 
 constexpr int MAX_COLS = 4 * 64 * 8 * 4;  // of a LayerNorm's row
 
-// A row's wavefronts and accesses per lane: one wavefront up to 2048 columns, four beyond.
+// A row's lanes and accesses per lane: 16 lanes up to 128 columns, 32 up to 256, a wavefront up to 2048, a block beyond.  131 072 rows in bf16 with dropout, this and a
+// wavefront per row: 128 columns 18.5 and 47 us (gradient 30 and 82), 256 columns 35 and 47 (59 and 85); over 4096 rows and fewer both take a launch's time.
 template <class F>
 int with_row_shape(int cols, F f)
 {
     const int chunks = (cols + 7) / 8;
-    if (chunks <= 64) return f(std::integral_constant<int, 1>(), std::integral_constant<int, 1>());
-    if (chunks <= 128) return f(std::integral_constant<int, 1>(), std::integral_constant<int, 2>());
-    if (chunks <= 192) return f(std::integral_constant<int, 1>(), std::integral_constant<int, 3>());
-    if (chunks <= 256) return f(std::integral_constant<int, 1>(), std::integral_constant<int, 4>());
-    if (chunks <= 512) return f(std::integral_constant<int, 4>(), std::integral_constant<int, 2>());
-    return f(std::integral_constant<int, 4>(), std::integral_constant<int, 4>());
+    if (chunks <= 16) return f(std::integral_constant<int, 16>(), std::integral_constant<int, 1>());
+    if (chunks <= 32) return f(std::integral_constant<int, 32>(), std::integral_constant<int, 1>());
+    if (chunks <= 64) return f(std::integral_constant<int, 64>(), std::integral_constant<int, 1>());
+    if (chunks <= 128) return f(std::integral_constant<int, 64>(), std::integral_constant<int, 2>());
+    if (chunks <= 192) return f(std::integral_constant<int, 64>(), std::integral_constant<int, 3>());
+    if (chunks <= 256) return f(std::integral_constant<int, 64>(), std::integral_constant<int, 4>());
+    if (chunks <= 512) return f(std::integral_constant<int, 256>(), std::integral_constant<int, 2>());
+    return f(std::integral_constant<int, 256>(), std::integral_constant<int, 4>());
 }
-
-// Outputs that the caches would not hold until they are read go past them: dropout + LayerNorm, dropout and the gradient in a row over 131 072 x 768 bf16 take 421
-// instead of 436 us, over 65 536 rows 215 and 217; over 16 384 rows it would be 64 instead of 62.
-int streams(int64_t rows, int64_t cols, size_t size) { return (double)rows * cols * size >= 96e6; }
 
 template <class F>
 int with_type(int dtype, F f)
@@ -307,6 +336,10 @@ int with_type(int dtype, F f)
     if (dtype == LEANN_BF16) return f((bf16_t *)nullptr);
     return f((f16_t *)nullptr);
 }
+
+// Outputs that the caches would not hold until they are read go past them: dropout + LayerNorm, dropout and the gradient in a row over 131 072 x 768 bf16 take 421
+// instead of 436 us, over 65 536 rows 215 and 217; over 16 384 rows it would be 64 instead of 62.
+int streams(int64_t rows, int64_t cols, size_t size) { return (double)rows * cols * size >= 96e6; }
 
 int check_matrix(const char *call, int64_t rows, int64_t cols, int dtype)
 {
@@ -418,17 +451,17 @@ int leann_layernorm(leann_ctx *ctx, const void *x_dev, int64_t ldx, const void *
     LEANN_HIP(hipSetDevice(ctx->device));
     return with_type(dtype, [&](auto *type) {
         typedef std::remove_pointer_t<decltype(type)> T;
-        return with_row_shape(cols, [&](auto wpr, auto nc) {
-            constexpr int WPR = decltype(wpr)::value, NC = decltype(nc)::value;
-            const int64_t blocks = WPR == 1 ? (rows + 3) / 4 : rows;
+        return with_row_shape(cols, [&](auto lpr, auto nc) {
+            constexpr int LPR = decltype(lpr)::value, NC = decltype(nc)::value;
+            const int64_t blocks = (rows + 256 / LPR - 1) / (256 / LPR);
             const unsigned grid = (unsigned)std::min<int64_t>(blocks, (int64_t)ctx->num_cus * 8);
             auto go = [&](auto kernel) {
-                hipLaunchKernelGGL(kernel, dim3(grid), dim3(WPR == 1 ? 256 : WPR * 64), 0, ctx->stream, (const T *)x_dev, ldx,
+                hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, ctx->stream, (const T *)x_dev, ldx,
                                    (const T *)residual_dev, ldr, (int)rows, (int)cols, gamma_dev, beta_dev, eps, (T *)out_dev, ldo, (T *)total_dev,
                                    ldt, mean_dev, rstd_dev, streams(rows, cols, sizeof(T)), d);
             };
-            if (d.below) go(layernorm_kernel<T, WPR, NC, true>);
-            else go(layernorm_kernel<T, WPR, NC, false>);
+            if (d.below) go(layernorm_kernel<T, LPR, NC, true>);
+            else go(layernorm_kernel<T, LPR, NC, false>);
             return launched(call);
         });
     });
@@ -465,20 +498,20 @@ int leann_layernorm_backward(leann_ctx *ctx, const void *dout_dev, int64_t ldd, 
     LEANN_HIP(hipSetDevice(ctx->device));
     return with_type(dtype, [&](auto *type) {
         typedef std::remove_pointer_t<decltype(type)> T;
-        return with_row_shape(cols, [&](auto wpr, auto nc) {
-            constexpr int WPR = decltype(wpr)::value, NC = decltype(nc)::value;
-            const int64_t wanted = WPR == 1 ? (rows + 3) / 4 : rows;
+        return with_row_shape(cols, [&](auto lpr, auto nc) {
+            constexpr int LPR = decltype(lpr)::value, NC = decltype(nc)::value;
+            const int64_t wanted = (rows + 256 / LPR - 1) / (256 / LPR);
             const unsigned grid = (unsigned)std::min<int64_t>(wanted, (int64_t)ctx->num_cus * 2);
             LEANN_TRY(ctx->reserve(ctx->op_work, std::max<size_t>(1, (size_t)grid * 2 * cols * sizeof(float))));
             float *partial = (float *)ctx->op_work.p;
             if (grid) {
                 auto go = [&](auto kernel) {
-                    hipLaunchKernelGGL(kernel, dim3(grid), dim3(WPR == 1 ? 256 : WPR * 64), WPR == 1 ? NC * 64 * 8 * 2 * sizeof(float) : 0,
+                    hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), LPR <= 64 ? NC * LPR * 8 * 2 * sizeof(float) : 0,
                                        ctx->stream, (const T *)dout_dev, ldd, (const T *)total_dev, ldt, (int)rows, (int)cols, gamma_dev, mean_dev,
                                        rstd_dev, (const T *)dtotal_dev, lde, (T *)dresidual_dev, ldr, (T *)dx_dev, ldx, partial, streams(rows, cols, sizeof(T)), d);
                 };
-                if (d.below) go(layernorm_grad_kernel<T, WPR, NC, true>);
-                else go(layernorm_grad_kernel<T, WPR, NC, false>);
+                if (d.below) go(layernorm_grad_kernel<T, LPR, NC, true>);
+                else go(layernorm_grad_kernel<T, LPR, NC, false>);
             }
             hipLaunchKernelGGL(column_sum_kernel, dim3((2 * cols + 15) / 16), dim3(1024), 0, ctx->stream, partial, (int)grid, (int)cols, dgamma_dev,
                                dbeta_dev);

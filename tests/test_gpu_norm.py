@@ -9,7 +9,7 @@ pytestmark = pytest.mark.gpu
 EPS32 = 2.0 ** -24
 EPS = 1e-12
 DTYPES = ["float32", "bfloat16", "float16"]
-COLS = [1, 2, 7, 8, 9, 64, 65, 384, 513, 768, 1021, 1025, 1537, 2047, 2049, 4100, 5001, 8192]
+COLS = [1, 2, 7, 8, 9, 64, 65, 128, 129, 200, 256, 257, 384, 513, 768, 1021, 1025, 1537, 2047, 2049, 4100, 5001, 8192]
 
 
 @pytest.fixture(scope="module")
@@ -191,6 +191,31 @@ def test_rows_do_not_touch_each_other(ctx):
     assert bool((got[rest] == want[rest]).all())
     assert bool((got[20] == beta.bfloat16()).all()) and bool((got[36] == beta.bfloat16()).all())  # 0.5 * 768 / 768 is exact
     assert bool(got[3].isnan().all())
+
+
+@pytest.mark.parametrize("cols", [1, 72, 128, 130, 250])
+def test_many_narrow_rows(ctx, cols):
+    """Several rows per wavefront, each wavefront several times: every row as in a call of a part of them; the sums against 64 bits."""
+    import torch
+    import paper_2506_08276_amd as L
+    rng = np.random.default_rng(cols + 5)
+    rows, part = 70003, 2047
+    x, x64 = matrix(rng, rows, cols, "bfloat16", 5)
+    d, d64 = matrix(rng, rows, cols, "bfloat16")
+    (gamma, g64), (beta, _) = vector(rng, cols, 1.0), vector(rng, cols, 0.0)
+    out, _, mean, rstd = L.leann_layernorm(ctx, x, gamma, beta, 1e-3, residual=d, keep=True)
+    total = (x.float() + d.float()).bfloat16()
+    dres, _, dgamma, dbeta = L.leann_layernorm_backward(ctx, d, total, mean, rstd, gamma)
+    for at in range(0, rows, 20 * part):
+        of = slice(at, at + part)
+        want = L.leann_layernorm(ctx, x[of], gamma, beta, 1e-3, residual=d[of], keep=True)
+        assert bool((out[of] == want[0]).all()) and bool((mean[of] == want[2]).all()) and bool((rstd[of] == want[3]).all()), at
+        assert bool((dres[of] == L.leann_layernorm_backward(ctx, d[of], total[of], mean[of], rstd[of], gamma)[0]).all()), at
+    t64, m64, s64 = (v.double().cpu().numpy() for v in (total, mean, rstd))
+    _, dgamma64, dbeta64 = plain64.layernorm_backward(d64, t64, m64, s64, g64)
+    depth = 64 + rows / 64
+    close(dgamma, dgamma64, "float32", depth * EPS32 * (np.abs(d64) * np.abs((np.abs(t64) + np.abs(m64[:, None])) * s64[:, None])).sum(0), "dgamma")
+    close(dbeta, dbeta64, "float32", depth * EPS32 * np.abs(d64).sum(0), "dbeta")
 
 
 def test_same_bits_twice_and_large_offsets(ctx):
