@@ -181,10 +181,11 @@ __global__ __launch_bounds__(256) void low_kernel(const T *x, int64_t ldx, const
 }
 
 // ------------------------------------------------------------------ the projection
-// out[row][n] = sum over k of x[row][k] W[n][k] + bias[n] + the adapter's part, tiles of 32 TM x 32 TN slots and columns.  Four wavefronts share K, operands from
-// memory to registers, U steps of 16 ahead; their sums meet in LDS.  The adapters come first, while the first operands are on their way.  For few rows, where the time
-// of one tile is what counts: 48 x 768 x 768 5.8 us, bound by the reads that wait for each other (row number, x; runs, pieces, `up`); 3391 x 384 x 1536 in tiles of
-// 64 x 64 21 us.  Beyond that the larger tile reads less.
+// out[row][n] = sum over k of x[row][k] W[n][k] + bias[n] + the adapter's part, tiles of 32 TM x 32 TN slots and columns.  Four wavefronts share K, every fourth step of 16
+// each, so that together they read whole lines of x (2000 x 384 x 1536, the whole call: 14.2 us, with a quarter of K in a row each 16.6); operands from memory
+// to registers, U steps ahead; their sums meet in LDS.  The adapters come first, while the first operands are on their way.  For few rows, where the time
+// of one tile is what counts: 48 x 768 x 768 4.4 to 5.8 us by the number of runs, bound by the reads that wait for each other (row number, x; runs, pieces,
+// `up`); 3391 x 384 x 1536 in tiles of 64 x 96 13.4 us, in 64 x 64 (two on some units) 18.8.  Beyond that the larger tile reads less.
 template <class T, int TM, int TN, int U>
 __global__ __launch_bounds__(256, 2) void project_kernel(const T *x, int64_t ldx, const T *w, const float *bias, int N, int K, const int32_t *row_of,
                                                       int rows, const int32_t *run_ptr, const int4 *runs, const bf16_t *pieces, int R16,
@@ -194,11 +195,12 @@ __global__ __launch_bounds__(256, 2) void project_kernel(const T *x, int64_t ldx
     constexpr int BM = 32 * TM, BN = 32 * TN, PITCH = BN + 4;
     __shared__ float sums[4][BM][PITCH];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, l32 = lane & 31;
-    // Blocks go round-robin to the 8 XCDs: those of one take a run of tiles, all columns of a few rows (3391 x 384 x 1536: 18 us, with columns apart 24).
+    // Blocks go round-robin to the 8 XCDs: those of one take a run of tiles, all columns of a few rows (3391 x 384 x 1536 in 64 x 64: 18 us, with
+    // columns apart 24).
     const int tiles_n = (N + BN - 1) / BN, tile = (int)((blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3));
     const int tile_n = tile % tiles_n, tile_m = tile / tiles_n;
     if (tile_m * BM >= rows) return;
-    const int ksteps = project_ksteps(K), used = (K + 15) >> 4, per = (used + 3) >> 2, from = wave * per, to = min(used, from + per);
+    const int ksteps = project_ksteps(K), used = (K + 15) >> 4;
     const T *xp[TM], *wp[TN];
     int4 my_run[TM];
     int count[TM];
@@ -220,30 +222,37 @@ __global__ __launch_bounds__(256, 2) void project_kernel(const T *x, int64_t ldx
 #pragma unroll
         for (int ni = 0; ni < TN; ++ni) acc[mi][ni] = f32x16{};
     F xf[U][TM], wf[U][TN];
-    auto fetch = [&](int i, int s) {  // behind the share's end: zeros of x
-        const bool in = s < to && s * 16 + half * 8 < K;
-        const int ws = max(min(s, to - 1), 0);
+    auto fetch = [&](int i, int s) {  // zeros of x beyond K; behind the last step that one again, for nothing
+        s = min(s, used - 1);
+        const bool in = s * 16 + half * 8 < K;
 #pragma unroll
-        for (int ni = 0; ni < TN; ++ni) wf[i][ni] = *reinterpret_cast<const F *>(wp[ni] + (size_t)ws * 512);
+        for (int ni = 0; ni < TN; ++ni) wf[i][ni] = *reinterpret_cast<const F *>(wp[ni] + (size_t)s * 512);
 #pragma unroll
         for (int mi = 0; mi < TM; ++mi) xf[i][mi] = *(in ? reinterpret_cast<const F *>(xp[mi] + s * 16) : reinterpret_cast<const F *>(&zero_piece));
     };
 #pragma unroll
-    for (int i = 0; i < U; ++i) fetch(i, from + i);
+    for (int i = 0; i < U; ++i) fetch(i, wave + 4 * i);
 #pragma unroll
     for (int mi = 0; mi < TM; ++mi)
         add_adapters<TN, Frag<T>::PIECES>(acc[mi], my_run[mi], count[mi], tile_m * TM + mi, wave, 4,
                                           pieces + (int64_t)min(tile_m * BM + mi * 32 + l32, rows - 1) * R16 * 32, up, R16, last_ct + 1, tile_n * TN);
-    for (int s = from; s < to; s += U) {
+    auto multiply = [&](int i) {
+#pragma unroll
+        for (int mi = 0; mi < TM; ++mi)
+#pragma unroll
+            for (int ni = 0; ni < TN; ++ni) acc[mi][ni] = mfma32(wf[i][ni], xf[i][mi], acc[mi][ni]);
+    };
+    int s = wave;
+    for (; s + 4 * U < used; s += 4 * U) {
 #pragma unroll
         for (int i = 0; i < U; ++i) {
-#pragma unroll
-            for (int mi = 0; mi < TM; ++mi)
-#pragma unroll
-                for (int ni = 0; ni < TN; ++ni) acc[mi][ni] = mfma32(wf[i][ni], xf[i][mi], acc[mi][ni]);
-            fetch(i, s + U + i);
+            multiply(i);
+            fetch(i, s + 4 * (U + i));
         }
     }
+#pragma unroll
+    for (int i = 0; i < U; ++i)  // a step beyond the last is not multiplied: W may hold infinities
+        if (s + 4 * i < used) multiply(i);
 #pragma unroll
     for (int mi = 0; mi < TM; ++mi)
 #pragma unroll
@@ -499,14 +508,15 @@ void enqueue_project(leann_ctx *ctx, const leann_adapter_rows *rows, const T *x,
                            tiles_n);
         return;
     }
-    const int size = tile == PROJECT_32 ? 32 : 64;
-    const int64_t blocks = (rows->T + size - 1) / size * ((N + size - 1) / size);
+    const int height = tile == PROJECT_32 ? 32 : 64, width = tile == PROJECT_96 ? 96 : height;
+    const int64_t blocks = (rows->T + height - 1) / height * ((N + width - 1) / width);
     auto go = [&](auto kernel) {
         hipLaunchKernelGGL(kernel, dim3((unsigned)((blocks + 7) / 8 * 8)), dim3(256), 0, ctx->stream, x, ldx, w, bias, N, K, rows->row_of, (int)rows->T,
                            rows->run_ptr, rows->runs, pieces, R16, up, out, ldo);
     };
     if (tile == PROJECT_32) go(project_kernel<T, 1, 1, 8>);
-    else go(project_kernel<T, 2, 2, 4>);
+    else if (tile == PROJECT_64) go(project_kernel<T, 2, 2, 4>);
+    else go(project_kernel<T, 2, 3, 4>);
 }
 
 size_t pieces_bytes(const leann_adapter_rows *rows) { return up256((size_t)rows->T * rank_groups(rows->max_rank) * 64 + 64); }  // 64: read past the last one's, see request_pieces

@@ -22,5 +22,5 @@ def library():
 
 
 def tile(rows, N, K, cus=256):
-    """32, 64 or 256."""
-    return (32, 64, 256)[library().choose(cus, ctypes.c_long(rows), N, K)]
+    """32, 64, 256 or 96 (64 rows)."""
+    return (32, 64, 256, 96)[library().choose(cus, ctypes.c_long(rows), N, K)]

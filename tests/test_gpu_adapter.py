@@ -280,6 +280,7 @@ LARGE = {
     "one adapter": ([11000], [0], [16]),
     "many runs": ([70, 1, 33, 400, 129, 64] * 18, [(5 * i) % 13 - 1 for i in range(108)], [16, 3, 40, 128, 64, 1, 24, 17, 8, 100, 32, 9]),
     "few adapted": ([9000, 5, 2500, 300], [-1, 0, -1, 1], [8, 33]),
+    "between": ([70, 1, 33, 400, 129, 64] * 2, [(5 * i) % 13 - 1 for i in range(12)], [16, 3, 40, 128, 64, 1, 24, 17, 8, 100, 32, 9]),
 }
 
 
@@ -316,6 +317,30 @@ def test_large_batches(ctx, batch, n_in, n_out, dtype):
     p.up[sick], p.down[sick] = float("inf"), float("nan")
     assert bool((p.forward()[rest] == out[rest]).all())
     p.close()
+
+
+@pytest.mark.parametrize("rows", [5, 1000, 1394, 11000])
+@pytest.mark.parametrize("n_in", [8, 40, 776])
+def test_infinite_weights(ctx, rows, n_in):
+    """An infinity of the shared weight is met once by every row, and nothing else meets it."""
+    import torch
+    import paper_2506_08276_amd as L
+    rng = np.random.default_rng(n_in)
+    x = torch.from_numpy(rng.uniform(0.5, 1.5, size=(rows, n_in))).bfloat16().to("cuda:0")
+    w = torch.from_numpy(rng.normal(size=(768, n_in))).bfloat16().to("cuda:0")
+    down, up = (torch.zeros(s, dtype=torch.bfloat16, device="cuda:0") for s in ((1, 8, n_in), (1, 768, 8)))
+    table = L.leann_adapter_rows_create(ctx, [rows], [-1], [8], [1.0], 8)
+    outs = []
+    for bad in (False, True):
+        if bad:
+            w[7, n_in - 1], w[765, 0] = float("inf"), float("-inf")
+        proj = L.leann_projection_create(ctx, w, None, gradient=False)
+        outs.append(L.leann_adapter_project(ctx, proj, table, x, down, up))
+        L.leann_projection_free(proj)
+    L.leann_adapter_rows_free(table)
+    want = outs[0].clone()
+    want[:, 7], want[:, 765] = float("inf"), float("-inf")
+    assert bool((outs[1] == want).all())
 
 
 def test_rows_far_apart_in_large_batches(ctx):
