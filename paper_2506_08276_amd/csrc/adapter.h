@@ -60,16 +60,29 @@ __device__ inline f32x16 mfma32(const f16x8 &a, const f16x8 &b, const f32x16 &c)
 __device__ inline f32x4 mfma16(const bf16x8 &a, const bf16x8 &b, const f32x4 &c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 __device__ inline f32x4 mfma16(const f16x8 &a, const f16x8 &b, const f32x4 &c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
-// The next 8 bits of eight values: what is left of v is exact.  Two pieces hold 16 bits of a value, three all 24.
+// A number as a sum of bf16 pieces of 8 bits each, cut off, not rounded: all have the number's sign and none is zero unless the number is (where nothing is left, 2^-126 stands
+// for it), so that an infinity on either side of a product is the definition's infinity, where a piece of zero or of the other sign would make NaN of it.  An infinity is
+// its first piece, NaN stays NaN.  Two pieces hold 16 bits of a value (11 of fp16's), three all 24.  (Numbers below 2^-126 may be lost.)
+constexpr float LEAST_PIECE = 0x1p-126f;
+__device__ inline float first_piece(float v) { return __uint_as_float(__float_as_uint(v) & 0xffff0000u); }
+__device__ inline float behind_first(float v)  // max takes the number where the difference of infinities is none
+{
+    return __builtin_copysignf(__builtin_fmaxf(__builtin_fabsf(v - first_piece(v)), __builtin_fminf(__builtin_fabsf(v), LEAST_PIECE)), v);
+}
+
+// The first pieces of eight values; v becomes what is behind them.
 __device__ inline bf16x8 take_piece(f32x8 &v)
 {
-    const bf16x8 p = __builtin_convertvector(v, bf16x8);
-    v -= __builtin_convertvector(p, f32x8);
-    return p;
+    u32x4 p;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_perm(__float_as_uint(v[2 * i + 1]), __float_as_uint(v[2 * i]), 0x07060302);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = behind_first(v[i]);
+    return __builtin_bit_cast(bf16x8, p);
 }
 
 // Low-rank activations go into the matrix instructions as two pieces of 8 bits, 16 ranks of a row as 32 numbers, first pieces first: [slot][ranks / 16][32],
-// times the adapter's scale.  On bf16 MFMAs for both types: they are sums in fp32 and may leave fp16's range.  What is left out is 2^-17 of each term, where the
+// times the adapter's scale.  On bf16 MFMAs for both types: they are sums in fp32 and may leave fp16's range.  What is left out is 2^-16 of each term, where the
 // output's own rounding is 2^-9 or 2^-12.  `up` is laid out anew in each call, as its values change from step to step in training: in operand order
 // [used adapter][columns / 32][ranks / 16][piece][lane][8], zeros beyond rank and columns; fp16 numbers are two pieces exactly.
 __host__ __device__ inline int rank_groups(int R) { return (R + 15) >> 4; }

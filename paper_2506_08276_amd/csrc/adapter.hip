@@ -169,12 +169,14 @@ __global__ __launch_bounds__(256) void low_kernel(const T *x, int64_t ldx, const
             if (low && r < R) *reinterpret_cast<f32x4 *>(low + row[t] * R + r) = v;
             if (g < groups) {
                 v *= scale;
-                const bf16x4 first = __builtin_convertvector(v, bf16x4);
-                const f32x4 taken = __builtin_convertvector(first, f32x4);
+                f32x4 first, second;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) v[i] = __builtin_isfinite(taken[i]) ? v[i] - taken[i] : 0.f;  // an infinity is its first piece
-                *reinterpret_cast<bf16x4 *>(to + g * 32 + q * 4) = first;
-                *reinterpret_cast<bf16x4 *>(to + g * 32 + 16 + q * 4) = __builtin_convertvector(v, bf16x4);
+                for (int i = 0; i < 4; ++i) {
+                    first[i] = first_piece(v[i]);
+                    second[i] = behind_first(v[i]);  // rounded, as nothing comes behind it
+                }
+                *reinterpret_cast<bf16x4 *>(to + g * 32 + q * 4) = __builtin_convertvector(first, bf16x4);
+                *reinterpret_cast<bf16x4 *>(to + g * 32 + 16 + q * 4) = __builtin_convertvector(second, bf16x4);
             }
         }
     }
@@ -298,6 +300,7 @@ __device__ inline f32x4 outer_step(const bf16x8 (&h)[3], const f16x8 &p, f32x4 c
 {
     f32x8 v = __builtin_convertvector(p, f32x8);
     const bf16x8 p1 = take_piece(v), p2 = take_piece(v);
+    c = mfma16(h[2], p2, c);
     c = mfma16(h[2], p1, c);
     c = mfma16(h[1], p2, c);
     c = mfma16(h[1], p1, c);
@@ -370,6 +373,8 @@ __global__ __launch_bounds__(256) void outer_kernel(const T *x, int64_t ldx, con
         for (int g = 0; g < NR; ++g) {
             f32x8 v;
             __builtin_memcpy(&v, __builtin_assume_aligned(&turned[wave][g * 16 + j][q * 8], 16), sizeof(v));
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = __builtin_canonicalizef(v[i]);  // a NaN whose upper half is an infinity's
 #pragma unroll
             for (int i = 0; i < 3; ++i) piece[g][i] = take_piece(v);
         }
