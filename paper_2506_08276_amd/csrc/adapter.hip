@@ -201,7 +201,7 @@ __global__ __launch_bounds__(256, 2) void project_kernel(const T *x, int64_t ldx
     // columns apart 24).
     const int tiles_n = (N + BN - 1) / BN, tile = (int)((blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3));
     const int tile_n = tile % tiles_n, tile_m = tile / tiles_n;
-    if (tile_m * BM >= rows) return;
+    if (!tile_has_rows(tile_m, BM, rows)) return;
     const int ksteps = project_ksteps(K), used = (K + 15) >> 4;
     const T *xp[TM], *wp[TN];
     int4 my_run[TM];
@@ -315,7 +315,7 @@ __device__ inline f32x4 outer_step(const bf16x8 (&h)[3], const f16x8 &p, f32x4 c
 // 82 953 rows, 768 + 768 columns, rank up to 32: 72 us, 3.5 TB/s.
 template <class T, int NR>
 __global__ __launch_bounds__(256) void outer_kernel(const T *x, int64_t ldx, const T *dout, int64_t ldd, const float *grad_low, const float *low, int R,
-                                                    int K, int N, const int32_t *row_of, const int4 *chunks, int last_slots, float *partial)
+                                                    int K, int N, const int32_t *row_of, const int4 *chunks, float *partial)
 {
     constexpr int PITCH = 36;  // rows of a rank's 32, in steps of 16 bytes, and all banks by ranks
     __shared__ __attribute__((aligned(16))) float sums[16 * NR][128];
@@ -340,9 +340,9 @@ __global__ __launch_bounds__(256) void outer_kernel(const T *x, int64_t ldx, con
     u32x4 d[8];
     f32x4 hv[NR][2];
     auto number = [&](int base) {  // the table goes on behind the last slot: what is read there is not used
-        __builtin_memcpy(row, row_of + min(chunk.y + base + q * 8, last_slots), sizeof(row));
+        __builtin_memcpy(row, row_of + chunk_slot(chunk.y, n, base + q * 8), sizeof(row));
 #pragma unroll
-        for (int i = 0; i < 2; ++i) h_row[i] = row_of[min(chunk.y + base + i * 16 + (lane >> 2), last_slots)];
+        for (int i = 0; i < 2; ++i) h_row[i] = row_of[chunk_slot(chunk.y, n, base + i * 16 + (lane >> 2))];
     };
     auto request = [&](int base) {
 #pragma unroll
@@ -537,7 +537,7 @@ void enqueue_outer(leann_ctx *ctx, const leann_adapter_rows *rows, const T *x, i
     const int R = rows->max_rank, strips = (K + 127) / 128 + (N + 127) / 128;
     auto go = [&](auto kernel, int ranks) {
         hipLaunchKernelGGL(kernel, dim3(strips * rows->n_chunks, (R + ranks - 1) / ranks), dim3(256), 0, ctx->stream, x, ldx, dout, ldd, grad_low, low, R,
-                           K, N, rows->row_of, rows->chunks, (int)((rows->T + 255) / 256 * 256), partial);
+                           K, N, rows->row_of, rows->chunks, partial);
     };
     if (R <= 16) go(outer_kernel<T, 1>, 16);
     else go(outer_kernel<T, 2>, 32);
@@ -560,7 +560,7 @@ int make_rows(leann_ctx *ctx, const int32_t *rows_of_request, const int32_t *ada
               const float *scale, int32_t n_adapters, int32_t max_rank, leann_adapter_rows *out)
 {
     int64_t T = 0;
-    std::vector<int64_t> start(n_requests + 1, 0);
+    std::vector<int64_t> start((size_t)n_requests + 1, 0);
     for (int i = 0; i < n_requests; ++i) start[i + 1] = T += rows_of_request[i];
     auto of = [&](int i) { return adapter_of_request[i] >= 0 && rank[adapter_of_request[i]] > 0 ? adapter_of_request[i] : n_adapters; };
     // requests by adapter (those without one, or with one of rank 0, last), in their order

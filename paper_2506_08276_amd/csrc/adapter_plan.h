@@ -1,6 +1,17 @@
-// Which kernel a projection with adapters goes through.  Host code without HIP types.
+// Which kernel a projection with adapters goes through, and sums of row numbers that stay below 2^31.  Code without HIP types.
 #pragma once
 #include <stdint.h>
+
+#ifdef __HIPCC__
+#define PLAN_FN __host__ __device__ inline
+#else
+#define PLAN_FN inline
+#endif
+
+// Whether a tile of `height` rows has any of `rows`: tile * height may pass 2^31 behind the last one.
+PLAN_FN bool tile_has_rows(int tile, int height, int rows) { return tile <= (rows - 1) / height; }
+// Slot `base` of a chunk of n, or the one behind the chunk: what a wavefront asks for ahead may lie some hundred behind it.
+PLAN_FN int chunk_slot(int first, int n, int base) { return first + (base < n ? base : n); }
 
 enum ProjectTile { PROJECT_32 = 0, PROJECT_64, PROJECT_256, PROJECT_96 };
 
