@@ -391,7 +391,8 @@ int leann_layernorm_backward(leann_ctx *ctx, const void *dout_dev, int64_t ldd, 
  * row t belongs to: many requests, each with its own adapter or none, in one call beside the weight that all of them share.
  * The adapters lie in two pools, down[n_adapters][max_rank][n_in] and up[n_adapters][n_out][max_rank], of which adapter a uses the
  * first rank[a] ranks; what the pools hold beyond may be anything.  Activations, W and pools have one type, LEANN_BF16 or LEANN_F16, and
- * 16-byte alignment (rows: a multiple of 8 elements apart). */
+ * 16-byte alignment (rows: a multiple of 8 elements apart).  What would take more than 2^24 - 1 workgroups in a launch is refused before the first one (LEANN_ESHAPE):
+ * many rows with W wide or n_in below 256 (n_out, for dx) go in tiles of 64 x 64, one each; the gradients take one for 32 ranks and 32 columns of n_out of every adapter. */
 
 /* The shared weight W[n_out][n_in] (rows without gaps) and bias fp32[n_out] (NULL for none), copied in the order that the kernels read; with_gradient: a
  * second time, transposed, for leann_adapter_project_backward's dx.  W stays as it is for the handle's life (adapters are

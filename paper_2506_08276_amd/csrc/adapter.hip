@@ -4,6 +4,7 @@
 
 #include <algorithm>
 #include <exception>
+#include <initializer_list>
 #include <new>
 #include <vector>
 
@@ -472,6 +473,23 @@ int check_half_rows(const char *call, const char *what, const void *p, int64_t l
     return LEANN_OK;
 }
 
+// The launch of the low-rank activations: blocks for them, for rows without adapter, too, if those are to be zeros, and for `up` of N columns in the product's order.
+struct LowLaunch {
+    bool split;  // four wavefronts share K
+    int tiles;
+    int64_t low_blocks, blocks;
+};
+LowLaunch plan_low(const leann_ctx *ctx, const leann_adapter_rows *rows, bool with_zeros, int N)
+{
+    LowLaunch l;
+    l.split = rows->n_tiles < ctx->num_cus * 4;
+    l.tiles = l.split ? (with_zeros ? rows->n_tiles : rows->n_adapted_tiles) : with_zeros ? rows->n_wide_tiles : rows->n_adapted_wide_tiles;
+    l.low_blocks = l.split ? l.tiles : (l.tiles + 3) / 4;
+    const int64_t laying = ((int64_t)rows->n_used * ((N + 31) / 32) * rank_groups(rows->max_rank) * 64 + 255) / 256;
+    l.blocks = l.low_blocks ? l.low_blocks + std::min<int64_t>(laying, ctx->num_cus * 4) : 0;
+    return l;
+}
+
 // What a product's adapters need: the low-rank activations in pieces (and as they are, if wanted; with_zeros: zeros for rows without adapter, too), `up` laid
 // out (up: from here, in the same launch; null: it is there already).
 template <class T>
@@ -479,21 +497,32 @@ void enqueue_low(leann_ctx *ctx, const leann_adapter_rows *rows, const T *x, int
                  bf16_t *pieces, const T *up, int N, bf16_t *up_packed)
 {
     const int R = rows->max_rank;
-    const bool split = rows->n_tiles < ctx->num_cus * 4;
-    const int n = split ? (with_zeros ? rows->n_tiles : rows->n_adapted_tiles) : with_zeros ? rows->n_wide_tiles : rows->n_adapted_wide_tiles;
-    if (!n) return;
-    const int low_blocks = split ? n : (n + 3) / 4;
-    const int64_t laying = up ? ((int64_t)rows->n_used * ((N + 31) / 32) * rank_groups(R) * 64 + 255) / 256 : 0;
+    const LowLaunch l = plan_low(ctx, rows, with_zeros, up ? N : 0);
+    if (!l.blocks) return;
     auto go = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3(low_blocks + (unsigned)std::min<int64_t>(laying, ctx->num_cus * 4)), dim3(256), 0, ctx->stream, x, ldx, down, R,
-                           K, rows->row_of, split ? rows->tiles : rows->wide_tiles, n, low_blocks, compact, low, pieces, rows->adapters, up, N, rows->used,
-                           rows->n_used, up_packed);
+        hipLaunchKernelGGL(kernel, dim3((unsigned)l.blocks), dim3(256), 0, ctx->stream, x, ldx, down, R, K, rows->row_of, l.split ? rows->tiles : rows->wide_tiles,
+                           l.tiles, (int)l.low_blocks, compact, low, pieces, rows->adapters, up, N, rows->used, rows->n_used, up_packed);
     };
     static_assert(WIDE_ROWS == 32, "two tiles of 16");
-    if (R <= 16) split ? go(low_kernel<T, 1, 1, true>) : go(low_kernel<T, 1, 2, false>);
-    else if (R <= 32) split ? go(low_kernel<T, 2, 1, true>) : go(low_kernel<T, 2, 2, false>);
-    else if (R <= 64) split ? go(low_kernel<T, 4, 1, true>) : go(low_kernel<T, 4, 2, false>);
-    else split ? go(low_kernel<T, 8, 1, true>) : go(low_kernel<T, 8, 2, false>);
+    if (R <= 16) l.split ? go(low_kernel<T, 1, 1, true>) : go(low_kernel<T, 1, 2, false>);
+    else if (R <= 32) l.split ? go(low_kernel<T, 2, 1, true>) : go(low_kernel<T, 2, 2, false>);
+    else if (R <= 64) l.split ? go(low_kernel<T, 4, 1, true>) : go(low_kernel<T, 4, 2, false>);
+    else l.split ? go(low_kernel<T, 8, 1, true>) : go(low_kernel<T, 8, 2, false>);
+}
+
+struct ProjectLaunch {
+    ProjectTile tile;
+    int64_t blocks;
+};
+ProjectLaunch plan_project(const leann_ctx *ctx, const leann_adapter_rows *rows, int64_t ldx, int N, int K)
+{
+    ProjectLaunch l;
+    l.tile = choose_project(ctx->num_cus, rows->T, N, K);
+    if (l.tile == PROJECT_256 && rows->T * ldx / 8 >= 0xffffff00ll) l.tile = PROJECT_64;  // beyond the large tiles' offsets
+    const int height = l.tile == PROJECT_32 ? 32 : l.tile == PROJECT_256 ? 256 : 64, width = l.tile == PROJECT_96 ? 96 : height;
+    l.blocks = ((rows->T + height - 1) / height * ((N + width - 1) / width) + 7) / 8 * 8;
+    if (l.tile == PROJECT_256) l.blocks = std::min<int64_t>(l.blocks, ctx->num_cus);
+    return l;
 }
 
 // out = x w^T + bias + the adapters' part
@@ -502,26 +531,34 @@ void enqueue_project(leann_ctx *ctx, const leann_adapter_rows *rows, const T *x,
                      const bf16_t *pieces, const bf16_t *up, T *out, int64_t ldo)
 {
     const int R16 = rank_groups(rows->max_rank);
-    ProjectTile tile = choose_project(ctx->num_cus, rows->T, N, K);
-    if (tile == PROJECT_256 && rows->T * ldx / 8 >= 0xffffff00ll) tile = PROJECT_64;  // beyond the large tiles' offsets
-    if (tile == PROJECT_256) {
+    const ProjectLaunch l = plan_project(ctx, rows, ldx, N, K);
+    if (l.tile == PROJECT_256) {
         typedef ProjectCfg<2, 4, 2> Cfg;
+        static_assert(Cfg::BM == 256 && Cfg::BN == 256, "");
         const int tiles_n = (N + Cfg::BN - 1) / Cfg::BN;
-        const int64_t tiles = (rows->T + Cfg::BM - 1) / Cfg::BM * tiles_n;
-        hipLaunchKernelGGL((project_large_kernel<T, 2, 4, 2>), dim3((unsigned)std::min<int64_t>((tiles + 7) / 8 * 8, ctx->num_cus)), dim3(512), Cfg::SMEM,
-                           ctx->stream, x, ldx, w, bias, N, K, rows->row_of, (int)rows->T, rows->seg_ptr, rows->segs, pieces, R16, up, out, ldo, tiles_n,
-                           tiles_n);
+        hipLaunchKernelGGL((project_large_kernel<T, 2, 4, 2>), dim3((unsigned)l.blocks), dim3(512), Cfg::SMEM, ctx->stream, x, ldx, w, bias, N, K, rows->row_of,
+                           (int)rows->T, rows->seg_ptr, rows->segs, pieces, R16, up, out, ldo, tiles_n, tiles_n);
         return;
     }
-    const int height = tile == PROJECT_32 ? 32 : 64, width = tile == PROJECT_96 ? 96 : height;
-    const int64_t blocks = (rows->T + height - 1) / height * ((N + width - 1) / width);
     auto go = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3((unsigned)((blocks + 7) / 8 * 8)), dim3(256), 0, ctx->stream, x, ldx, w, bias, N, K, rows->row_of, (int)rows->T,
-                           rows->run_ptr, rows->runs, pieces, R16, up, out, ldo);
+        hipLaunchKernelGGL(kernel, dim3((unsigned)l.blocks), dim3(256), 0, ctx->stream, x, ldx, w, bias, N, K, rows->row_of, (int)rows->T, rows->run_ptr,
+                           rows->runs, pieces, R16, up, out, ldo);
     };
-    if (tile == PROJECT_32) go(project_kernel<T, 1, 1, 8>);
-    else if (tile == PROJECT_64) go(project_kernel<T, 2, 2, 4>);
+    if (l.tile == PROJECT_32) go(project_kernel<T, 1, 1, 8>);
+    else if (l.tile == PROJECT_64) go(project_kernel<T, 2, 2, 4>);
     else go(project_kernel<T, 2, 3, 4>);
+}
+
+// Before the first launch of a call: all of its launches.
+int check_launches(const char *call, std::initializer_list<int64_t> blocks)
+{
+    for (int64_t b : blocks)
+        if (b > MAX_BLOCKS) {
+            leann_set_error("%s: rows, columns and adapters of this number are not covered (%lld workgroups in a launch, at most %lld)", call, (long long)b,
+                            (long long)MAX_BLOCKS);
+            return LEANN_ESHAPE;
+        }
+    return LEANN_OK;
 }
 
 size_t pieces_bytes(const leann_adapter_rows *rows) { return up256((size_t)rows->T * rank_groups(rows->max_rank) * 64 + 64); }  // 64: read past the last one's, see request_pieces
@@ -805,6 +842,7 @@ int leann_adapter_project(leann_ctx *ctx, const leann_projection *proj, const le
     }
     LEANN_HIP(hipSetDevice(ctx->device));
     const int N = proj->n_out, K = proj->n_in;
+    LEANN_TRY(check_launches(call, {plan_low(ctx, rows, low_dev != nullptr, N).blocks, plan_project(ctx, rows, ldx, N, K).blocks}));
     LEANN_TRY(ctx->reserve(ctx->op_work, pieces_bytes(rows) + packed_bytes(rows, N)));
     bf16_t *pieces = (bf16_t *)ctx->op_work.p, *packed = (bf16_t *)((char *)ctx->op_work.p + pieces_bytes(rows));
     return with_half_type(proj->dtype, [&](auto *type) {
@@ -839,6 +877,12 @@ int leann_adapter_project_backward(leann_ctx *ctx, const leann_projection *proj,
             return LEANN_EINVAL;
         }
     }
+    const int64_t transposing = (int64_t)rows->n_used * ((N + 31) / 32) * ((R + 31) / 32);
+    const int64_t laying = dx_dev ? ((int64_t)rows->n_used * ((K + 31) / 32) * rank_groups(R) * 64 + 255) / 256 : 0;
+    const int64_t lay_out_blocks = transposing + std::min<int64_t>(laying, ctx->num_cus * 4);
+    const int64_t outer_blocks = ddown_dev ? (int64_t)rows->n_chunks * ((K + 127) / 128 + (N + 127) / 128) : 0;
+    LEANN_TRY(check_launches(call, {lay_out_blocks, plan_low(ctx, rows, false, 0).blocks, dx_dev && rows->T ? plan_project(ctx, rows, ldd, K, N).blocks : 0,
+                                    outer_blocks}));
     LEANN_HIP(hipSetDevice(ctx->device));
     const size_t low_bytes = up256((size_t)rows->T * R * sizeof(float)), up_bytes = up256((size_t)rows->n_used * R * N * 2),
                  partial_bytes = ddown_dev ? (size_t)rows->n_chunks * R * (K + N) * sizeof(float) : 0;
@@ -858,11 +902,8 @@ int leann_adapter_project_backward(leann_ctx *ctx, const leann_projection *proj,
         typedef std::remove_pointer_t<decltype(type)> T;
         T *up_t = (T *)up_at;
         if (rows->n_used) {
-            const int64_t transposing = (int64_t)rows->n_used * ((N + 31) / 32) * ((R + 31) / 32);
-            const int64_t laying = dx_dev ? ((int64_t)rows->n_used * ((K + 31) / 32) * rank_groups(R) * 64 + 255) / 256 : 0;
-            hipLaunchKernelGGL(lay_out_kernel<T>, dim3((unsigned)(transposing + std::min<int64_t>(laying, ctx->num_cus * 4))), dim3(256), 0, ctx->stream,
-                               (const T *)down_dev, (const T *)up_dev, rows->used, rows->adapters, rows->n_used, R, K, N, up_t, packed,
-                               (int)transposing);
+            hipLaunchKernelGGL(lay_out_kernel<T>, dim3((unsigned)lay_out_blocks), dim3(256), 0, ctx->stream, (const T *)down_dev, (const T *)up_dev, rows->used,
+                               rows->adapters, rows->n_used, R, K, N, up_t, packed, (int)transposing);
             enqueue_low<T>(ctx, rows, (const T *)dout_dev, ldd, N, up_t, 1, ddown_dev ? grad_low : nullptr, false, pieces, (const T *)nullptr, 0,
                            (bf16_t *)nullptr);
         }

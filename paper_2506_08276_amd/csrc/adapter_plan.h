@@ -8,6 +8,8 @@
 #define PLAN_FN inline
 #endif
 
+constexpr int64_t MAX_BLOCKS = (1 << 24) - 1;  // of 256 threads in a launch, which takes fewer than 2^32 threads
+
 // Whether a tile of `height` rows has any of `rows`: tile * height may pass 2^31 behind the last one.
 PLAN_FN bool tile_has_rows(int tile, int height, int rows) { return tile <= (rows - 1) / height; }
 // Slot `base` of a chunk of n, or the one behind the chunk: what a wavefront asks for ahead may lie some hundred behind it.
