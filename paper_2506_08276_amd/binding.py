@@ -376,7 +376,7 @@ def _rows(t, what, like=None):
         return None, 0
     assert t.is_cuda and t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] <= 1), f"{what}: need a 2-D CUDA tensor with unit column stride"
     assert like is None or (t.shape == like.shape and t.dtype == like.dtype), f"{what}: shape or type differs"
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1]  # a single row's stride is none
 
 
 def _drop(drop):
