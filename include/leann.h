@@ -411,14 +411,14 @@ int leann_adapter_rows_create(leann_ctx *ctx, const int32_t *rows_of_request_hos
 void leann_adapter_rows_free(leann_adapter_rows *rows);
 
 /* The forward pass over x[T][n_in], T the rows of the handle.  low_dev (NULL, or fp32[T][max_rank]) receives down_a x_t, which the backward pass
- * needs; zeros beyond the adapter's rank and for rows without one.  out must not overlap x.  A row's values do not depend on other rows; its bits
+ * needs; zeros beyond the adapter's rank and for rows without one.  out must not overlap x (LEANN_EINVAL; their rows may lie between each other's).  A row's values do not depend on other rows; its bits
  * may depend on their number, as products of different sizes add up in different orders. */
 int leann_adapter_project(leann_ctx *ctx, const leann_projection *proj, const leann_adapter_rows *rows, const void *x_dev, int64_t ldx,
                           const void *down_dev, const void *up_dev, void *out_dev, int64_t ldo, float *low_dev);
 
 /* Gradients from dout[T][n_out]: dx[T][n_in] = W^T dout + scale_a down_a^T (up_a^T dout) (NULL: not wanted; else the projection needs with_gradient), and
  * ddown[n_adapters][max_rank][n_in], dup[n_adapters][n_out][max_rank] in fp32 (both or neither; written, not added to; zeros for adapters without
- * rows and beyond their rank), which need x and the forward pass's low.  dx must not overlap dout or x. */
+ * rows and beyond their rank), which need x and the forward pass's low.  dx must not overlap dout or x (LEANN_EINVAL). */
 int leann_adapter_project_backward(leann_ctx *ctx, const leann_projection *proj, const leann_adapter_rows *rows, const void *dout_dev, int64_t ldd,
                                    const void *x_dev, int64_t ldx, const float *low_dev, const void *down_dev, const void *up_dev, void *dx_dev,
                                    int64_t lddx, float *ddown_dev, float *dup_dev);

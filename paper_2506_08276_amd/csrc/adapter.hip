@@ -580,6 +580,14 @@ void enqueue_outer(leann_ctx *ctx, const leann_adapter_rows *rows, const T *x, i
     else go(outer_kernel<T, 2>, 32);
 }
 
+int check_apart(const char *call, const char *a, const void *a_dev, int64_t lda, int64_t a_cols, const char *b, const void *b_dev, int64_t ldb, int64_t b_cols,
+                int64_t rows)
+{
+    if (!rows_overlap((uint64_t)a_dev, lda, a_cols, (uint64_t)b_dev, ldb, b_cols, rows, 2)) return LEANN_OK;
+    leann_set_error("%s: %s overlaps %s", call, a, b);
+    return LEANN_EINVAL;
+}
+
 int check_pair(const char *call, const leann_ctx *ctx, const leann_projection *proj, const leann_adapter_rows *rows)
 {
     if (!ctx || !proj || !rows) {
@@ -843,6 +851,7 @@ int leann_adapter_project(leann_ctx *ctx, const leann_projection *proj, const le
     LEANN_HIP(hipSetDevice(ctx->device));
     const int N = proj->n_out, K = proj->n_in;
     LEANN_TRY(check_launches(call, {plan_low(ctx, rows, low_dev != nullptr, N).blocks, plan_project(ctx, rows, ldx, N, K).blocks}));
+    LEANN_TRY(check_apart(call, "out", out_dev, ldo, N, "x", x_dev, ldx, K, rows->T));
     LEANN_TRY(ctx->reserve(ctx->op_work, pieces_bytes(rows) + packed_bytes(rows, N)));
     bf16_t *pieces = (bf16_t *)ctx->op_work.p, *packed = (bf16_t *)((char *)ctx->op_work.p + pieces_bytes(rows));
     return with_half_type(proj->dtype, [&](auto *type) {
@@ -883,6 +892,8 @@ int leann_adapter_project_backward(leann_ctx *ctx, const leann_projection *proj,
     const int64_t outer_blocks = ddown_dev ? (int64_t)rows->n_chunks * ((K + 127) / 128 + (N + 127) / 128) : 0;
     LEANN_TRY(check_launches(call, {lay_out_blocks, plan_low(ctx, rows, false, 0).blocks, dx_dev && rows->T ? plan_project(ctx, rows, ldd, K, N).blocks : 0,
                                     outer_blocks}));
+    if (dx_dev) LEANN_TRY(check_apart(call, "dx", dx_dev, lddx, K, "dout", dout_dev, ldd, N, rows->T));
+    if (dx_dev && ddown_dev) LEANN_TRY(check_apart(call, "dx", dx_dev, lddx, K, "x", x_dev, ldx, K, rows->T));
     LEANN_HIP(hipSetDevice(ctx->device));
     const size_t low_bytes = up256((size_t)rows->T * R * sizeof(float)), up_bytes = up256((size_t)rows->n_used * R * N * 2),
                  partial_bytes = ddown_dev ? (size_t)rows->n_chunks * R * (K + N) * sizeof(float) : 0;

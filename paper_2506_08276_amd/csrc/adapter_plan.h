@@ -1,4 +1,4 @@
-// Which kernel a projection with adapters goes through, and sums of row numbers that stay below 2^31.  Code without HIP types.
+// Which kernel a projection with adapters goes through, sums of row numbers that stay below 2^31, which matrices share bytes.  Code without HIP types.
 #pragma once
 #include <stdint.h>
 
@@ -40,4 +40,23 @@ inline ProjectTile choose_project(int cus, int64_t rows, int N, int K)
     if (tiles(64) > cus && tiles_of(64, 96) <= cus) return PROJECT_96;
     const double us64 = 4.0 + rounds(64) * (1.2 + 0.0044 * K), us256 = rounds(256) * (13.5 + 0.0155 * K);
     return K >= 256 && us256 < us64 ? PROJECT_256 : PROJECT_64;
+}
+
+// Whether any of `rows` rows of a_cols elements at `a`, lda elements apart, shares a byte with any of b's; lda >= a_cols, ldb >= b_cols.  Rows of one may lie between those of
+// the other.
+inline bool rows_overlap(uint64_t a, int64_t lda, int64_t a_cols, uint64_t b, int64_t ldb, int64_t b_cols, int64_t rows, int size)
+{
+    typedef __int128 Wide;
+    const Wide a_step = (Wide)lda * size, b_step = (Wide)ldb * size, a_bytes = (Wide)a_cols * size, b_bytes = (Wide)b_cols * size, d = (Wide)b - a;
+    if (rows < 1 || d >= (rows - 1) * a_step + a_bytes || -d >= (rows - 1) * b_step + b_bytes) return false;
+    auto meets = [&](int64_t j) {  // b's row j against the last of a's rows that begin before its end: those before that one end earlier
+        const Wide start = d + j * b_step, last = start + b_bytes - 1;
+        if (last < 0) return false;
+        const Wide i = last / a_step < rows - 1 ? last / a_step : rows - 1;
+        return i * a_step + a_bytes > start;
+    };
+    if (lda == ldb || rows == 1) return meets(0) || meets(rows - 1);  // all rows lie alike; the first or the last one has a's rows on both sides
+    for (int64_t j = 0; j < rows; ++j)
+        if (meets(j)) return true;
+    return false;
 }
