@@ -1,5 +1,6 @@
 // What the kernels of projections with low-rank adapters share: handles, tables, MFMA operands (gfx950).
 #pragma once
+#include "adapter_plan.h"
 #include "rows.h"
 
 // The shared projection, as the kernels read it: W and, for gradients, its transpose in the MFMA's operand order.
@@ -20,6 +21,7 @@ struct leann_adapter_rows {
     int32_t n_tiles = 0, n_adapted_tiles = 0;  // of 16 slots of one adapter; tiles of rows without one come last
     int32_t n_wide_tiles = 0, n_adapted_wide_tiles = 0;  // likewise, of 32
     int32_t n_chunks = 0;                      // of up to chunk_rows slots of one adapter
+    AdapterLoad load[2];                       // by the pieces of an element of `up`, less one
     DevBuf mem;
     const int32_t *row_of = nullptr;     // [T, up to a multiple of 256: the last row again, 8 more]
     const int32_t *run_ptr = nullptr;    // [32-slot groups + 1]

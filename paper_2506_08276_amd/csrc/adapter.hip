@@ -6,10 +6,10 @@
 #include <exception>
 #include <initializer_list>
 #include <new>
+#include <type_traits>
 #include <vector>
 
 #include "adapter_gemm.h"
-#include "adapter_plan.h"
 
 namespace {
 
@@ -514,10 +514,10 @@ struct ProjectLaunch {
     ProjectTile tile;
     int64_t blocks;
 };
-ProjectLaunch plan_project(const leann_ctx *ctx, const leann_adapter_rows *rows, int64_t ldx, int N, int K)
+ProjectLaunch plan_project(const leann_ctx *ctx, const leann_adapter_rows *rows, int dtype, int64_t ldx, int N, int K)
 {
     ProjectLaunch l;
-    l.tile = choose_project(ctx->num_cus, rows->T, N, K);
+    l.tile = choose_project(ctx->num_cus, rows->T, N, K, rows->load[(dtype == LEANN_F16 ? Frag<f16_t>::PIECES : Frag<bf16_t>::PIECES) - 1]);
     if (l.tile == PROJECT_256 && rows->T * ldx / 8 >= 0xffffff00ll) l.tile = PROJECT_64;  // beyond the large tiles' offsets
     const int height = l.tile == PROJECT_32 ? 32 : l.tile == PROJECT_256 ? 256 : 64, width = l.tile == PROJECT_96 ? 96 : height;
     l.blocks = ((rows->T + height - 1) / height * ((N + width - 1) / width) + 7) / 8 * 8;
@@ -531,7 +531,7 @@ void enqueue_project(leann_ctx *ctx, const leann_adapter_rows *rows, const T *x,
                      const bf16_t *pieces, const bf16_t *up, T *out, int64_t ldo)
 {
     const int R16 = rank_groups(rows->max_rank);
-    const ProjectLaunch l = plan_project(ctx, rows, ldx, N, K);
+    const ProjectLaunch l = plan_project(ctx, rows, std::is_same_v<T, f16_t> ? LEANN_F16 : LEANN_BF16, ldx, N, K);
     if (l.tile == PROJECT_256) {
         typedef ProjectCfg<2, 4, 2> Cfg;
         static_assert(Cfg::BM == 256 && Cfg::BN == 256, "");
@@ -667,7 +667,18 @@ int make_rows(leann_ctx *ctx, const int32_t *rows_of_request, const int32_t *ada
         }
         if (to > from) used.push_back(a);
     }
-    for (size_t g = 1; g < seg_ptr.size(); ++g) seg_ptr[g] += seg_ptr[g - 1];
+    for (size_t g = 1; g < seg_ptr.size(); ++g) {
+        seg_ptr[g] += seg_ptr[g - 1];
+        for (int pieces = 1; pieces <= 2; ++pieces) {
+            int n = 0;
+            for (int i = seg_ptr[g - 1]; i < seg_ptr[g]; ++i) n += segment_pairs(segs[i].z, pieces);
+            AdapterLoad &l = out->load[pieces - 1];
+            l.most_pairs = std::max(l.most_pairs, n);
+            l.pairs += n;
+        }
+    }
+    for (AdapterLoad &l : out->load)
+        for (const int4 &run : runs) l.sixteens += rank_groups(run.z >> 8 & 255);
     for (size_t g = 1; g < run_ptr.size(); ++g) run_ptr[g] += run_ptr[g - 1];
 
     out->device = ctx->device;
@@ -850,7 +861,7 @@ int leann_adapter_project(leann_ctx *ctx, const leann_projection *proj, const le
     }
     LEANN_HIP(hipSetDevice(ctx->device));
     const int N = proj->n_out, K = proj->n_in;
-    LEANN_TRY(check_launches(call, {plan_low(ctx, rows, low_dev != nullptr, N).blocks, plan_project(ctx, rows, ldx, N, K).blocks}));
+    LEANN_TRY(check_launches(call, {plan_low(ctx, rows, low_dev != nullptr, N).blocks, plan_project(ctx, rows, proj->dtype, ldx, N, K).blocks}));
     LEANN_TRY(check_apart(call, "out", out_dev, ldo, N, "x", x_dev, ldx, K, rows->T));
     LEANN_TRY(ctx->reserve(ctx->op_work, pieces_bytes(rows) + packed_bytes(rows, N)));
     bf16_t *pieces = (bf16_t *)ctx->op_work.p, *packed = (bf16_t *)((char *)ctx->op_work.p + pieces_bytes(rows));
@@ -890,7 +901,7 @@ int leann_adapter_project_backward(leann_ctx *ctx, const leann_projection *proj,
     const int64_t laying = dx_dev ? ((int64_t)rows->n_used * ((K + 31) / 32) * rank_groups(R) * 64 + 255) / 256 : 0;
     const int64_t lay_out_blocks = transposing + std::min<int64_t>(laying, ctx->num_cus * 4);
     const int64_t outer_blocks = ddown_dev ? (int64_t)rows->n_chunks * ((K + 127) / 128 + (N + 127) / 128) : 0;
-    LEANN_TRY(check_launches(call, {lay_out_blocks, plan_low(ctx, rows, false, 0).blocks, dx_dev && rows->T ? plan_project(ctx, rows, ldd, K, N).blocks : 0,
+    LEANN_TRY(check_launches(call, {lay_out_blocks, plan_low(ctx, rows, false, 0).blocks, dx_dev && rows->T ? plan_project(ctx, rows, proj->dtype, ldd, K, N).blocks : 0,
                                     outer_blocks}));
     if (dx_dev) LEANN_TRY(check_apart(call, "dx", dx_dev, lddx, K, "dout", dout_dev, ldd, N, rows->T));
     if (dx_dev && ddown_dev) LEANN_TRY(check_apart(call, "dx", dx_dev, lddx, K, "x", x_dev, ldx, K, rows->T));

@@ -31,14 +31,33 @@ enum ProjectTile { PROJECT_32 = 0, PROJECT_64, PROJECT_256, PROJECT_96 };
 //   800 x 2304 x  768   22.5    13.2       -      26 | 32000 x  384 x 1536     101       -      48
 //  1300 x  384 x 1536   10.7    10.6       -      36 |  2000 x 2304 x  768      25       -      27
 //  2000 x  768 x  768   18.5    11.0     9.0      25 |  3391 x  384 x 1536      19    13.4      38
-inline ProjectTile choose_project(int cus, int64_t rows, int N, int K)
+// Those are with one or two adapters per tile.  In project_large_kernel every adapter of a tile is a pair of slabs for each 32 of its ranks (16, in fp16), 1.7 us however few
+// rows it has; in project_kernel up to 32 of a group's are on their way together, 0.08 us of a tile's for 16 ranks of one.  Single tokens, the whole call, K of 768, the
+// chosen one marked; worst of 270 cases with K of 384 to 2304: 7 % behind the better of the two, without these terms 4 times.
+//   rows x N, adapters x rank, type   pairs of a tile      64      256 |  rows x N, adapters x rank, type   pairs of a tile      64      256
+//   4000 x  768   1024 x 16  bf16          70            *36.4   155.7 |   8000 x 2304     64 x 64  fp16          16            130.4  *138.8
+//   8000 x  768   1024 x 16  bf16          39            *48.0   103.0 |   8000 x 2304     64 x 64  bf16           8            123.1   *98.6
+//   8000 x  768   4000 x 16  bf16         122            *99.1   284.4 |  32000 x 2304   1024 x 64  bf16          22            721.6  *530.1
+//   8000 x 2304   4000 x 16  bf16         122           *301.6   638.7 |  64000 x 2304   4000 x 16  bf16          20            922.5  *691.2
+inline int segment_pairs(int rank, int pieces) { return ((rank + 15) / 16 * pieces + 1) / 2; }  // pieces: bf16 numbers that hold one of `up`'s
+
+// What the adapters of a batch are to the tiles: pairs of slabs in tiles of 256 rows, and sixteens of ranks of every adapter in every group of 32 rows.
+struct AdapterLoad {
+    int most_pairs = 0;  // of one tile
+    int64_t pairs = 0, sixteens = 0;
+};
+
+inline ProjectTile choose_project(int cus, int64_t rows, int N, int K, AdapterLoad load = AdapterLoad())
 {
     auto tiles_of = [&](int height, int width) { return ((rows + height - 1) / height) * ((N + width - 1) / width); };
     auto tiles = [&](int size) { return tiles_of(size, size); };
     auto rounds = [&](int size) { return (double)((tiles(size) + cus - 1) / cus); };
     if (tiles(32) <= cus) return PROJECT_32;
     if (tiles(64) > cus && tiles_of(64, 96) <= cus) return PROJECT_96;
-    const double us64 = 4.0 + rounds(64) * (1.2 + 0.0044 * K), us256 = rounds(256) * (13.5 + 0.0155 * K);
+    auto beyond_two = [](double v) { return v > 2 ? v - 2 : 0; };
+    const double us64 = 4.0 + rounds(64) * (1.2 + 0.0044 * K + 0.08 * beyond_two((double)load.sixteens / ((rows + 63) / 64)));
+    const double mean = rounds(256) * beyond_two((double)load.pairs / ((rows + 255) / 256)), most = beyond_two(load.most_pairs);
+    const double us256 = rounds(256) * (13.5 + 0.0155 * K) + 1.7 * (mean > most ? mean : most);
     return K >= 256 && us256 < us64 ? PROJECT_256 : PROJECT_64;
 }
 
