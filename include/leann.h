@@ -348,6 +348,9 @@ int leann_bench_l1pull(leann_ctx *ctx, int64_t panel_rows, int32_t launches, dou
  *     says so).  Element offsets are 64-bit.
  *   - Everything is enqueued on the context's stream and nothing synchronises, except that a workspace which has to grow is
  *     allocated in the call; a buffer that another stream writes or reads has to be ordered with it by the caller.
+ *   - The workspace stays with the context, as large as the largest call needed.  For every 16 of max_rank a projection takes 64 bytes per row and 64 n_out per adapter that has
+ *     rows; its gradient 128 per row and, per adapter, 64 n_in + 32 n_out and 64 (n_in + n_out) for each of its chunks of up to 2048 rows.  It is freed when another
+ *     allocation of the context finds no memory, and by leann_destroy.
  *   - Sums and statistics are fp32; every output is rounded once, to nearest.  No atomics: the bits repeat from call to call.
  *   - Zero rows are no error.  leann_profile_begin does not bracket their kernels.
  */

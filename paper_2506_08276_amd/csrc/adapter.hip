@@ -863,6 +863,7 @@ int leann_adapter_project(leann_ctx *ctx, const leann_projection *proj, const le
     const int N = proj->n_out, K = proj->n_in;
     LEANN_TRY(check_launches(call, {plan_low(ctx, rows, low_dev != nullptr, N).blocks, plan_project(ctx, rows, proj->dtype, ldx, N, K).blocks}));
     LEANN_TRY(check_apart(call, "out", out_dev, ldo, N, "x", x_dev, ldx, K, rows->T));
+    std::lock_guard<std::mutex> turn(ctx->op_work_mutex);
     LEANN_TRY(ctx->reserve(ctx->op_work, pieces_bytes(rows) + packed_bytes(rows, N)));
     bf16_t *pieces = (bf16_t *)ctx->op_work.p, *packed = (bf16_t *)((char *)ctx->op_work.p + pieces_bytes(rows));
     return with_half_type(proj->dtype, [&](auto *type) {
@@ -908,6 +909,7 @@ int leann_adapter_project_backward(leann_ctx *ctx, const leann_projection *proj,
     LEANN_HIP(hipSetDevice(ctx->device));
     const size_t low_bytes = up256((size_t)rows->T * R * sizeof(float)), up_bytes = up256((size_t)rows->n_used * R * N * 2),
                  partial_bytes = ddown_dev ? (size_t)rows->n_chunks * R * (K + N) * sizeof(float) : 0;
+    std::lock_guard<std::mutex> turn(ctx->op_work_mutex);
     LEANN_TRY(ctx->reserve(ctx->op_work,
                            std::max<size_t>(1, pieces_bytes(rows) + packed_bytes(rows, K) + low_bytes + up_bytes + partial_bytes)));
     char *work = (char *)ctx->op_work.p;

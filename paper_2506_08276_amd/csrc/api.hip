@@ -42,12 +42,25 @@ void DevBuf::release()
 
 int leann_ctx::reserve(DevBuf &buf, size_t need)
 {
-    const int rc = buf.reserve(need);
+    int rc = buf.reserve(need);
     if (rc == LEANN_OK) return rc;
-    std::unique_lock<std::mutex> turn(pq_work_mutex, std::try_to_lock);
-    if (!turn.owns_lock() || !pq_work.p) return rc;  // a training on another thread needs it now
-    pq_work.release();
+    {
+        std::unique_lock<std::mutex> turn(pq_work_mutex, std::try_to_lock);
+        if (turn.owns_lock() && pq_work.p) {  // else a training on another thread needs it now
+            pq_work.release();
+            rc = buf.reserve(need);
+        }
+    }
+    if (rc == LEANN_OK || &buf == &op_work || !give_back_op_work()) return rc;
     return buf.reserve(need);
+}
+
+bool leann_ctx::give_back_op_work()
+{
+    std::unique_lock<std::mutex> turn(op_work_mutex, std::try_to_lock);
+    if (!turn.owns_lock() || !op_work.p) return false;  // an operator on another thread needs it now
+    op_work.release();
+    return true;
 }
 
 int leann_ctx::reserve_for_pass(DevBuf &buf, size_t need)

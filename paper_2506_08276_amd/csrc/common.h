@@ -81,7 +81,10 @@ struct leann_ctx {
     int *host_flags = nullptr;           // pinned host memory: what kernels report, see clear_host_flags
     hipEvent_t pass_event = nullptr;     // recorded behind the kernel that counts an encoder pass's tokens
     double clock_khz = 1e5;              // of the kernels' wall_clock64()
-    DevBuf op_work;  // partial sums and intermediate matrices of the operators for adapting an encoder
+    // Partial sums and intermediate matrices of the operators for adapting an encoder: as much as the largest call took, given back when another
+    // allocation of the context finds no memory.  A call holds the mutex from where it reserves to its last launch; what is launched is waited for by hipFree.
+    DevBuf op_work;
+    std::mutex op_work_mutex;
     int64_t memo_rows = 0;  // rows of the per-call embedding memo (leann_set_call_memo), 0 = off
     // optional per-kernel timing (leann_profile_begin / leann_profile_end)
     bool prof_on = false;
@@ -93,7 +96,8 @@ struct leann_ctx {
     std::vector<ProfSpan> prof_spans;
     std::vector<hipEvent_t> prof_pool;
 
-    int reserve(DevBuf &buf, size_t need);  // all device memory of a call: as buf.reserve, with pq_work given back if that fails
+    int reserve(DevBuf &buf, size_t need);  // all device memory of a call: as buf.reserve, with pq_work given back if that fails, then op_work
+    bool give_back_op_work();  // whether there is memory to be had by it
     int reserve_for_pass(DevBuf &buf, size_t need);  // for calls that run the encoder: then the packed matrices, too
 };
 

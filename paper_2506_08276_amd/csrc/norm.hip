@@ -496,6 +496,7 @@ int leann_layernorm_backward(leann_ctx *ctx, const void *dout_dev, int64_t ldd, 
         }
     }
     LEANN_HIP(hipSetDevice(ctx->device));
+    std::lock_guard<std::mutex> turn(ctx->op_work_mutex);
     return with_type(dtype, [&](auto *type) {
         typedef std::remove_pointer_t<decltype(type)> T;
         return with_row_shape(cols, [&](auto lpr, auto nc) {

@@ -880,7 +880,7 @@ int leann_build_pq(leann_ctx *ctx, const float *emb_dev, int64_t n, int32_t d, i
             if (work.bytes > PQ_WORK_KEEP) work.release();
         }
     } mem{ctx->pq_work, {}};
-    if (ctx->pq_work.reserve(off) != LEANN_OK) return fail(LEANN_ENOMEM);
+    if (ctx->pq_work.reserve(off) != LEANN_OK && !(ctx->give_back_op_work() && ctx->pq_work.reserve(off) == LEANN_OK)) return fail(LEANN_ENOMEM);
     // The steps take 16 bytes per row, beside rows of at least 4: on the host where that is more than a context ever keeps, or where the
     // device has no room; also where its loop is over before three more launches would be (whole calls of 384 dimensions,
     // 32 subspaces and 2 iterations, host and device: 1000 rows 168 and 176 us, 4000 rows 197 and 196, 6000 rows 223 and 215, 40 000 rows 560 and 463).
