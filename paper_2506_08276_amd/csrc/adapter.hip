@@ -482,7 +482,7 @@ struct LowLaunch {
 LowLaunch plan_low(const leann_ctx *ctx, const leann_adapter_rows *rows, bool with_zeros, int N)
 {
     LowLaunch l;
-    l.split = rows->n_tiles < ctx->num_cus * 4;
+    l.split = low_shares_k(ctx->num_cus, rows->n_tiles);
     l.tiles = l.split ? (with_zeros ? rows->n_tiles : rows->n_adapted_tiles) : with_zeros ? rows->n_wide_tiles : rows->n_adapted_wide_tiles;
     l.low_blocks = l.split ? l.tiles : (l.tiles + 3) / 4;
     const int64_t laying = ((int64_t)rows->n_used * ((N + 31) / 32) * rank_groups(rows->max_rank) * 64 + 255) / 256;

@@ -10,6 +10,9 @@
 
 constexpr int64_t MAX_BLOCKS = (1 << 24) - 1;  // of 256 threads in a launch, which takes fewer than 2^32 threads
 
+// Whether low_kernel's blocks share K, one per tile of 16 rows: up to four of them per CU; beyond, wavefronts of their own for 32 rows each read less.
+inline bool low_shares_k(int cus, int tiles) { return tiles < 4 * cus; }
+
 // Whether a tile of `height` rows has any of `rows`: tile * height may pass 2^31 behind the last one.
 PLAN_FN bool tile_has_rows(int tile, int height, int rows) { return tile <= (rows - 1) / height; }
 // Slot `base` of a chunk of n, or the one behind the chunk: what a wavefront asks for ahead may lie some hundred behind it.

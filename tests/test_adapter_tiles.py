@@ -10,6 +10,7 @@ import pytest
 import adapter_plan
 import plain64
 import test_gpu_adapter as gpu
+import test_gpu_adapter_many_rows as more
 from gpu_util import say
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
@@ -23,6 +24,7 @@ extern "C" int choose(int cus, int64_t rows, int N, int K, int most, int64_t pai
     l.sixteens = sixteens;
     return choose_project(cus, rows, N, K, l);
 }
+extern "C" int shares_k(int cus, int tiles) { return low_shares_k(cus, tiles); }
 extern "C" int pairs(int rank, int pieces) { return segment_pairs(rank, pieces); }
 """
 MANY = (2560, 1100, 8, 8192, 4096)  # single tokens, adapters, ranks, n_in, n_out
@@ -85,6 +87,19 @@ def test_gpu_tests_still_reach_all_tiles(plan):
                     reached[True].add(plan[0](lengths, of, ranks, n_out, n_in, pieces)[0])
                     reached[False].add(plan[0](lengths, of, ranks, n_in, n_out, pieces)[0])
         assert reached[True] == reached[False] == {32, 64, 96, 256}
+
+
+def test_gpu_tests_reach_both_kernels_of_the_low_rank_activations(plan):
+    """For 16, 32, 64 and 128 ranks, in tests that compare with 64 bits."""
+    reached = set()
+    for lengths, of, ranks in [*gpu.BATCHES.values(), *gpu.LARGE.values(), *((more.LENGTHS, more.OF, r) for r in more.RANKS.values())]:
+        rows_of = {}
+        for n, a in zip(lengths, of):
+            a = a if a >= 0 and ranks[a] else -1
+            rows_of[a] = rows_of.get(a, 0) + n
+        room = (max(max(ranks), 1) + 7) // 8 * 8
+        reached.add((next(r for r in (16, 32, 64, 128) if room <= r), bool(plan[1].shares_k(256, sum(-(-n // 16) for n in rows_of.values())))))
+    assert reached == {(r, s) for r in (16, 32, 64, 128) for s in (False, True)}
 
 
 def test_many_segments_go_through_the_large_tiles(plan):
