@@ -25,12 +25,12 @@ struct leann_adapter_rows {
     DevBuf mem;
     const int32_t *row_of = nullptr;     // [T, up to a multiple of 256: the last row again, 8 more]
     const int32_t *run_ptr = nullptr;    // [32-slot groups + 1]
-    const int4 *runs = nullptr;          // adapter, first slot, slots | rank << 8 | number among the used adapters << 16, scale
+    const int2 *runs = nullptr;          // first slot, slots | rank << 8 | number among the used adapters << 16
     const int32_t *seg_ptr = nullptr;    // [256-slot tiles + 1]
     const int4 *segs = nullptr;          // a tile's adapters: first slot, slot behind the last, rank, number among the used adapters
     const int4 *tiles = nullptr;         // adapter, first slot, slots | rank << 16, number among the used adapters
     const int4 *wide_tiles = nullptr;    // likewise
-    const int4 *chunks = nullptr;        // likewise, by adapter
+    const int2 *chunks = nullptr;        // by adapter: first slot, slots | rank << 16
     const int4 *adapters = nullptr;      // [n_adapters] first chunk, chunks, rank, scale
     const int32_t *used = nullptr;       // [n_used] adapters that have rows
 };
@@ -94,7 +94,7 @@ __host__ __device__ inline int rank_groups(int R) { return (R + 15) >> 4; }
 // infinities stay with it.  Lane l holds run l of the group's `count`; with an adapter per row, what bounds it is the runs' latency, so B of them have
 // their first 16 ranks on the way together.
 template <int TN, int UP>
-__device__ inline void add_adapters(f32x16 (&acc)[TN], const int4 &my_run, int count, int group, int first, int step, const bf16_t *pieces,
+__device__ inline void add_adapters(f32x16 (&acc)[TN], const int2 &my_run, int count, int group, int first, int step, const bf16_t *pieces,
                                     const bf16_t *up, int R16, int column_tiles, int column_tile)
 {
     const int lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31;
@@ -111,8 +111,8 @@ __device__ inline void add_adapters(f32x16 (&acc)[TN], const int4 &my_run, int c
 #pragma unroll
         for (int r = 0; r < B; ++r) {
             const int from = min(i + r * step, count - 1);
-            slot[r] = __builtin_amdgcn_readlane(my_run.y, from) - group * 32;
-            z[r] = __builtin_amdgcn_readlane(my_run.z, from);
+            slot[r] = __builtin_amdgcn_readlane(my_run.x, from) - group * 32;
+            z[r] = __builtin_amdgcn_readlane(my_run.y, from);
             const bf16_t *u = up + (size_t)((uint32_t)z[r] >> 16) * column_tiles * R16 * UP * 512;
 #pragma unroll
             for (int ni = 0; ni < TN; ++ni)

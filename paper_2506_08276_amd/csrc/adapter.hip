@@ -191,7 +191,7 @@ __global__ __launch_bounds__(256) void low_kernel(const T *x, int64_t ldx, const
 // `up`); 3391 x 384 x 1536 in tiles of 64 x 96 13.4 us, in 64 x 64 (two on some units) 18.8.  Beyond that the larger tile reads less.
 template <class T, int TM, int TN, int U>
 __global__ __launch_bounds__(256, 2) void project_kernel(const T *x, int64_t ldx, const T *w, const float *bias, int N, int K, const int32_t *row_of,
-                                                      int rows, const int32_t *run_ptr, const int4 *runs, const bf16_t *pieces, int R16,
+                                                      int rows, const int32_t *run_ptr, const int2 *runs, const bf16_t *pieces, int R16,
                                                       const bf16_t *up, T *out, int64_t ldo)
 {
     typedef typename Frag<T>::type F;
@@ -205,7 +205,7 @@ __global__ __launch_bounds__(256, 2) void project_kernel(const T *x, int64_t ldx
     if (!tile_has_rows(tile_m, BM, rows)) return;
     const int ksteps = project_ksteps(K), used = (K + 15) >> 4;
     const T *xp[TM], *wp[TN];
-    int4 my_run[TM];
+    int2 my_run[TM];
     int count[TM];
 #pragma unroll
     for (int mi = 0; mi < TM; ++mi) xp[mi] = x + (int64_t)row_of[tile_m * BM + mi * 32 + l32] * ldx + half * 8;
@@ -213,7 +213,7 @@ __global__ __launch_bounds__(256, 2) void project_kernel(const T *x, int64_t ldx
     for (int mi = 0; mi < TM; ++mi) {
         const int group = tile_m * TM + mi, begin = group * 32 < rows ? run_ptr[group] : 0;
         count[mi] = group * 32 < rows ? run_ptr[group + 1] - begin : 0;
-        my_run[mi] = int4{};
+        my_run[mi] = int2{};
         if (lane < count[mi]) my_run[mi] = runs[begin + lane];
     }
     const int last_ct = (N - 1) >> 5;
@@ -316,15 +316,15 @@ __device__ inline f32x4 outer_step(const bf16x8 (&h)[3], const f16x8 &p, f32x4 c
 // 82 953 rows, 768 + 768 columns, rank up to 32: 72 us, 3.5 TB/s.
 template <class T, int NR>
 __global__ __launch_bounds__(256) void outer_kernel(const T *x, int64_t ldx, const T *dout, int64_t ldd, const float *grad_low, const float *low, int R,
-                                                    int K, int N, const int32_t *row_of, const int4 *chunks, float *partial)
+                                                    int K, int N, const int32_t *row_of, const int2 *chunks, float *partial)
 {
     constexpr int PITCH = 36;  // rows of a rank's 32, in steps of 16 bytes, and all banks by ranks
     __shared__ __attribute__((aligned(16))) float sums[16 * NR][128];
     __shared__ __attribute__((aligned(16))) float turned[4][16 * NR][PITCH];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, j = lane & 15;
     const int strips_k = (K + 127) / 128, strips = strips_k + (N + 127) / 128, strip = blockIdx.x % strips;
-    const int4 chunk = chunks[blockIdx.x / strips];
-    const int n = chunk.z & 0xffff, rank = chunk.z >> 16, r0 = blockIdx.y * 16 * NR;
+    const int2 chunk = chunks[blockIdx.x / strips];
+    const int n = chunk.y & 0xffff, rank = chunk.y >> 16, r0 = blockIdx.y * 16 * NR;
     if (r0 >= rank) return;
     const bool of_x = strip < strips_k;
     const T *p = of_x ? x : dout;
@@ -341,9 +341,9 @@ __global__ __launch_bounds__(256) void outer_kernel(const T *x, int64_t ldx, con
     u32x4 d[8];
     f32x4 hv[NR][2];
     auto number = [&](int base) {  // the table goes on behind the last slot: what is read there is not used
-        __builtin_memcpy(row, row_of + chunk_slot(chunk.y, n, base + q * 8), sizeof(row));
+        __builtin_memcpy(row, row_of + chunk_slot(chunk.x, n, base + q * 8), sizeof(row));
 #pragma unroll
-        for (int i = 0; i < 2; ++i) h_row[i] = row_of[chunk_slot(chunk.y, n, base + i * 16 + (lane >> 2))];
+        for (int i = 0; i < 2; ++i) h_row[i] = row_of[chunk_slot(chunk.x, n, base + i * 16 + (lane >> 2))];
     };
     auto request = [&](int base) {
 #pragma unroll
@@ -537,7 +537,7 @@ void enqueue_project(leann_ctx *ctx, const leann_adapter_rows *rows, const T *x,
         static_assert(Cfg::BM == 256 && Cfg::BN == 256, "");
         const int tiles_n = (N + Cfg::BN - 1) / Cfg::BN;
         hipLaunchKernelGGL((project_large_kernel<T, 2, 4, 2>), dim3((unsigned)l.blocks), dim3(512), Cfg::SMEM, ctx->stream, x, ldx, w, bias, N, K, rows->row_of,
-                           (int)rows->T, rows->seg_ptr, rows->segs, pieces, R16, up, out, ldo, tiles_n, tiles_n);
+                           (int)rows->T, rows->seg_ptr, rows->segs, pieces, R16, up, out, ldo, tiles_n);
         return;
     }
     auto go = [&](auto kernel) {
@@ -631,8 +631,8 @@ int make_rows(leann_ctx *ctx, const int32_t *rows_of_request, const int32_t *ada
     // Rows of a chunk of outer_kernel: as many as leave one chunk for every third CU (times the blocks of 128 columns, twelve at 768 + 768), 64 at least, 2048 at most.
     // 82 953 rows 768 -> 768, ranks up to 32: 229 us for the whole gradient, with chunks half as long 239 (their sums are written and read again).
     const int chunk_rows = (int)std::min<int64_t>(2048, std::max<int64_t>(64, (adapted / std::max(1, ctx->num_cus / 3) + 63) / 64 * 64));
-    std::vector<int4> tiles, wide, chunks, runs, adapters(n_adapters);
-    std::vector<int4> segs;
+    std::vector<int4> tiles, wide, segs, adapters(n_adapters);
+    std::vector<int2> runs, chunks;
     std::vector<int32_t> used, run_ptr((T + 31) / 32 + 1, 0), seg_ptr((T + 255) / 256 + 1, 0);
     auto bits = [](float f) {
         int32_t i;
@@ -651,11 +651,11 @@ int make_rows(leann_ctx *ctx, const int32_t *rows_of_request, const int32_t *ada
         for (int64_t s = from; s < to; s += 16) tiles.push_back(int4{a < n_adapters ? a : -1, (int)s, (int)std::min<int64_t>(16, to - s) | r << 16, number});
         if (a == n_adapters) break;
         adapters[a] = int4{(int)chunks.size(), 0, r, bits(scale[a])};
-        for (int64_t s = from; s < to; s += chunk_rows) chunks.push_back(int4{a, (int)s, (int)std::min<int64_t>(chunk_rows, to - s) | r << 16, number});
+        for (int64_t s = from; s < to; s += chunk_rows) chunks.push_back(int2{(int)s, (int)std::min<int64_t>(chunk_rows, to - s) | r << 16});
         adapters[a].y = (int)chunks.size() - adapters[a].x;
         for (int64_t s = from; s < to;) {
             const int64_t group = s / 32, end = std::min<int64_t>(to, (group + 1) * 32);
-            runs.push_back(int4{a, (int)s, (int)(end - s) | r << 8 | (int)((uint32_t)number << 16), bits(scale[a])});
+            runs.push_back(int2{(int)s, (int)(end - s) | r << 8 | (int)((uint32_t)number << 16)});
             ++run_ptr[group + 1];
             s = end;
         }
@@ -678,7 +678,7 @@ int make_rows(leann_ctx *ctx, const int32_t *rows_of_request, const int32_t *ada
         }
     }
     for (AdapterLoad &l : out->load)
-        for (const int4 &run : runs) l.sixteens += rank_groups(run.z >> 8 & 255);
+        for (const int2 &run : runs) l.sixteens += rank_groups(run.y >> 8 & 255);
     for (size_t g = 1; g < run_ptr.size(); ++g) run_ptr[g] += run_ptr[g - 1];
 
     out->device = ctx->device;
@@ -703,9 +703,9 @@ int make_rows(leann_ctx *ctx, const int32_t *rows_of_request, const int32_t *ada
     const char *base = (const char *)out->mem.p;
     out->row_of = (const int32_t *)(base + at[0]);
     out->run_ptr = (const int32_t *)(base + at[1]);
-    out->runs = (const int4 *)(base + at[2]);
+    out->runs = (const int2 *)(base + at[2]);
     out->tiles = (const int4 *)(base + at[3]);
-    out->chunks = (const int4 *)(base + at[4]);
+    out->chunks = (const int2 *)(base + at[4]);
     out->adapters = (const int4 *)(base + at[5]);
     out->used = (const int32_t *)(base + at[6]);
     out->seg_ptr = (const int32_t *)(base + at[7]);

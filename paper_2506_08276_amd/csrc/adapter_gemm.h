@@ -69,8 +69,7 @@ __device__ inline void store_past_l2(const u32x4 &v, __amdgpu_buffer_rsrc_t b, i
 template <class T, int WM, int TM, int TN>
 __global__ __launch_bounds__(512, 1) void project_large_kernel(const T *x, int64_t ldx, const T *w, const float *bias, int N, int K,
                                                                const int32_t *row_of, int rows, const int32_t *seg_ptr, const int4 *segs,
-                                                               const bf16_t *pieces, int R16, const bf16_t *up, T *out, int64_t ldo, int tiles_n,
-                                                               int gcols)
+                                                               const bf16_t *pieces, int R16, const bf16_t *up, T *out, int64_t ldo, int tiles_n)
 {
     typedef ProjectCfg<WM, TM, TN> Cfg;
     typedef typename Frag<T>::type F;
@@ -81,15 +80,14 @@ __global__ __launch_bounds__(512, 1) void project_large_kernel(const T *x, int64
     const int wm = wave / Cfg::WN, wn = wave % Cfg::WN;
     const bool second = wave >= 4;  // the group that multiplies in the other's memory phases
 
-    const int n_tiles = ((rows + BM - 1) / BM) * tiles_n, tiles_m = n_tiles / tiles_n;
+    const int n_tiles = ((rows + BM - 1) / BM) * tiles_n;
     const int per_xcd = (n_tiles + 7) >> 3, blocks_per_xcd = gridDim.x >> 3;
-    auto tile_at = [&](int step, int &tm, int &tn) -> bool {
+    auto tile_at = [&](int step, int &tm, int &tn) -> bool {  // an XCD takes a run of tiles, all columns of a few rows
         const int in_xcd = step * blocks_per_xcd + (int)(blockIdx.x >> 3);
-        const int logical = (int)(blockIdx.x & 7) * per_xcd + in_xcd;
-        if (in_xcd >= per_xcd || logical >= n_tiles) return false;
-        const int g = logical / (tiles_m * gcols), r = logical - g * tiles_m * gcols, cg = min(gcols, tiles_n - g * gcols);
-        tm = r / cg;
-        tn = g * gcols + r % cg;
+        const int tile = (int)(blockIdx.x & 7) * per_xcd + in_xcd;
+        if (in_xcd >= per_xcd || tile >= n_tiles) return false;
+        tm = tile / tiles_n;
+        tn = tile % tiles_n;
         return true;
     };
     int tile_m = 0, tile_n = 0;
