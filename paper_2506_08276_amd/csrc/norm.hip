@@ -84,7 +84,8 @@ __device__ inline float sum8(const f32x8 &v) { return ((v[0] + v[1]) + (v[2] + v
 
 // t = residual + dropout(x); out = (t - mean) rstd gamma + beta.  LPR lanes per row, NC accesses of eight elements per lane.
 // Mean first, then the squares of what is left, both from registers in 32 bits: rows whose mean is large lose nothing, and x is read once.  The next row is on its
-// way while this one is added up.  Bound by memory: 131 072 x 768 bf16 with dropout, residual, total and statistics 149 us, 5.4 TB/s; a dozen rows 9.2 us.
+// way while this one is added up, where there is one: eight blocks per compute unit, so from 8192 rows of a wavefront each on (4099 x 1021 fp32: 9.6 us, 3.5 TB/s).  Bound by
+// memory: 131 072 x 768 bf16 with dropout, residual, total and statistics 148 us, 5.4 TB/s; a dozen rows 9.1 us.
 template <class T, int LPR, int NC, bool DROP>
 __global__ __launch_bounds__(256) void layernorm_kernel(const T *x, int64_t ldx, const T *res, int64_t ldr, int rows, int cols,
                                                         const float *gamma, const float *beta, float eps, T *out, int64_t ldo, T *total,
