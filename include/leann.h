@@ -42,6 +42,7 @@ typedef struct leann_ctx leann_ctx;
 typedef struct leann_pq leann_pq;
 typedef struct leann_projection leann_projection;
 typedef struct leann_adapter_rows leann_adapter_rows;
+typedef struct leann_attention_plan leann_attention_plan;
 
 /* Encoder shape.  The paper fixes a BERT-style encoder of 110 M parameters with
  * 768-d output over 256-token chunks (Sec. 7 set-up); the layer equations are the
@@ -425,6 +426,40 @@ int leann_adapter_project(leann_ctx *ctx, const leann_projection *proj, const le
 int leann_adapter_project_backward(leann_ctx *ctx, const leann_projection *proj, const leann_adapter_rows *rows, const void *dout_dev, int64_t ldd,
                                    const void *x_dev, int64_t ldx, const float *low_dev, const void *down_dev, const void *up_dev, void *dx_dev,
                                    int64_t lddx, float *ddown_dev, float *dup_dev);
+
+/*
+ * Attention over ragged sequences.  Sequence s has the next q_rows[s] rows of q and the next k_rows[s] rows of k and v; its query i stands at position p = first[s] + i, its keys
+ * at 0, 1, ...  Head h has the columns [h dim, (h + 1) dim) of q, and of k and v those of key head h / (heads / kv_heads).
+ *   visible: j <= p + right and (j >= p - left or j < sinks); left or right -1: no limit to that side
+ *   s_ij = scale q_i . k_j + bias[bucket_of[clamp(j - p, -distance, distance) + distance]][h]  (without buckets: no bias)
+ *   lse_i = log sum over visible j of exp s_ij,  out_i = sum over visible j of exp(s_ij - lse_i) v_j;  where nothing is visible out_i is 0 and lse_i -inf
+ * Sums, maxima and scores are fp32; weights exp(s - max), and in gradients exp(s - lse) and the scores' gradients, are rounded to the inputs' type where they enter a product of
+ * matrices.  What a query does not see does not reach it, be it infinite or NaN.  Rows and columns behind the last sequence and head are neither read nor written.
+ */
+typedef struct {
+    int32_t heads, kv_heads, dim;     /* heads: a multiple of kv_heads, at most 1024; dim: a multiple of 8 up to 128 */
+    int32_t left, right, sinks;
+    int32_t buckets, distance;        /* 0, 0 without a bias; buckets up to 4096, distance up to 1024 */
+    const int32_t *bucket_of_host;    /* [2 distance + 1], copied; NULL without a bias */
+} leann_attention_desc;
+
+/* The bucket of each relative position (key minus query) from -distance to distance.  Of the buckets of a direction the first half hold one distance each, the others ranges that
+ * grow by equal factors up to `distance`, which belongs to the last one.  both: half of the buckets (an even number) to each direction, the upper half for keys ahead; else keys
+ * ahead count as distance 0.  Any other table may be given instead.  distance above half of a direction's buckets, up to 1024, else LEANN_EINVAL. */
+int leann_position_buckets(int32_t buckets, int32_t distance, int both, int32_t *bucket_of_host);
+
+/* The sequences of a batch, one plan for the layers and directions that it goes through.  k_rows_host NULL: as q_rows (self-attention); first_host NULL: 0.  Host arrays, copied;
+ * lengths of 0 are allowed.  Synchronises the stream.  Errors: negative lengths or positions, windows below -1, buckets outside the table -> LEANN_EINVAL; sizes beyond those above,
+ * positions of 2^30, 2^31 - 256 rows, 2^24 workgroups -> LEANN_ESHAPE. */
+int leann_attention_create(leann_ctx *ctx, const int32_t *q_rows_host, const int32_t *k_rows_host, const int32_t *first_host, int32_t n_sequences,
+                           const leann_attention_desc *desc, leann_attention_plan **out);
+void leann_attention_free(leann_attention_plan *plan);
+
+/* out[Tq][heads * dim] from q[Tq][heads * dim], k and v[Tk][kv_heads * dim]: bf16 or f16, 16-byte alignment, rows a multiple of 8 elements apart (slices of one projection's output
+ * are fine).  bias: fp32[buckets][heads].  lse (NULL, or fp32[heads][Tq]): what the backward pass needs.  out must not overlap q, k or v (LEANN_EINVAL).
+ * Where there are few queries, their keys are split over blocks whose sums are joined: a row's bits may depend on the other sequences' lengths, its value does not. */
+int leann_attention(leann_ctx *ctx, const leann_attention_plan *plan, const void *q_dev, int64_t ldq, const void *k_dev, int64_t ldk, const void *v_dev, int64_t ldv, int dtype,
+                    float scale, const float *bias_dev, void *out_dev, int64_t ldo, float *lse_dev);
 
 #ifdef __cplusplus
 }

@@ -24,7 +24,8 @@ EXPORTS = ["leann_last_error", "leann_create", "leann_destroy", "leann_embed", "
            "leann_set_limits", "leann_set_call_memo", "leann_set_gemm_tiles", "leann_profile_begin", "leann_profile_end", "leann_bench_mfma", "leann_bench_gather", "leann_bench_l1pull",
            "leann_dropout", "leann_layernorm", "leann_layernorm_backward",
            "leann_projection_create", "leann_projection_free", "leann_adapter_rows_create", "leann_adapter_rows_free",
-           "leann_adapter_project", "leann_adapter_project_backward"]
+           "leann_adapter_project", "leann_adapter_project_backward",
+           "leann_position_buckets", "leann_attention_create", "leann_attention_free", "leann_attention"]
 PROF_KINDS = ["gemm_qkv", "gemm_o", "gemm_ffn1", "gemm_ffn2", "attention", "layernorm", "enc_other", "traverse",
               "collect", "score_insert", "lut", "adc"]
 
@@ -80,7 +81,7 @@ def load_library(path=LIB_PATH):
         for name in EXPORTS:
             getattr(lib, name)
         lib.leann_destroy.restype = None
-        for name in ("leann_pq_free", "leann_projection_free", "leann_adapter_rows_free"):
+        for name in ("leann_pq_free", "leann_projection_free", "leann_adapter_rows_free", "leann_attention_free"):
             getattr(lib, name).restype = None
         V, I, N, F = C.c_void_p, C.c_int32, C.c_int64, C.c_float
         for name, args in {  # argument types: plain numbers are converted by ctypes, which small calls are faster with
@@ -90,7 +91,10 @@ def load_library(path=LIB_PATH):
                 "leann_projection_create": [V, V, V, I, I, I, I, V], "leann_projection_free": [V],
                 "leann_adapter_rows_create": [V, V, V, I, V, V, I, I, V], "leann_adapter_rows_free": [V],
                 "leann_adapter_project": [V, V, V, V, N, V, V, V, N, V],
-                "leann_adapter_project_backward": [V, V, V, V, N, V, N, V, V, V, V, N, V, V]}.items():
+                "leann_adapter_project_backward": [V, V, V, V, N, V, N, V, V, V, V, N, V, V],
+                "leann_position_buckets": [I, I, I, V],
+                "leann_attention_create": [V, V, V, V, I, V, V], "leann_attention_free": [V],
+                "leann_attention": [V, V, V, N, V, N, V, N, I, F, V, V, N, V]}.items():
             getattr(lib, name).argtypes = args
         _lib = lib
     return _lib
@@ -509,3 +513,66 @@ def leann_adapter_project_backward(ctx, proj, rows, dout, x, low, down, up, need
     _check(load_library().leann_adapter_project_backward(ctx, proj, rows, gp, ldd, xp, ldx, None if low is None else low.data_ptr(), dp, up, op, lddx,
                                                          ddown.data_ptr() if need_adapters else None, dup.data_ptr() if need_adapters else None))
     return dx, ddown, dup
+
+
+# ---- attention over ragged sequences
+class AttentionDesc(C.Structure):
+    _fields_ = [("heads", C.c_int32), ("kv_heads", C.c_int32), ("dim", C.c_int32), ("left", C.c_int32), ("right", C.c_int32),
+                ("sinks", C.c_int32), ("buckets", C.c_int32), ("distance", C.c_int32), ("bucket_of", C.c_void_p)]
+
+
+def leann_position_buckets(buckets, distance, both=True):
+    """int32 [2 distance + 1]: the bucket of each relative position (key minus query), single distances first, then ranges that grow by equal factors."""
+    found = np.empty(2 * max(0, int(distance)) + 1, np.int32)
+    _check(load_library().leann_position_buckets(buckets, distance, int(both), found.ctypes.data))
+    return found
+
+
+def leann_attention_create(ctx, q_rows, k_rows=None, *, heads, head_dim, kv_heads=None, first=None, window=None, sinks=0, bucket_of=None):
+    """The sequences of a batch: rows of queries, rows of keys (None: the same rows), position of each first query (None: 0); window = (left, right)
+    keys that a query sees to either side (-1 or None: all), the first `sinks` keys beside it; bucket_of: int [2 distance + 1], the bias's
+    bucket of each relative position (leann_position_buckets makes one)."""
+    q = _int32(q_rows)
+    k, at = None if k_rows is None else _int32(k_rows), None if first is None else _int32(first)
+    assert q.ndim == 1 and (k is None or k.shape == q.shape) and (at is None or at.shape == q.shape), "q_rows, k_rows, first: need one number per sequence"
+    table = None if bucket_of is None else _int32(bucket_of)
+    assert table is None or table.ndim == 1 and len(table) >= 3 and len(table) % 2 == 1, "bucket_of: need 2 distance + 1 buckets"
+    left, right = (-1, -1) if window is None else window
+    h = _Handle()
+    h.heads, h.kv_heads, h.dim = heads, heads if kv_heads is None else kv_heads, head_dim
+    h.buckets = 0 if table is None else max(0, int(table.max())) + 1
+    desc = AttentionDesc(heads, h.kv_heads, head_dim, left, right, sinks, h.buckets, 0 if table is None else len(table) // 2,
+                         None if table is None else table.ctypes.data)
+    _check(load_library().leann_attention_create(ctx, q.ctypes.data, None if k is None else k.ctypes.data, None if at is None else at.ctypes.data,
+                                                 len(q), C.byref(desc), C.byref(h)))
+    h.Tq = int(q.sum(dtype=np.int64))
+    h.Tk = h.Tq if k is None else int(k.sum(dtype=np.int64))
+    return h
+
+
+def leann_attention_free(plan):
+    load_library().leann_attention_free(plan)
+
+
+def _attention_inputs(plan, q, k, v, bias):
+    """Pointers and distances of the rows of q, k and v, and the bias's pointer."""
+    assert q.shape == (plan.Tq, plan.heads * plan.dim), "q: need [Tq][heads * head_dim]"
+    assert k.shape == v.shape == (plan.Tk, plan.kv_heads * plan.dim), "k, v: need [Tk][kv_heads * head_dim]"
+    assert q.dtype == k.dtype == v.dtype and q.dtype in (torch.bfloat16, torch.float16), "q, k, v: need bfloat16 or float16"
+    assert (bias is None) == (plan.buckets == 0), "bias: goes with a plan that has buckets"
+    assert bias is None or bias.dim() == 2 and bias.shape[0] >= plan.buckets and bias.shape[1] == plan.heads, "bias: need [buckets][heads]"
+    return (*_rows(q, "q"), *_rows(k, "k"), *_rows(v, "v")), None if bias is None else _vector(bias, bias.numel(), "bias")
+
+
+def leann_attention(ctx, plan, q, k, v, scale=None, bias=None, keep=False, out=None):
+    """softmax(scale q k^T + bias) v for every sequence and head of the plan; q [Tq][heads * head_dim], k and v [Tk][kv_heads * head_dim], bias float32
+    [buckets][heads]; scale None: head_dim ** -0.5.  keep: returns (out, lse), what the backward pass needs; else out."""
+    (qp, ldq, kp, ldk, vp, ldv), bp = _attention_inputs(plan, q, k, v, bias)
+    if out is None:
+        out = torch.empty((plan.Tq, plan.heads * plan.dim), dtype=q.dtype, device=q.device)
+    assert out.shape == q.shape and out.dtype == q.dtype, "out: shape or type differs"
+    lse = torch.empty((plan.heads, plan.Tq), dtype=torch.float32, device=q.device) if keep else None
+    op, ldo = _rows(out, "out")
+    scale = plan.dim ** -0.5 if scale is None else scale
+    _check(load_library().leann_attention(ctx, plan, qp, ldq, kp, ldk, vp, ldv, _dtype(q), scale, bp, op, ldo, lse.data_ptr() if keep else None))
+    return (out, lse) if keep else out

@@ -1,0 +1,253 @@
+// What the kernels of attention and of its gradient share: the plan, tiles in LDS, MFMA operands, masks and the bias (gfx950).
+#pragma once
+#include "attention_plan.h"
+#include "rows.h"
+
+constexpr int ATT_MOST_DISTANCE = 1024;
+constexpr int ATT_EXT = 96;  // a wavefront's 32 rows and 64 of the other side have relative positions in a range of 95
+
+// One batch's sequences: tables on the device, in one allocation.
+struct leann_attention_plan {
+    int device = 0;
+    int32_t heads = 0, kv_heads = 0, dim = 0;
+    int64_t Tq = 0, Tk = 0;
+    int32_t left = -1, right = -1, sinks = 0;  // as the kernels take them: no limit is a bound behind every position
+    int32_t distance = 0, buckets = 0;         // distance: of the table below, no longer than the sequences make it
+    int32_t query_waves = 0;                   // wavefronts of a forward block, 32 queries each
+    int32_t n_items = 0, n_grad_items = 0, n_key_items = 0, n_joins = 0, n_slots = 0, n_grad_tiles = 0, n_key_tiles = 0;
+    DevBuf mem;
+    const AttentionTile *tiles = nullptr, *grad_tiles = nullptr, *key_tiles = nullptr;  // of queries, for the gradient of queries, of keys
+    const AttentionItem *items = nullptr, *grad_items = nullptr, *key_items = nullptr;
+    const AttentionJoin *joins = nullptr;
+    const int32_t *bucket_of = nullptr;  // [2 distance + 1]
+};
+
+// A matrix of a call, for its checks.
+struct AttentionMatrix {
+    const char *name;
+    const void *p;
+    int64_t ld, cols, rows;
+};
+
+int att_launched(const char *call);
+int att_check_call(const char *call, const leann_ctx *ctx, const leann_attention_plan *plan, int dtype, float scale, const float *bias_dev);
+int att_check_rows(const char *call, const char *what, const void *p, int64_t ld, int64_t cols);
+int att_check_apart(const char *call, const AttentionMatrix &a, const AttentionMatrix &b);
+
+// What a kernel needs of a plan besides tables.
+struct AttentionShape {
+    int32_t heads, share;  // heads, and how many of them share a key head
+    int32_t dim;
+    int32_t left, right, sinks, distance;
+    float scale;
+};
+AttentionShape att_shape(const leann_attention_plan *p, float scale);
+
+namespace {
+
+constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.693147180559945309417f;
+
+template <class T>
+struct Half8;
+template <>
+struct Half8<bf16_t> {
+    typedef bf16x8 type;
+    static constexpr uint32_t EXPONENT = 0x7f80;
+};
+template <>
+struct Half8<f16_t> {
+    typedef f16x8 type;
+    static constexpr uint32_t EXPONENT = 0x7c00;
+};
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+
+__device__ inline f32x16 att_mfma(const bf16x8 &a, const bf16x8 &b, const f32x16 &c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+__device__ inline f32x16 att_mfma(const f16x8 &a, const f16x8 &b, const f32x16 &c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+
+// Tiles of 64 rows of DP elements (the head's size, zeros up to 32, 64 or 128) lie in LDS as rows of 16-byte chunks, chunk c of row r at c ^ att_swizzle(r): 16 rows' reads
+// of one chunk, and the reads of four adjacent rows' 64 bytes that transpose, reach all banks.
+template <int DP>
+__device__ inline int att_swizzle(int row)
+{
+    if constexpr (DP == 32) return (row >> 2) & 3;
+    else if constexpr (DP == 64) return ((row >> 1) & 1) << 2 | ((row >> 2) & 3);
+    else return (row & 3) << 2 | ((row >> 2) & 3);
+}
+
+// A tile on its way from memory to LDS, NT threads' chunks of it.
+template <class T, int DP, int NT>
+struct TileInFlight {
+    static constexpr int CPR = DP / 8, N = ATT_STEP * CPR / NT;
+    static_assert(N * NT == ATT_STEP * CPR, "whole chunks per thread");
+    u32x4 v[N];
+
+    // rows [row, row + 64) of `base`, of which those from `rows` on are zeros
+    __device__ inline void load(const T *base, int64_t ld, int row, int rows, int dim)
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int c = threadIdx.x + i * NT, r = c / CPR, ch = c % CPR;
+            if (row + r < rows && ch * 8 < dim) v[i] = *reinterpret_cast<const u32x4 *>(base + (int64_t)(row + r) * ld + ch * 8);
+            else v[i] = u32x4{0, 0, 0, 0};
+        }
+    }
+    __device__ inline void store(T *lds) const
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int c = threadIdx.x + i * NT, r = c / CPR, ch = c % CPR;
+            *reinterpret_cast<u32x4 *>(lds + r * DP + ((ch ^ att_swizzle<DP>(r)) << 3)) = v[i];
+        }
+    }
+    // Infinities and NaN become zeros, and their rows' bits are set in bad[2]: a row of the other side that does not see them would get NaN from a product with zero.
+    __device__ inline void take_out_nonfinite(uint32_t *bad)
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            bool any = false;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                constexpr uint32_t E = Half8<T>::EXPONENT;
+                const bool lo = (v[i][w] & E) == E, hi = (v[i][w] & E << 16) == E << 16;
+                v[i][w] &= (lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u);
+                any |= lo | hi;
+            }
+            if (any) {
+                const int r = (threadIdx.x + i * NT) / CPR;
+                atomicOr(&bad[r >> 5], 1u << (r & 31));
+            }
+        }
+    }
+};
+
+// Operand A (or B) of a 32x32x16 product: rows row0 + lane % 32 of a tile, elements 16 step + 8 (lane / 32) and on.
+template <class T, int DP>
+__device__ inline typename Half8<T>::type row_operand(const T *lds, int row0, int step, int lane)
+{
+    const int row = row0 + (lane & 31), ch = step * 2 + (lane >> 5);
+    return *reinterpret_cast<const typename Half8<T>::type *>(lds + row * DP + ((ch ^ att_swizzle<DP>(row)) << 3));
+}
+
+// Operand A of the transposed tile: lane l holds column col0 + l % 32 and, in slots 0..3 and 4..7, the rows row0 + 4 (l / 32) + {0..3} and 8 more: exactly the rows that
+// accumulator registers 8u .. 8u + 7 of a 32x32 product hold (row0 = 16 u), so that those are the other operand as they are.  16 lanes read four rows of 16 elements and
+// get a column of four each.
+template <class T, int DP>
+__device__ inline typename Half8<T>::type column_operand(const T *lds, int row0, int col0, int lane)
+{
+    const int i = lane & 15, row = row0 + 4 * (lane >> 5) + (i >> 2), col = col0 + (lane & 16) + 4 * (i & 3);
+    auto read = [&](int r) {
+        const T *p = lds + r * DP + (((col >> 3) ^ att_swizzle<DP>(r)) << 3) + (col & 7);
+        return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)p);
+    };
+    const s16x4 a = read(row), b = read(row + 8);
+    return __builtin_bit_cast(typename Half8<T>::type, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// A lane's operand row from memory: `p` points at the row's head, nullptr for zeros.
+template <class T, int DP>
+__device__ inline void load_rows(const T *p, int dim, int lane, typename Half8<T>::type (&f)[DP / 16])
+{
+#pragma unroll
+    for (int s = 0; s < DP / 16; ++s) {
+        const int at = s * 16 + (lane >> 5) * 8;
+        u32x4 v = {0, 0, 0, 0};
+        if (p && at < dim) v = *reinterpret_cast<const u32x4 *>(p + at);
+        f[s] = __builtin_bit_cast(typename Half8<T>::type, v);
+    }
+}
+
+// Number of accumulator register r's row, less 4 (lane / 32).
+constexpr __device__ int acc_row(int r) { return 8 * (r >> 2) + (r & 3); }
+
+// Eight registers of an accumulator, rounded to nearest: an operand.
+template <class T>
+__device__ inline typename Half8<T>::type rounded(const f32x16 &a, int u)
+{
+    f32x8 v;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = a[8 * u + i];
+    return __builtin_convertvector(v, typename Half8<T>::type);
+}
+
+// Sum, or maximum, over the two lanes that hold one column.
+__device__ inline float both_halves_sum(float v)
+{
+    const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(p[0]) + __uint_as_float(p[1]);
+}
+__device__ inline float both_halves_max(float v)
+{
+    const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __builtin_fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+}
+
+// Stores a transposed result: lane l holds column (row of the output) l % 32 of ND tiles of 32 elements.  Two groups of four rows are swapped between the halves
+// so that a lane has eight adjacent elements.
+template <class T, int ND>
+__device__ inline void store_columns(const f32x16 (&o)[ND], float factor, T *row, bool valid, int dim, int lane)
+{
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            f32x8 f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] = o[dt][8 * g + i] * factor;
+            u32x4 w = __builtin_bit_cast(u32x4, __builtin_convertvector(f, typename Half8<T>::type));
+            const auto a = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false), b = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+            const int at = dt * 32 + 16 * g + 8 * (lane >> 5);
+            if (valid && at < dim) *reinterpret_cast<u32x4 *>(row + at) = u32x4{a[0], b[0], a[1], b[1]};
+        }
+}
+
+// Adds to a transposed result (see store_columns) the infinities and NaN that were taken out of 64 rows from row j0 on, where the lane's column sees the row.
+template <class T, int ND, class Seen>
+__device__ inline void add_nonfinite(f32x16 (&o)[ND], const uint32_t *bad, const T *base, int64_t ld, int j0, int dim, int half, Seen seen)
+{
+    for (int i = 0; i < ATT_STEP; ++i) {
+        if (!(bad[i >> 5] >> (i & 31) & 1)) continue;
+        const bool mine = seen(j0 + i);
+        const T *row = base + (int64_t)(j0 + i) * ld;
+        int from = 4 * half;
+        asm volatile("" : "+v"(from));  // else the tests below leave the loop, and take scalar registers from the common path
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const int d = dt * 32 + 8 * c + from;
+                if (d >= dim) continue;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float x = (float)row[d + e];
+                    if (mine && !(__builtin_fabsf(x) < INFINITY)) o[dt][4 * c + e] += x;
+                }
+            }
+    }
+}
+
+// The bias of one head by relative position, times log2 e: [2 distance + 1 + 2 ATT_EXT], the ends repeated.
+__device__ inline int bias_entries(int distance) { return 2 * distance + 1 + 2 * ATT_EXT; }
+__device__ inline void make_bias(float *table, const float *bias, const int32_t *bucket_of, const AttentionShape &a, int head)
+{
+    for (int i = threadIdx.x; i < bias_entries(a.distance); i += blockDim.x) {
+        const int d = min(max(i - ATT_EXT, 0), 2 * a.distance);
+        table[i] = bias[(int64_t)bucket_of[d] * a.heads + head] * LOG2E;
+    }
+}
+
+// What the 32 rows (or queries) at positions from p of a wavefront see of 64 keys from key j on.
+struct Sight {
+    bool none, all;
+};
+__device__ inline Sight sight(const AttentionShape &a, int p, int queries, int j, int keys_left)
+{
+    // the first query sees the fewest keys ahead, the last one the fewest behind
+    const int last = p + queries - 1, end = j + min(ATT_STEP, keys_left) - 1;
+    const bool none = queries <= 0 || j > last + a.right || (end < p - a.left && j >= a.sinks);
+    const bool all = keys_left >= ATT_STEP && end <= p + a.right && (j >= last - a.left || end < a.sinks);
+    return {none, all};
+}
+
+}  // namespace

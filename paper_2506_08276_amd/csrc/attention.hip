@@ -1,0 +1,551 @@
+// Attention over ragged sequences with a bias by relative position, a sliding window and first tokens that stay visible: the forward pass and the plan (gfx950).
+#include <math.h>
+#include <string.h>
+
+#include <new>
+
+#include "adapter_plan.h"
+#include "attention.h"
+
+namespace {
+
+// ------------------------------------------------------------------ forward
+// A block takes NW * 32 queries of one head through their keys, 64 at a time; a wavefront has 32 queries.  S^T = K Q^T, so that a lane owns one query: its maximum and sum
+// run over its own registers, the other half of the keys is lane ^ 32's.  One pass: s = scale q.k + bias in units of log 2, m the largest so far, l = sum 2^(s - m),
+// O = sum 2^(s - m) v, l and O scaled when m grows.  P^T, rounded to the inputs' type (an error of half a step in each term, as the inputs themselves have), is the
+// other operand of O^T = V^T P^T without leaving its registers, see column_operand.
+// K and V tiles go through registers to LDS, two buffers, the next tile's loads before this one's products.
+template <int DP, int NW>
+struct AttendCfg {
+    static constexpr int NT = NW * 64, TILE = ATT_STEP * DP;
+    static constexpr int FIXED = 4 * TILE * 2 + 64;  // bytes; the bias's table follows
+};
+
+template <class T, int DP, int NW, bool BIAS>
+__global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attend_kernel(const AttentionItem *__restrict__ items, const AttentionTile *__restrict__ tiles, AttentionShape a,
+                                                                         const T *__restrict__ q, int64_t ldq, const T *__restrict__ k, int64_t ldk,
+                                                                         const T *__restrict__ v, int64_t ldv, const float *__restrict__ bias,
+                                                                         const int32_t *__restrict__ bucket_of, T *__restrict__ out, int64_t ldo,
+                                                                         float *__restrict__ lse, int64_t Tq, float *__restrict__ part_o,
+                                                                         float2 *__restrict__ part_ml)
+{
+    typedef typename Half8<T>::type V8;
+    constexpr int NT = AttendCfg<DP, NW>::NT, TILE = AttendCfg<DP, NW>::TILE, ND = DP / 32, NS = DP / 16;
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    T *Ks = reinterpret_cast<T *>(smem), *Vs = Ks + 2 * TILE;
+    uint32_t *bad = reinterpret_cast<uint32_t *>(smem + 4 * TILE * 2);  // [3][2]
+    float *table = reinterpret_cast<float *>(smem + AttendCfg<DP, NW>::FIXED);
+
+    const AttentionItem item = items[blockIdx.x];
+    if (item.tile < 0) return;
+    const AttentionTile t = tiles[item.tile];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, l32 = lane & 31;
+    const int h = item.head, g = h / a.share;
+    const T *kb = k + (int64_t)t.other0 * ldk + g * a.dim, *vb = v + (int64_t)t.other0 * ldv + g * a.dim;
+    auto tile_at = [&](int u) { return u < t.sink_tiles ? u : t.first_tile + u - t.sink_tiles; };
+
+    TileInFlight<T, DP, NT> kin, vin;
+    auto fetch = [&](int u) {
+        const int row = tile_at(u) * ATT_STEP;
+        kin.load(kb, ldk, row, t.others, a.dim);
+        vin.load(vb, ldv, row, t.others, a.dim);
+    };
+    if (t.begin < t.end) fetch(t.begin);
+    const int my_rows = min(32, t.rows - wave * 32), p0 = t.at + wave * 32;  // of this wavefront
+    const int my_row = t.row0 + wave * 32 + l32;
+    V8 qf[NS];
+    load_rows<T, DP>(l32 < my_rows ? q + (int64_t)my_row * ldq + h * a.dim : nullptr, a.dim, lane, qf);
+    if (BIAS) make_bias(table, bias, bucket_of, a, h);
+    if (tid < 6) bad[tid] = 0;
+    __syncthreads();
+
+    f32x16 o[ND];
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[dt][r] = 0.f;
+    float m = -INFINITY, l = 0.f;
+    const float scale2 = a.scale * LOG2E;
+    const int p = p0 + l32;
+
+    for (int u = t.begin, n = 0; u < t.end; ++u, ++n) {
+        const int j0 = tile_at(u) * ATT_STEP, buf = n & 1;
+        uint32_t *bad_now = bad + 2 * (n % 3);
+        const T *Kt = Ks + buf * TILE, *Vt = Vs + buf * TILE;
+        const bool edge = !sight(a, t.at, t.rows, j0, t.others - j0).all;
+        if (edge) vin.take_out_nonfinite(bad_now);
+        kin.store(Ks + buf * TILE);
+        vin.store(Vs + buf * TILE);
+        __syncthreads();
+        if (tid < 2) bad[2 * ((n + 2) % 3) + tid] = 0;  // read before this barrier, set again behind the next
+        if (u + 1 < t.end) fetch(u + 1);
+        const Sight see = sight(a, p0, my_rows, j0, t.others - j0);
+        if (see.none) continue;
+
+        f32x16 s[2];
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[kt][r] = 0.f;
+#pragma unroll
+            for (int i = 0; i < NS; ++i) s[kt] = att_mfma(row_operand<T, DP>(Kt, kt * 32, i, lane), qf[i], s[kt]);
+        }
+        // register r of tile kt is key j0 + 32 kt + 4 half + acc_row(r)
+        const int j = j0 + 4 * half;
+        if (BIAS) {
+            const int least = j0 - (p0 + 31), most = j0 + ATT_STEP - 1 - p0;  // relative positions
+            if (most <= -a.distance || least >= a.distance) {
+                const float c = table[most <= -a.distance ? 0 : bias_entries(a.distance) - 1];
+#pragma unroll
+                for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[kt][r] = fmaf(s[kt][r], scale2, c);
+            } else {
+                const float *at = table + (j - p + a.distance + ATT_EXT);
+#pragma unroll
+                for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[kt][r] = fmaf(s[kt][r], scale2, at[kt * 32 + acc_row(r)]);
+            }
+        } else {
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[kt][r] *= scale2;
+        }
+        if (!see.all) {
+            const int most = min(t.others - 1, p + a.right) - j, least = p - a.left - j, sinks = a.sinks - j;
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int c = kt * 32 + acc_row(r);
+                    if (c > most || (c < least && c >= sinks)) s[kt][r] = -INFINITY;
+                }
+        }
+        float top = m;
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) top = __builtin_fmaxf(top, s[kt][r]);
+        top = both_halves_max(top);
+        if (__ballot(top != m)) {  // else no lane's maximum grew
+            const float alpha = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - top);
+            m = top;
+            l *= alpha;
+#pragma unroll
+            for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[dt][r] *= alpha;
+        }
+        const float base = m == -INFINITY ? 0.f : m;
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                s[kt][r] = __builtin_amdgcn_exp2f(s[kt][r] - base);
+                l += s[kt][r];
+            }
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+                const V8 pf = rounded<T>(s[kt], w);
+#pragma unroll
+                for (int dt = 0; dt < ND; ++dt) o[dt] = att_mfma(column_operand<T, DP>(Vt, kt * 32 + w * 16, dt * 32, lane), pf, o[dt]);
+            }
+        // what was taken out reaches the queries that see it
+        if (edge && (bad_now[0] | bad_now[1]))
+            add_nonfinite<T, ND>(o, bad_now, vb, ldv, j0, a.dim, half, [&](int at) { return at <= p + a.right && (at >= p - a.left || at < a.sinks); });
+    }
+    l = both_halves_sum(l);
+    const bool valid = l32 < my_rows;
+    if (t.slot >= 0) {
+        const int64_t at = ((int64_t)t.slot * a.heads + h) * (NW * 32) + wave * 32 + l32;
+        if (valid) {
+#pragma unroll
+            for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    f32x4 x;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[i] = o[dt][4 * c + i];
+                    *reinterpret_cast<f32x4 *>(part_o + at * DP + dt * 32 + 8 * c + 4 * half) = x;
+                }
+            if (half == 0) part_ml[at] = make_float2(m, l);
+        }
+        return;
+    }
+    if (valid && half == 0 && lse) lse[(int64_t)h * Tq + my_row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * LN2;
+    store_columns<T, ND>(o, l == 0.f ? 0.f : 1.f / l, out + (int64_t)my_row * ldo + h * a.dim, valid, a.dim, lane);
+}
+
+// The parts of split rows: m the largest, l and O summed under it in the parts' order.  A thread has eight elements of one row of one head.
+template <class T>
+__global__ __launch_bounds__(256) void join_kernel(const AttentionJoin *__restrict__ joins, int heads, int dim, int DP, int block_rows, const float *__restrict__ part_o,
+                                                   const float2 *__restrict__ part_ml, T *__restrict__ out, int64_t ldo, float *__restrict__ lse, int64_t Tq)
+{
+    const AttentionJoin jn = joins[blockIdx.x];
+    const int h = blockIdx.y, chunks = dim / 8;
+    for (int i = threadIdx.x; i < jn.rows * chunks; i += 256) {
+        const int row = i / chunks, c = i % chunks;
+        auto at = [&](int s) { return ((int64_t)(jn.slot0 + s) * heads + h) * block_rows + row; };
+        float m = -INFINITY;
+        for (int s = 0; s < jn.slots; ++s) {
+            const float ms = part_ml[at(s)].x;
+            if (!(ms <= m)) m = ms;  // NaN stays
+        }
+        float l = 0.f;
+        f32x8 o = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        for (int s = 0; s < jn.slots; ++s) {
+            const float2 ml = part_ml[at(s)];
+            const float w = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - m);
+            l = fmaf(w, ml.y, l);
+            const f32x4 *p = reinterpret_cast<const f32x4 *>(part_o + at(s) * DP + c * 8);
+            const f32x4 x = p[0], y = p[1];
+            if (ml.x != -INFINITY || ml.y != 0.f) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    o[e] = fmaf(w, x[e], o[e]);
+                    o[4 + e] = fmaf(w, y[e], o[4 + e]);
+                }
+            }
+        }
+        const float factor = l == 0.f ? 0.f : 1.f / l;
+        Raw8<T> r;
+        r.round(o * factor);
+        r.store(out + (int64_t)(jn.row0 + row) * ldo + h * dim + c * 8, 8);
+        if (c == 0 && lse) lse[(int64_t)h * Tq + jn.row0 + row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * LN2;
+    }
+}
+
+// ------------------------------------------------------------------ host
+template <class F>
+int with_type16(int dtype, F f)
+{
+    return dtype == LEANN_BF16 ? f((bf16_t *)nullptr) : f((f16_t *)nullptr);
+}
+template <class F>
+int with_dim(int dim, F f)
+{
+    if (dim <= 32) return f(std::integral_constant<int, 32>());
+    if (dim <= 64) return f(std::integral_constant<int, 64>());
+    return f(std::integral_constant<int, 128>());
+}
+
+size_t att_up256(size_t v) { return (v + 255) & ~(size_t)255; }
+
+// A forward block's table and tiles; the largest table with the largest tiles is 65 + 9 KB.
+template <class T, int DP, int NW, bool BIAS>
+int launch_attend(leann_ctx *ctx, const leann_attention_plan *p, const AttentionShape &a, const T *q, int64_t ldq, const T *k, int64_t ldk, const T *v, int64_t ldv,
+                  const float *bias, T *out, int64_t ldo, float *lse, float *part_o, float2 *part_ml)
+{
+    const int smem = AttendCfg<DP, NW>::FIXED + (BIAS ? (2 * p->distance + 1 + 2 * ATT_EXT) * 4 : 0);
+    hipLaunchKernelGGL((attend_kernel<T, DP, NW, BIAS>), dim3(p->n_items), dim3(NW * 64), smem, ctx->stream, p->items, p->tiles, a, q, ldq, k, ldk, v, ldv, bias,
+                       p->bucket_of, out, ldo, lse, p->Tq, part_o, part_ml);
+    if (p->n_joins)
+        hipLaunchKernelGGL(join_kernel<T>, dim3(p->n_joins, p->heads), dim3(256), 0, ctx->stream, p->joins, p->heads, p->dim, DP, NW * 32, part_o, part_ml, out, ldo, lse,
+                           p->Tq);
+    return att_launched("leann_attention");
+}
+
+int make_plan(leann_ctx *ctx, const int32_t *q_rows, const int32_t *k_rows, const int32_t *first, int n, const AttentionRules &r, const int32_t *bucket_of,
+              int distance, leann_attention_plan *p)
+{
+    std::vector<int32_t> zeros;
+    if (!first) {
+        zeros.assign(std::max(1, n), 0);
+        first = zeros.data();
+    }
+    int64_t longest = 0, furthest = 1;
+    for (int s = 0; s < n; ++s) {
+        longest = std::max<int64_t>(longest, q_rows[s]);
+        p->Tq += q_rows[s];
+        p->Tk += k_rows[s];
+        if (q_rows[s] && k_rows[s]) furthest = std::max<int64_t>({furthest, (int64_t)first[s] + q_rows[s] - 1, (int64_t)k_rows[s] - 1 - first[s]});
+    }
+    // 32 queries per block where no sequence has more: the other wavefronts would only load.  128 where they share the keys' tiles.
+    p->query_waves = longest <= 32 ? 1 : 4;
+    std::vector<AttentionTile> tiles, grad_tiles, key_tiles;
+    std::vector<int32_t> of, grad_of, key_of;
+    std::vector<AttentionJoin> joins, none;
+    att_make_tiles(r, n, q_rows, k_rows, first, false, p->query_waves * 32, 0, tiles, of, joins);
+    // Keys are split where there are fewer than two blocks per compute unit, into parts that make four, of four tiles at least: each costs a block's start and its
+    // sums' way through memory.
+    if ((int64_t)tiles.size() * p->heads < 2 * ctx->num_cus) {
+        int64_t work = 0, most = 0;
+        for (const AttentionTile &t : tiles) {
+            work += t.end - t.begin;
+            most = std::max<int64_t>(most, t.end - t.begin);
+        }
+        const int64_t split = std::max<int64_t>(4, (work * p->heads + 4 * ctx->num_cus - 1) / (4 * ctx->num_cus));
+        if (2 * most > 3 * split) {
+            tiles.clear();
+            att_make_tiles(r, n, q_rows, k_rows, first, false, p->query_waves * 32, (int)split, tiles, of, joins);
+        }
+    }
+    for (const AttentionJoin &j : joins) p->n_slots += j.slots;
+    att_make_tiles(r, n, q_rows, k_rows, first, false, 128, 0, grad_tiles, grad_of, none);
+    att_make_tiles(r, n, q_rows, k_rows, first, true, 128, 0, key_tiles, key_of, none);
+    for (int s = 0; s < n; ++s) {
+        for (int t = grad_of[s]; t < grad_of[s + 1]; ++t) grad_tiles[t].peer0 = key_of[s], grad_tiles[t].peers = key_of[s + 1] - key_of[s];
+        for (int t = key_of[s]; t < key_of[s + 1]; ++t) key_tiles[t].peer0 = grad_of[s], key_tiles[t].peers = grad_of[s + 1] - grad_of[s];
+    }
+    const int share = p->heads / p->kv_heads;
+    const std::vector<AttentionItem> items = att_order(tiles, of, p->heads, share), grad_items = att_order(grad_tiles, grad_of, p->heads, share),
+                                     key_items = att_order(key_tiles, key_of, p->kv_heads, 1);
+    if (std::max({items.size(), grad_items.size(), key_items.size(), joins.size()}) > ((size_t)1 << 24) - 1) {
+        leann_set_error("leann_attention_create: sequences of this number and length are not covered (more than 2^24 - 1 workgroups in a launch)");
+        return LEANN_ESHAPE;
+    }
+    p->n_items = (int32_t)items.size();
+    p->n_grad_items = (int32_t)grad_items.size();
+    p->n_key_items = (int32_t)key_items.size();
+    p->n_joins = (int32_t)joins.size();
+    p->n_grad_tiles = (int32_t)grad_tiles.size();
+    p->n_key_tiles = (int32_t)key_tiles.size();
+    std::vector<int32_t> buckets;
+    if (bucket_of) {  // no longer than the sequences
+        p->distance = (int32_t)std::min<int64_t>(distance, furthest);
+        buckets.assign(bucket_of + distance - p->distance, bucket_of + distance + p->distance + 1);
+    }
+    std::vector<char> image;
+    auto put = [&](const auto &v) {
+        const size_t at = att_up256(image.size()), bytes = v.size() * sizeof(v[0]);
+        image.resize(at + bytes);
+        if (bytes) memcpy(image.data() + at, v.data(), bytes);
+        return at;
+    };
+    const size_t at[8] = {put(tiles), put(grad_tiles), put(key_tiles), put(items), put(grad_items), put(key_items), put(joins), put(buckets)};
+    LEANN_TRY(ctx->reserve(p->mem, std::max<size_t>(image.size(), 1)));
+    if (!image.empty()) LEANN_HIP(hipMemcpyAsync(p->mem.p, image.data(), image.size(), hipMemcpyHostToDevice, ctx->stream));
+    LEANN_HIP(hipStreamSynchronize(ctx->stream));
+    const char *base = (const char *)p->mem.p;
+    p->tiles = (const AttentionTile *)(base + at[0]);
+    p->grad_tiles = (const AttentionTile *)(base + at[1]);
+    p->key_tiles = (const AttentionTile *)(base + at[2]);
+    p->items = (const AttentionItem *)(base + at[3]);
+    p->grad_items = (const AttentionItem *)(base + at[4]);
+    p->key_items = (const AttentionItem *)(base + at[5]);
+    p->joins = (const AttentionJoin *)(base + at[6]);
+    p->bucket_of = (const int32_t *)(base + at[7]);
+    return LEANN_OK;
+}
+
+template <class T, int DP>
+int allow_attend()
+{
+    for (const void *f : {(const void *)attend_kernel<T, DP, 1, false>, (const void *)attend_kernel<T, DP, 1, true>, (const void *)attend_kernel<T, DP, 4, false>,
+                          (const void *)attend_kernel<T, DP, 4, true>})
+        LEANN_HIP(hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, AttendCfg<DP, 1>::FIXED + (2 * ATT_MOST_DISTANCE + 1 + 2 * ATT_EXT) * 4));
+    return LEANN_OK;
+}
+
+}  // namespace
+
+int att_launched(const char *call)
+{
+    const hipError_t e = hipGetLastError();
+    if (e == hipSuccess) return LEANN_OK;
+    leann_set_error("%s: launch failed: %s", call, hipGetErrorString(e));
+    return LEANN_EDEVICE;
+}
+
+int att_check_call(const char *call, const leann_ctx *ctx, const leann_attention_plan *plan, int dtype, float scale, const float *bias_dev)
+{
+    if (!ctx || !plan || (dtype != LEANN_BF16 && dtype != LEANN_F16)) {
+        leann_set_error("%s: null context or plan, or a type other than bf16 and f16", call);
+        return LEANN_EINVAL;
+    }
+    if (plan->device != ctx->device) {
+        leann_set_error("%s: the plan belongs to another device", call);
+        return LEANN_EINVAL;
+    }
+    if (!(fabsf(scale) < INFINITY) || !bias_dev != !plan->buckets) {
+        leann_set_error("%s: scale is not finite, or there is a bias without buckets or buckets without a bias", call);
+        return LEANN_EINVAL;
+    }
+    return LEANN_OK;
+}
+
+int att_check_rows(const char *call, const char *what, const void *p, int64_t ld, int64_t cols)
+{
+    if (!p || ((uintptr_t)p & 15)) {
+        leann_set_error("%s: %s is null or not aligned to 16 bytes", call, what);
+        return LEANN_EINVAL;
+    }
+    if (ld < cols || ld % 8) {
+        leann_set_error("%s: rows of %s are %lld elements apart, need at least %lld and a multiple of 8", call, what, (long long)ld, (long long)cols);
+        return LEANN_ESHAPE;
+    }
+    return LEANN_OK;
+}
+
+int att_check_apart(const char *call, const AttentionMatrix &a, const AttentionMatrix &b)
+{
+    if (!att_overlap((uint64_t)a.p, a.ld, a.cols, a.rows, (uint64_t)b.p, b.ld, b.cols, b.rows, 2)) return LEANN_OK;
+    leann_set_error("%s: %s overlaps %s", call, a.name, b.name);
+    return LEANN_EINVAL;
+}
+
+AttentionShape att_shape(const leann_attention_plan *p, float scale)
+{
+    return AttentionShape{p->heads, p->heads / p->kv_heads, p->dim, p->left, p->right, p->sinks, p->distance, scale};
+}
+
+int attention_init_device()
+{
+    LEANN_TRY((allow_attend<bf16_t, 32>()));
+    LEANN_TRY((allow_attend<bf16_t, 64>()));
+    LEANN_TRY((allow_attend<bf16_t, 128>()));
+    LEANN_TRY((allow_attend<f16_t, 32>()));
+    LEANN_TRY((allow_attend<f16_t, 64>()));
+    return allow_attend<f16_t, 128>();
+}
+
+extern "C" {
+
+int leann_position_buckets(int32_t buckets, int32_t distance, int both, int32_t *bucket_of_host)
+{
+    static const char *call = "leann_position_buckets";
+    const int half = both ? buckets / 2 : buckets;
+    if (!bucket_of_host || buckets < 2 || (both && buckets % 2) || half < 2 || half > 2048 || distance > ATT_MOST_DISTANCE || distance <= half / 2) {
+        leann_set_error("%s: null output, fewer than two buckets of a direction or more than 2048, an odd number for two, or a distance that is not above half of a direction's or above %d", call,
+                        ATT_MOST_DISTANCE);
+        return LEANN_EINVAL;
+    }
+    att_position_buckets(buckets, distance, both != 0, bucket_of_host);
+    return LEANN_OK;
+}
+
+void leann_attention_free(leann_attention_plan *p)
+{
+    if (!p) return;
+    (void)hipSetDevice(p->device);
+    p->mem.release();
+    delete p;
+}
+
+int leann_attention_create(leann_ctx *ctx, const int32_t *q_rows_host, const int32_t *k_rows_host, const int32_t *first_host, int32_t n_sequences,
+                           const leann_attention_desc *desc, leann_attention_plan **out)
+{
+    static const char *call = "leann_attention_create";
+    if (!ctx || !out || !desc || n_sequences < 0 || (n_sequences > 0 && !q_rows_host)) {
+        leann_set_error("%s: null argument or negative number of sequences", call);
+        return LEANN_EINVAL;
+    }
+    const leann_attention_desc &d = *desc;
+    if (d.left < -1 || d.right < -1 || d.sinks < 0) {
+        leann_set_error("%s: a window below -1 (no limit) or a negative number of first keys", call);
+        return LEANN_EINVAL;
+    }
+    if (d.heads < 1 || d.heads > 1024 || d.kv_heads < 1 || d.heads % d.kv_heads || d.dim < 8 || d.dim > 128 || d.dim % 8) {
+        leann_set_error("%s: %d heads (%d of keys) of size %d are not covered (at most 1024, a multiple of those of keys; a multiple of 8, at most 128)", call, d.heads,
+                        d.kv_heads, d.dim);
+        return LEANN_ESHAPE;
+    }
+    if (!d.bucket_of_host != !d.buckets || !d.bucket_of_host != !d.distance || d.buckets < 0 || d.distance < 0) {
+        leann_set_error("%s: buckets, their distance and their table have to be given together", call);
+        return LEANN_EINVAL;
+    }
+    if (d.buckets > 4096 || d.distance > ATT_MOST_DISTANCE) {
+        leann_set_error("%s: %d buckets to a distance of %d are not covered (at most 4096 and %d)", call, d.buckets, d.distance, ATT_MOST_DISTANCE);
+        return LEANN_ESHAPE;
+    }
+    for (int i = 0; d.bucket_of_host && i <= 2 * d.distance; ++i)
+        if (d.bucket_of_host[i] < 0 || d.bucket_of_host[i] >= d.buckets) {
+            leann_set_error("%s: relative position %d has bucket %d of %d", call, i - d.distance, d.bucket_of_host[i], d.buckets);
+            return LEANN_EINVAL;
+        }
+    const int32_t *k_rows = k_rows_host ? k_rows_host : q_rows_host;
+    int64_t Tq = 0, Tk = 0;
+    constexpr int64_t MOST = (int64_t)1 << 30;  // positions and windows, so that their sums are 32-bit numbers
+    for (int s = 0; s < n_sequences; ++s) {
+        const int64_t f = first_host ? first_host[s] : 0;
+        if (q_rows_host[s] < 0 || k_rows[s] < 0 || f < 0) {
+            leann_set_error("%s: sequence %d has a negative number of queries or keys or a negative first position", call, s);
+            return LEANN_EINVAL;
+        }
+        if (f + q_rows_host[s] >= MOST || k_rows[s] >= MOST) {
+            leann_set_error("%s: sequence %d has positions that are not covered (below 2^30)", call, s);
+            return LEANN_ESHAPE;
+        }
+        Tq += q_rows_host[s];
+        Tk += k_rows[s];
+    }
+    if (Tq > 0x7fffffffll - 256 || Tk > 0x7fffffffll - 256) {
+        leann_set_error("%s: %lld and %lld rows are not covered (below 2^31 - 256)", call, (long long)Tq, (long long)Tk);
+        return LEANN_ESHAPE;
+    }
+    LEANN_HIP(hipSetDevice(ctx->device));
+    leann_attention_plan *p = nullptr;
+    int rc;
+    try {
+        p = new leann_attention_plan();
+        p->device = ctx->device;
+        p->heads = d.heads;
+        p->kv_heads = d.kv_heads;
+        p->dim = d.dim;
+        p->buckets = d.buckets;
+        p->left = d.left < 0 ? (int32_t)MOST : std::min<int32_t>(d.left, (int32_t)MOST);
+        p->right = d.right < 0 ? (int32_t)MOST : std::min<int32_t>(d.right, (int32_t)MOST);
+        p->sinks = std::min<int32_t>(d.sinks, (int32_t)MOST);
+        rc = make_plan(ctx, q_rows_host, k_rows, first_host, n_sequences, AttentionRules{p->left, p->right, p->sinks}, d.bucket_of_host, d.distance, p);
+    } catch (const std::exception &) {
+        leann_set_error("%s: no host memory", call);
+        rc = LEANN_ENOMEM;
+    }
+    if (rc != LEANN_OK) {
+        leann_attention_free(p);
+        return rc;
+    }
+    *out = p;
+    return LEANN_OK;
+}
+
+int leann_attention(leann_ctx *ctx, const leann_attention_plan *plan, const void *q_dev, int64_t ldq, const void *k_dev, int64_t ldk, const void *v_dev, int64_t ldv,
+                    int dtype, float scale, const float *bias_dev, void *out_dev, int64_t ldo, float *lse_dev)
+{
+    static const char *call = "leann_attention";
+    LEANN_TRY(att_check_call(call, ctx, plan, dtype, scale, bias_dev));
+    if (plan->Tq == 0) return LEANN_OK;
+    const int64_t nq = (int64_t)plan->heads * plan->dim, nk = (int64_t)plan->kv_heads * plan->dim;
+    LEANN_TRY(att_check_rows(call, "q", q_dev, ldq, nq));
+    LEANN_TRY(att_check_rows(call, "out", out_dev, ldo, nq));
+    if (plan->Tk > 0) {
+        LEANN_TRY(att_check_rows(call, "k", k_dev, ldk, nk));
+        LEANN_TRY(att_check_rows(call, "v", v_dev, ldv, nk));
+    }
+    const AttentionMatrix o = {"out", out_dev, ldo, nq, plan->Tq};
+    LEANN_TRY(att_check_apart(call, o, AttentionMatrix{"q", q_dev, ldq, nq, plan->Tq}));
+    LEANN_TRY(att_check_apart(call, o, AttentionMatrix{"k", k_dev, ldk, nk, plan->Tk}));
+    LEANN_TRY(att_check_apart(call, o, AttentionMatrix{"v", v_dev, ldv, nk, plan->Tk}));
+    LEANN_HIP(hipSetDevice(ctx->device));
+    const AttentionShape a = att_shape(plan, scale);
+    std::unique_lock<std::mutex> turn(ctx->op_work_mutex, std::defer_lock);
+    return with_dim(plan->dim, [&](auto dp) {
+        constexpr int DP = decltype(dp)::value;
+        float *part_o = nullptr;
+        float2 *part_ml = nullptr;
+        if (plan->n_slots) {
+            const size_t rows = (size_t)plan->n_slots * plan->heads * plan->query_waves * 32;
+            turn.lock();
+            LEANN_TRY(ctx->reserve(ctx->op_work, rows * (DP * sizeof(float) + sizeof(float2))));
+            part_o = (float *)ctx->op_work.p;
+            part_ml = (float2 *)(part_o + rows * DP);
+        }
+        return with_type16(dtype, [&](auto *type) {
+            typedef std::remove_pointer_t<decltype(type)> T;
+            auto go = [&](auto waves, auto with_bias) {
+                return launch_attend<T, DP, decltype(waves)::value, decltype(with_bias)::value>(ctx, plan, a, (const T *)q_dev, ldq, (const T *)k_dev, ldk, (const T *)v_dev,
+                                                                                               ldv, bias_dev, (T *)out_dev, ldo, lse_dev, part_o, part_ml);
+            };
+            using One = std::integral_constant<int, 1>;
+            using Four = std::integral_constant<int, 4>;
+            if (plan->query_waves == 1) return bias_dev ? go(One(), std::true_type()) : go(One(), std::false_type());
+            return bias_dev ? go(Four(), std::true_type()) : go(Four(), std::false_type());
+        });
+    });
+}
+
+}  // extern "C"

@@ -132,6 +132,7 @@ int enc_ln_blocks_per_cu(int d, int *out);  // resident blocks of the LayerNorm 
 int pq_init_device();
 int search_init_device();
 int adapter_init_device();
+int attention_init_device();
 
 // ---- encoder.hip
 // Embeds the chunks named by ids_dev[0..n) (NULL: first_id .. first_id+n) into out[n][d] (fp32), in passes of at
