@@ -461,6 +461,15 @@ void leann_attention_free(leann_attention_plan *plan);
 int leann_attention(leann_ctx *ctx, const leann_attention_plan *plan, const void *q_dev, int64_t ldq, const void *k_dev, int64_t ldk, const void *v_dev, int64_t ldv, int dtype,
                     float scale, const float *bias_dev, void *out_dev, int64_t ldo, float *lse_dev);
 
+/* Gradients from dout, the gradient of out, and what the forward call left in out and lse, under the same scale and bias: dq[Tq][heads * dim], dk and dv[Tk][kv_heads * dim] (the sums
+ * over the heads that share a key head), dbias fp32[buckets][heads] (NULL: not wanted).  Written, not added to; dq, dk and dv may be slices of one matrix, and must not overlap
+ * each other or an input (LEANN_EINVAL).  No atomics in memory: the bits repeat, and a sequence's dq, dk and dv do not depend on the others.
+ * A query or key that is infinite or NaN makes NaN of the gradients of the keys or queries that it meets and of no others.
+ * Workspace: 4 bytes per query and head; with dbias 4 (2 distance + 1) more per head and 128 queries (of every sequence), distance no more than the sequences' longest. */
+int leann_attention_backward(leann_ctx *ctx, const leann_attention_plan *plan, const void *dout_dev, int64_t ldd, const void *q_dev, int64_t ldq, const void *k_dev, int64_t ldk,
+                             const void *v_dev, int64_t ldv, const void *out_dev, int64_t ldo, const float *lse_dev, int dtype, float scale, const float *bias_dev, void *dq_dev,
+                             int64_t lddq, void *dk_dev, int64_t lddk, void *dv_dev, int64_t lddv, float *dbias_dev);
+
 #ifdef __cplusplus
 }
 #endif

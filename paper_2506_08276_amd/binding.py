@@ -25,7 +25,8 @@ EXPORTS = ["leann_last_error", "leann_create", "leann_destroy", "leann_embed", "
            "leann_dropout", "leann_layernorm", "leann_layernorm_backward",
            "leann_projection_create", "leann_projection_free", "leann_adapter_rows_create", "leann_adapter_rows_free",
            "leann_adapter_project", "leann_adapter_project_backward",
-           "leann_position_buckets", "leann_attention_create", "leann_attention_free", "leann_attention"]
+           "leann_position_buckets", "leann_attention_create", "leann_attention_free", "leann_attention",
+           "leann_attention_backward"]
 PROF_KINDS = ["gemm_qkv", "gemm_o", "gemm_ffn1", "gemm_ffn2", "attention", "layernorm", "enc_other", "traverse",
               "collect", "score_insert", "lut", "adc"]
 
@@ -94,7 +95,8 @@ def load_library(path=LIB_PATH):
                 "leann_adapter_project_backward": [V, V, V, V, N, V, N, V, V, V, V, N, V, V],
                 "leann_position_buckets": [I, I, I, V],
                 "leann_attention_create": [V, V, V, V, I, V, V], "leann_attention_free": [V],
-                "leann_attention": [V, V, V, N, V, N, V, N, I, F, V, V, N, V]}.items():
+                "leann_attention": [V, V, V, N, V, N, V, N, I, F, V, V, N, V],
+                "leann_attention_backward": [V, V, V, N, V, N, V, N, V, N, V, N, V, I, F, V, V, N, V, N, V, N, V]}.items():
             getattr(lib, name).argtypes = args
         _lib = lib
     return _lib
@@ -576,3 +578,22 @@ def leann_attention(ctx, plan, q, k, v, scale=None, bias=None, keep=False, out=N
     scale = plan.dim ** -0.5 if scale is None else scale
     _check(load_library().leann_attention(ctx, plan, qp, ldq, kp, ldk, vp, ldv, _dtype(q), scale, bp, op, ldo, lse.data_ptr() if keep else None))
     return (out, lse) if keep else out
+
+
+def leann_attention_backward(ctx, plan, dout, q, k, v, out, lse, scale=None, bias=None, dq=None, dk=None, dv=None, need_bias=True):
+    """(dq, dk, dv, dbias) from the gradient of leann_attention's output, its inputs and what it kept; dbias None without a bias or need_bias.  dq, dk, dv may be
+    given, as slices of one projection's gradient, say."""
+    (qp, ldq, kp, ldk, vp, ldv), bp = _attention_inputs(plan, q, k, v, bias)
+    assert dout.shape == out.shape == q.shape and dout.dtype == out.dtype == q.dtype, "dout, out: shape or type differs"
+    assert lse.is_cuda and lse.is_contiguous() and lse.shape == (plan.heads, plan.Tq) and lse.dtype == torch.float32, "lse: need float32 [heads][Tq]"
+    dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) if d is None else d for d, t in ((dq, q), (dk, k), (dv, v)))
+    for d, t in ((dq, q), (dk, k), (dv, v)):
+        assert d.shape == t.shape and d.dtype == t.dtype, "dq, dk, dv: shape or type differs"
+    dbias = None
+    if bias is not None and need_bias:  # rows that no relative position has stay zero
+        dbias = torch.empty_like(bias) if bias.shape[0] == plan.buckets else torch.zeros_like(bias)
+    (gp, ldd), (op, ldo), (dqp, lddq), (dkp, lddk), (dvp, lddv) = _rows(dout, "dout"), _rows(out, "out"), _rows(dq, "dq"), _rows(dk, "dk"), _rows(dv, "dv")
+    scale = plan.dim ** -0.5 if scale is None else scale
+    _check(load_library().leann_attention_backward(ctx, plan, gp, ldd, qp, ldq, kp, ldk, vp, ldv, op, ldo, lse.data_ptr(), _dtype(q), scale, bp, dqp, lddq,
+                                                   dkp, lddk, dvp, lddv, None if dbias is None else dbias.data_ptr()))
+    return dq, dk, dv, dbias

@@ -14,7 +14,7 @@ struct leann_attention_plan {
     int32_t left = -1, right = -1, sinks = 0;  // as the kernels take them: no limit is a bound behind every position
     int32_t distance = 0, buckets = 0;         // distance: of the table below, no longer than the sequences make it
     int32_t query_waves = 0;                   // wavefronts of a forward block, 32 queries each
-    int32_t n_items = 0, n_grad_items = 0, n_key_items = 0, n_joins = 0, n_slots = 0, n_grad_tiles = 0, n_key_tiles = 0;
+    int32_t n_items = 0, n_grad_items = 0, n_key_items = 0, n_joins = 0, n_slots = 0, n_grad_tiles = 0;
     DevBuf mem;
     const AttentionTile *tiles = nullptr, *grad_tiles = nullptr, *key_tiles = nullptr;  // of queries, for the gradient of queries, of keys
     const AttentionItem *items = nullptr, *grad_items = nullptr, *key_items = nullptr;

@@ -287,10 +287,6 @@ int make_plan(leann_ctx *ctx, const int32_t *q_rows, const int32_t *k_rows, cons
     for (const AttentionJoin &j : joins) p->n_slots += j.slots;
     att_make_tiles(r, n, q_rows, k_rows, first, false, 128, 0, grad_tiles, grad_of, none);
     att_make_tiles(r, n, q_rows, k_rows, first, true, 128, 0, key_tiles, key_of, none);
-    for (int s = 0; s < n; ++s) {
-        for (int t = grad_of[s]; t < grad_of[s + 1]; ++t) grad_tiles[t].peer0 = key_of[s], grad_tiles[t].peers = key_of[s + 1] - key_of[s];
-        for (int t = key_of[s]; t < key_of[s + 1]; ++t) key_tiles[t].peer0 = grad_of[s], key_tiles[t].peers = grad_of[s + 1] - grad_of[s];
-    }
     const int share = p->heads / p->kv_heads;
     const std::vector<AttentionItem> items = att_order(tiles, of, p->heads, share), grad_items = att_order(grad_tiles, grad_of, p->heads, share),
                                      key_items = att_order(key_tiles, key_of, p->kv_heads, 1);
@@ -303,7 +299,6 @@ int make_plan(leann_ctx *ctx, const int32_t *q_rows, const int32_t *k_rows, cons
     p->n_key_items = (int32_t)key_items.size();
     p->n_joins = (int32_t)joins.size();
     p->n_grad_tiles = (int32_t)grad_tiles.size();
-    p->n_key_tiles = (int32_t)key_tiles.size();
     std::vector<int32_t> buckets;
     if (bucket_of) {  // no longer than the sequences
         p->distance = (int32_t)std::min<int64_t>(distance, furthest);

@@ -48,8 +48,7 @@ struct AttentionTile {
     int32_t sink_tiles, first_tile;
     int32_t begin, end;            // of the tiles on the other side, numbered as in AttentionSpan
     int32_t slot;                  // where a part of the keys leaves its sums, -1: it has all keys
-    int32_t peer0, peers;          // the sequence's tiles on the other side
-    int32_t pad[3];
+    int32_t pad[5];
 };
 
 // Rows whose keys were split: the parts' slots.

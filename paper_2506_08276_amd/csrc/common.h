@@ -133,6 +133,7 @@ int pq_init_device();
 int search_init_device();
 int adapter_init_device();
 int attention_init_device();
+int attention_grad_init_device();
 
 // ---- encoder.hip
 // Embeds the chunks named by ids_dev[0..n) (NULL: first_id .. first_id+n) into out[n][d] (fp32), in passes of at

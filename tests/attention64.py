@@ -110,9 +110,9 @@ class Sequences:
                 eds = es * ds.abs() + (self.dim + 4) * 2.0 ** -24 * p * size
                 ep = (es + step) * p
                 erow = eds + step * ds.abs()
-                if step < 2.0 ** -9:  # fp16: P below 2^-14 is off by up to 2^-25; dS is scaled so that 2^14 to 2^15 bounds it: by up to 2^-25 of 2^-14 of its bound
-                    ep = ep + 2.0 ** -25 * see
-                    erow = erow + see * 2.0 ** -38 * 2 * self.dim * dout[rows, cq].double().abs().amax().clamp(min=dout[:, cq].double().abs().amax()) * v.abs().amax()
+                if step < 2.0 ** -9:  # fp16: 2^15 P, off by 2^-25 where that is no normal number; dS likewise, or scaled so that its largest is 2^14 at least
+                    ep = ep + 2.0 ** -40 * see
+                    erow = erow + see * (2.0 ** -40 + 2.0 ** -39 * ds.abs().amax())
                 n = 2.0 ** -24 * (len(q) + len(k))
                 fq[rows, cq] = self.scale * (erow + n * ds.abs()) @ k.abs()
                 fk[keys, ck] += self.scale * (erow + n * ds.abs()).t().contiguous() @ q.abs()
