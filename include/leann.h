@@ -455,8 +455,8 @@ int leann_attention_create(leann_ctx *ctx, const int32_t *q_rows_host, const int
                            const leann_attention_desc *desc, leann_attention_plan **out);
 void leann_attention_free(leann_attention_plan *plan);
 
-/* out[Tq][heads * dim] from q[Tq][heads * dim], k and v[Tk][kv_heads * dim]: bf16 or f16, 16-byte alignment, rows a multiple of 8 elements apart (slices of one projection's output
- * are fine).  bias: fp32[buckets][heads].  lse (NULL, or fp32[heads][Tq]): what the backward pass needs.  out must not overlap q, k or v (LEANN_EINVAL).
+/* out[Tq][heads * dim] from q[Tq][heads * dim], k and v[Tk][kv_heads * dim]: bf16 or f16, 16-byte alignment, rows a multiple of 8 elements apart and at most 2^23 (slices of one
+ * projection's output are fine).  bias: fp32[buckets][heads].  lse (NULL, or fp32[heads][Tq]): what the backward pass needs.  out must not overlap q, k or v (LEANN_EINVAL).
  * Where there are few queries, their keys are split over blocks whose sums are joined: a row's bits may depend on the other sequences' lengths, its value does not. */
 int leann_attention(leann_ctx *ctx, const leann_attention_plan *plan, const void *q_dev, int64_t ldq, const void *k_dev, int64_t ldk, const void *v_dev, int64_t ldv, int dtype,
                     float scale, const float *bias_dev, void *out_dev, int64_t ldo, float *lse_dev);
@@ -465,7 +465,7 @@ int leann_attention(leann_ctx *ctx, const leann_attention_plan *plan, const void
  * over the heads that share a key head), dbias fp32[buckets][heads] (NULL: not wanted).  Written, not added to; dq, dk and dv may be slices of one matrix, and must not overlap
  * each other or an input (LEANN_EINVAL).  No atomics in memory: the bits repeat, and a sequence's dq, dk and dv do not depend on the others.
  * A query or key that is infinite or NaN makes NaN of the gradients of the keys or queries that it meets and of no others.
- * Workspace: 4 bytes per query and head; with dbias 4 (2 distance + 1) more per head and 128 queries (of every sequence), distance no more than the sequences' longest. */
+ * Workspace: 8 bytes per query and head; with dbias 4 (2 distance + 1) more per head and 128 queries (of every sequence), distance no more than the sequences' longest. */
 int leann_attention_backward(leann_ctx *ctx, const leann_attention_plan *plan, const void *dout_dev, int64_t ldd, const void *q_dev, int64_t ldq, const void *k_dev, int64_t ldk,
                              const void *v_dev, int64_t ldv, const void *out_dev, int64_t ldo, const float *lse_dev, int dtype, float scale, const float *bias_dev, void *dq_dev,
                              int64_t lddq, void *dk_dev, int64_t lddk, void *dv_dev, int64_t lddv, float *dbias_dev);

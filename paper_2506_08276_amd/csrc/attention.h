@@ -4,6 +4,7 @@
 #include "rows.h"
 
 constexpr int ATT_MOST_DISTANCE = 1024;
+constexpr int64_t ATT_MOST_LD = (int64_t)1 << 23;  // 64 rows are within a buffer's 2^31 bytes
 constexpr int ATT_EXT = 96;  // a wavefront's 32 rows and 64 of the other side have relative positions in a range of 95
 
 // One batch's sequences: tables on the device, in one allocation.
@@ -76,49 +77,81 @@ __device__ inline int att_swizzle(int row)
     else return (row & 3) << 2 | ((row >> 2) & 3);
 }
 
-// A tile on its way from memory to LDS, NT threads' chunks of it.
-template <class T, int DP, int NT>
-struct TileInFlight {
-    static constexpr int CPR = DP / 8, N = ATT_STEP * CPR / NT;
-    static_assert(N * NT == ATT_STEP * CPR, "whole chunks per thread");
-    u32x4 v[N];
+typedef __attribute__((address_space(3))) void lds_t;
+__device__ inline void lds_request(__amdgpu_buffer_rsrc_t b, uint32_t offset, void *to)  // 16 bytes per lane, to `to` and on in the lanes' order
+{
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(b, (lds_t *)to, 16, (int)offset, 0, 0, 0);
+}
 
-    // rows [row, row + 64) of `base`, of which those from `rows` on are zeros
-    __device__ inline void load(const T *base, int64_t ld, int row, int rows, int dim)
+// Requests for a tile, from memory to LDS without registers: 1 KB each, one of NW wavefronts' share of them.  A lane fetches the chunk that belongs at its place.  Rows behind the
+// sequence's last and columns behind the head's are out of the buffer's bounds and come as zeros.
+template <class T, int DP, int NW>
+struct TileRequests {
+    static constexpr int CPR = DP / 8, RPI = 64 / CPR, N = ATT_STEP / RPI / NW;
+    uint32_t at[N];  // byte offsets in the tile
+
+    __device__ inline void init(int64_t ld, int dim, int wave, int lane)
     {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int c = threadIdx.x + i * NT, r = c / CPR, ch = c % CPR;
-            if (row + r < rows && ch * 8 < dim) v[i] = *reinterpret_cast<const u32x4 *>(base + (int64_t)(row + r) * ld + ch * 8);
-            else v[i] = u32x4{0, 0, 0, 0};
+            const int row = (i * NW + wave) * RPI + lane / CPR, ch = (lane % CPR) ^ att_swizzle<DP>(row);
+            at[i] = ch * 8 < dim ? (uint32_t)(row * ld + ch * 8) * 2 : 0x80000000u;
         }
     }
-    __device__ inline void store(T *lds) const
+    // 64 rows from `base` on, of which `rows` are the sequence's; all arguments are the same in every lane
+    __device__ inline void request(const T *base, int64_t ld, int rows, int dim, T *lds, int wave) const
     {
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<T *>(base), 0, (int)(((min(rows, ATT_STEP) - 1) * ld + dim) * 2), 0x00020000);
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int c = threadIdx.x + i * NT, r = c / CPR, ch = c % CPR;
-            *reinterpret_cast<u32x4 *>(lds + r * DP + ((ch ^ att_swizzle<DP>(r)) << 3)) = v[i];
-        }
+        for (int i = 0; i < N; ++i) lds_request(rsrc, at[i], lds + (i * NW + wave) * 512);
     }
-    // Infinities and NaN become zeros, and their rows' bits are set in bad[2]: a row of the other side that does not see them would get NaN from a product with zero.
-    __device__ inline void take_out_nonfinite(uint32_t *bad)
+};
+
+// Waits until no more than VM of the wavefront's memory requests are on their way, and for its LDS accesses; then for the other wavefronts.  Nothing is moved across.
+template <int VM>
+__device__ inline void wait_for_requests()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt((VM & 15) | ((VM >> 4) << 14) | 0x70);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+__device__ inline void block_barrier()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+// What the lanes of a wavefront wrote to LDS, its other lanes read behind this: the accesses are served in their order.
+__device__ inline void wave_fence()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// Infinities and NaN of an operand.  Where a tile is partly hidden they have to be taken out: a row of the other side that does not see them would get NaN from a product with
+// zero.
+template <class T>
+struct Finite {
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+    u16x2 most = {0, 0};
+    __device__ inline void look(const typename Half8<T>::type &f)
     {
+        const u32x4 v = __builtin_bit_cast(u32x4, f);
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            bool any = false;
+        for (int w = 0; w < 4; ++w) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, v[w] & 0x7fff7fffu));
+    }
+    __device__ inline bool all() const { return !__ballot((most[0] >= Half8<T>::EXPONENT) | (most[1] >= Half8<T>::EXPONENT)); }  // in every lane
+    __device__ static inline void keep(typename Half8<T>::type &f)
+    {
+        u32x4 v = __builtin_bit_cast(u32x4, f);
+        constexpr uint32_t E = Half8<T>::EXPONENT;
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                constexpr uint32_t E = Half8<T>::EXPONENT;
-                const bool lo = (v[i][w] & E) == E, hi = (v[i][w] & E << 16) == E << 16;
-                v[i][w] &= (lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u);
-                any |= lo | hi;
-            }
-            if (any) {
-                const int r = (threadIdx.x + i * NT) / CPR;
-                atomicOr(&bad[r >> 5], 1u << (r & 31));
-            }
-        }
+        for (int w = 0; w < 4; ++w) v[w] &= ((v[w] & E) == E ? 0u : 0xffffu) | ((v[w] & E << 16) == E << 16 ? 0u : 0xffff0000u);
+        f = __builtin_bit_cast(typename Half8<T>::type, v);
     }
 };
 
@@ -145,16 +178,16 @@ __device__ inline typename Half8<T>::type column_operand(const T *lds, int row0,
     return __builtin_bit_cast(typename Half8<T>::type, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-// A lane's operand row from memory: `p` points at the row's head, nullptr for zeros.
+// A lane's operand row from memory: row lane % 32 from `base` on, zeros behind the `rows` that there are.
 template <class T, int DP>
-__device__ inline void load_rows(const T *p, int dim, int lane, typename Half8<T>::type (&f)[DP / 16])
+__device__ inline void load_rows(const T *base, int64_t ld, int rows, int dim, int lane, typename Half8<T>::type (&f)[DP / 16])
 {
+    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<T *>(base), 0, rows > 0 ? (int)(((min(rows, 32) - 1) * ld + dim) * 2) : 0, 0x00020000);
+    const uint32_t from = (uint32_t)((lane & 31) * ld + (lane >> 5) * 8) * 2;
 #pragma unroll
     for (int s = 0; s < DP / 16; ++s) {
-        const int at = s * 16 + (lane >> 5) * 8;
-        u32x4 v = {0, 0, 0, 0};
-        if (p && at < dim) v = *reinterpret_cast<const u32x4 *>(p + at);
-        f[s] = __builtin_bit_cast(typename Half8<T>::type, v);
+        const uint32_t at = s * 16 + (lane >> 5) * 8 < dim ? from + s * 32 : 0x80000000u;
+        f[s] = __builtin_bit_cast(typename Half8<T>::type, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, 0, 0));
     }
 }
 
@@ -202,15 +235,25 @@ __device__ inline void store_columns(const f32x16 (&o)[ND], float factor, T *row
         }
 }
 
-// Adds to a transposed result (see store_columns) the infinities and NaN that were taken out of 64 rows from row j0 on, where the lane's column sees the row.
-template <class T, int ND, class Seen>
-__device__ inline void add_nonfinite(f32x16 (&o)[ND], const uint32_t *bad, const T *base, int64_t ld, int j0, int dim, int half, Seen seen)
+// Goes through `rows` rows of memory from row j0 on and calls f(row number, row) for those that have an infinity or NaN; all lanes together.
+template <class T, class F>
+__device__ inline void for_nonfinite_rows(const T *base, int64_t ld, int j0, int rows, int dim, int lane, F f)
 {
-    for (int i = 0; i < ATT_STEP; ++i) {
-        if (!(bad[i >> 5] >> (i & 31) & 1)) continue;
-        const bool mine = seen(j0 + i);
+    for (int i = 0; i < rows; ++i) {
         const T *row = base + (int64_t)(j0 + i) * ld;
-        int from = 4 * half;
+        bool any = false;
+        for (int d = lane; d < dim; d += 64) any |= !(__builtin_fabsf((float)row[d]) < INFINITY);
+        if (__ballot(any)) f(j0 + i, row);
+    }
+}
+
+// Adds to a transposed result (see store_columns) what was taken out of those rows, where the lane's column sees the row.
+template <class T, int ND, class Seen>
+__device__ inline void add_nonfinite(f32x16 (&o)[ND], const T *base, int64_t ld, int j0, int rows, int dim, int lane, Seen seen)
+{
+    for_nonfinite_rows<T>(base, ld, j0, min(rows, ATT_STEP), dim, lane, [&](int j, const T *row) {
+        const bool mine = seen(j);
+        int from = 4 * (lane >> 5);
         asm volatile("" : "+v"(from));  // else the tests below leave the loop, and take scalar registers from the common path
 #pragma unroll
         for (int dt = 0; dt < ND; ++dt)
@@ -224,7 +267,7 @@ __device__ inline void add_nonfinite(f32x16 (&o)[ND], const uint32_t *bad, const
                     if (mine && !(__builtin_fabsf(x) < INFINITY)) o[dt][4 * c + e] += x;
                 }
             }
-    }
+    });
 }
 
 // The bias of one head by relative position, times log2 e: [2 distance + 1 + 2 ATT_EXT], the ends repeated.
@@ -237,16 +280,16 @@ __device__ inline void make_bias(float *table, const float *bias, const int32_t 
     }
 }
 
-// What the 32 rows (or queries) at positions from p of a wavefront see of 64 keys from key j on.
+// What `queries` queries at positions from p on see of `keys` keys from key j on: nothing, or all of them.
 struct Sight {
     bool none, all;
 };
-__device__ inline Sight sight(const AttentionShape &a, int p, int queries, int j, int keys_left)
+__device__ inline Sight sight(const AttentionShape &a, int p, int queries, int j, int keys)
 {
     // the first query sees the fewest keys ahead, the last one the fewest behind
-    const int last = p + queries - 1, end = j + min(ATT_STEP, keys_left) - 1;
-    const bool none = queries <= 0 || j > last + a.right || (end < p - a.left && j >= a.sinks);
-    const bool all = keys_left >= ATT_STEP && end <= p + a.right && (j >= last - a.left || end < a.sinks);
+    const int last = p + queries - 1, end = j + keys - 1;
+    const bool none = queries <= 0 || keys <= 0 || j > last + a.right || (end < p - a.left && j >= a.sinks);
+    const bool all = end <= p + a.right && (j >= last - a.left || end < a.sinks);
     return {none, all};
 }
 

@@ -14,15 +14,15 @@ namespace {
 // run over its own registers, the other half of the keys is lane ^ 32's.  One pass: s = scale q.k + bias in units of log 2, m the largest so far, l = sum 2^(s - m),
 // O = sum 2^(s - m) v, l and O scaled when m grows.  P^T, rounded to the inputs' type (an error of half a step in each term, as the inputs themselves have), is the
 // other operand of O^T = V^T P^T without leaving its registers, see column_operand.
-// K and V tiles go through registers to LDS, two buffers, the next tile's loads before this one's products.
+// K and V tiles go from memory to LDS without registers, STAGES - 1 tiles ahead.
 template <int DP, int NW>
 struct AttendCfg {
-    static constexpr int NT = NW * 64, TILE = ATT_STEP * DP;
-    static constexpr int FIXED = 4 * TILE * 2 + 64;  // bytes; the bias's table follows
+    static constexpr int STAGES = NW == 1 || DP == 128 ? 2 : 3, TILE = ATT_STEP * DP;
+    static constexpr int FIXED = STAGES * 2 * TILE * 2;  // bytes; the bias's table follows
 };
 
 template <class T, int DP, int NW, bool BIAS>
-__global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attend_kernel(const AttentionItem *__restrict__ items, const AttentionTile *__restrict__ tiles, AttentionShape a,
+__global__ __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : 1) void attend_kernel(const AttentionItem *__restrict__ items, const AttentionTile *__restrict__ tiles, AttentionShape a,
                                                                          const T *__restrict__ q, int64_t ldq, const T *__restrict__ k, int64_t ldk,
                                                                          const T *__restrict__ v, int64_t ldv, const float *__restrict__ bias,
                                                                          const int32_t *__restrict__ bucket_of, T *__restrict__ out, int64_t ldo,
@@ -30,10 +30,10 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attend_kernel(const 
                                                                          float2 *__restrict__ part_ml)
 {
     typedef typename Half8<T>::type V8;
-    constexpr int NT = AttendCfg<DP, NW>::NT, TILE = AttendCfg<DP, NW>::TILE, ND = DP / 32, NS = DP / 16;
+    typedef TileRequests<T, DP, NW> Requests;
+    constexpr int STAGES = AttendCfg<DP, NW>::STAGES, TILE = AttendCfg<DP, NW>::TILE, ND = DP / 32, NS = DP / 16;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    T *Ks = reinterpret_cast<T *>(smem), *Vs = Ks + 2 * TILE;
-    uint32_t *bad = reinterpret_cast<uint32_t *>(smem + 4 * TILE * 2);  // [3][2]
+    T *Ks = reinterpret_cast<T *>(smem), *Vs = Ks + STAGES * TILE;
     float *table = reinterpret_cast<float *>(smem + AttendCfg<DP, NW>::FIXED);
 
     const AttentionItem item = items[blockIdx.x];
@@ -42,22 +42,24 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attend_kernel(const 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, l32 = lane & 31;
     const int h = item.head, g = h / a.share;
     const T *kb = k + (int64_t)t.other0 * ldk + g * a.dim, *vb = v + (int64_t)t.other0 * ldv + g * a.dim;
-    auto tile_at = [&](int u) { return u < t.sink_tiles ? u : t.first_tile + u - t.sink_tiles; };
+    auto key_of = [&](int u) { return (u < t.sink_tiles ? u : t.first_tile + u - t.sink_tiles) * ATT_STEP; };
 
-    TileInFlight<T, DP, NT> kin, vin;
-    auto fetch = [&](int u) {
-        const int row = tile_at(u) * ATT_STEP;
-        kin.load(kb, ldk, row, t.others, a.dim);
-        vin.load(vb, ldv, row, t.others, a.dim);
+    Requests kr, vr;
+    kr.init(ldk, a.dim, wave, lane);
+    vr.init(ldv, a.dim, wave, lane);
+    auto request = [&](int u, int stage) {
+        const int j = key_of(u);
+        kr.request(kb + j * ldk, ldk, t.others - j, a.dim, Ks + stage * TILE, wave);
+        vr.request(vb + j * ldv, ldv, t.others - j, a.dim, Vs + stage * TILE, wave);
     };
-    if (t.begin < t.end) fetch(t.begin);
     const int my_rows = min(32, t.rows - wave * 32), p0 = t.at + wave * 32;  // of this wavefront
     const int my_row = t.row0 + wave * 32 + l32;
     V8 qf[NS];
-    load_rows<T, DP>(l32 < my_rows ? q + (int64_t)my_row * ldq + h * a.dim : nullptr, a.dim, lane, qf);
+    load_rows<T, DP>(q + (int64_t)(t.row0 + wave * 32) * ldq + h * a.dim, ldq, my_rows, a.dim, lane, qf);
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i)
+        if (t.begin + i < t.end) request(t.begin + i, i);
     if (BIAS) make_bias(table, bias, bucket_of, a, h);
-    if (tid < 6) bad[tid] = 0;
-    __syncthreads();
 
     f32x16 o[ND];
 #pragma unroll
@@ -68,18 +70,17 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attend_kernel(const 
     const float scale2 = a.scale * LOG2E;
     const int p = p0 + l32;
 
-    for (int u = t.begin, n = 0; u < t.end; ++u, ++n) {
-        const int j0 = tile_at(u) * ATT_STEP, buf = n & 1;
-        uint32_t *bad_now = bad + 2 * (n % 3);
-        const T *Kt = Ks + buf * TILE, *Vt = Vs + buf * TILE;
-        const bool edge = !sight(a, t.at, t.rows, j0, t.others - j0).all;
-        if (edge) vin.take_out_nonfinite(bad_now);
-        kin.store(Ks + buf * TILE);
-        vin.store(Vs + buf * TILE);
-        __syncthreads();
-        if (tid < 2) bad[2 * ((n + 2) % 3) + tid] = 0;  // read before this barrier, set again behind the next
-        if (u + 1 < t.end) fetch(u + 1);
-        const Sight see = sight(a, p0, my_rows, j0, t.others - j0);
+    int stage = 0;
+    for (int u = t.begin; u < t.end; ++u) {
+        const int j0 = key_of(u);
+        const T *Kt = Ks + stage * TILE, *Vt = Vs + stage * TILE;
+        if (STAGES > 2 && u + 1 < t.end) wait_for_requests<2 * Requests::N>();
+        else wait_for_requests<0>();
+        block_barrier();  // this tile is there, and the stage of the last one has been read
+        if (u + STAGES - 1 < t.end) request(u + STAGES - 1, stage == 0 ? STAGES - 1 : stage - 1);
+        stage = stage == STAGES - 1 ? 0 : stage + 1;
+        const int keys = min(ATT_STEP, t.others - j0);
+        const Sight see = sight(a, p0, my_rows, j0, keys);
         if (see.none) continue;
 
         f32x16 s[2];
@@ -90,6 +91,11 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attend_kernel(const 
 #pragma unroll
             for (int i = 0; i < NS; ++i) s[kt] = att_mfma(row_operand<T, DP>(Kt, kt * 32, i, lane), qf[i], s[kt]);
         }
+        V8 vf[2][ND];  // of the first 32 keys, on their way while the scores become weights
+#pragma unroll
+        for (int w = 0; w < 2; ++w)
+#pragma unroll
+            for (int dt = 0; dt < ND; ++dt) vf[w][dt] = column_operand<T, DP>(Vt, w * 16, dt * 32, lane);
         // register r of tile kt is key j0 + 32 kt + 4 half + acc_row(r)
         const int j = j0 + 4 * half;
         if (BIAS) {
@@ -120,8 +126,14 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attend_kernel(const 
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const int c = kt * 32 + acc_row(r);
-                    if (c > most || (c < least && c >= sinks)) s[kt][r] = -INFINITY;
+                    s[kt][r] = (c > most) | ((c < least) & (c >= sinks)) ? -INFINITY : s[kt][r];
                 }
+        } else if (keys < ATT_STEP) {
+            const int most = keys - 1 - 4 * half;
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[kt][r] = kt * 32 + acc_row(r) > most ? -INFINITY : s[kt][r];
         }
         float top = m;
 #pragma unroll
@@ -146,17 +158,35 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attend_kernel(const 
                 s[kt][r] = __builtin_amdgcn_exp2f(s[kt][r] - base);
                 l += s[kt][r];
             }
+        bool taken_out = false;
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt)
+        for (int kt = 0; kt < 2; ++kt) {
+            if (!see.all) {
+                Finite<T> f;
+#pragma unroll
+                for (int w = 0; w < 2; ++w)
+#pragma unroll
+                    for (int dt = 0; dt < ND; ++dt) f.look(vf[w][dt]);
+                if (!f.all()) {
+                    taken_out = true;
+#pragma unroll
+                    for (int w = 0; w < 2; ++w)
+#pragma unroll
+                        for (int dt = 0; dt < ND; ++dt) f.keep(vf[w][dt]);
+                }
+            }
 #pragma unroll
             for (int w = 0; w < 2; ++w) {
                 const V8 pf = rounded<T>(s[kt], w);
 #pragma unroll
-                for (int dt = 0; dt < ND; ++dt) o[dt] = att_mfma(column_operand<T, DP>(Vt, kt * 32 + w * 16, dt * 32, lane), pf, o[dt]);
+                for (int dt = 0; dt < ND; ++dt) {
+                    o[dt] = att_mfma(vf[w][dt], pf, o[dt]);
+                    if (kt == 0) vf[w][dt] = column_operand<T, DP>(Vt, 32 + w * 16, dt * 32, lane);
+                }
             }
-        // what was taken out reaches the queries that see it
-        if (edge && (bad_now[0] | bad_now[1]))
-            add_nonfinite<T, ND>(o, bad_now, vb, ldv, j0, a.dim, half, [&](int at) { return at <= p + a.right && (at >= p - a.left || at < a.sinks); });
+        }
+        if (taken_out)  // it reaches the queries that see it
+            add_nonfinite<T, ND>(o, vb, ldv, j0, keys, a.dim, lane, [&](int at) { return at <= p + a.right && (at >= p - a.left || at < a.sinks); });
     }
     l = both_halves_sum(l);
     const bool valid = l32 < my_rows;
@@ -332,7 +362,7 @@ int allow_attend()
 {
     for (const void *f : {(const void *)attend_kernel<T, DP, 1, false>, (const void *)attend_kernel<T, DP, 1, true>, (const void *)attend_kernel<T, DP, 4, false>,
                           (const void *)attend_kernel<T, DP, 4, true>})
-        LEANN_HIP(hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, AttendCfg<DP, 1>::FIXED + (2 * ATT_MOST_DISTANCE + 1 + 2 * ATT_EXT) * 4));
+        LEANN_HIP(hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, std::max(AttendCfg<DP, 1>::FIXED, AttendCfg<DP, 4>::FIXED) + (2 * ATT_MOST_DISTANCE + 1 + 2 * ATT_EXT) * 4));
     return LEANN_OK;
 }
 
@@ -369,8 +399,8 @@ int att_check_rows(const char *call, const char *what, const void *p, int64_t ld
         leann_set_error("%s: %s is null or not aligned to 16 bytes", call, what);
         return LEANN_EINVAL;
     }
-    if (ld < cols || ld % 8) {
-        leann_set_error("%s: rows of %s are %lld elements apart, need at least %lld and a multiple of 8", call, what, (long long)ld, (long long)cols);
+    if (ld < cols || ld % 8 || ld > ATT_MOST_LD) {
+        leann_set_error("%s: rows of %s are %lld elements apart, need a multiple of 8 from %lld to 2^23", call, what, (long long)ld, (long long)cols);
         return LEANN_ESHAPE;
     }
     return LEANN_OK;

@@ -21,11 +21,14 @@ constexpr float shift_of = 0.f;
 template <>
 constexpr float shift_of<f16_t> = 15.f;
 
+// LDS: tiles, then what the kernels say.  Two blocks fit on a CU up to heads of 64.
 template <int DP>
 struct GradCfg {
-    static constexpr int NT = GRAD_WAVES * 64, TILE = ATT_STEP * DP;
-    static constexpr int TILES = 4 * TILE * 2;  // bytes
-    static constexpr int FIXED = TILES + 1024 + 128;
+    static constexpr int TILE = ATT_STEP * DP;
+    static constexpr int QUERY_STAGES = DP == 128 ? 2 : 3, KEY_STAGES = DP == 128 ? 2 : 4;
+    static constexpr int QUERY_TILES = QUERY_STAGES * 2 * TILE * 2, KEY_TILES = KEY_STAGES * 2 * TILE * 2;  // bytes
+    static constexpr int STATS = ATT_STEP * (int)sizeof(float2);                                             // per stage
+    static constexpr int DIAGONALS = GRAD_WAVES * 16 * 68 * (int)sizeof(float);
 };
 
 // fp16: lowers `factor` and scales `sums` where a value of this step would pass 2^15.
@@ -60,28 +63,71 @@ __device__ inline float lse_in_log2(float lse)  // of rows that see nothing: P i
     return lse == -INFINITY ? INFINITY : lse * LOG2E;
 }
 
+// Sums of a wavefront's dS^T (a query per lane, 64 keys in its registers) by relative position: added to sums[0 .. 94], of which place 31 + key - query, numbers within the tile, is
+// key - query's.  16 queries at a time lie in LDS as rows of 64 keys (and 4 more, so that 16 lanes' writes reach all banks), where lane l walks along its diagonal,
+// query by query from the last: key l - 15 + query until that is below 0, which is from there on lane l's other diagonal, 64 further.
+// Sums in LDS by atomic additions, 32 instead of these 48 accesses, took 160 cycles each.
+__device__ inline void add_diagonals(const f32x16 (&d)[2], bool valid, float *rows, float *sums, int lane)
+{
+    const int half = lane >> 5, l32 = lane & 31;
+    float first[2], other[2];
+#pragma unroll
+    for (int part = 0; part < 2; ++part) {
+        wave_fence();
+        if ((l32 >> 4) == part) {
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    f32x4 x;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[e] = valid ? d[kt][4 * c + e] : 0.f;
+                    *reinterpret_cast<f32x4 *>(rows + (l32 & 15) * 68 + kt * 32 + 8 * c + 4 * half) = x;
+                }
+        }
+        wave_fence();
+        const float *near = rows + lane, *far = rows + lane + 64;
+        float sum = 0.f, until = 0.f;
+#pragma unroll
+        for (int step = 0; step < 16; ++step) {  // query 15 - step, key lane - step or lane - step + 64
+            // masks of low lanes only: one with its upper half set became a scalar move whose literal the hardware extends with zeros
+            const bool over = __builtin_amdgcn_inverse_ballot_w64((1ull << step) - 1);  // lanes below step
+            sum += (over ? far : near)[(15 - step) * 68 - step];
+            if (step < 15) until = __builtin_amdgcn_inverse_ballot_w64(1ull << step) ? sum : until;
+        }
+        first[part] = lane < 15 ? until : sum;
+        other[part] = sum - until;
+    }
+    // lane l of part 0 stands for key - query = l - 15, of part 1 for l - 31: places l + 16 and l
+    wave_fence();
+    sums[lane + 16] += first[0];
+    if (lane < 15) sums[lane + 80] += other[0];
+    wave_fence();
+    sums[lane] += first[1];
+    if (lane < 15) sums[lane + 64] += other[1];
+    wave_fence();
+}
+
 // A block takes 128 queries of one head through their keys, as the forward pass does.  S^T and dP^T = V dO^T have a query per lane; dS^T, rounded, is the other operand of
-// dQ^T = K^T dS^T.
-// The bias's gradient is summed by relative position: each wavefront has, for either half of its lanes, an array of its own in LDS, to which 32 lanes add at 32 places that
-// differ; so the order of the additions is the program's.  Tiles behind `distance` add to one place, in a register.
+// dQ^T = K^T dS^T.  It leaves what the other kernel needs of each query: the log-sum in units of log 2 and delta.
+// The bias's gradient is summed by relative position, each wavefront into an array of its own in LDS, so that the order of the additions is the program's.  Tiles
+// behind `distance` add to one place, in a register.
 template <class T, int DP, bool BIAS>
-__global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void query_grad_kernel(const AttentionItem *__restrict__ items, const AttentionTile *__restrict__ tiles, AttentionShape a,
-                                                                       const T *__restrict__ dout, int64_t ldd, const T *__restrict__ q, int64_t ldq, const T *__restrict__ k,
-                                                                       int64_t ldk, const T *__restrict__ v, int64_t ldv, const T *__restrict__ o, int64_t ldo,
-                                                                       const float *__restrict__ lse, int64_t Tq, const float *__restrict__ bias,
-                                                                       const int32_t *__restrict__ bucket_of, T *__restrict__ dq, int64_t lddq, float *__restrict__ delta,
-                                                                       float *__restrict__ by_position)
+__global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void query_grad_kernel(
+    const AttentionItem *__restrict__ items, const AttentionTile *__restrict__ tiles, AttentionShape a, const T *__restrict__ dout, int64_t ldd, const T *__restrict__ q,
+    int64_t ldq, const T *__restrict__ k, int64_t ldk, const T *__restrict__ v, int64_t ldv, const T *__restrict__ o, int64_t ldo, const float *__restrict__ lse, int64_t Tq,
+    const float *__restrict__ bias, const int32_t *__restrict__ bucket_of, T *__restrict__ dq, int64_t lddq, float2 *__restrict__ stats, float *__restrict__ by_position)
 {
     typedef typename Half8<T>::type V8;
-    constexpr int NT = GradCfg<DP>::NT, TILE = GradCfg<DP>::TILE, ND = DP / 32, NS = DP / 16;
+    typedef GradCfg<DP> Cfg;
+    typedef TileRequests<T, DP, GRAD_WAVES> Requests;
+    constexpr int NT = GRAD_WAVES * 64, STAGES = Cfg::QUERY_STAGES, TILE = Cfg::TILE, ND = DP / 32, NS = DP / 16;
     constexpr bool F16 = shift_of<T> != 0.f;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    T *Ks = reinterpret_cast<T *>(smem), *Vs = Ks + 2 * TILE;
-    uint32_t *bad = reinterpret_cast<uint32_t *>(smem + GradCfg<DP>::TILES);             // [3][2]
-    float *far_sums = reinterpret_cast<float *>(smem + GradCfg<DP>::TILES + 64);          // [4][2]
-    float *table = reinterpret_cast<float *>(smem + GradCfg<DP>::FIXED);
-    const int entries = bias_entries(a.distance);
-    float *sums = table + entries;  // [4 wavefronts][2 halves][entries]
+    T *Ks = reinterpret_cast<T *>(smem), *Vs = Ks + STAGES * TILE;
+    float *table = reinterpret_cast<float *>(smem + Cfg::QUERY_TILES);
+    const int entries = bias_entries(a.distance), room = (entries + 3) & ~3;
+    float *sums = table + room, *rows = sums + GRAD_WAVES * room;  // per wavefront: sums by position, 16 rows of dS
 
     const AttentionItem item = items[blockIdx.x];
     if (item.tile < 0) return;
@@ -89,40 +135,39 @@ __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void query_grad
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, l32 = lane & 31;
     const int h = item.head, g = h / a.share;
     const T *kb = k + (int64_t)t.other0 * ldk + g * a.dim, *vb = v + (int64_t)t.other0 * ldv + g * a.dim;
-    auto tile_at = [&](int u) { return u < t.sink_tiles ? u : t.first_tile + u - t.sink_tiles; };
+    auto key_of = [&](int u) { return (u < t.sink_tiles ? u : t.first_tile + u - t.sink_tiles) * ATT_STEP; };
 
-    TileInFlight<T, DP, NT> kin, vin;
-    auto fetch = [&](int u) {
-        const int row = tile_at(u) * ATT_STEP;
-        kin.load(kb, ldk, row, t.others, a.dim);
-        vin.load(vb, ldv, row, t.others, a.dim);
+    Requests kr, vr;
+    kr.init(ldk, a.dim, wave, lane);
+    vr.init(ldv, a.dim, wave, lane);
+    auto request = [&](int u, int stage) {
+        const int j = key_of(u);
+        kr.request(kb + j * ldk, ldk, t.others - j, a.dim, Ks + stage * TILE, wave);
+        vr.request(vb + j * ldv, ldv, t.others - j, a.dim, Vs + stage * TILE, wave);
     };
-    if (t.begin < t.end) fetch(t.begin);
     const int my_rows = min(32, t.rows - wave * 32), p0 = t.at + wave * 32;
     const int64_t my_row = t.row0 + wave * 32 + l32;
     const bool valid = l32 < my_rows;
-    V8 qf[NS], gf[NS];
-    float my_delta = 0.f;
-    load_rows<T, DP>(valid ? q + my_row * ldq + h * a.dim : nullptr, a.dim, lane, qf);
-    load_rows<T, DP>(valid ? dout + my_row * ldd + h * a.dim : nullptr, a.dim, lane, gf);
-    {
-        V8 of[NS];
-        load_rows<T, DP>(valid ? o + my_row * ldo + h * a.dim : nullptr, a.dim, lane, of);
-#pragma unroll
-        for (int s = 0; s < NS; ++s)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) my_delta = fmaf((float)gf[s][i], (float)of[s][i], my_delta);
-        my_delta = both_halves_sum(my_delta);
-        if (valid && half == 0) delta[(int64_t)h * Tq + my_row] = my_delta;
-    }
+    V8 qf[NS], gf[NS], of[NS];
+    load_rows<T, DP>(q + (int64_t)(t.row0 + wave * 32) * ldq + h * a.dim, ldq, my_rows, a.dim, lane, qf);
+    load_rows<T, DP>(dout + (int64_t)(t.row0 + wave * 32) * ldd + h * a.dim, ldd, my_rows, a.dim, lane, gf);
+    load_rows<T, DP>(o + (int64_t)(t.row0 + wave * 32) * ldo + h * a.dim, ldo, my_rows, a.dim, lane, of);
     const float my_lse = valid ? lse_in_log2(lse[(int64_t)h * Tq + my_row]) - shift_of<T> : INFINITY;
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i)
+        if (t.begin + i < t.end) request(t.begin + i, i);
     if (BIAS) {
         make_bias(table, bias, bucket_of, a, h);
         if (by_position)
-            for (int i = tid; i < GRAD_WAVES * 2 * entries; i += NT) sums[i] = 0.f;
+            for (int i = tid; i < GRAD_WAVES * room; i += NT) sums[i] = 0.f;
     }
-    if (tid < 6) bad[tid] = 0;
-    __syncthreads();
+    float my_delta = 0.f;
+#pragma unroll
+    for (int s = 0; s < NS; ++s)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) my_delta = fmaf((float)gf[s][i], (float)of[s][i], my_delta);
+    my_delta = both_halves_sum(my_delta);
+    if (valid && half == 0) stats[(int64_t)h * Tq + my_row] = make_float2(my_lse, my_delta);
 
     f32x16 acc[ND];
 #pragma unroll
@@ -133,20 +178,18 @@ __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void query_grad
     bool hurt = false;  // sees a key that is not finite
     const float scale2 = a.scale * LOG2E;
     const int p = p0 + l32;
-    float *my_sums = sums + (wave * 2 + half) * entries;
 
-    for (int u = t.begin, n = 0; u < t.end; ++u, ++n) {
-        const int j0 = tile_at(u) * ATT_STEP, buf = n & 1;
-        uint32_t *bad_now = bad + 2 * (n % 3);
-        const T *Kt = Ks + buf * TILE, *Vt = Vs + buf * TILE;
-        const bool edge = !sight(a, t.at, t.rows, j0, t.others - j0).all;
-        if (edge) kin.take_out_nonfinite(bad_now);
-        kin.store(Ks + buf * TILE);
-        vin.store(Vs + buf * TILE);
-        __syncthreads();
-        if (tid < 2) bad[2 * ((n + 2) % 3) + tid] = 0;  // read before this barrier, set again behind the next
-        if (u + 1 < t.end) fetch(u + 1);
-        const Sight see = sight(a, p0, my_rows, j0, t.others - j0);
+    int stage = 0;
+    for (int u = t.begin; u < t.end; ++u) {
+        const int j0 = key_of(u);
+        const T *Kt = Ks + stage * TILE, *Vt = Vs + stage * TILE;
+        if (STAGES > 2 && u + 1 < t.end) wait_for_requests<2 * Requests::N>();
+        else wait_for_requests<0>();
+        block_barrier();  // this tile is there, and the stage of the last one has been read
+        if (u + STAGES - 1 < t.end) request(u + STAGES - 1, stage == 0 ? STAGES - 1 : stage - 1);
+        stage = stage == STAGES - 1 ? 0 : stage + 1;
+        const int keys = min(ATT_STEP, t.others - j0);
+        const Sight see = sight(a, p0, my_rows, j0, keys);
         if (see.none) continue;
 
         f32x16 s[2], d[2];
@@ -160,15 +203,20 @@ __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void query_grad
                 d[kt] = att_mfma(row_operand<T, DP>(Vt, kt * 32, i, lane), gf[i], d[kt]);
             }
         }
+        V8 kf[2][ND];  // of the first 32 keys
+#pragma unroll
+        for (int w = 0; w < 2; ++w)
+#pragma unroll
+            for (int dt = 0; dt < ND; ++dt) kf[w][dt] = column_operand<T, DP>(Kt, w * 16, dt * 32, lane);
         const int j = j0 + 4 * half;
         const int least = j0 - (p0 + 31), most = j0 + ATT_STEP - 1 - p0;  // relative positions
         const bool near = most > -a.distance && least < a.distance;
-        const int at = j - p + a.distance + ATT_EXT;
         if (BIAS && near) {
+            const float *at = table + (j - p + a.distance + ATT_EXT);
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[kt][r] = fmaf(s[kt][r], scale2, table[at + kt * 32 + acc_row(r)] - my_lse);
+                for (int r = 0; r < 16; ++r) s[kt][r] = fmaf(s[kt][r], scale2, at[kt * 32 + acc_row(r)] - my_lse);
         } else {
             const float c = (BIAS ? table[most <= -a.distance ? 0 : entries - 1] : 0.f) - my_lse;
 #pragma unroll
@@ -180,6 +228,7 @@ __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void query_grad
         for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
             for (int r = 0; r < 16; ++r) d[kt][r] = __builtin_amdgcn_exp2f(s[kt][r]) * (d[kt][r] - my_delta);
+        // what is hidden is a choice, not a product; keys behind the last one are zeros, which add nothing to dQ
         if (!see.all) {
             const int last = min(t.others - 1, p + a.right) - j, from = p - a.left - j, sinks = a.sinks - j;
 #pragma unroll
@@ -187,16 +236,18 @@ __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void query_grad
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const int c = kt * 32 + acc_row(r);
-                    if (c > last || (c < from && c >= sinks)) d[kt][r] = 0.f;  // a choice, not a product
+                    d[kt][r] = (c > last) | ((c < from) & (c >= sinks)) ? 0.f : d[kt][r];
                 }
+        } else if (BIAS && keys < ATT_STEP) {
+            const int last = keys - 1 - 4 * half;
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) d[kt][r] = kt * 32 + acc_row(r) > last ? 0.f : d[kt][r];
         }
         if (BIAS && by_position) {
             if (near) {
-#pragma unroll
-                for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if (valid) __hip_atomic_fetch_add(my_sums + at + kt * 32 + acc_row(r), d[kt][r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+                add_diagonals(d, valid, rows + wave * 16 * 68, sums + wave * room + (j0 - p0 - 31 + a.distance + ATT_EXT), lane);
             } else {
                 float sum = 0.f;
 #pragma unroll
@@ -209,34 +260,62 @@ __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void query_grad
             }
         }
         if (F16) stay_in_range(d, acc, factor);
+        bool taken_out = false;
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt)
+        for (int kt = 0; kt < 2; ++kt) {
+            if (!see.all) {
+                Finite<T> f;
+#pragma unroll
+                for (int w = 0; w < 2; ++w)
+#pragma unroll
+                    for (int dt = 0; dt < ND; ++dt) f.look(kf[w][dt]);
+                if (!f.all()) {
+                    taken_out = true;
+#pragma unroll
+                    for (int w = 0; w < 2; ++w)
+#pragma unroll
+                        for (int dt = 0; dt < ND; ++dt) f.keep(kf[w][dt]);
+                }
+            }
 #pragma unroll
             for (int w = 0; w < 2; ++w) {
                 const V8 df = rounded<T>(d[kt], w);
 #pragma unroll
-                for (int dt = 0; dt < ND; ++dt) acc[dt] = att_mfma(column_operand<T, DP>(Kt, kt * 32 + w * 16, dt * 32, lane), df, acc[dt]);
+                for (int dt = 0; dt < ND; ++dt) {
+                    acc[dt] = att_mfma(kf[w][dt], df, acc[dt]);
+                    if (kt == 0) kf[w][dt] = column_operand<T, DP>(Kt, 32 + w * 16, dt * 32, lane);
+                }
             }
-        if (edge && (bad_now[0] | bad_now[1]))
-            for (int i = 0; i < ATT_STEP; ++i)
-                if (bad_now[i >> 5] >> (i & 31) & 1) hurt |= j0 + i <= p + a.right && (j0 + i >= p - a.left || j0 + i < a.sinks);
+        }
+        if (taken_out)
+            for_nonfinite_rows<T>(kb, ldk, j0, keys, a.dim, lane, [&](int at, const T *) { hurt |= at <= p + a.right && (at >= p - a.left || at < a.sinks); });
     }
     if (hurt) factor = __builtin_nanf("");
     store_columns<T, ND>(acc, a.scale / factor * (F16 ? 0x1p-15f : 1.f), dq + my_row * lddq + h * a.dim, valid, a.dim, lane);
 
     if (BIAS && by_position) {
-        const float b = wave_sum(behind), c = wave_sum(ahead);
-        if (lane == 0) far_sums[wave * 2] = b, far_sums[wave * 2 + 1] = c;
-        __syncthreads();
+        // the ends have what lies beyond: each wavefront's, lane by lane, then over the lanes
         const int positions = 2 * a.distance + 1;
+        const float *mine = sums + wave * room;
+        if (t.begin == t.end) block_barrier();  // the sums are cleared
+        for (int e = lane; e < ATT_EXT; e += 64) {
+            behind += mine[e];
+            ahead += mine[entries - 1 - e];
+        }
+        behind = wave_sum(behind);
+        ahead = wave_sum(ahead);
+        float *far_sums = rows;
+        __syncthreads();
+        if (lane == 0) far_sums[wave * 2] = behind, far_sums[wave * 2 + 1] = ahead;
+        __syncthreads();
         float *to = by_position + ((int64_t)item.tile * a.heads + h) * positions;
         for (int i = tid; i < positions; i += NT) {
             float sum = 0.f;
-            const int from = i == 0 ? 0 : i + ATT_EXT, last = i == positions - 1 ? entries - 1 : i + ATT_EXT;  // the ends have what lies beyond
+#pragma unroll
             for (int w = 0; w < GRAD_WAVES; ++w) {
+                sum += sums[w * room + i + ATT_EXT];
                 if (i == 0) sum += far_sums[w * 2];
                 if (i == positions - 1) sum += far_sums[w * 2 + 1];
-                for (int e = from; e <= last; ++e) sum += sums[(2 * w) * entries + e] + sums[(2 * w + 1) * entries + e];
             }
             to[i] = sum * (F16 ? 0x1p-15f : 1.f);
         }
@@ -244,22 +323,22 @@ __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void query_grad
 }
 
 // A block takes 128 keys of one key head through the queries that see them, of every head that shares it: S = Q K^T and dP = dO V^T have a key per lane; P and dS, rounded, are the
-// other operands of dV^T = dO^T P and dK^T = Q^T dS.  K and V stay in registers.
+// other operands of dV^T = dO^T P and dK^T = Q^T dS.  K and V stay in registers; Q, dO and the queries' numbers come from memory to LDS, STAGES - 1 tiles ahead.
 template <class T, int DP, bool BIAS>
-__global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void key_grad_kernel(const AttentionItem *__restrict__ items, const AttentionTile *__restrict__ tiles, AttentionShape a,
-                                                                     const T *__restrict__ dout, int64_t ldd, const T *__restrict__ q, int64_t ldq, const T *__restrict__ k,
-                                                                     int64_t ldk, const T *__restrict__ v, int64_t ldv, const float *__restrict__ lse,
-                                                                     const float *__restrict__ delta, int64_t Tq, const float *__restrict__ bias,
-                                                                     const int32_t *__restrict__ bucket_of, T *__restrict__ dk, int64_t lddk, T *__restrict__ dv, int64_t lddv)
+__global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void key_grad_kernel(
+    const AttentionItem *__restrict__ items, const AttentionTile *__restrict__ tiles, AttentionShape a, const T *__restrict__ dout, int64_t ldd, const T *__restrict__ q,
+    int64_t ldq, const T *__restrict__ k, int64_t ldk, const T *__restrict__ v, int64_t ldv, const float2 *__restrict__ stats, int64_t Tq, const float *__restrict__ bias,
+    const int32_t *__restrict__ bucket_of, T *__restrict__ dk, int64_t lddk, T *__restrict__ dv, int64_t lddv)
 {
     typedef typename Half8<T>::type V8;
-    constexpr int NT = GradCfg<DP>::NT, TILE = GradCfg<DP>::TILE, ND = DP / 32, NS = DP / 16;
+    typedef GradCfg<DP> Cfg;
+    typedef TileRequests<T, DP, GRAD_WAVES> Requests;
+    constexpr int STAGES = Cfg::KEY_STAGES, TILE = Cfg::TILE, ND = DP / 32, NS = DP / 16;
     constexpr bool F16 = shift_of<T> != 0.f;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    T *Qs = reinterpret_cast<T *>(smem), *Gs = Qs + 2 * TILE;
-    float *stats = reinterpret_cast<float *>(smem + GradCfg<DP>::TILES);                    // [2 buffers][lse, delta][64]
-    uint32_t *bad = reinterpret_cast<uint32_t *>(smem + GradCfg<DP>::TILES + 1024);          // [3][Q, dO][2]
-    float *table = reinterpret_cast<float *>(smem + GradCfg<DP>::FIXED);
+    T *Qs = reinterpret_cast<T *>(smem), *Gs = Qs + STAGES * TILE;
+    float *numbers = reinterpret_cast<float *>(smem + Cfg::KEY_TILES);  // [stage][64][2]
+    float *table = reinterpret_cast<float *>(smem + Cfg::KEY_TILES + STAGES * Cfg::STATS);
 
     const AttentionItem item = items[blockIdx.x];
     if (item.tile < 0) return;
@@ -270,9 +349,36 @@ __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void key_grad_k
     const int64_t my_row = t.row0 + wave * 32 + l32;
     const bool valid = l32 < my_rows;
     V8 kf[NS], vf[NS];
-    load_rows<T, DP>(valid ? k + my_row * ldk + g * a.dim : nullptr, a.dim, lane, kf);
-    load_rows<T, DP>(valid ? v + my_row * ldv + g * a.dim : nullptr, a.dim, lane, vf);
-    if (tid < 12) bad[tid] = 0;
+    load_rows<T, DP>(k + (int64_t)(t.row0 + wave * 32) * ldk + g * a.dim, ldk, my_rows, a.dim, lane, kf);
+    load_rows<T, DP>(v + (int64_t)(t.row0 + wave * 32) * ldv + g * a.dim, ldv, my_rows, a.dim, lane, vf);
+
+    Requests qr, gr;
+    qr.init(ldq, a.dim, wave, lane);
+    gr.init(ldd, a.dim, wave, lane);
+    // tile by tile, head by head
+    struct At {
+        int h, tile;
+    };
+    const int per_head = t.end - t.begin, total = per_head * a.share, last_tile = t.first_tile + per_head - 1;
+    auto behind = [&](At at) { return at.tile == last_tile ? At{at.h + 1, t.first_tile} : At{at.h, at.tile + 1}; };
+    auto request = [&](At at, int stage) {
+        const int i0 = at.tile * ATT_STEP;
+        if (wave == 0) {
+            const float2 *from = stats + (int64_t)at.h * Tq + t.other0 + i0;
+            // whole pieces of two queries; what is read behind the last one is masked
+            const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<float2 *>(from), 0, ((min(t.others - i0, ATT_STEP) + 1) & ~1) * 8, 0x00020000);
+            if (lane < 32) lds_request(rsrc, lane * 16, numbers + stage * 128);
+        }
+        qr.request(q + (int64_t)(t.other0 + i0) * ldq + at.h * a.dim, ldq, t.others - i0, a.dim, Qs + stage * TILE, wave);
+        gr.request(dout + (int64_t)(t.other0 + i0) * ldd + at.h * a.dim, ldd, t.others - i0, a.dim, Gs + stage * TILE, wave);
+    };
+    At now = {g * a.share, t.first_tile}, next = now;
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i)
+        if (i < total) {
+            request(next, i);
+            next = behind(next);
+        }
 
     f32x16 dk_acc[ND], dv_acc[ND];
 #pragma unroll
@@ -282,54 +388,30 @@ __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void key_grad_k
     float factor = 1.f;
     bool hurt = false;
     const float scale2 = a.scale * LOG2E;
-    const int per_head = t.end - t.begin;
-    // what keys `from` .. `from + keys - 1` get from the queries i0 .. i0 + 63
-    auto look = [&](int from, int keys, int i0) {
-        const int p = t.first + i0, last_p = t.first + min(i0 + ATT_STEP, t.others) - 1, last = from + keys - 1;
-        const bool none = keys <= 0 || from > last_p + a.right || (last < p - a.left && from >= a.sinks);
-        const bool all = i0 + ATT_STEP <= t.others && last <= p + a.right && (from >= last_p - a.left || last < a.sinks);
-        return Sight{none, all};
-    };
-
-    TileInFlight<T, DP, NT> qin, gin;
-    float stat = 0.f;
-    auto fetch = [&](int n) {
-        const int h = g * a.share + n / per_head, i0 = (t.first_tile + n % per_head) * ATT_STEP;
-        qin.load(q + (int64_t)t.other0 * ldq + h * a.dim, ldq, i0, t.others, a.dim);
-        gin.load(dout + (int64_t)t.other0 * ldd + h * a.dim, ldd, i0, t.others, a.dim);
-        if (tid < 128) {
-            const int i = i0 + (tid & 63);
-            const int64_t at = (int64_t)h * Tq + t.other0 + i;
-            stat = i < t.others ? (tid < 64 ? lse[at] : delta[at]) : -INFINITY;
-        }
-    };
-    const int total = per_head * a.share;
-    if (total) fetch(0);
-    int of_table = -1;
-    for (int n = 0; n < total; ++n) {
-        const int h = g * a.share + n / per_head, i0 = (t.first_tile + n % per_head) * ATT_STEP, buf = n & 1;
-        uint32_t *bad_now = bad + 4 * (n % 3);
-        const T *Qt = Qs + buf * TILE, *Gt = Gs + buf * TILE;
+    int stage = 0, of_table = -1;
+    for (int n = 0; n < total; ++n, now = behind(now)) {
+        const int h = now.h, i0 = now.tile * ATT_STEP;
+        const T *Qt = Qs + stage * TILE, *Gt = Gs + stage * TILE;
+        const float *nt = numbers + stage * 128;
         if (BIAS && h != of_table) {
-            __syncthreads();  // the last head's table has been read
+            if (n) block_barrier();  // the last head's table has been read
             make_bias(table, bias, bucket_of, a, h);
             of_table = h;
         }
-        if (n == 0) __syncthreads();  // bad[] is cleared
-        const bool edge = !look(t.at, t.rows, i0).all;
-        if (edge) {
-            qin.take_out_nonfinite(bad_now);
-            gin.take_out_nonfinite(bad_now + 2);
+        if (STAGES > 3 && n + 2 < total) wait_for_requests<4 * Requests::N>();
+        else if (STAGES > 2 && n + 1 < total) wait_for_requests<2 * Requests::N>();
+        else wait_for_requests<0>();
+        block_barrier();  // this tile is there, and the stage of the last one has been read
+        if (n + STAGES - 1 < total) {
+            request(next, stage == 0 ? STAGES - 1 : stage - 1);
+            next = behind(next);
         }
-        qin.store(Qs + buf * TILE);
-        gin.store(Gs + buf * TILE);
-        if (tid < 128) stats[buf * 128 + tid] = tid < 64 ? lse_in_log2(stat) - shift_of<T> : stat;
-        __syncthreads();
-        if (tid < 4) bad[4 * ((n + 2) % 3) + tid] = 0;
-        if (n + 1 < total) fetch(n + 1);
-        const Sight see = look(jw, my_rows, i0);
+        stage = stage == STAGES - 1 ? 0 : stage + 1;
+        const int rows = min(ATT_STEP, t.others - i0);
+        const Sight see = sight(a, t.first + i0, rows, jw, my_rows);
         if (see.none) continue;
 
+        bool taken_out = false;
 #pragma unroll
         for (int qs = 0; qs < 2; ++qs) {
             f32x16 s[1], d[1];
@@ -340,15 +422,19 @@ __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void key_grad_k
                 s[0] = att_mfma(row_operand<T, DP>(Qt, qs * 32, i, lane), kf[i], s[0]);
                 d[0] = att_mfma(row_operand<T, DP>(Gt, qs * 32, i, lane), vf[i], d[0]);
             }
-            // register r is query i0 + 32 qs + 4 half + acc_row(r)
+            V8 qc[ND], gc[ND];  // of the first 16 queries
+#pragma unroll
+            for (int dt = 0; dt < ND; ++dt) {
+                gc[dt] = column_operand<T, DP>(Gt, qs * 32, dt * 32, lane);
+                qc[dt] = column_operand<T, DP>(Qt, qs * 32, dt * 32, lane);
+            }
+            // register r is query i0 + 32 qs + 4 half + acc_row(r); queries behind the last one have rows of zeros and any numbers
             const int from = i0 + qs * 32 + 4 * half, p = t.first + from;
             float ls[16], de[16];
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                const f32x4 x = *reinterpret_cast<const f32x4 *>(stats + buf * 128 + qs * 32 + 4 * half + 8 * c);
-                const f32x4 y = *reinterpret_cast<const f32x4 *>(stats + buf * 128 + 64 + qs * 32 + 4 * half + 8 * c);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) ls[4 * c + e] = x[e], de[4 * c + e] = y[e];
+            for (int c = 0; c < 8; ++c) {
+                const f32x4 x = *reinterpret_cast<const f32x4 *>(nt + 2 * (qs * 32 + 4 * half + 8 * (c >> 1) + 2 * (c & 1)));
+                ls[2 * c] = x[0], de[2 * c] = x[1], ls[2 * c + 1] = x[2], de[2 * c + 1] = x[3];
             }
             if (BIAS) {
                 const int pw = t.first + i0 + qs * 32, least = jw - (pw + 31), most = jw + 31 - pw;
@@ -371,29 +457,57 @@ __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void key_grad_k
                 d[0][r] = s[0][r] * (d[0][r] - de[r]);
             }
             if (!see.all) {
-                const int rows = t.others - from, first = j - a.right - p, last = j < a.sinks ? ATT_STEP : j + a.left - p;
+                const int count = t.others - from, first = j - a.right - p, last = j < a.sinks ? ATT_STEP : j + a.left - p;
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const int c = acc_row(r);
-                    if (c >= rows || c < first || c > last) s[0][r] = d[0][r] = 0.f;
+                    const bool hidden = (c >= count) | (c < first) | (c > last);
+                    s[0][r] = hidden ? 0.f : s[0][r];
+                    d[0][r] = hidden ? 0.f : d[0][r];
+                }
+            } else if (rows < ATT_STEP) {
+                const int count = t.others - from;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    s[0][r] = acc_row(r) >= count ? 0.f : s[0][r];
+                    d[0][r] = acc_row(r) >= count ? 0.f : d[0][r];
                 }
             }
             if (F16) stay_in_range(d, dk_acc, factor);
 #pragma unroll
             for (int w = 0; w < 2; ++w) {
+                if (!see.all) {
+                    Finite<T> f;
+#pragma unroll
+                    for (int dt = 0; dt < ND; ++dt) {
+                        f.look(gc[dt]);
+                        f.look(qc[dt]);
+                    }
+                    if (!f.all()) {
+                        taken_out = true;
+#pragma unroll
+                        for (int dt = 0; dt < ND; ++dt) {
+                            f.keep(gc[dt]);
+                            f.keep(qc[dt]);
+                        }
+                    }
+                }
                 const V8 pf = rounded<T>(s[0], w), df = rounded<T>(d[0], w);
 #pragma unroll
                 for (int dt = 0; dt < ND; ++dt) {
-                    dv_acc[dt] = att_mfma(column_operand<T, DP>(Gt, qs * 32 + w * 16, dt * 32, lane), pf, dv_acc[dt]);
-                    dk_acc[dt] = att_mfma(column_operand<T, DP>(Qt, qs * 32 + w * 16, dt * 32, lane), df, dk_acc[dt]);
+                    dv_acc[dt] = att_mfma(gc[dt], pf, dv_acc[dt]);
+                    dk_acc[dt] = att_mfma(qc[dt], df, dk_acc[dt]);
+                    if (w == 0) {
+                        gc[dt] = column_operand<T, DP>(Gt, qs * 32 + 16, dt * 32, lane);
+                        qc[dt] = column_operand<T, DP>(Qt, qs * 32 + 16, dt * 32, lane);
+                    }
                 }
             }
         }
-        if (edge && (bad_now[0] | bad_now[1] | bad_now[2] | bad_now[3])) {
+        if (taken_out) {
             auto seen = [&](int i) { return j <= t.first + i + a.right && (j >= t.first + i - a.left || j < a.sinks); };
-            for (int i = 0; i < ATT_STEP; ++i)
-                if (bad_now[i >> 5] >> (i & 31) & 1) hurt |= seen(i0 + i);
-            add_nonfinite<T, ND>(dv_acc, bad_now + 2, dout + (int64_t)t.other0 * ldd + h * a.dim, ldd, i0, a.dim, half, seen);
+            for_nonfinite_rows<T>(q + (int64_t)t.other0 * ldq + h * a.dim, ldq, i0, rows, a.dim, lane, [&](int i, const T *) { hurt |= seen(i); });
+            add_nonfinite<T, ND>(dv_acc, dout + (int64_t)t.other0 * ldd + h * a.dim, ldd, i0, rows, a.dim, lane, seen);
         }
     }
     if (hurt) factor = __builtin_nanf("");
@@ -484,24 +598,27 @@ extern "C" int leann_attention_backward(leann_ctx *ctx, const leann_attention_pl
     LEANN_HIP(hipSetDevice(ctx->device));
     const AttentionShape a = att_shape(plan, scale);
     const int positions = 2 * plan->distance + 1, n = plan->n_grad_tiles, groups = (n + POSITION_ROWS - 1) / POSITION_ROWS;
-    const size_t delta_bytes = ((size_t)plan->heads * plan->Tq * sizeof(float) + 255) & ~(size_t)255;
+    const size_t stats_bytes = ((size_t)plan->heads * plan->Tq * sizeof(float2) + 8 + 255) & ~(size_t)255;  // 8: see key_grad_kernel's requests
     const size_t row_bytes = (size_t)plan->heads * positions * sizeof(float);
     std::lock_guard<std::mutex> turn(ctx->op_work_mutex);
-    LEANN_TRY(ctx->reserve(ctx->op_work, std::max<size_t>(1, delta_bytes + (dbias_dev ? row_bytes * (n + groups) : 0))));
-    float *delta = (float *)ctx->op_work.p, *by_position = dbias_dev ? (float *)((char *)ctx->op_work.p + delta_bytes) : nullptr;
+    LEANN_TRY(ctx->reserve(ctx->op_work, std::max<size_t>(1, stats_bytes + (dbias_dev ? row_bytes * (n + groups) : 0))));
+    float2 *stats = (float2 *)ctx->op_work.p;
+    float *by_position = dbias_dev ? (float *)((char *)ctx->op_work.p + stats_bytes) : nullptr;
     auto go = [&](auto *type, auto dp, auto with_bias) {
         typedef std::remove_pointer_t<decltype(type)> T;
         constexpr int DP = decltype(dp)::value;
         constexpr bool BIAS = decltype(with_bias)::value;
-        const int table = BIAS ? (positions + 2 * ATT_EXT) * 4 : 0;
+        typedef GradCfg<DP> Cfg;
+        const int table = BIAS ? ((positions + 2 * ATT_EXT + 3) & ~3) * 4 : 0;
+        const int query_smem = Cfg::QUERY_TILES + (by_position ? table * (1 + GRAD_WAVES) + Cfg::DIAGONALS : table);
         if (plan->n_grad_items)
             hipLaunchKernelGGL((query_grad_kernel<T, DP, BIAS>), dim3(plan->n_grad_items), dim3(GRAD_WAVES * 64),
-                               GradCfg<DP>::FIXED + table * (by_position ? 1 + 2 * GRAD_WAVES : 1), ctx->stream, plan->grad_items, plan->grad_tiles, a, (const T *)dout_dev, ldd,
+                               query_smem, ctx->stream, plan->grad_items, plan->grad_tiles, a, (const T *)dout_dev, ldd,
                                (const T *)q_dev, ldq, (const T *)k_dev, ldk, (const T *)v_dev, ldv, (const T *)out_dev, ldo, lse_dev, plan->Tq, bias_dev, plan->bucket_of,
-                               (T *)dq_dev, lddq, delta, by_position);
+                               (T *)dq_dev, lddq, stats, by_position);
         if (plan->n_key_items)
-            hipLaunchKernelGGL((key_grad_kernel<T, DP, BIAS>), dim3(plan->n_key_items), dim3(GRAD_WAVES * 64), GradCfg<DP>::FIXED + table, ctx->stream, plan->key_items,
-                               plan->key_tiles, a, (const T *)dout_dev, ldd, (const T *)q_dev, ldq, (const T *)k_dev, ldk, (const T *)v_dev, ldv, lse_dev, delta, plan->Tq,
+            hipLaunchKernelGGL((key_grad_kernel<T, DP, BIAS>), dim3(plan->n_key_items), dim3(GRAD_WAVES * 64), Cfg::KEY_TILES + Cfg::KEY_STAGES * Cfg::STATS + table, ctx->stream, plan->key_items,
+                               plan->key_tiles, a, (const T *)dout_dev, ldd, (const T *)q_dev, ldq, (const T *)k_dev, ldk, (const T *)v_dev, ldv, stats, plan->Tq,
                                bias_dev, plan->bucket_of, (T *)dk_dev, lddk, (T *)dv_dev, lddv);
     };
     auto with_type = [&](auto *type) {
