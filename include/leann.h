@@ -470,6 +470,26 @@ int leann_attention_backward(leann_ctx *ctx, const leann_attention_plan *plan, c
                              const void *v_dev, int64_t ldv, const void *out_dev, int64_t ldo, const float *lse_dev, int dtype, float scale, const float *bias_dev, void *dq_dev,
                              int64_t lddq, void *dk_dev, int64_t lddk, void *dv_dev, int64_t lddv, float *dbias_dev);
 
+/*
+ * Activations kept in 8 bits between the forward and the backward pass.  Of each row's 128 columns (the last ones of a row may be fewer) a = max |x|, scale = a / 127 (fp32) and
+ * code = 127 x / a to the nearest whole number, ties to even; a checkpoint stands for code * scale, off by at most half a scale.  codes: int8 rows ldc bytes apart, scales:
+ * fp32[rows][ceil(cols / 128)].  128 columns with an infinity or NaN come back as NaN, all of them.  x and outputs are LEANN_F32, LEANN_BF16 or LEANN_F16; what an fp16 output cannot
+ * hold becomes infinite.  Errors: as leann_dropout; 2^32 - 2^24 times 128 columns or more in all rows -> LEANN_ESHAPE.
+ */
+int leann_checkpoint(leann_ctx *ctx, const void *x_dev, int64_t ldx, int64_t rows, int64_t cols, int dtype, int8_t *codes_dev, int64_t ldc, float *scales_dev);
+/* out = code * scale, rounded to dtype, any of the three: what a backward pass that needs x (leann_layernorm_backward, leann_adapter_project_backward, leann_attention_backward) is given. */
+int leann_checkpoint_restore(leann_ctx *ctx, const int8_t *codes_dev, int64_t ldc, const float *scales_dev, int64_t rows, int64_t cols, int dtype, void *out_dev, int64_t ldo);
+
+/* out = x Phi(x): LEANN_GELU with the normal distribution function (to 1e-7), LEANN_GELU_TANH with (1 + tanh(sqrt(2 / pi) (x + 0.044715 x^3))) / 2 for it.  out may be x itself.
+ * codes and scales (both or neither) receive x as a checkpoint. */
+enum { LEANN_GELU = 0, LEANN_GELU_TANH = 1 };
+int leann_activation(leann_ctx *ctx, const void *x_dev, int64_t ldx, int64_t rows, int64_t cols, int dtype, int kind, void *out_dev, int64_t ldo, int8_t *codes_dev, int64_t ldc,
+                     float *scales_dev);
+/* dx = dout times the activation's derivative at x, which is given as it was (x) or as a checkpoint (codes, scales); again (NULL for none) receives the activation of that x, which
+ * the gradient of a projection behind it needs and which then need not be kept.  dx may be dout or x itself; again must not be dout, dx or x. */
+int leann_activation_backward(leann_ctx *ctx, const void *dout_dev, int64_t ldd, const void *x_dev, int64_t ldx, const int8_t *codes_dev, int64_t ldc, const float *scales_dev,
+                              int64_t rows, int64_t cols, int dtype, int kind, void *dx_dev, int64_t lddx, void *again_dev, int64_t lda);
+
 #ifdef __cplusplus
 }
 #endif

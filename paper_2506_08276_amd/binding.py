@@ -26,7 +26,7 @@ EXPORTS = ["leann_last_error", "leann_create", "leann_destroy", "leann_embed", "
            "leann_projection_create", "leann_projection_free", "leann_adapter_rows_create", "leann_adapter_rows_free",
            "leann_adapter_project", "leann_adapter_project_backward",
            "leann_position_buckets", "leann_attention_create", "leann_attention_free", "leann_attention",
-           "leann_attention_backward"]
+           "leann_attention_backward", "leann_checkpoint", "leann_checkpoint_restore", "leann_activation", "leann_activation_backward"]
 PROF_KINDS = ["gemm_qkv", "gemm_o", "gemm_ffn1", "gemm_ffn2", "attention", "layernorm", "enc_other", "traverse",
               "collect", "score_insert", "lut", "adc"]
 
@@ -96,7 +96,10 @@ def load_library(path=LIB_PATH):
                 "leann_position_buckets": [I, I, I, V],
                 "leann_attention_create": [V, V, V, V, I, V, V], "leann_attention_free": [V],
                 "leann_attention": [V, V, V, N, V, N, V, N, I, F, V, V, N, V],
-                "leann_attention_backward": [V, V, V, N, V, N, V, N, V, N, V, N, V, I, F, V, V, N, V, N, V, N, V]}.items():
+                "leann_attention_backward": [V, V, V, N, V, N, V, N, V, N, V, N, V, I, F, V, V, N, V, N, V, N, V],
+                "leann_checkpoint": [V, V, N, N, N, I, V, N, V], "leann_checkpoint_restore": [V, V, N, V, N, N, I, V, N],
+                "leann_activation": [V, V, N, N, N, I, I, V, N, V, N, V],
+                "leann_activation_backward": [V, V, N, V, N, V, N, V, N, N, I, I, V, N, V, N]}.items():
             getattr(lib, name).argtypes = args
         _lib = lib
     return _lib
@@ -597,3 +600,68 @@ def leann_attention_backward(ctx, plan, dout, q, k, v, out, lse, scale=None, bia
     _check(load_library().leann_attention_backward(ctx, plan, gp, ldd, qp, ldq, kp, ldk, vp, ldv, op, ldo, lse.data_ptr(), _dtype(q), scale, bp, dqp, lddq,
                                                    dkp, lddk, dvp, lddv, None if dbias is None else dbias.data_ptr()))
     return dq, dk, dv, dbias
+
+
+# ---- activations, and their checkpoints in 8 bits
+ACTIVATIONS = {"gelu": 0, "gelu_tanh": 1}
+
+
+def _kind(kind):
+    assert kind in ACTIVATIONS, f"kind: need one of {', '.join(ACTIVATIONS)}"
+    return ACTIVATIONS[kind]
+
+
+def _checkpoint_like(x):
+    assert x.dim() == 2, "x: need a 2-D CUDA tensor with unit column stride"
+    return (torch.empty(x.shape, dtype=torch.int8, device=x.device),
+            torch.empty((x.shape[0], (x.shape[1] + 127) // 128), dtype=torch.float32, device=x.device))
+
+
+def _checkpoint(kept):
+    """(codes' pointer and distance of rows, scales' pointer) of a checkpoint."""
+    codes, scales = kept
+    assert codes.dtype == torch.int8, "checkpoint: codes have to be int8"
+    return *_rows(codes, "codes"), _vector(scales, codes.shape[0] * ((codes.shape[1] + 127) // 128), "scales")
+
+
+def leann_checkpoint(ctx, x):
+    """A 2-D tensor in 8 bits: (codes int8 [rows][cols], scales float32 [rows][ceil(cols / 128)]), the largest of 128 columns being 127 steps."""
+    kept = _checkpoint_like(x)
+    (xp, ldx), (cp, ldc, sp) = _rows(x, "x"), _checkpoint(kept)
+    _check(load_library().leann_checkpoint(ctx, xp, ldx, x.shape[0], x.shape[1], _dtype(x), cp, ldc, sp))
+    return kept
+
+
+def leann_checkpoint_restore(ctx, kept, dtype=None, out=None):
+    """The tensor that a checkpoint stands for, in `dtype` (or into `out`)."""
+    rows, cols = kept[0].shape
+    if out is None:
+        assert dtype in _DTYPES, "need float32, bfloat16 or float16"
+        out = torch.empty((rows, cols), dtype=dtype, device=kept[0].device)
+    assert out.shape == kept[0].shape and dtype in (None, out.dtype), "out: shape or type differs"
+    (cp, ldc, sp), (op, ldo) = _checkpoint(kept), _rows(out, "out")
+    _check(load_library().leann_checkpoint_restore(ctx, cp, ldc, sp, rows, cols, _dtype(out), op, ldo))
+    return out
+
+
+def leann_activation(ctx, x, kind="gelu", keep=False, out=None):
+    """GELU of a 2-D tensor ("gelu", or "gelu_tanh" for its approximation); keep: returns (out, checkpoint of x), what the backward pass needs; else out."""
+    if out is None:
+        out = torch.empty_like(x)
+    kept = _checkpoint_like(x) if keep else None
+    (xp, ldx), (op, ldo), (cp, ldc, sp) = _rows(x, "x"), _rows(out, "out", x), _checkpoint(kept) if keep else (None, 0, None)
+    _check(load_library().leann_activation(ctx, xp, ldx, x.shape[0], x.shape[1], _dtype(x), _kind(kind), op, ldo, cp, ldc, sp))
+    return (out, kept) if keep else out
+
+
+def leann_activation_backward(ctx, dout, kept, kind="gelu", again=False, dx=None):
+    """The gradient of leann_activation's input from that of its output and the input, a checkpoint or the tensor itself; again: (dx, output once more)."""
+    if dx is None:
+        dx = torch.empty_like(dout)
+    y = torch.empty_like(dout) if again else None
+    plain = isinstance(kept, torch.Tensor)
+    assert plain or kept[0].shape == dout.shape, "checkpoint: shape differs"
+    (gp, ldd), (dp, lddx), (yp, lda) = _rows(dout, "dout"), _rows(dx, "dx", dout), _rows(y, "again")
+    (xp, ldx), (cp, ldc, sp) = (_rows(kept, "x", dout), (None, 0, None)) if plain else ((None, 0), _checkpoint(kept))
+    _check(load_library().leann_activation_backward(ctx, gp, ldd, xp, ldx, cp, ldc, sp, dout.shape[0], dout.shape[1], _dtype(dout), _kind(kind), dp, lddx, yp, lda))
+    return (dx, y) if again else dx

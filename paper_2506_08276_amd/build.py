@@ -6,14 +6,14 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libleann.so")
-SOURCES = ["api.hip", "encoder.hip", "pq.hip", "search.hip", "build.hip", "peak.hip", "norm.hip", "adapter.hip", "attention.hip", "attention_grad.hip"]
+SOURCES = ["api.hip", "encoder.hip", "pq.hip", "search.hip", "build.hip", "peak.hip", "norm.hip", "adapter.hip", "attention.hip", "attention_grad.hip", "activation.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Xclang", "-target-feature", "-Xclang",
          "-packed-fp32-ops", "-Wno-unused-command-line-argument"]
 # Kernel arguments come in scalar registers with the dispatch, as many as there is room for: read from memory, they are the first
 # link of every kernel's chain of latencies.  Embedding one chunk, 87 dependent launches, took 424 us without, 401 with it.  For the files
 # with such chains; arguments in a struct stay in memory, as those of a launch that nothing runs ahead of should (adc_direct_kernel).
 PRELOAD = ["-mllvm", "-amdgpu-kernarg-preload-count=16"]
-FLAGS_OF = {"encoder.hip": PRELOAD, "pq.hip": PRELOAD, "norm.hip": PRELOAD}
+FLAGS_OF = {"encoder.hip": PRELOAD, "pq.hip": PRELOAD, "norm.hip": PRELOAD, "activation.hip": PRELOAD}
 
 
 def build_library(verbose=False):
