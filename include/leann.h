@@ -433,6 +433,7 @@ int leann_adapter_project_backward(leann_ctx *ctx, const leann_projection *proj,
  *   visible: j <= p + right and (j >= p - left or j < sinks); left or right -1: no limit to that side
  *   s_ij = scale q_i . k_j + bias[bucket_of[clamp(j - p, -distance, distance) + distance]][h]  (without buckets: no bias)
  *   lse_i = log sum over visible j of exp s_ij,  out_i = sum over visible j of exp(s_ij - lse_i) v_j;  where nothing is visible out_i is 0 and lse_i -inf
+ * The scale's magnitude lies between 2^-20 and 2^20; a finite bias beyond 2^100 counts as 2^100.
  * Sums, maxima and scores are fp32; weights exp(s - max), and in gradients exp(s - lse) and the scores' gradients, are rounded to the inputs' type where they enter a product of
  * matrices.  What a query does not see does not reach it, be it infinite or NaN.  Rows and columns behind the last sequence and head are neither read nor written.
  */
@@ -465,7 +466,8 @@ int leann_attention(leann_ctx *ctx, const leann_attention_plan *plan, const void
  * over the heads that share a key head), dbias fp32[buckets][heads] (NULL: not wanted).  Written, not added to; dq, dk and dv may be slices of one matrix, and must not overlap
  * each other or an input (LEANN_EINVAL).  No atomics in memory: the bits repeat, and a sequence's dq, dk and dv do not depend on the others.
  * A query or key that is infinite or NaN makes NaN of the gradients of the keys or queries that it meets and of no others.
- * Workspace: 8 bytes per query and head; with dbias 4 (2 distance + 1) more per head and 128 queries (of every sequence), distance no more than the sequences' longest. */
+ * Workspace: 8 bytes per query and head; with dbias 4 (2 distance + 1) more per head and 128 queries (of every sequence), distance no more than the sequences' longest;
+ * where keys have their queries split (a few that all of a long sequence see), 256 * 32, 64 or 128 floats per part and key head. */
 int leann_attention_backward(leann_ctx *ctx, const leann_attention_plan *plan, const void *dout_dev, int64_t ldd, const void *q_dev, int64_t ldq, const void *k_dev, int64_t ldk,
                              const void *v_dev, int64_t ldv, const void *out_dev, int64_t ldo, const float *lse_dev, int dtype, float scale, const float *bias_dev, void *dq_dev,
                              int64_t lddq, void *dk_dev, int64_t lddk, void *dv_dev, int64_t lddv, float *dbias_dev);

@@ -4,6 +4,7 @@
 #include "rows.h"
 
 constexpr int ATT_MOST_DISTANCE = 1024;
+constexpr float ATT_LEAST_SCALE = 0x1p-20f, ATT_MOST_SCALE = 0x1p20f;
 constexpr int64_t ATT_MOST_LD = (int64_t)1 << 23;  // 64 rows are within a buffer's 2^31 bytes
 constexpr int ATT_EXT = 96;  // a wavefront's 32 rows and 64 of the other side have relative positions in a range of 95
 
@@ -15,11 +16,11 @@ struct leann_attention_plan {
     int32_t left = -1, right = -1, sinks = 0;  // as the kernels take them: no limit is a bound behind every position
     int32_t distance = 0, buckets = 0;         // distance: of the table below, no longer than the sequences make it
     int32_t query_waves = 0;                   // wavefronts of a forward block, 32 queries each
-    int32_t n_items = 0, n_grad_items = 0, n_key_items = 0, n_joins = 0, n_slots = 0, n_grad_tiles = 0;
+    int32_t n_items = 0, n_grad_items = 0, n_key_items = 0, n_joins = 0, n_slots = 0, n_grad_tiles = 0, n_key_joins = 0, n_key_slots = 0;
     DevBuf mem;
     const AttentionTile *tiles = nullptr, *grad_tiles = nullptr, *key_tiles = nullptr;  // of queries, for the gradient of queries, of keys
     const AttentionItem *items = nullptr, *grad_items = nullptr, *key_items = nullptr;
-    const AttentionJoin *joins = nullptr;
+    const AttentionJoin *joins = nullptr, *key_joins = nullptr;
     const int32_t *bucket_of = nullptr;  // [2 distance + 1]
 };
 
@@ -270,14 +271,36 @@ __device__ inline void add_nonfinite(f32x16 (&o)[ND], const T *base, int64_t ld,
     });
 }
 
-// The bias of one head by relative position, times log2 e: [2 distance + 1 + 2 ATT_EXT], the ends repeated.
+// The bias of one head by relative position, in units of the scores before they are scaled, so that the products of queries and keys add to it:
+// [2 distance + 1 + 2 ATT_EXT], the ends repeated.  A finite bias beyond 2^100 counts as 2^100, which scores of any size are lost against: a row of them is
+// even, as it would be in numbers without end, and no difference is one of infinities.
 __device__ inline int bias_entries(int distance) { return 2 * distance + 1 + 2 * ATT_EXT; }
 __device__ inline void make_bias(float *table, const float *bias, const int32_t *bucket_of, const AttentionShape &a, int head)
 {
+    const float inverse = 1.f / __builtin_fabsf(a.scale);
     for (int i = threadIdx.x; i < bias_entries(a.distance); i += blockDim.x) {
         const int d = min(max(i - ATT_EXT, 0), 2 * a.distance);
-        table[i] = bias[(int64_t)bucket_of[d] * a.heads + head] * LOG2E;
+        const float b = bias[(int64_t)bucket_of[d] * a.heads + head];
+        table[i] = (__builtin_fabsf(b) < INFINITY ? __builtin_fmaxf(__builtin_fminf(b, 0x1p100f), -0x1p100f) : b) * inverse;
     }
+}
+
+// The scale's sign goes into the queries.
+template <class V8, int NS>
+__device__ inline void take_sign(V8 (&f)[NS], float scale)
+{
+    const uint32_t flip = scale < 0.f ? 0x80008000u : 0u;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) f[s] = __builtin_bit_cast(V8, __builtin_bit_cast(u32x4, f[s]) ^ flip);
+}
+
+// Which of 64 keys hide from some of the wavefront's queries: those behind a query's last one, those before its first one, or neither.
+struct Edges {
+    bool behind, before;
+};
+__device__ inline Edges edges(const AttentionShape &a, int p, int queries, int j, int keys)
+{
+    return {j + keys - 1 > p + a.right || keys < ATT_STEP, j < p + queries - 1 - a.left && j + keys > a.sinks};
 }
 
 // What `queries` queries at positions from p on see of `keys` keys from key j on: nothing, or all of them.

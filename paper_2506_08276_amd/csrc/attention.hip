@@ -6,13 +6,14 @@
 
 #include "adapter_plan.h"
 #include "attention.h"
+#include "wave.h"
 
 namespace {
 
 // ------------------------------------------------------------------ forward
 // A block takes NW * 32 queries of one head through their keys, 64 at a time; a wavefront has 32 queries.  S^T = K Q^T, so that a lane owns one query: its maximum and sum
-// run over its own registers, the other half of the keys is lane ^ 32's.  One pass: s = scale q.k + bias in units of log 2, m the largest so far, l = sum 2^(s - m),
-// O = sum 2^(s - m) v, l and O scaled when m grows.  P^T, rounded to the inputs' type (an error of half a step in each term, as the inputs themselves have), is the
+// run over its own registers, the other half of the keys is lane ^ 32's.  The bias is what the products are added to.  One pass: m the largest score so far, l = sum of
+// weights 2^(scale log2 e (s - m)), O = sum of weights times v, l and O scaled when m grows.  P^T, rounded to the inputs' type (an error of half a step in each term, as the inputs themselves have), is the
 // other operand of O^T = V^T P^T without leaving its registers, see column_operand.
 // K and V tiles go from memory to LDS without registers, STAGES - 1 tiles ahead.
 template <int DP, int NW>
@@ -67,7 +68,8 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : 1) void at
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[dt][r] = 0.f;
     float m = -INFINITY, l = 0.f;
-    const float scale2 = a.scale * LOG2E;
+    take_sign(qf, a.scale);
+    const float scale2 = __builtin_fabsf(a.scale) * LOG2E;
     const int p = p0 + l32;
 
     int stage = 0;
@@ -84,13 +86,33 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : 1) void at
         if (see.none) continue;
 
         f32x16 s[2];
+        float c = 0.f;  // added to all of the tile's scores
+        if (BIAS) {
+            const int least = j0 - (p0 + 31), most = j0 + ATT_STEP - 1 - p0;  // relative positions
+            const bool near = most > -a.distance && least < a.distance;
+            if (near) {
+                const float *at = table + (j0 + 4 * half - p + a.distance + ATT_EXT);
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt) {
+                for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[kt][r] = 0.f;
+                    for (int r = 0; r < 16; ++r) s[kt][r] = at[kt * 32 + acc_row(r)];
+            } else {
+                c = table[most <= -a.distance ? 0 : bias_entries(a.distance) - 1];
+#pragma unroll
+                for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[kt][r] = 0.f;
+            }
+        } else {
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[kt][r] = 0.f;
+        }
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
             for (int i = 0; i < NS; ++i) s[kt] = att_mfma(row_operand<T, DP>(Kt, kt * 32, i, lane), qf[i], s[kt]);
-        }
         V8 vf[2][ND];  // of the first 32 keys, on their way while the scores become weights
 #pragma unroll
         for (int w = 0; w < 2; ++w)
@@ -98,51 +120,32 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : 1) void at
             for (int dt = 0; dt < ND; ++dt) vf[w][dt] = column_operand<T, DP>(Vt, w * 16, dt * 32, lane);
         // register r of tile kt is key j0 + 32 kt + 4 half + acc_row(r)
         const int j = j0 + 4 * half;
-        if (BIAS) {
-            const int least = j0 - (p0 + 31), most = j0 + ATT_STEP - 1 - p0;  // relative positions
-            if (most <= -a.distance || least >= a.distance) {
-                const float c = table[most <= -a.distance ? 0 : bias_entries(a.distance) - 1];
-#pragma unroll
-                for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) s[kt][r] = fmaf(s[kt][r], scale2, c);
-            } else {
-                const float *at = table + (j - p + a.distance + ATT_EXT);
-#pragma unroll
-                for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) s[kt][r] = fmaf(s[kt][r], scale2, at[kt * 32 + acc_row(r)]);
-            }
-        } else {
-#pragma unroll
-            for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[kt][r] *= scale2;
-        }
-        if (!see.all) {
-            const int most = min(t.others - 1, p + a.right) - j, least = p - a.left - j, sinks = a.sinks - j;
-#pragma unroll
-            for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int c = kt * 32 + acc_row(r);
-                    s[kt][r] = (c > most) | ((c < least) & (c >= sinks)) ? -INFINITY : s[kt][r];
-                }
-        } else if (keys < ATT_STEP) {
-            const int most = keys - 1 - 4 * half;
+        const Edges e = edges(a, p0, my_rows, j0, keys);
+        if (e.behind) {
+            const int most = min(t.others - 1, p + a.right) - j;
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[kt][r] = kt * 32 + acc_row(r) > most ? -INFINITY : s[kt][r];
         }
-        float top = m;
+        if (e.before) {
+            const int least = p - a.left - j, sinks = a.sinks - j;
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int key = kt * 32 + acc_row(r);
+                    s[kt][r] = (key < least) & (key >= sinks) ? -INFINITY : s[kt][r];
+                }
+        }
+        float top = s[0][0];
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
             for (int r = 0; r < 16; ++r) top = __builtin_fmaxf(top, s[kt][r]);
-        top = both_halves_max(top);
+        top = __builtin_fmaxf(m, both_halves_max(top) + c);
         if (__ballot(top != m)) {  // else no lane's maximum grew
-            const float alpha = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - top);
+            const float alpha = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - top) * scale2);
             m = top;
             l *= alpha;
 #pragma unroll
@@ -150,12 +153,12 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : 1) void at
 #pragma unroll
                 for (int r = 0; r < 16; ++r) o[dt][r] *= alpha;
         }
-        const float base = m == -INFINITY ? 0.f : m;
+        const float base = m == -INFINITY ? 0.f : (c - m) * scale2;
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                s[kt][r] = __builtin_amdgcn_exp2f(s[kt][r] - base);
+                s[kt][r] = __builtin_amdgcn_exp2f(fmaf(s[kt][r], scale2, base));
                 l += s[kt][r];
             }
         bool taken_out = false;
@@ -202,50 +205,58 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : 1) void at
                     for (int i = 0; i < 4; ++i) x[i] = o[dt][4 * c + i];
                     *reinterpret_cast<f32x4 *>(part_o + at * DP + dt * 32 + 8 * c + 4 * half) = x;
                 }
-            if (half == 0) part_ml[at] = make_float2(m, l);
+            if (half == 0) part_ml[at] = make_float2(m * scale2, l);
         }
         return;
     }
-    if (valid && half == 0 && lse) lse[(int64_t)h * Tq + my_row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * LN2;
+    if (valid && half == 0 && lse) lse[(int64_t)h * Tq + my_row] = l == 0.f ? -INFINITY : fmaf(m, scale2, __builtin_amdgcn_logf(l)) * LN2;
     store_columns<T, ND>(o, l == 0.f ? 0.f : 1.f / l, out + (int64_t)my_row * ldo + h * a.dim, valid, a.dim, lane);
 }
 
-// The parts of split rows: m the largest, l and O summed under it in the parts' order.  A thread has eight elements of one row of one head.
-template <class T>
-__global__ __launch_bounds__(256) void join_kernel(const AttentionJoin *__restrict__ joins, int heads, int dim, int DP, int block_rows, const float *__restrict__ part_o,
+// The parts of split rows: m the largest, l and O summed under it.  A wavefront has one row of one head; its lanes have the parts in turn for m and l, and for O the row's
+// pieces of eight elements of every 8th part (of DP 32: 16th, 128: 4th), added up over the lanes at the end: the order is the same in every call.
+template <class T, int DP>
+__global__ __launch_bounds__(256) void join_kernel(const AttentionJoin *__restrict__ joins, int heads, int dim, int block_rows, const float *__restrict__ part_o,
                                                    const float2 *__restrict__ part_ml, T *__restrict__ out, int64_t ldo, float *__restrict__ lse, int64_t Tq)
 {
+    constexpr int CH = DP / 8, GROUPS = 64 / CH;
     const AttentionJoin jn = joins[blockIdx.x];
-    const int h = blockIdx.y, chunks = dim / 8;
-    for (int i = threadIdx.x; i < jn.rows * chunks; i += 256) {
-        const int row = i / chunks, c = i % chunks;
+    const int h = blockIdx.y, lane = threadIdx.x & 63, c = lane % CH, group = lane / CH;
+    for (int row = threadIdx.x >> 6; row < jn.rows; row += 4) {
         auto at = [&](int s) { return ((int64_t)(jn.slot0 + s) * heads + h) * block_rows + row; };
         float m = -INFINITY;
-        for (int s = 0; s < jn.slots; ++s) {
-            const float ms = part_ml[at(s)].x;
-            if (!(ms <= m)) m = ms;  // NaN stays
-        }
+        for (int s = lane; s < jn.slots; s += 64) m = __builtin_fmaxf(m, part_ml[at(s)].x);
+#pragma unroll
+        for (int i = 32; i; i >>= 1) m = __builtin_fmaxf(m, __shfl_xor(m, i));
+        auto weight = [&](float2 ml) { return ml.x == -INFINITY && ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml.x - (m == -INFINITY ? 0.f : m)); };
         float l = 0.f;
-        f32x8 o = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        for (int s = 0; s < jn.slots; ++s) {
+        for (int s = lane; s < jn.slots; s += 64) {
             const float2 ml = part_ml[at(s)];
-            const float w = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - m);
-            l = fmaf(w, ml.y, l);
+            l = fmaf(weight(ml), ml.y, l);
+        }
+        l = wave_sum(l);
+        f32x8 o = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        for (int s = group; s < jn.slots; s += GROUPS) {
+            const float2 ml = part_ml[at(s)];
             const f32x4 *p = reinterpret_cast<const f32x4 *>(part_o + at(s) * DP + c * 8);
             const f32x4 x = p[0], y = p[1];
-            if (ml.x != -INFINITY || ml.y != 0.f) {
+            const float w = weight(ml);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    o[e] = fmaf(w, x[e], o[e]);
-                    o[4 + e] = fmaf(w, y[e], o[4 + e]);
-                }
+            for (int e = 0; e < 4; ++e) {
+                o[e] = fmaf(w, x[e], o[e]);
+                o[4 + e] = fmaf(w, y[e], o[4 + e]);
             }
         }
-        const float factor = l == 0.f ? 0.f : 1.f / l;
-        Raw8<T> r;
-        r.round(o * factor);
-        r.store(out + (int64_t)(jn.row0 + row) * ldo + h * dim + c * 8, 8);
-        if (c == 0 && lse) lse[(int64_t)h * Tq + jn.row0 + row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * LN2;
+#pragma unroll
+        for (int i = CH; i < 64; i <<= 1)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[e] += __shfl_xor(o[e], i);
+        if (group == 0 && c * 8 < dim) {
+            Raw8<T> r;
+            r.round(o * (l == 0.f ? 0.f : 1.f / l));
+            r.store(out + (int64_t)(jn.row0 + row) * ldo + h * dim + c * 8, 8);
+        }
+        if (lane == 0 && lse) lse[(int64_t)h * Tq + jn.row0 + row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * LN2;
     }
 }
 
@@ -274,7 +285,7 @@ int launch_attend(leann_ctx *ctx, const leann_attention_plan *p, const Attention
     hipLaunchKernelGGL((attend_kernel<T, DP, NW, BIAS>), dim3(p->n_items), dim3(NW * 64), smem, ctx->stream, p->items, p->tiles, a, q, ldq, k, ldk, v, ldv, bias,
                        p->bucket_of, out, ldo, lse, p->Tq, part_o, part_ml);
     if (p->n_joins)
-        hipLaunchKernelGGL(join_kernel<T>, dim3(p->n_joins, p->heads), dim3(256), 0, ctx->stream, p->joins, p->heads, p->dim, DP, NW * 32, part_o, part_ml, out, ldo, lse,
+        hipLaunchKernelGGL((join_kernel<T, DP>), dim3(p->n_joins, p->heads), dim3(256), 0, ctx->stream, p->joins, p->heads, p->dim, NW * 32, part_o, part_ml, out, ldo, lse,
                            p->Tq);
     return att_launched("leann_attention");
 }
@@ -298,29 +309,28 @@ int make_plan(leann_ctx *ctx, const int32_t *q_rows, const int32_t *k_rows, cons
     p->query_waves = longest <= 32 ? 1 : 4;
     std::vector<AttentionTile> tiles, grad_tiles, key_tiles;
     std::vector<int32_t> of, grad_of, key_of;
-    std::vector<AttentionJoin> joins, none;
-    att_make_tiles(r, n, q_rows, k_rows, first, false, p->query_waves * 32, 0, tiles, of, joins);
+    std::vector<AttentionJoin> joins, key_joins, none;
+    const int share = p->heads / p->kv_heads, cus = ctx->num_cus;
+    att_make_tiles(r, n, q_rows, k_rows, first, false, share, p->query_waves * 32, 0, tiles, of, joins);
     // Keys are split where there are fewer than two blocks per compute unit, into parts that make four, of four tiles at least: each costs a block's start and its
     // sums' way through memory.
-    if ((int64_t)tiles.size() * p->heads < 2 * ctx->num_cus) {
-        int64_t work = 0, most = 0;
-        for (const AttentionTile &t : tiles) {
-            work += t.end - t.begin;
-            most = std::max<int64_t>(most, t.end - t.begin);
-        }
-        const int64_t split = std::max<int64_t>(4, (work * p->heads + 4 * ctx->num_cus - 1) / (4 * ctx->num_cus));
-        if (2 * most > 3 * split) {
+    if ((int64_t)tiles.size() * p->heads < 2 * cus)
+        if (const int split = att_split(tiles, p->heads, cus, 4, 4)) {
             tiles.clear();
-            att_make_tiles(r, n, q_rows, k_rows, first, false, p->query_waves * 32, (int)split, tiles, of, joins);
+            att_make_tiles(r, n, q_rows, k_rows, first, false, share, p->query_waves * 32, split, tiles, of, joins);
         }
-    }
     for (const AttentionJoin &j : joins) p->n_slots += j.slots;
-    att_make_tiles(r, n, q_rows, k_rows, first, false, 128, 0, grad_tiles, grad_of, none);
-    att_make_tiles(r, n, q_rows, k_rows, first, true, 128, 0, key_tiles, key_of, none);
-    const int share = p->heads / p->kv_heads;
+    att_make_tiles(r, n, q_rows, k_rows, first, false, share, 128, 0, grad_tiles, grad_of, none);
+    // Keys that many queries see, as a sequence's first ones, have their queries split, so that no block has much more than a compute unit's share of the work.
+    att_make_tiles(r, n, q_rows, k_rows, first, true, share, 128, 0, key_tiles, key_of, key_joins);
+    if (const int split = att_split(key_tiles, p->kv_heads, cus, 1, 16)) {
+        key_tiles.clear();
+        att_make_tiles(r, n, q_rows, k_rows, first, true, share, 128, split, key_tiles, key_of, key_joins);
+    }
+    for (const AttentionJoin &j : key_joins) p->n_key_slots += j.slots;
     const std::vector<AttentionItem> items = att_order(tiles, of, p->heads, share), grad_items = att_order(grad_tiles, grad_of, p->heads, share),
                                      key_items = att_order(key_tiles, key_of, p->kv_heads, 1);
-    if (std::max({items.size(), grad_items.size(), key_items.size(), joins.size()}) > ((size_t)1 << 24) - 1) {
+    if (std::max({items.size(), grad_items.size(), key_items.size(), joins.size(), key_joins.size()}) > ((size_t)1 << 24) - 1) {
         leann_set_error("leann_attention_create: sequences of this number and length are not covered (more than 2^24 - 1 workgroups in a launch)");
         return LEANN_ESHAPE;
     }
@@ -328,6 +338,7 @@ int make_plan(leann_ctx *ctx, const int32_t *q_rows, const int32_t *k_rows, cons
     p->n_grad_items = (int32_t)grad_items.size();
     p->n_key_items = (int32_t)key_items.size();
     p->n_joins = (int32_t)joins.size();
+    p->n_key_joins = (int32_t)key_joins.size();
     p->n_grad_tiles = (int32_t)grad_tiles.size();
     std::vector<int32_t> buckets;
     if (bucket_of) {  // no longer than the sequences
@@ -341,7 +352,7 @@ int make_plan(leann_ctx *ctx, const int32_t *q_rows, const int32_t *k_rows, cons
         if (bytes) memcpy(image.data() + at, v.data(), bytes);
         return at;
     };
-    const size_t at[8] = {put(tiles), put(grad_tiles), put(key_tiles), put(items), put(grad_items), put(key_items), put(joins), put(buckets)};
+    const size_t at[9] = {put(tiles), put(grad_tiles), put(key_tiles), put(items), put(grad_items), put(key_items), put(joins), put(key_joins), put(buckets)};
     LEANN_TRY(ctx->reserve(p->mem, std::max<size_t>(image.size(), 1)));
     if (!image.empty()) LEANN_HIP(hipMemcpyAsync(p->mem.p, image.data(), image.size(), hipMemcpyHostToDevice, ctx->stream));
     LEANN_HIP(hipStreamSynchronize(ctx->stream));
@@ -353,7 +364,8 @@ int make_plan(leann_ctx *ctx, const int32_t *q_rows, const int32_t *k_rows, cons
     p->grad_items = (const AttentionItem *)(base + at[4]);
     p->key_items = (const AttentionItem *)(base + at[5]);
     p->joins = (const AttentionJoin *)(base + at[6]);
-    p->bucket_of = (const int32_t *)(base + at[7]);
+    p->key_joins = (const AttentionJoin *)(base + at[7]);
+    p->bucket_of = (const int32_t *)(base + at[8]);
     return LEANN_OK;
 }
 
@@ -386,8 +398,8 @@ int att_check_call(const char *call, const leann_ctx *ctx, const leann_attention
         leann_set_error("%s: the plan belongs to another device", call);
         return LEANN_EINVAL;
     }
-    if (!(fabsf(scale) < INFINITY) || !bias_dev != !plan->buckets) {
-        leann_set_error("%s: scale is not finite, or there is a bias without buckets or buckets without a bias", call);
+    if (!(fabsf(scale) >= ATT_LEAST_SCALE && fabsf(scale) <= ATT_MOST_SCALE) || !bias_dev != !plan->buckets) {
+        leann_set_error("%s: a scale whose magnitude is outside 2^-20 to 2^20, or a bias without buckets or buckets without a bias", call);
         return LEANN_EINVAL;
     }
     return LEANN_OK;

@@ -109,7 +109,7 @@ __device__ inline void add_diagonals(const f32x16 (&d)[2], bool valid, float *ro
 }
 
 // A block takes 128 queries of one head through their keys, as the forward pass does.  S^T and dP^T = V dO^T have a query per lane; dS^T, rounded, is the other operand of
-// dQ^T = K^T dS^T.  It leaves what the other kernel needs of each query: the log-sum in units of log 2 and delta.
+// dQ^T = K^T dS^T.  It leaves what the other kernel needs of each query: the log-sum in units of log 2 and delta, both negative.
 // The bias's gradient is summed by relative position, each wavefront into an array of its own in LDS, so that the order of the additions is the program's.  Tiles
 // behind `distance` add to one place, in a register.
 template <class T, int DP, bool BIAS>
@@ -167,16 +167,20 @@ __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void query_grad
 #pragma unroll
         for (int i = 0; i < 8; ++i) my_delta = fmaf((float)gf[s][i], (float)of[s][i], my_delta);
     my_delta = both_halves_sum(my_delta);
-    if (valid && half == 0) stats[(int64_t)h * Tq + my_row] = make_float2(my_lse, my_delta);
+    if (valid && half == 0) stats[(int64_t)h * Tq + my_row] = make_float2(-my_lse, -my_delta);
 
     f32x16 acc[ND];
 #pragma unroll
     for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[dt][r] = 0.f;
+    f32x16 minus_delta;  // what the products dO V^T are added to
+#pragma unroll
+    for (int r = 0; r < 16; ++r) minus_delta[r] = -my_delta;
     float factor = 1.f, behind = 0.f, ahead = 0.f;
     bool hurt = false;  // sees a key that is not finite
-    const float scale2 = a.scale * LOG2E;
+    take_sign(qf, a.scale);
+    const float scale2 = __builtin_fabsf(a.scale) * LOG2E;
     const int p = p0 + l32;
 
     int stage = 0;
@@ -193,10 +197,26 @@ __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void query_grad
         if (see.none) continue;
 
         f32x16 s[2], d[2];
+        const int j = j0 + 4 * half;
+        const int least = j0 - (p0 + 31), most = j0 + ATT_STEP - 1 - p0;  // relative positions
+        const bool near = most > -a.distance && least < a.distance;
+        float c = -my_lse;
+        if (BIAS && near) {
+            const float *at = table + (j - p + a.distance + ATT_EXT);
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[kt][r] = at[kt * 32 + acc_row(r)];
+        } else {
+            if (BIAS) c = fmaf(table[most <= -a.distance ? 0 : entries - 1], scale2, c);
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[kt][r] = 0.f;
+        }
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s[kt][r] = d[kt][r] = 0.f;
+            d[kt] = minus_delta;
 #pragma unroll
             for (int i = 0; i < NS; ++i) {
                 s[kt] = att_mfma(row_operand<T, DP>(Kt, kt * 32, i, lane), qf[i], s[kt]);
@@ -208,42 +228,28 @@ __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void query_grad
         for (int w = 0; w < 2; ++w)
 #pragma unroll
             for (int dt = 0; dt < ND; ++dt) kf[w][dt] = column_operand<T, DP>(Kt, w * 16, dt * 32, lane);
-        const int j = j0 + 4 * half;
-        const int least = j0 - (p0 + 31), most = j0 + ATT_STEP - 1 - p0;  // relative positions
-        const bool near = most > -a.distance && least < a.distance;
-        if (BIAS && near) {
-            const float *at = table + (j - p + a.distance + ATT_EXT);
-#pragma unroll
-            for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[kt][r] = fmaf(s[kt][r], scale2, at[kt * 32 + acc_row(r)] - my_lse);
-        } else {
-            const float c = (BIAS ? table[most <= -a.distance ? 0 : entries - 1] : 0.f) - my_lse;
-#pragma unroll
-            for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[kt][r] = fmaf(s[kt][r], scale2, c);
-        }
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) d[kt][r] = __builtin_amdgcn_exp2f(s[kt][r]) * (d[kt][r] - my_delta);
+            for (int r = 0; r < 16; ++r) d[kt][r] *= __builtin_amdgcn_exp2f(fmaf(s[kt][r], scale2, c));
         // what is hidden is a choice, not a product; keys behind the last one are zeros, which add nothing to dQ
-        if (!see.all) {
-            const int last = min(t.others - 1, p + a.right) - j, from = p - a.left - j, sinks = a.sinks - j;
-#pragma unroll
-            for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int c = kt * 32 + acc_row(r);
-                    d[kt][r] = (c > last) | ((c < from) & (c >= sinks)) ? 0.f : d[kt][r];
-                }
-        } else if (BIAS && keys < ATT_STEP) {
-            const int last = keys - 1 - 4 * half;
+        const Edges e = edges(a, p0, my_rows, j0, keys);
+        if (e.behind && (BIAS || !see.all)) {
+            const int last = min(t.others - 1, p + a.right) - j;
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) d[kt][r] = kt * 32 + acc_row(r) > last ? 0.f : d[kt][r];
+        }
+        if (e.before) {
+            const int from = p - a.left - j, sinks = a.sinks - j;
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int key = kt * 32 + acc_row(r);
+                    d[kt][r] = (key < from) & (key >= sinks) ? 0.f : d[kt][r];
+                }
         }
         if (BIAS && by_position) {
             if (near) {
@@ -328,7 +334,7 @@ template <class T, int DP, bool BIAS>
 __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void key_grad_kernel(
     const AttentionItem *__restrict__ items, const AttentionTile *__restrict__ tiles, AttentionShape a, const T *__restrict__ dout, int64_t ldd, const T *__restrict__ q,
     int64_t ldq, const T *__restrict__ k, int64_t ldk, const T *__restrict__ v, int64_t ldv, const float2 *__restrict__ stats, int64_t Tq, const float *__restrict__ bias,
-    const int32_t *__restrict__ bucket_of, T *__restrict__ dk, int64_t lddk, T *__restrict__ dv, int64_t lddv)
+    const int32_t *__restrict__ bucket_of, T *__restrict__ dk, int64_t lddk, T *__restrict__ dv, int64_t lddv, float *__restrict__ parts)
 {
     typedef typename Half8<T>::type V8;
     typedef GradCfg<DP> Cfg;
@@ -359,7 +365,7 @@ __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void key_grad_k
     struct At {
         int h, tile;
     };
-    const int per_head = t.end - t.begin, total = per_head * a.share, last_tile = t.first_tile + per_head - 1;
+    const int total = t.end - t.begin, last_tile = t.first_tile + t.per_head - 1;
     auto behind = [&](At at) { return at.tile == last_tile ? At{at.h + 1, t.first_tile} : At{at.h, at.tile + 1}; };
     auto request = [&](At at, int stage) {
         const int i0 = at.tile * ATT_STEP;
@@ -372,7 +378,9 @@ __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void key_grad_k
         qr.request(q + (int64_t)(t.other0 + i0) * ldq + at.h * a.dim, ldq, t.others - i0, a.dim, Qs + stage * TILE, wave);
         gr.request(dout + (int64_t)(t.other0 + i0) * ldd + at.h * a.dim, ldd, t.others - i0, a.dim, Gs + stage * TILE, wave);
     };
-    At now = {g * a.share, t.first_tile}, next = now;
+    At now = {g * a.share, t.first_tile};
+    if (total) now = At{now.h + t.begin / t.per_head, now.tile + t.begin % t.per_head};
+    At next = now;
 #pragma unroll
     for (int i = 0; i < STAGES - 1; ++i)
         if (i < total) {
@@ -387,7 +395,8 @@ __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void key_grad_k
         for (int r = 0; r < 16; ++r) dk_acc[dt][r] = dv_acc[dt][r] = 0.f;
     float factor = 1.f;
     bool hurt = false;
-    const float scale2 = a.scale * LOG2E;
+    take_sign(kf, a.scale);
+    const float scale2 = __builtin_fabsf(a.scale) * LOG2E;
     int stage = 0, of_table = -1;
     for (int n = 0; n < total; ++n, now = behind(now)) {
         const int h = now.h, i0 = now.tile * ATT_STEP;
@@ -415,8 +424,26 @@ __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void key_grad_k
 #pragma unroll
         for (int qs = 0; qs < 2; ++qs) {
             f32x16 s[1], d[1];
+            // register r is query i0 + 32 qs + 4 half + acc_row(r); queries behind the last one have rows of zeros and any numbers
+            const int from = i0 + qs * 32 + 4 * half, p = t.first + from;
+            float ls[16];
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[0][r] = d[0][r] = 0.f;
+            for (int c = 0; c < 8; ++c) {  // -lse, and -delta, to which the products dO V^T are added
+                const f32x4 x = *reinterpret_cast<const f32x4 *>(nt + 2 * (qs * 32 + 4 * half + 8 * (c >> 1) + 2 * (c & 1)));
+                ls[2 * c] = x[0], d[0][2 * c] = x[1], ls[2 * c + 1] = x[2], d[0][2 * c + 1] = x[3];
+            }
+            const int pw = t.first + i0 + qs * 32, least = jw - (pw + 31), most = jw + 31 - pw;
+            const bool near = most > -a.distance && least < a.distance;
+            float c = 0.f;
+            if (BIAS && near) {
+                const float *at = table + (j - p + a.distance + ATT_EXT);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[0][r] = at[-acc_row(r)];
+            } else {
+                if (BIAS) c = table[most <= -a.distance ? 0 : bias_entries(a.distance) - 1] * scale2;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[0][r] = 0.f;
+            }
 #pragma unroll
             for (int i = 0; i < NS; ++i) {
                 s[0] = att_mfma(row_operand<T, DP>(Qt, qs * 32, i, lane), kf[i], s[0]);
@@ -428,33 +455,14 @@ __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void key_grad_k
                 gc[dt] = column_operand<T, DP>(Gt, qs * 32, dt * 32, lane);
                 qc[dt] = column_operand<T, DP>(Qt, qs * 32, dt * 32, lane);
             }
-            // register r is query i0 + 32 qs + 4 half + acc_row(r); queries behind the last one have rows of zeros and any numbers
-            const int from = i0 + qs * 32 + 4 * half, p = t.first + from;
-            float ls[16], de[16];
+            if (BIAS && !near) {
 #pragma unroll
-            for (int c = 0; c < 8; ++c) {
-                const f32x4 x = *reinterpret_cast<const f32x4 *>(nt + 2 * (qs * 32 + 4 * half + 8 * (c >> 1) + 2 * (c & 1)));
-                ls[2 * c] = x[0], de[2 * c] = x[1], ls[2 * c + 1] = x[2], de[2 * c + 1] = x[3];
-            }
-            if (BIAS) {
-                const int pw = t.first + i0 + qs * 32, least = jw - (pw + 31), most = jw + 31 - pw;
-                if (most > -a.distance && least < a.distance) {
-                    const float *at = table + (j - p + a.distance + ATT_EXT);
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) s[0][r] = fmaf(s[0][r], scale2, at[-acc_row(r)] - ls[r]);
-                } else {
-                    const float c = table[most <= -a.distance ? 0 : bias_entries(a.distance) - 1];
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) s[0][r] = fmaf(s[0][r], scale2, c - ls[r]);
-                }
-            } else {
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[0][r] = fmaf(s[0][r], scale2, -ls[r]);
+                for (int r = 0; r < 16; ++r) ls[r] += c;
             }
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                s[0][r] = __builtin_amdgcn_exp2f(s[0][r]);
-                d[0][r] = s[0][r] * (d[0][r] - de[r]);
+                s[0][r] = __builtin_amdgcn_exp2f(fmaf(s[0][r], scale2, ls[r]));
+                d[0][r] *= s[0][r];
             }
             if (!see.all) {
                 const int count = t.others - from, first = j - a.right - p, last = j < a.sinks ? ATT_STEP : j + a.left - p;
@@ -511,17 +519,58 @@ __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void key_grad_k
         }
     }
     if (hurt) factor = __builtin_nanf("");
-    store_columns<T, ND>(dk_acc, a.scale / factor * (F16 ? 0x1p-15f : 1.f), dk + my_row * lddk + g * a.dim, valid, a.dim, lane);
-    store_columns<T, ND>(dv_acc, F16 ? 0x1p-15f : 1.f, dv + my_row * lddv + g * a.dim, valid, a.dim, lane);
+    const float dk_factor = a.scale / factor * (F16 ? 0x1p-15f : 1.f), dv_factor = F16 ? 0x1p-15f : 1.f;
+    if (t.slot >= 0) {  // a part of the queries: [slot][key head][dK, dV][128][DP]
+        float *to = parts + ((((int64_t)t.slot * (a.heads / a.share) + g) * 2) * GRAD_WAVES * 32 + wave * 32 + l32) * DP + 4 * half;
+        if (valid)
+#pragma unroll
+            for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    f32x4 x, y;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[e] = dk_acc[dt][4 * c + e] * dk_factor, y[e] = dv_acc[dt][4 * c + e] * dv_factor;
+                    *reinterpret_cast<f32x4 *>(to + dt * 32 + 8 * c) = x;
+                    *reinterpret_cast<f32x4 *>(to + GRAD_WAVES * 32 * DP + dt * 32 + 8 * c) = y;
+                }
+        return;
+    }
+    store_columns<T, ND>(dk_acc, dk_factor, dk + my_row * lddk + g * a.dim, valid, a.dim, lane);
+    store_columns<T, ND>(dv_acc, dv_factor, dv + my_row * lddv + g * a.dim, valid, a.dim, lane);
+}
+
+// dK and dV of keys whose queries were split: the parts in their order.  A thread has eight elements of one key.
+template <class T>
+__global__ __launch_bounds__(256) void key_join_kernel(const AttentionJoin *__restrict__ joins, int kv_heads, int dim, int DP, const float *__restrict__ parts, T *__restrict__ dk,
+                                                       int64_t lddk, T *__restrict__ dv, int64_t lddv)
+{
+    const AttentionJoin jn = joins[blockIdx.x];
+    const int g = blockIdx.y, which = blockIdx.z, chunks = dim / 8;
+    for (int i = threadIdx.x; i < jn.rows * chunks; i += 256) {
+        const int row = i / chunks, c = i % chunks;
+        const float *p = parts + ((((int64_t)jn.slot0 * kv_heads + g) * 2 + which) * GRAD_WAVES * 32 + row) * DP + c * 8;
+        const int64_t step = (int64_t)kv_heads * 2 * GRAD_WAVES * 32 * DP;
+        f32x8 sum = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+        for (int s = 0; s < jn.slots; ++s) {
+            f32x8 x;
+            __builtin_memcpy(&x, p + s * step, sizeof(x));
+            sum += x;
+        }
+        Raw8<T> r;
+        r.round(sum);
+        r.store((which ? dv + (int64_t)(jn.row0 + row) * lddv : dk + (int64_t)(jn.row0 + row) * lddk) + g * dim + c * 8, 8);
+    }
 }
 
 // Sums of the bias's gradient by relative position over up to POSITION_ROWS tiles each, in their order.
-constexpr int POSITION_ROWS = 32;
+constexpr int POSITION_ROWS = 16;
 __global__ __launch_bounds__(256) void position_sum_kernel(const float *__restrict__ from, int n, int heads, int positions, float *__restrict__ to)
 {
     const int h = blockIdx.y, first = blockIdx.x * POSITION_ROWS, last = min(first + POSITION_ROWS, n);
     for (int i = threadIdx.x; i < positions; i += 256) {
         float sum = 0.f;
+#pragma unroll 8
         for (int r = first; r < last; ++r) sum += from[((int64_t)r * heads + h) * positions + i];
         to[((int64_t)blockIdx.x * heads + h) * positions + i] = sum;
     }
@@ -535,6 +584,7 @@ __global__ __launch_bounds__(1024) void bucket_sum_kernel(const float *__restric
     const int h = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     for (int i = threadIdx.x; i < positions; i += 1024) {
         float sum = 0.f;
+#pragma unroll 8
         for (int r = 0; r < n; ++r) sum += from[((int64_t)r * heads + h) * positions + i];
         sums[i] = sum;
     }
@@ -601,9 +651,11 @@ extern "C" int leann_attention_backward(leann_ctx *ctx, const leann_attention_pl
     const size_t stats_bytes = ((size_t)plan->heads * plan->Tq * sizeof(float2) + 8 + 255) & ~(size_t)255;  // 8: see key_grad_kernel's requests
     const size_t row_bytes = (size_t)plan->heads * positions * sizeof(float);
     std::lock_guard<std::mutex> turn(ctx->op_work_mutex);
-    LEANN_TRY(ctx->reserve(ctx->op_work, std::max<size_t>(1, stats_bytes + (dbias_dev ? row_bytes * (n + groups) : 0))));
+    const int DP = plan->dim <= 32 ? 32 : plan->dim <= 64 ? 64 : 128;
+    const size_t part_bytes = (size_t)plan->n_key_slots * plan->kv_heads * 2 * GRAD_WAVES * 32 * DP * sizeof(float);
+    LEANN_TRY(ctx->reserve(ctx->op_work, stats_bytes + part_bytes + (dbias_dev ? row_bytes * (n + groups) : 0)));
     float2 *stats = (float2 *)ctx->op_work.p;
-    float *by_position = dbias_dev ? (float *)((char *)ctx->op_work.p + stats_bytes) : nullptr;
+    float *parts = (float *)((char *)ctx->op_work.p + stats_bytes), *by_position = dbias_dev ? (float *)((char *)parts + part_bytes) : nullptr;
     auto go = [&](auto *type, auto dp, auto with_bias) {
         typedef std::remove_pointer_t<decltype(type)> T;
         constexpr int DP = decltype(dp)::value;
@@ -619,7 +671,10 @@ extern "C" int leann_attention_backward(leann_ctx *ctx, const leann_attention_pl
         if (plan->n_key_items)
             hipLaunchKernelGGL((key_grad_kernel<T, DP, BIAS>), dim3(plan->n_key_items), dim3(GRAD_WAVES * 64), Cfg::KEY_TILES + Cfg::KEY_STAGES * Cfg::STATS + table, ctx->stream, plan->key_items,
                                plan->key_tiles, a, (const T *)dout_dev, ldd, (const T *)q_dev, ldq, (const T *)k_dev, ldk, (const T *)v_dev, ldv, stats, plan->Tq,
-                               bias_dev, plan->bucket_of, (T *)dk_dev, lddk, (T *)dv_dev, lddv);
+                               bias_dev, plan->bucket_of, (T *)dk_dev, lddk, (T *)dv_dev, lddv, parts);
+        if (plan->n_key_joins)
+            hipLaunchKernelGGL(key_join_kernel<T>, dim3(plan->n_key_joins, plan->kv_heads, 2), dim3(256), 0, ctx->stream, plan->key_joins, plan->kv_heads, plan->dim, DP, parts,
+                               (T *)dk_dev, lddk, (T *)dv_dev, lddv);
     };
     auto with_type = [&](auto *type) {
         auto with_bias = [&](auto dp) {

@@ -46,12 +46,13 @@ struct AttentionTile {
     int32_t at;                    // position of the first own query; of key tiles, number of the first key
     int32_t first;                 // position of the sequence's first query
     int32_t sink_tiles, first_tile;
-    int32_t begin, end;            // of the tiles on the other side, numbered as in AttentionSpan
-    int32_t slot;                  // where a part of the keys leaves its sums, -1: it has all keys
-    int32_t pad[5];
+    int32_t begin, end;            // of the tiles on the other side, numbered as in AttentionSpan; of key tiles: those of every head that shares the key head, one head after another
+    int32_t slot;                  // where a part of them leaves its sums, -1: the block has all
+    int32_t per_head;              // tiles on the other side
+    int32_t pad[4];
 };
 
-// Rows whose keys were split: the parts' slots.
+// Rows whose other side was split: the parts' slots.
 struct AttentionJoin {
     int32_t row0, rows, slot0, slots;
 };
@@ -60,8 +61,8 @@ struct AttentionItem {
     int32_t tile, head;  // tile -1: nothing to do
 };
 
-// A side's tiles of `block_rows` rows of every sequence, and after them the joins.  split > 0: no block has more than `split` tiles of keys (queries only).
-inline void att_make_tiles(const AttentionRules &r, int n, const int32_t *q_rows, const int32_t *k_rows, const int32_t *first, bool keys, int block_rows,
+// A side's tiles of `block_rows` rows of every sequence, and the joins.  share: heads per key head.  split > 0: no block has more than `split` tiles of the other side.
+inline void att_make_tiles(const AttentionRules &r, int n, const int32_t *q_rows, const int32_t *k_rows, const int32_t *first, bool keys, int share, int block_rows,
                            int split, std::vector<AttentionTile> &tiles, std::vector<int32_t> &tiles_of, std::vector<AttentionJoin> &joins)
 {
     int64_t q0 = 0, k0 = 0;
@@ -82,10 +83,12 @@ inline void att_make_tiles(const AttentionRules &r, int n, const int32_t *q_rows
             t.sink_tiles = span.sink_tiles;
             t.first_tile = span.first_tile;
             t.slot = -1;
-            const int parts = split > 0 ? std::max(1, (span.tiles + split - 1) / split) : 1;
+            t.per_head = span.tiles;
+            const int64_t count = (int64_t)span.tiles * (keys ? share : 1);
+            const int parts = split > 0 ? (int)std::max<int64_t>(1, (count + split - 1) / split) : 1;
             for (int p = 0; p < parts; ++p) {
-                t.begin = (int32_t)((int64_t)span.tiles * p / parts);
-                t.end = (int32_t)((int64_t)span.tiles * (p + 1) / parts);
+                t.begin = (int32_t)(count * p / parts);
+                t.end = (int32_t)(count * (p + 1) / parts);
                 if (parts > 1) t.slot = slots + p;
                 tiles.push_back(t);
             }
@@ -98,6 +101,18 @@ inline void att_make_tiles(const AttentionRules &r, int n, const int32_t *q_rows
         q0 += lq;
         k0 += lk;
     }
+}
+
+// How many tiles a block may have so that parts of the longest ones fill the compute units: `blocks` of them per unit, `least` tiles at least; 0: nothing is long enough.
+inline int att_split(const std::vector<AttentionTile> &tiles, int heads, int cus, int blocks, int least)
+{
+    int64_t work = 0, most = 0;
+    for (const AttentionTile &t : tiles) {
+        work += t.end - t.begin;
+        most = std::max<int64_t>(most, t.end - t.begin);
+    }
+    const int64_t split = std::max<int64_t>(least, (work * heads + blocks * cus - 1) / (blocks * cus));
+    return 2 * most > 3 * split ? (int)std::min<int64_t>(split, 0x7fffffff) : 0;
 }
 
 // In which order blocks take (tile, head).  A sequence's tiles that read the same rows of the other side (all of them, and the heads that share a key head) go to one

@@ -67,7 +67,7 @@ class Sequences:
                 lse[h, rows] = total
                 # A score is a sum of dim products in fp32, scaled, with the bias added and multiplied by log2 e: dim + 6 roundings of 2^-24 of its terms' sum.
                 # The exponential's argument is the difference to the maximum (2 more of the scores), the function good to 2^-22.
-                terms = self.scale * self.q[rows, cq].double().abs().nan_to_num(0, 0, 0) @ self.k[keys, ck].double().abs().nan_to_num(0, 0, 0).t().contiguous()
+                terms = abs(self.scale) * self.q[rows, cq].double().abs().nan_to_num(0, 0, 0) @ self.k[keys, ck].double().abs().nan_to_num(0, 0, 0).t().contiguous()
                 if buckets is not None:
                     terms = terms + self.bias[:, h].double().abs().nan_to_num(0, 0, 0)[buckets]
                 ds = 2 * (self.dim + 8) * 2.0 ** -24 * (torch.where(see, terms, 0).amax(1, keepdim=True) + 1) + 2.0 ** -22
@@ -102,7 +102,7 @@ class Sequences:
                 dk[keys, ck] += self.scale * ds.t().contiguous() @ q
                 dv[keys, ck] += p.t().contiguous() @ g
                 # fp32: the score's error as in forward(), dp's and delta's sums of dim products; then one rounding of P and of dS where they enter products
-                terms = self.scale * q.abs() @ k.abs().t().contiguous()
+                terms = abs(self.scale) * q.abs() @ k.abs().t().contiguous()
                 if buckets is not None:
                     terms = terms + self.bias[:, h].double().abs().nan_to_num(0, 0, 0)[buckets]
                 es = 2 * (self.dim + 8) * 2.0 ** -24 * (terms + 1) + 2.0 ** -22 * (1 + ls.abs().nan_to_num(0, 0, 0)[:, None])
@@ -114,8 +114,8 @@ class Sequences:
                     ep = ep + 2.0 ** -40 * see
                     erow = erow + see * (2.0 ** -40 + 2.0 ** -39 * ds.abs().amax())
                 n = 2.0 ** -24 * (len(q) + len(k))
-                fq[rows, cq] = self.scale * (erow + n * ds.abs()) @ k.abs()
-                fk[keys, ck] += self.scale * (erow + n * ds.abs()).t().contiguous() @ q.abs()
+                fq[rows, cq] = abs(self.scale) * (erow + n * ds.abs()) @ k.abs()
+                fk[keys, ck] += abs(self.scale) * (erow + n * ds.abs()).t().contiguous() @ q.abs()
                 fv[keys, ck] += (ep + n * p).t().contiguous() @ g.abs()
                 if buckets is not None:
                     db[:, h] += torch.zeros(len(db), dtype=torch.float64, device=dev).index_add_(0, buckets.reshape(-1), ds.reshape(-1))
