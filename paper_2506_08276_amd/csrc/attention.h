@@ -167,17 +167,110 @@ __device__ inline typename Half8<T>::type row_operand(const T *lds, int row0, in
 // Operand A of the transposed tile: lane l holds column col0 + l % 32 and, in slots 0..3 and 4..7, the rows row0 + 4 (l / 32) + {0..3} and 8 more: exactly the rows that
 // accumulator registers 8u .. 8u + 7 of a 32x32 product hold (row0 = 16 u), so that those are the other operand as they are.  16 lanes read four rows of 16 elements and
 // get a column of four each.
-template <class T, int DP>
-__device__ inline typename Half8<T>::type column_operand(const T *lds, int row0, int col0, int lane)
+// The reads are written out, each group with its wait behind it: before the builtin's, the compiler waits for every request from memory to LDS that is on its way, the tiles ahead
+// among them (LDS arrays and requests look alike to it).
+template <int FROM>
+__device__ inline void transposed4(const uint32_t (&a)[4], s16x4 (&o)[4])
 {
-    const int i = lane & 15, row = row0 + 4 * (lane >> 5) + (i >> 2), col = col0 + (lane & 16) + 4 * (i & 3);
-    auto read = [&](int r) {
-        const T *p = lds + r * DP + (((col >> 3) ^ att_swizzle<DP>(r)) << 3) + (col & 7);
-        return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)p);
-    };
-    const s16x4 a = read(row), b = read(row + 8);
-    return __builtin_bit_cast(typename Half8<T>::type, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+    asm volatile("ds_read_b64_tr_b16 %0, %4 offset:%8\n\tds_read_b64_tr_b16 %1, %5 offset:%8\n\t"
+                 "ds_read_b64_tr_b16 %2, %6 offset:%8\n\tds_read_b64_tr_b16 %3, %7 offset:%8\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(o[0]), "=&v"(o[1]), "=&v"(o[2]), "=&v"(o[3])
+                 : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "n"(FROM));
 }
+template <int FROM>
+__device__ inline void transposed8(const uint32_t (&a)[8], s16x4 (&o)[8])
+{
+    asm volatile("ds_read_b64_tr_b16 %0, %8 offset:%16\n\tds_read_b64_tr_b16 %1, %9 offset:%16\n\tds_read_b64_tr_b16 %2, %10 offset:%16\n\t"
+                 "ds_read_b64_tr_b16 %3, %11 offset:%16\n\tds_read_b64_tr_b16 %4, %12 offset:%16\n\tds_read_b64_tr_b16 %5, %13 offset:%16\n\t"
+                 "ds_read_b64_tr_b16 %6, %14 offset:%16\n\tds_read_b64_tr_b16 %7, %15 offset:%16\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(o[0]), "=&v"(o[1]), "=&v"(o[2]), "=&v"(o[3]), "=&v"(o[4]), "=&v"(o[5]), "=&v"(o[6]), "=&v"(o[7])
+                 : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "v"(a[4]), "v"(a[5]), "v"(a[6]), "v"(a[7]), "n"(FROM));
+}
+template <int FROM, int NEXT>
+__device__ inline void transposed4_twice(const uint32_t (&a)[4], s16x4 (&o)[8])
+{
+    asm volatile("ds_read_b64_tr_b16 %0, %8 offset:%12\n\tds_read_b64_tr_b16 %1, %9 offset:%12\n\tds_read_b64_tr_b16 %2, %10 offset:%12\n\t"
+                 "ds_read_b64_tr_b16 %3, %11 offset:%12\n\tds_read_b64_tr_b16 %4, %8 offset:%13\n\tds_read_b64_tr_b16 %5, %9 offset:%13\n\t"
+                 "ds_read_b64_tr_b16 %6, %10 offset:%13\n\tds_read_b64_tr_b16 %7, %11 offset:%13\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(o[0]), "=&v"(o[1]), "=&v"(o[2]), "=&v"(o[3]), "=&v"(o[4]), "=&v"(o[5]), "=&v"(o[6]), "=&v"(o[7])
+                 : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "n"(FROM), "n"(NEXT));
+}
+
+template <class T, int DP>
+struct Columns {
+    typedef typename Half8<T>::type V8;
+    static constexpr int ND = DP / 32, GROUP = 16 * DP * 2;  // bytes of 16 rows
+    uint32_t at[2 * ND];                                     // of rows 0 and 8 of each 32 columns
+
+    __device__ inline void init(int lane)
+    {
+#pragma unroll
+        for (int i = 0; i < 2 * ND; ++i) {
+            const int row = 4 * (lane >> 5) + ((lane & 15) >> 2) + 8 * (i & 1), col = (i >> 1) * 32 + (lane & 16) + 4 * (lane & 3);
+            at[i] = (row * DP + (((col >> 3) ^ att_swizzle<DP>(row)) << 3) + (col & 7)) * 2;
+        }
+    }
+    __device__ static inline V8 join(const s16x4 &a, const s16x4 &b) { return __builtin_bit_cast(V8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7)); }
+    __device__ static inline uint32_t place(const T *lds) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const T *)lds; }
+
+    // two groups, rows ROW .. ROW + 15 and the next 16
+    template <int ROW>
+    __device__ inline void two(const T *tile, V8 (&f)[2][ND]) const
+    {
+        constexpr int FROM = ROW / 16 * GROUP;
+        const uint32_t base = place(tile);
+        if constexpr (ND == 1) {
+            const uint32_t a[4] = {base + at[0], base + at[1], base + at[0] + GROUP, base + at[1] + GROUP};
+            s16x4 o[4];
+            transposed4<FROM>(a, o);
+            f[0][0] = join(o[0], o[1]);
+            f[1][0] = join(o[2], o[3]);
+        } else if constexpr (ND == 2) {
+            const uint32_t a[4] = {base + at[0], base + at[1], base + at[2], base + at[3]};
+            s16x4 o[8];
+            transposed4_twice<FROM, FROM + GROUP>(a, o);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f[i >> 1][i & 1] = join(o[2 * i], o[2 * i + 1]);
+        } else {
+            uint32_t a[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) a[i] = base + at[i];
+            s16x4 o[8];
+            transposed8<FROM>(a, o);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f[0][i] = join(o[2 * i], o[2 * i + 1]);
+            transposed8<FROM + GROUP>(a, o);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f[1][i] = join(o[2 * i], o[2 * i + 1]);
+        }
+    }
+    // one group of two tiles, rows ROW .. ROW + 15
+    template <int ROW>
+    __device__ inline void both(const T *one, const T *other, V8 (&f)[ND], V8 (&g)[ND]) const
+    {
+        constexpr int FROM = ROW / 16 * GROUP;
+        const uint32_t b = place(one), c = place(other);
+        if constexpr (ND == 1) {
+            const uint32_t a[4] = {b + at[0], b + at[1], c + at[0], c + at[1]};
+            s16x4 o[4];
+            transposed4<FROM>(a, o);
+            f[0] = join(o[0], o[1]);
+            g[0] = join(o[2], o[3]);
+        } else {
+#pragma unroll
+            for (int d = 0; d < ND; d += 2) {
+                const uint32_t a[8] = {b + at[2 * d], b + at[2 * d + 1], b + at[2 * d + 2], b + at[2 * d + 3],
+                                       c + at[2 * d], c + at[2 * d + 1], c + at[2 * d + 2], c + at[2 * d + 3]};
+                s16x4 o[8];
+                transposed8<FROM>(a, o);
+                f[d] = join(o[0], o[1]);
+                f[d + 1] = join(o[2], o[3]);
+                g[d] = join(o[4], o[5]);
+                g[d + 1] = join(o[6], o[7]);
+            }
+        }
+    }
+};
 
 // A lane's operand row from memory: row lane % 32 from `base` on, zeros behind the `rows` that there are.
 template <class T, int DP>
@@ -189,6 +282,19 @@ __device__ inline void load_rows(const T *base, int64_t ld, int rows, int dim, i
     for (int s = 0; s < DP / 16; ++s) {
         const uint32_t at = s * 16 + (lane >> 5) * 8 < dim ? from + s * 32 : 0x80000000u;
         f[s] = __builtin_bit_cast(typename Half8<T>::type, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, 0, 0));
+    }
+}
+
+// Waits here until operands from memory are there.  Left to the compiler, the wait is where they are first used, in the loop over tiles, and there it is one for all of the
+// tiles that are on their way, in every turn.
+template <class V8, int NS>
+__device__ inline void arrived(V8 (&f)[NS])
+{
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+        u32x4 v = __builtin_bit_cast(u32x4, f[s]);
+        asm volatile("" : "+v"(v));
+        f[s] = __builtin_bit_cast(V8, v);
     }
 }
 
@@ -285,13 +391,21 @@ __device__ inline void make_bias(float *table, const float *bias, const int32_t 
     }
 }
 
+// An index into LDS that is one register: the compiler would otherwise put the array's own place into each of the offsets that follow, which a read of two numbers has no
+// room for.
+__device__ inline int one_register(int i)
+{
+    asm volatile("" : "+v"(i));
+    return i;
+}
+
 // The scale's sign goes into the queries.
 template <class V8, int NS>
 __device__ inline void take_sign(V8 (&f)[NS], float scale)
 {
-    const uint32_t flip = scale < 0.f ? 0x80008000u : 0u;
+    if (scale >= 0.f) return;
 #pragma unroll
-    for (int s = 0; s < NS; ++s) f[s] = __builtin_bit_cast(V8, __builtin_bit_cast(u32x4, f[s]) ^ flip);
+    for (int s = 0; s < NS; ++s) f[s] = __builtin_bit_cast(V8, __builtin_bit_cast(u32x4, f[s]) ^ 0x80008000u);
 }
 
 // Which of 64 keys hide from some of the wavefront's queries: those behind a query's last one, those before its first one, or neither.

@@ -14,11 +14,11 @@ namespace {
 // A block takes NW * 32 queries of one head through their keys, 64 at a time; a wavefront has 32 queries.  S^T = K Q^T, so that a lane owns one query: its maximum and sum
 // run over its own registers, the other half of the keys is lane ^ 32's.  The bias is what the products are added to.  One pass: m the largest score so far, l = sum of
 // weights 2^(scale log2 e (s - m)), O = sum of weights times v, l and O scaled when m grows.  P^T, rounded to the inputs' type (an error of half a step in each term, as the inputs themselves have), is the
-// other operand of O^T = V^T P^T without leaving its registers, see column_operand.
-// K and V tiles go from memory to LDS without registers, STAGES - 1 tiles ahead.
+// other operand of O^T = V^T P^T without leaving its registers, see Columns.
+// K and V tiles go from memory to LDS without registers, one tile ahead (two ahead, with a third stage, took the same time).
 template <int DP, int NW>
 struct AttendCfg {
-    static constexpr int STAGES = NW == 1 || DP == 128 ? 2 : 3, TILE = ATT_STEP * DP;
+    static constexpr int STAGES = 2, TILE = ATT_STEP * DP;
     static constexpr int FIXED = STAGES * 2 * TILE * 2;  // bytes; the bias's table follows
 };
 
@@ -57,9 +57,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : 1) void at
     const int my_row = t.row0 + wave * 32 + l32;
     V8 qf[NS];
     load_rows<T, DP>(q + (int64_t)(t.row0 + wave * 32) * ldq + h * a.dim, ldq, my_rows, a.dim, lane, qf);
-#pragma unroll
-    for (int i = 0; i < STAGES - 1; ++i)
-        if (t.begin + i < t.end) request(t.begin + i, i);
+    if (t.begin < t.end) request(t.begin, 0);
     if (BIAS) make_bias(table, bias, bucket_of, a, h);
 
     f32x16 o[ND];
@@ -68,19 +66,21 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : 1) void at
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[dt][r] = 0.f;
     float m = -INFINITY, l = 0.f;
+    arrived(qf);
     take_sign(qf, a.scale);
     const float scale2 = __builtin_fabsf(a.scale) * LOG2E;
     const int p = p0 + l32;
 
+    Columns<T, DP> columns;
+    columns.init(lane);
     int stage = 0;
     for (int u = t.begin; u < t.end; ++u) {
         const int j0 = key_of(u);
         const T *Kt = Ks + stage * TILE, *Vt = Vs + stage * TILE;
-        if (STAGES > 2 && u + 1 < t.end) wait_for_requests<2 * Requests::N>();
-        else wait_for_requests<0>();
+        wait_for_requests<0>();
         block_barrier();  // this tile is there, and the stage of the last one has been read
-        if (u + STAGES - 1 < t.end) request(u + STAGES - 1, stage == 0 ? STAGES - 1 : stage - 1);
-        stage = stage == STAGES - 1 ? 0 : stage + 1;
+        if (u + 1 < t.end) request(u + 1, stage ^ 1);
+        stage ^= 1;
         const int keys = min(ATT_STEP, t.others - j0);
         const Sight see = sight(a, p0, my_rows, j0, keys);
         if (see.none) continue;
@@ -91,11 +91,11 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : 1) void at
             const int least = j0 - (p0 + 31), most = j0 + ATT_STEP - 1 - p0;  // relative positions
             const bool near = most > -a.distance && least < a.distance;
             if (near) {
-                const float *at = table + (j0 + 4 * half - p + a.distance + ATT_EXT);
+                const int at = one_register(AttendCfg<DP, NW>::FIXED / 4 + j0 + 4 * half - p + a.distance + ATT_EXT);
 #pragma unroll
                 for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) s[kt][r] = at[kt * 32 + acc_row(r)];
+                    for (int r = 0; r < 16; ++r) s[kt][r] = reinterpret_cast<const float *>(smem)[at + kt * 32 + acc_row(r)];
             } else {
                 c = table[most <= -a.distance ? 0 : bias_entries(a.distance) - 1];
 #pragma unroll
@@ -114,10 +114,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : 1) void at
 #pragma unroll
             for (int i = 0; i < NS; ++i) s[kt] = att_mfma(row_operand<T, DP>(Kt, kt * 32, i, lane), qf[i], s[kt]);
         V8 vf[2][ND];  // of the first 32 keys, on their way while the scores become weights
-#pragma unroll
-        for (int w = 0; w < 2; ++w)
-#pragma unroll
-            for (int dt = 0; dt < ND; ++dt) vf[w][dt] = column_operand<T, DP>(Vt, w * 16, dt * 32, lane);
+        columns.template two<0>(Vt, vf);
         // register r of tile kt is key j0 + 32 kt + 4 half + acc_row(r)
         const int j = j0 + 4 * half;
         const Edges e = edges(a, p0, my_rows, j0, keys);
@@ -144,7 +141,8 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : 1) void at
 #pragma unroll
             for (int r = 0; r < 16; ++r) top = __builtin_fmaxf(top, s[kt][r]);
         top = __builtin_fmaxf(m, both_halves_max(top) + c);
-        if (__ballot(top != m)) {  // else no lane's maximum grew
+        // m follows the largest score only where that is more than 2^8 times m's weight: sums and fp16's weights have room for it
+        if (__ballot((top - m) * scale2 > 8.f)) {
             const float alpha = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - top) * scale2);
             m = top;
             l *= alpha;
@@ -182,11 +180,9 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : 1) void at
             for (int w = 0; w < 2; ++w) {
                 const V8 pf = rounded<T>(s[kt], w);
 #pragma unroll
-                for (int dt = 0; dt < ND; ++dt) {
-                    o[dt] = att_mfma(vf[w][dt], pf, o[dt]);
-                    if (kt == 0) vf[w][dt] = column_operand<T, DP>(Vt, 32 + w * 16, dt * 32, lane);
-                }
+                for (int dt = 0; dt < ND; ++dt) o[dt] = att_mfma(vf[w][dt], pf, o[dt]);
             }
+            if (kt == 0) columns.template two<32>(Vt, vf);
         }
         if (taken_out)  // it reaches the queries that see it
             add_nonfinite<T, ND>(o, vb, ldv, j0, keys, a.dim, lane, [&](int at) { return at <= p + a.right && (at >= p - a.left || at < a.sinks); });

@@ -179,10 +179,14 @@ __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void query_grad
     for (int r = 0; r < 16; ++r) minus_delta[r] = -my_delta;
     float factor = 1.f, behind = 0.f, ahead = 0.f;
     bool hurt = false;  // sees a key that is not finite
+    arrived(qf);
+    arrived(gf);
     take_sign(qf, a.scale);
     const float scale2 = __builtin_fabsf(a.scale) * LOG2E;
     const int p = p0 + l32;
 
+    Columns<T, DP> columns;
+    columns.init(lane);
     int stage = 0;
     for (int u = t.begin; u < t.end; ++u) {
         const int j0 = key_of(u);
@@ -202,11 +206,11 @@ __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void query_grad
         const bool near = most > -a.distance && least < a.distance;
         float c = -my_lse;
         if (BIAS && near) {
-            const float *at = table + (j - p + a.distance + ATT_EXT);
+            const int at = one_register(Cfg::QUERY_TILES / 4 + j - p + a.distance + ATT_EXT);
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[kt][r] = at[kt * 32 + acc_row(r)];
+                for (int r = 0; r < 16; ++r) s[kt][r] = reinterpret_cast<const float *>(smem)[at + kt * 32 + acc_row(r)];
         } else {
             if (BIAS) c = fmaf(table[most <= -a.distance ? 0 : entries - 1], scale2, c);
 #pragma unroll
@@ -224,10 +228,7 @@ __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void query_grad
             }
         }
         V8 kf[2][ND];  // of the first 32 keys
-#pragma unroll
-        for (int w = 0; w < 2; ++w)
-#pragma unroll
-            for (int dt = 0; dt < ND; ++dt) kf[w][dt] = column_operand<T, DP>(Kt, w * 16, dt * 32, lane);
+        columns.template two<0>(Kt, kf);
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
@@ -287,11 +288,9 @@ __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void query_grad
             for (int w = 0; w < 2; ++w) {
                 const V8 df = rounded<T>(d[kt], w);
 #pragma unroll
-                for (int dt = 0; dt < ND; ++dt) {
-                    acc[dt] = att_mfma(kf[w][dt], df, acc[dt]);
-                    if (kt == 0) kf[w][dt] = column_operand<T, DP>(Kt, 32 + w * 16, dt * 32, lane);
-                }
+                for (int dt = 0; dt < ND; ++dt) acc[dt] = att_mfma(kf[w][dt], df, acc[dt]);
             }
+            if (kt == 0) columns.template two<32>(Kt, kf);
         }
         if (taken_out)
             for_nonfinite_rows<T>(kb, ldk, j0, keys, a.dim, lane, [&](int at, const T *) { hurt |= at <= p + a.right && (at >= p - a.left || at < a.sinks); });
@@ -395,8 +394,12 @@ __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void key_grad_k
         for (int r = 0; r < 16; ++r) dk_acc[dt][r] = dv_acc[dt][r] = 0.f;
     float factor = 1.f;
     bool hurt = false;
+    arrived(kf);
+    arrived(vf);
     take_sign(kf, a.scale);
     const float scale2 = __builtin_fabsf(a.scale) * LOG2E;
+    Columns<T, DP> columns;
+    columns.init(lane);
     int stage = 0, of_table = -1;
     for (int n = 0; n < total; ++n, now = behind(now)) {
         const int h = now.h, i0 = now.tile * ATT_STEP;
@@ -436,9 +439,9 @@ __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void key_grad_k
             const bool near = most > -a.distance && least < a.distance;
             float c = 0.f;
             if (BIAS && near) {
-                const float *at = table + (j - p + a.distance + ATT_EXT);
+                const int at = one_register((Cfg::KEY_TILES + STAGES * Cfg::STATS) / 4 + j - p - 27 + a.distance + ATT_EXT);
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[0][r] = at[-acc_row(r)];
+                for (int r = 0; r < 16; ++r) s[0][r] = reinterpret_cast<const float *>(smem)[at + 27 - acc_row(r)];
             } else {
                 if (BIAS) c = table[most <= -a.distance ? 0 : bias_entries(a.distance) - 1] * scale2;
 #pragma unroll
@@ -450,11 +453,8 @@ __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void key_grad_k
                 d[0] = att_mfma(row_operand<T, DP>(Gt, qs * 32, i, lane), vf[i], d[0]);
             }
             V8 qc[ND], gc[ND];  // of the first 16 queries
-#pragma unroll
-            for (int dt = 0; dt < ND; ++dt) {
-                gc[dt] = column_operand<T, DP>(Gt, qs * 32, dt * 32, lane);
-                qc[dt] = column_operand<T, DP>(Qt, qs * 32, dt * 32, lane);
-            }
+            if (qs == 0) columns.template both<0>(Gt, Qt, gc, qc);
+            else columns.template both<32>(Gt, Qt, gc, qc);
             if (BIAS && !near) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) ls[r] += c;
@@ -505,10 +505,10 @@ __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void key_grad_k
                 for (int dt = 0; dt < ND; ++dt) {
                     dv_acc[dt] = att_mfma(gc[dt], pf, dv_acc[dt]);
                     dk_acc[dt] = att_mfma(qc[dt], df, dk_acc[dt]);
-                    if (w == 0) {
-                        gc[dt] = column_operand<T, DP>(Gt, qs * 32 + 16, dt * 32, lane);
-                        qc[dt] = column_operand<T, DP>(Qt, qs * 32 + 16, dt * 32, lane);
-                    }
+                }
+                if (w == 0) {
+                    if (qs == 0) columns.template both<16>(Gt, Qt, gc, qc);
+                    else columns.template both<48>(Gt, Qt, gc, qc);
                 }
             }
         }

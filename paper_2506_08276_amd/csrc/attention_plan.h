@@ -124,7 +124,7 @@ inline std::vector<AttentionItem> att_order(const std::vector<AttentionTile> &ti
         int64_t cost;
         int32_t from, to, head;  // tiles [from, to), heads head .. head + share - 1
     };
-    auto cost = [&](int t) { return (int64_t)(tiles[t].end - tiles[t].begin) + 2; };  // 2: what a block takes besides
+    auto cost = [&](int t) { return (int64_t)(tiles[t].end - tiles[t].begin) * ((tiles[t].rows + 31) / 32) + 8; };  // of a wavefront's tiles; 8: what a block takes besides
     int64_t total = 0;
     for (size_t t = 0; t < tiles.size(); ++t) total += cost((int)t);
     total *= own_heads / share;
