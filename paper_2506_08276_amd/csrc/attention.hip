@@ -141,10 +141,11 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : 1) void at
 #pragma unroll
             for (int r = 0; r < 16; ++r) top = __builtin_fmaxf(top, s[kt][r]);
         top = __builtin_fmaxf(m, both_halves_max(top) + c);
-        // m follows the largest score only where that is more than 2^8 times m's weight: sums and fp16's weights have room for it
-        if (__ballot((top - m) * scale2 > 8.f)) {
-            const float alpha = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - top) * scale2);
-            m = top;
+        // m follows the largest score only where that is more than 2^8 times m's weight: sums and fp16's weights have room for it.  Lane by lane: a row's bits are its own.
+        const bool grown = (top - m) * scale2 > 8.f;
+        if (__ballot(grown)) {
+            const float alpha = grown ? __builtin_amdgcn_exp2f((m - top) * scale2) : 1.f;
+            m = grown ? top : m;
             l *= alpha;
 #pragma unroll
             for (int dt = 0; dt < ND; ++dt)
