@@ -456,7 +456,7 @@ int leann_attention_create(leann_ctx *ctx, const int32_t *q_rows_host, const int
                            const leann_attention_desc *desc, leann_attention_plan **out);
 void leann_attention_free(leann_attention_plan *plan);
 
-/* out[Tq][heads * dim] from q[Tq][heads * dim], k and v[Tk][kv_heads * dim]: bf16 or f16, 16-byte alignment, rows a multiple of 8 elements apart and at most 2^23 (slices of one
+/* out[Tq][heads * dim] from q[Tq][heads * dim], k and v[Tk][kv_heads * dim]: bf16 or f16, 16-byte alignment, rows a multiple of 8 elements apart and at most 2^22 (slices of one
  * projection's output are fine).  bias: fp32[buckets][heads].  lse (NULL, or fp32[heads][Tq]): what the backward pass needs.  out must not overlap q, k or v (LEANN_EINVAL).
  * Where there are few queries, their keys are split over blocks whose sums are joined: a row's bits may depend on the other sequences' lengths, its value does not. */
 int leann_attention(leann_ctx *ctx, const leann_attention_plan *plan, const void *q_dev, int64_t ldq, const void *k_dev, int64_t ldk, const void *v_dev, int64_t ldv, int dtype,

@@ -5,8 +5,23 @@
 
 constexpr int ATT_MOST_DISTANCE = 1024;
 constexpr float ATT_LEAST_SCALE = 0x1p-20f, ATT_MOST_SCALE = 0x1p20f;
-constexpr int64_t ATT_MOST_LD = (int64_t)1 << 23;  // 64 rows are within a buffer's 2^31 bytes
+constexpr int64_t ATT_MOST_LD = (int64_t)1 << 22;  // 256 rows are within a buffer's 2^31 bytes
+constexpr int ATT_WHOLE = 256;                      // keys and queries that one block's gradient kernel takes
 constexpr int ATT_EXT = 96;  // a wavefront's 32 rows and 64 of the other side have relative positions in a range of 95
+
+// What the two gradient kernels go through.
+struct AttentionSides {
+    int32_t n_tiles = 0, n_query_items = 0, n_key_items = 0, n_joins = 0, n_slots = 0;  // tiles: of queries
+    const AttentionTile *query_tiles = nullptr, *key_tiles = nullptr;
+    const AttentionItem *query_items = nullptr, *key_items = nullptr;
+    const AttentionJoin *joins = nullptr;
+};
+// Sequences that one block takes whole, as tiles of all their keys.
+struct AttentionWhole {
+    int32_t n_tiles = 0, n_items = 0;
+    const AttentionTile *tiles = nullptr;
+    const AttentionItem *items = nullptr;
+};
 
 // One batch's sequences: tables on the device, in one allocation.
 struct leann_attention_plan {
@@ -16,11 +31,13 @@ struct leann_attention_plan {
     int32_t left = -1, right = -1, sinks = 0;  // as the kernels take them: no limit is a bound behind every position
     int32_t distance = 0, buckets = 0;         // distance: of the table below, no longer than the sequences make it
     int32_t query_waves = 0;                   // wavefronts of a forward block, 32 queries each
-    int32_t n_items = 0, n_grad_items = 0, n_key_items = 0, n_joins = 0, n_slots = 0, n_grad_tiles = 0, n_key_joins = 0, n_key_slots = 0;
+    int32_t n_items = 0, n_joins = 0, n_slots = 0;
     DevBuf mem;
-    const AttentionTile *tiles = nullptr, *grad_tiles = nullptr, *key_tiles = nullptr;  // of queries, for the gradient of queries, of keys
-    const AttentionItem *items = nullptr, *grad_items = nullptr, *key_items = nullptr;
-    const AttentionJoin *joins = nullptr, *key_joins = nullptr;
+    const AttentionTile *tiles = nullptr;
+    const AttentionItem *items = nullptr;
+    const AttentionJoin *joins = nullptr;
+    AttentionSides all, others;  // every sequence, and those that are not in:
+    AttentionWhole whole[2];     // up to 128 keys and queries, up to 256
     const int32_t *bucket_of = nullptr;  // [2 distance + 1]
 };
 
@@ -62,11 +79,25 @@ struct Half8<f16_t> {
     static constexpr uint32_t EXPONENT = 0x7c00;
 };
 
+template <class T>
+struct Half4;
+template <>
+struct Half4<bf16_t> {
+    typedef bf16x4 type;
+};
+template <>
+struct Half4<f16_t> {
+    typedef f16x4 type;
+};
+
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 
 __device__ inline f32x16 att_mfma(const bf16x8 &a, const bf16x8 &b, const f32x16 &c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 __device__ inline f32x16 att_mfma(const f16x8 &a, const f16x8 &b, const f32x16 &c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+
+__device__ inline f32x4 att_mfma16(const bf16x8 &a, const bf16x8 &b, const f32x4 &c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ inline f32x4 att_mfma16(const f16x8 &a, const f16x8 &b, const f32x4 &c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
 // Tiles of 64 rows of DP elements (the head's size, zeros up to 32, 64 or 128) lie in LDS as rows of 16-byte chunks, chunk c of row r at c ^ att_swizzle(r): 16 rows' reads
 // of one chunk, and the reads of four adjacent rows' 64 bytes that transpose, reach all banks.
@@ -169,6 +200,10 @@ __device__ inline typename Half8<T>::type row_operand(const T *lds, int row0, in
 // get a column of four each.
 // The reads are written out, each group with its wait behind it: before the builtin's, the compiler waits for every request from memory to LDS that is on its way, the tiles ahead
 // among them (LDS arrays and requests look alike to it).
+__device__ inline void transposed2(uint32_t a, uint32_t b, s16x4 (&o)[2])
+{
+    asm volatile("ds_read_b64_tr_b16 %0, %2\n\tds_read_b64_tr_b16 %1, %3\n\ts_waitcnt lgkmcnt(0)" : "=&v"(o[0]), "=&v"(o[1]) : "v"(a), "v"(b));
+}
 template <int FROM>
 __device__ inline void transposed4(const uint32_t (&a)[4], s16x4 (&o)[4])
 {

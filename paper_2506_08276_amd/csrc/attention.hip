@@ -304,9 +304,9 @@ int make_plan(leann_ctx *ctx, const int32_t *q_rows, const int32_t *k_rows, cons
     }
     // 32 queries per block where no sequence has more: the other wavefronts would only load.  128 where they share the keys' tiles.
     p->query_waves = longest <= 32 ? 1 : 4;
-    std::vector<AttentionTile> tiles, grad_tiles, key_tiles;
-    std::vector<int32_t> of, grad_of, key_of;
-    std::vector<AttentionJoin> joins, key_joins, none;
+    std::vector<AttentionTile> tiles;
+    std::vector<int32_t> of;
+    std::vector<AttentionJoin> joins;
     const int share = p->heads / p->kv_heads, cus = ctx->num_cus;
     att_make_tiles(r, n, q_rows, k_rows, first, false, share, p->query_waves * 32, 0, tiles, of, joins);
     // Keys are split where there are fewer than two blocks per compute unit, into parts that make four, of four tiles at least: each costs a block's start and its
@@ -317,31 +317,6 @@ int make_plan(leann_ctx *ctx, const int32_t *q_rows, const int32_t *k_rows, cons
             att_make_tiles(r, n, q_rows, k_rows, first, false, share, p->query_waves * 32, split, tiles, of, joins);
         }
     for (const AttentionJoin &j : joins) p->n_slots += j.slots;
-    att_make_tiles(r, n, q_rows, k_rows, first, false, share, 128, 0, grad_tiles, grad_of, none);
-    // Keys that many queries see, as a sequence's first ones, have their queries split, so that no block has much more than a compute unit's share of the work.
-    att_make_tiles(r, n, q_rows, k_rows, first, true, share, 128, 0, key_tiles, key_of, key_joins);
-    if (const int split = att_split(key_tiles, p->kv_heads, cus, 1, 16)) {
-        key_tiles.clear();
-        att_make_tiles(r, n, q_rows, k_rows, first, true, share, 128, split, key_tiles, key_of, key_joins);
-    }
-    for (const AttentionJoin &j : key_joins) p->n_key_slots += j.slots;
-    const std::vector<AttentionItem> items = att_order(tiles, of, p->heads, share), grad_items = att_order(grad_tiles, grad_of, p->heads, share),
-                                     key_items = att_order(key_tiles, key_of, p->kv_heads, 1);
-    if (std::max({items.size(), grad_items.size(), key_items.size(), joins.size(), key_joins.size()}) > ((size_t)1 << 24) - 1) {
-        leann_set_error("leann_attention_create: sequences of this number and length are not covered (more than 2^24 - 1 workgroups in a launch)");
-        return LEANN_ESHAPE;
-    }
-    p->n_items = (int32_t)items.size();
-    p->n_grad_items = (int32_t)grad_items.size();
-    p->n_key_items = (int32_t)key_items.size();
-    p->n_joins = (int32_t)joins.size();
-    p->n_key_joins = (int32_t)key_joins.size();
-    p->n_grad_tiles = (int32_t)grad_tiles.size();
-    std::vector<int32_t> buckets;
-    if (bucket_of) {  // no longer than the sequences
-        p->distance = (int32_t)std::min<int64_t>(distance, furthest);
-        buckets.assign(bucket_of + distance - p->distance, bucket_of + distance + p->distance + 1);
-    }
     std::vector<char> image;
     auto put = [&](const auto &v) {
         const size_t at = att_up256(image.size()), bytes = v.size() * sizeof(v[0]);
@@ -349,20 +324,98 @@ int make_plan(leann_ctx *ctx, const int32_t *q_rows, const int32_t *k_rows, cons
         if (bytes) memcpy(image.data() + at, v.data(), bytes);
         return at;
     };
-    const size_t at[9] = {put(tiles), put(grad_tiles), put(key_tiles), put(items), put(grad_items), put(key_items), put(joins), put(key_joins), put(buckets)};
+    size_t most_blocks = joins.size();
+    auto order = [&](const std::vector<AttentionTile> &t, const std::vector<int32_t> &t_of, int heads, int s, int32_t *count) {
+        const std::vector<AttentionItem> items = att_order(t, t_of, heads, s);
+        *count = (int32_t)items.size();
+        most_blocks = std::max(most_blocks, items.size());
+        return put(items);
+    };
+    const size_t tiles_at = put(tiles), items_at = order(tiles, of, p->heads, share, &p->n_items), joins_at = put(joins);
+    p->n_joins = (int32_t)joins.size();
+
+    // The gradient's two sides, of all sequences or of those that are not taken whole.
+    auto make_sides = [&](const std::vector<char> *taken, AttentionSides *sides, size_t (&at)[5]) {
+        std::vector<AttentionTile> query_tiles, key_tiles;
+        std::vector<int32_t> query_of, key_of;
+        std::vector<AttentionJoin> key_joins, none;
+        att_make_tiles(r, n, q_rows, k_rows, first, false, share, 128, 0, query_tiles, query_of, none, taken);
+        // Keys that many queries see, as a sequence's first ones, have their queries split, so that no block has much more than a compute unit's share of the work.
+        att_make_tiles(r, n, q_rows, k_rows, first, true, share, 128, 0, key_tiles, key_of, key_joins, taken);
+        if (const int split = att_split(key_tiles, p->kv_heads, cus, 1, 16)) {
+            key_tiles.clear();
+            att_make_tiles(r, n, q_rows, k_rows, first, true, share, 128, split, key_tiles, key_of, key_joins, taken);
+        }
+        for (const AttentionJoin &j : key_joins) sides->n_slots += j.slots;
+        sides->n_tiles = (int32_t)query_tiles.size();
+        sides->n_joins = (int32_t)key_joins.size();
+        most_blocks = std::max(most_blocks, key_joins.size());
+        at[0] = put(query_tiles);
+        at[1] = order(query_tiles, query_of, p->heads, share, &sides->n_query_items);
+        at[2] = put(key_tiles);
+        at[3] = order(key_tiles, key_of, p->kv_heads, 1, &sides->n_key_items);
+        at[4] = put(key_joins);
+    };
+    size_t all_at[5], others_at[5], whole_at[2][2] = {};
+    make_sides(nullptr, &p->all, all_at);
+    std::vector<char> taken(n, 0);
+    const bool sees_all = r.left >= (1 << 30) && r.right >= (1 << 30);
+    int n_taken = 0;
+    for (int s = 0; s < n; ++s) n_taken += taken[s] = sees_all && share == 1 && p->dim <= 64 && q_rows[s] <= ATT_WHOLE && k_rows[s] <= ATT_WHOLE;
+    if (n_taken) make_sides(&taken, &p->others, others_at);
+    for (int c = 0; n_taken && c < 2; ++c) {
+        std::vector<AttentionTile> whole;
+        std::vector<int32_t> whole_of(1, 0);
+        int64_t q0 = 0, k0 = 0;
+        for (int s = 0; s < n; q0 += q_rows[s], k0 += k_rows[s], ++s) {
+            if (!taken[s] || (q_rows[s] > ATT_WHOLE / 2 || k_rows[s] > ATT_WHOLE / 2) != (c == 1) || (!q_rows[s] && !k_rows[s])) continue;
+            AttentionTile t = {};
+            t.row0 = (int32_t)k0;
+            t.rows = k_rows[s];
+            t.other0 = (int32_t)q0;
+            t.others = q_rows[s];
+            t.first = first[s];
+            t.end = (q_rows[s] + 31) / 32;  // what the order goes by
+            t.slot = -1;
+            whole.push_back(t);
+            whole_of.push_back((int32_t)whole.size());
+        }
+        p->whole[c].n_tiles = (int32_t)whole.size();
+        whole_at[c][0] = put(whole);
+        whole_at[c][1] = order(whole, whole_of, p->heads, 1, &p->whole[c].n_items);
+    }
+    if (most_blocks > ((size_t)1 << 24) - 1) {
+        leann_set_error("leann_attention_create: sequences of this number and length are not covered (more than 2^24 - 1 workgroups in a launch)");
+        return LEANN_ESHAPE;
+    }
+    std::vector<int32_t> buckets;
+    if (bucket_of) {  // no longer than the sequences
+        p->distance = (int32_t)std::min<int64_t>(distance, furthest);
+        buckets.assign(bucket_of + distance - p->distance, bucket_of + distance + p->distance + 1);
+    }
+    const size_t buckets_at = put(buckets);
     LEANN_TRY(ctx->reserve(p->mem, std::max<size_t>(image.size(), 1)));
     if (!image.empty()) LEANN_HIP(hipMemcpyAsync(p->mem.p, image.data(), image.size(), hipMemcpyHostToDevice, ctx->stream));
     LEANN_HIP(hipStreamSynchronize(ctx->stream));
     const char *base = (const char *)p->mem.p;
-    p->tiles = (const AttentionTile *)(base + at[0]);
-    p->grad_tiles = (const AttentionTile *)(base + at[1]);
-    p->key_tiles = (const AttentionTile *)(base + at[2]);
-    p->items = (const AttentionItem *)(base + at[3]);
-    p->grad_items = (const AttentionItem *)(base + at[4]);
-    p->key_items = (const AttentionItem *)(base + at[5]);
-    p->joins = (const AttentionJoin *)(base + at[6]);
-    p->key_joins = (const AttentionJoin *)(base + at[7]);
-    p->bucket_of = (const int32_t *)(base + at[8]);
+    auto set_sides = [&](AttentionSides *sides, const size_t (&at)[5]) {
+        sides->query_tiles = (const AttentionTile *)(base + at[0]);
+        sides->query_items = (const AttentionItem *)(base + at[1]);
+        sides->key_tiles = (const AttentionTile *)(base + at[2]);
+        sides->key_items = (const AttentionItem *)(base + at[3]);
+        sides->joins = (const AttentionJoin *)(base + at[4]);
+    };
+    p->tiles = (const AttentionTile *)(base + tiles_at);
+    p->items = (const AttentionItem *)(base + items_at);
+    p->joins = (const AttentionJoin *)(base + joins_at);
+    p->bucket_of = (const int32_t *)(base + buckets_at);
+    set_sides(&p->all, all_at);
+    if (n_taken) set_sides(&p->others, others_at);
+    else p->others = p->all;
+    for (int c = 0; c < 2; ++c) {
+        p->whole[c].tiles = (const AttentionTile *)(base + whole_at[c][0]);
+        p->whole[c].items = (const AttentionItem *)(base + whole_at[c][1]);
+    }
     return LEANN_OK;
 }
 
@@ -409,7 +462,7 @@ int att_check_rows(const char *call, const char *what, const void *p, int64_t ld
         return LEANN_EINVAL;
     }
     if (ld < cols || ld % 8 || ld > ATT_MOST_LD) {
-        leann_set_error("%s: rows of %s are %lld elements apart, need a multiple of 8 from %lld to 2^23", call, what, (long long)ld, (long long)cols);
+        leann_set_error("%s: rows of %s are %lld elements apart, need a multiple of 8 from %lld to 2^22", call, what, (long long)ld, (long long)cols);
         return LEANN_ESHAPE;
     }
     return LEANN_OK;

@@ -563,6 +563,269 @@ __global__ __launch_bounds__(256) void key_join_kernel(const AttentionJoin *__re
     }
 }
 
+// ------------------------------------------------------------------ whole sequences
+// Sequences of up to 32 NW keys and queries, all of which see each other, one head per block: queries, keys, values, dO and O are read once and S and dO V^T computed once, where
+// the two kernels above read all but O twice, which bounds them there.  A wavefront has 32 keys in registers, K in LDS as well; the queries go by, 32 at a time: S = Q K^T and
+// dP = dO V^T with a key per lane, P and dS from registers into dV^T and dK^T as in key_grad_kernel; dS, rounded, through LDS into dQ^T = K^T dS^T, of which each
+// wavefront has tiles of 16 x 16, all keys of them.  The stores of a step's dQ are issued behind the next step's wait, which else would be for them.
+template <int DP, int NW>
+struct WholeCfg {
+    static constexpr int KEYS = 32 * NW, STAGE = 32 * DP;  // elements of a stage's Q, or dO
+    static constexpr int K_BYTES = KEYS * DP * 2, STAGES_BYTES = 2 * 2 * STAGE * 2, DS_BYTES = 32 * KEYS * 2, NUMBERS_BYTES = KEYS * 2 * (int)sizeof(float);
+    static constexpr int FIXED = K_BYTES + STAGES_BYTES + DS_BYTES + NUMBERS_BYTES;
+    static constexpr int DIAGONALS = NW * 32 * 36 * (int)sizeof(float);
+};
+
+// dS in LDS: rows of queries, 16-byte chunks of keys XORed with the row.
+template <int NW>
+__device__ inline int whole_swizzle(int row) { return NW == 4 ? row & 15 : row & 31; }
+
+// As add_diagonals, of 32 keys (one per lane) and 32 queries (in its registers): sums[31 + key - query].  Rows of keys in LDS; lane l and lane l + 32 walk along diagonal l, or l + 32,
+// for the queries 0 .. 15 and 16 .. 31.
+__device__ inline void add_diagonals_of_keys(const f32x16 &d, float *rows, float *sums, int lane)
+{
+    const int half = lane >> 5, l32 = lane & 31;
+    wave_fence();
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        const f32x4 x = {d[4 * c], d[4 * c + 1], d[4 * c + 2], d[4 * c + 3]};
+        *reinterpret_cast<f32x4 *>(rows + l32 * 36 + 8 * c + 4 * half) = x;
+    }
+    wave_fence();
+    // query 16 half + 15 - step, key l32 - 31 + query, or 32 more
+    const float *near = rows + (l32 - 16 + 16 * half) * 36 + 16 * half + 15, *far = near + 32 * 36;
+    float sum = 0.f, until = 0.f;
+#pragma unroll
+    for (int step = 0; step < 16; ++step) {
+        const bool over = __builtin_amdgcn_inverse_ballot_w64(((1ull << (step + 16)) - 1) | ((1ull << step) - 1) << 32);
+        sum += (over ? far : near)[-step * 37];
+        until = __builtin_amdgcn_inverse_ballot_w64(1ull << (step + 16) | 1ull << (32 + step)) ? sum : until;
+    }
+    const float first = lane < 48 ? until : sum, other = sum - first;
+    const float a = both_halves_sum(first), b = both_halves_sum(other);
+    wave_fence();
+    sums[lane] += half ? b : a;
+    wave_fence();
+}
+
+template <class T, int DP, int NW, bool BIAS>
+__global__ __launch_bounds__(NW * 64, 2) void whole_grad_kernel(const AttentionItem *__restrict__ items, const AttentionTile *__restrict__ tiles, AttentionShape a,
+                                                               const T *__restrict__ dout, int64_t ldd, const T *__restrict__ q, int64_t ldq, const T *__restrict__ k, int64_t ldk,
+                                                               const T *__restrict__ v, int64_t ldv, const T *__restrict__ o, int64_t ldo, const float *__restrict__ lse, int64_t Tq,
+                                                               const float *__restrict__ bias, const int32_t *__restrict__ bucket_of, T *__restrict__ dq, int64_t lddq,
+                                                               T *__restrict__ dk, int64_t lddk, T *__restrict__ dv, int64_t lddv, float *__restrict__ by_position)
+{
+    typedef typename Half8<T>::type V8;
+    typedef WholeCfg<DP, NW> Cfg;
+    constexpr int KEYS = Cfg::KEYS, STAGE = Cfg::STAGE, ND = DP / 32, NS = DP / 16, CPR = DP / 8, RPI = 64 / CPR;
+    constexpr int TILES = DP / 16 * 2, MINE = (TILES + NW - 1) / NW;  // 16 x 16 tiles of a step's dQ^T
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    T *Ks = reinterpret_cast<T *>(smem), *Qs = Ks + KEYS * DP, *Gs = Qs + 2 * STAGE, *Ds = Gs + 2 * STAGE;  // Q and dO: [2 stages][32][DP]
+    float *numbers = reinterpret_cast<float *>(smem + Cfg::K_BYTES + Cfg::STAGES_BYTES + Cfg::DS_BYTES);   // [-lse, -delta][KEYS]
+    float *table = reinterpret_cast<float *>(smem + Cfg::FIXED);
+    const int entries = bias_entries(a.distance), room = (entries + 3) & ~3;
+    float *sums = table + room, *diagonals = sums + NW * room;
+
+    const AttentionItem item = items[blockIdx.x];
+    if (item.tile < 0) return;
+    const AttentionTile t = tiles[item.tile];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, l32 = lane & 31;
+    const int h = item.head, lq = t.others, lk = t.rows, steps = (lq + 31) / 32;
+    const int my_keys = min(32, lk - wave * 32), j = wave * 32 + l32;  // keys from 0 on, queries from position t.first
+    const bool valid = l32 < my_keys;
+    const T *qb = q + (int64_t)t.other0 * ldq + h * a.dim, *gb = dout + (int64_t)t.other0 * ldd + h * a.dim;
+
+    // K: the wavefront's own rows.  Q and dO: pieces of 1 KB, those of Q first, in turn.
+    const auto k_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<T *>(k + (int64_t)t.row0 * ldk + h * a.dim), 0, lk > 0 ? (int)(((lk - 1) * ldk + a.dim) * 2) : 0, 0x00020000);
+    const int row_in = lane / CPR;
+    auto offset = [&](int row, int64_t ld) {
+        const int ch = (lane % CPR) ^ att_swizzle<DP>(row);
+        return ch * 8 < a.dim ? (uint32_t)(row * ld + ch * 8) * 2 : 0x80000000u;
+    };
+#pragma unroll
+    for (int i = 0; i < 32 / RPI; ++i) lds_request(k_rsrc, offset(wave * 32 + i * RPI + row_in, ldk), Ks + (wave * 32 + i * RPI) * DP);
+    const auto q_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<T *>(qb), 0, lq > 0 ? (int)(((lq - 1) * ldq + a.dim) * 2) : 0, 0x00020000);
+    const auto g_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<T *>(gb), 0, lq > 0 ? (int)(((lq - 1) * ldd + a.dim) * 2) : 0, 0x00020000);
+    auto request = [&](int step, int stage) {
+#pragma unroll
+        for (int p = wave; p < 2 * 32 / RPI; p += NW) {
+            const int i = p % (32 / RPI) * RPI;
+            if (p < 32 / RPI) lds_request(q_rsrc, offset(step * 32 + i + row_in, ldq), Qs + stage * STAGE + i * DP);
+            else lds_request(g_rsrc, offset(step * 32 + i + row_in, ldd), Gs + stage * STAGE + i * DP);
+        }
+    };
+    request(0, 0);
+    V8 vf[NS], gf[NS], of[NS];
+    load_rows<T, DP>(v + (int64_t)(t.row0 + wave * 32) * ldv + h * a.dim, ldv, my_keys, a.dim, lane, vf);
+    // delta and the log-sum of the queries, 32 per wavefront; behind the last query P is 0
+    load_rows<T, DP>(gb + (int64_t)wave * 32 * ldd, ldd, lq - wave * 32, a.dim, lane, gf);
+    load_rows<T, DP>(o + (int64_t)(t.other0 + wave * 32) * ldo + h * a.dim, ldo, lq - wave * 32, a.dim, lane, of);
+    const float my_lse = j < lq ? lse_in_log2(lse[(int64_t)h * Tq + t.other0 + j]) : INFINITY;
+    if (BIAS) {
+        make_bias(table, bias, bucket_of, a, h);
+        if (by_position)
+            for (int i = tid; i < NW * room; i += NW * 64) sums[i] = 0.f;
+    }
+    float my_delta = 0.f;
+#pragma unroll
+    for (int s = 0; s < NS; ++s)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) my_delta = fmaf((float)gf[s][i], (float)of[s][i], my_delta);
+    my_delta = both_halves_sum(my_delta);
+    if (half == 0) numbers[j] = -my_lse;
+    else numbers[KEYS + j] = -my_delta;
+
+    f32x16 dk_acc[ND], dv_acc[ND];
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) dk_acc[dt][r] = dv_acc[dt][r] = 0.f;
+    const float scale2 = __builtin_fabsf(a.scale) * LOG2E;
+    Columns<T, DP> columns;
+    columns.init(lane);
+    // operand A of dQ^T's tiles: 16 columns of K, eight adjacent keys per lane
+    uint32_t k_at[MINE][2];
+    const int l16 = lane & 15, g16 = lane >> 4;
+#pragma unroll
+    for (int m = 0; m < MINE; ++m) {
+        const int tile = (wave + m * NW) % TILES, d0 = tile % (DP / 16) * 16;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int row = 8 * g16 + 4 * i + (l16 >> 2), col = d0 + 4 * (l16 & 3);
+            k_at[m][i] = Columns<T, DP>::place(Ks) + (row * DP + (((col >> 3) ^ att_swizzle<DP>(row)) << 3) + (col & 7)) * 2;
+        }
+    }
+    const int key_groups = (lk + 31) / 32;
+    arrived(vf);
+    V8 kf[NS];
+    f32x4 dq_acc[MINE];
+    auto store_dq = [&](int step) {
+#pragma unroll
+        for (int m = 0; m < MINE; ++m) {
+            const int tile = wave + m * NW, d = tile % (DP / 16) * 16 + 4 * g16, row = step * 32 + tile / (DP / 16) * 16 + l16;
+            if (tile < TILES && row < lq && d < a.dim) {
+                typedef typename Half4<T>::type V4;
+                const f32x4 x = dq_acc[m] * a.scale;
+                *reinterpret_cast<V4 *>(dq + (int64_t)(t.other0 + row) * lddq + h * a.dim + d) = __builtin_convertvector(x, V4);
+            }
+        }
+    };
+    for (int step = 0; step < steps; ++step) {
+        const int stage = step & 1;
+        const T *Qt = Qs + stage * STAGE, *Gt = Gs + stage * STAGE;
+        wait_for_requests<0>();
+        block_barrier();  // this step's rows are there; the last one's, and its dS, have been read
+        if (step == 0) {
+#pragma unroll
+            for (int s = 0; s < NS; ++s) kf[s] = row_operand<T, DP>(Ks, wave * 32, s, lane);
+            take_sign(kf, a.scale);
+        } else {
+            store_dq(step - 1);
+        }
+        if (step + 1 < steps) request(step + 1, stage ^ 1);
+        if (my_keys > 0) {
+            f32x16 s, d;
+            const int i0 = step * 32, pw = t.first + i0;
+            const int least = wave * 32 - (pw + 31), most = wave * 32 + 31 - pw;  // relative positions
+            const bool near = most > -a.distance && least < a.distance;
+            float ls[16];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const f32x4 x = *reinterpret_cast<const f32x4 *>(numbers + i0 + 4 * half + 8 * c), y = *reinterpret_cast<const f32x4 *>(numbers + KEYS + i0 + 4 * half + 8 * c);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) ls[4 * c + e] = x[e], d[4 * c + e] = y[e];
+            }
+            if (BIAS && near) {
+                const int at = one_register(Cfg::FIXED / 4 + j - pw - 4 * half - 27 + a.distance + ATT_EXT);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[r] = reinterpret_cast<const float *>(smem)[at + 27 - acc_row(r)];
+            } else {
+                const float c = BIAS ? table[most <= -a.distance ? 0 : entries - 1] : 0.f;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[r] = c;
+            }
+#pragma unroll
+            for (int i = 0; i < NS; ++i) {
+                s = att_mfma(row_operand<T, DP>(Qt, 0, i, lane), kf[i], s);
+                d = att_mfma(row_operand<T, DP>(Gt, 0, i, lane), vf[i], d);
+            }
+            V8 gc[ND], qc[ND];
+            columns.template both<0>(Gt, Qt, gc, qc);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], scale2, ls[r]));
+                d[r] *= s[r];
+            }
+            if (!valid)  // keys behind the last one
+#pragma unroll
+                for (int r = 0; r < 16; ++r) d[r] = 0.f;
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+                const V8 pf = rounded<T>(s, w), df = rounded<T>(d, w);
+#pragma unroll
+                for (int dt = 0; dt < ND; ++dt) {
+                    dv_acc[dt] = att_mfma(gc[dt], pf, dv_acc[dt]);
+                    dk_acc[dt] = att_mfma(qc[dt], df, dk_acc[dt]);
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {  // dS to its rows
+                    const int row = acc_row(8 * w + i) + 4 * half;
+                    Ds[row * KEYS + (((j >> 3) ^ whole_swizzle<NW>(row)) << 3) + (j & 7)] = df[i];
+                }
+                if (w == 0) columns.template both<16>(Gt, Qt, gc, qc);
+            }
+            if (BIAS && by_position) {
+                // register r of a lane: query i0 + 4 half + acc_row(r), as add_diagonals_of_keys takes them
+                add_diagonals_of_keys(d, diagonals + wave * 32 * 36, sums + wave * room + min(max(wave * 32 - pw - 31, -a.distance - 62), a.distance) + a.distance + ATT_EXT, lane);
+            }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        block_barrier();  // dS is there
+#pragma unroll
+        for (int m = 0; m < MINE; ++m) {
+            const int tile = (wave + m * NW) % TILES, row = tile / (DP / 16) * 16 + l16;
+            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+            for (int u = 0; u < key_groups; ++u) {
+                const V8 b = *reinterpret_cast<const V8 *>(Ds + row * KEYS + (((u * 4 + g16) ^ whole_swizzle<NW>(row)) << 3));
+                s16x4 x[2];
+                transposed2(k_at[m][0] + u * 32 * DP * 2, k_at[m][1] + u * 32 * DP * 2, x);
+                acc = att_mfma16(Columns<T, DP>::join(x[0], x[1]), b, acc);
+            }
+            dq_acc[m] = acc;
+        }
+    }
+    if (steps) store_dq(steps - 1);
+    const int64_t my_row = t.row0 + j;
+    store_columns<T, ND>(dk_acc, a.scale, dk + my_row * lddk + h * a.dim, valid, a.dim, lane);
+    store_columns<T, ND>(dv_acc, 1.f, dv + my_row * lddv + h * a.dim, valid, a.dim, lane);
+
+    if (BIAS && by_position) {
+        const int positions = 2 * a.distance + 1;
+        const float *mine = sums + wave * room;
+        float behind = 0.f, ahead = 0.f;
+        __syncthreads();
+        for (int e = lane; e < ATT_EXT; e += 64) {
+            behind += mine[e];
+            ahead += mine[entries - 1 - e];
+        }
+        behind = wave_sum(behind);
+        ahead = wave_sum(ahead);
+        if (lane == 0) diagonals[wave * 2] = behind, diagonals[wave * 2 + 1] = ahead;
+        __syncthreads();
+        float *to = by_position + ((int64_t)item.tile * a.heads + h) * positions;
+        for (int i = tid; i < positions; i += NW * 64) {
+            float sum = 0.f;
+#pragma unroll
+            for (int w = 0; w < NW; ++w) {
+                sum += sums[w * room + i + ATT_EXT];
+                if (i == 0) sum += diagonals[w * 2];
+                if (i == positions - 1) sum += diagonals[w * 2 + 1];
+            }
+            to[i] = sum;
+        }
+    }
+}
+
 // Sums of the bias's gradient by relative position over up to POSITION_ROWS tiles each, in their order.
 constexpr int POSITION_ROWS = 16;
 __global__ __launch_bounds__(256) void position_sum_kernel(const float *__restrict__ from, int n, int heads, int positions, float *__restrict__ to)
@@ -597,6 +860,15 @@ __global__ __launch_bounds__(1024) void bucket_sum_kernel(const float *__restric
     }
 }
 
+template <int DP>
+int allow_whole()
+{
+    for (const void *f : {(const void *)whole_grad_kernel<bf16_t, DP, 4, false>, (const void *)whole_grad_kernel<bf16_t, DP, 4, true>,
+                          (const void *)whole_grad_kernel<bf16_t, DP, 8, false>, (const void *)whole_grad_kernel<bf16_t, DP, 8, true>})
+        LEANN_HIP(hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024));
+    return LEANN_OK;
+}
+
 template <class T, int DP>
 int allow_grad()
 {
@@ -610,6 +882,8 @@ int allow_grad()
 
 int attention_grad_init_device()
 {
+    LEANN_TRY((allow_whole<32>()));
+    LEANN_TRY((allow_whole<64>()));
     LEANN_TRY((allow_grad<bf16_t, 32>()));
     LEANN_TRY((allow_grad<bf16_t, 64>()));
     LEANN_TRY((allow_grad<bf16_t, 128>()));
@@ -647,12 +921,15 @@ extern "C" int leann_attention_backward(leann_ctx *ctx, const leann_attention_pl
     }
     LEANN_HIP(hipSetDevice(ctx->device));
     const AttentionShape a = att_shape(plan, scale);
-    const int positions = 2 * plan->distance + 1, n = plan->n_grad_tiles, groups = (n + POSITION_ROWS - 1) / POSITION_ROWS;
+    // bf16: short sequences go through one kernel, the others through two; what fp16 needs of a lane's own scale, one dS for two products cannot have
+    const AttentionSides &sides = dtype == LEANN_BF16 ? plan->others : plan->all;
+    const int n_whole = dtype == LEANN_BF16 ? plan->whole[0].n_tiles + plan->whole[1].n_tiles : 0;
+    const int positions = 2 * plan->distance + 1, n = sides.n_tiles + n_whole, groups = (n + POSITION_ROWS - 1) / POSITION_ROWS;
     const size_t stats_bytes = ((size_t)plan->heads * plan->Tq * sizeof(float2) + 8 + 255) & ~(size_t)255;  // 8: see key_grad_kernel's requests
     const size_t row_bytes = (size_t)plan->heads * positions * sizeof(float);
     std::lock_guard<std::mutex> turn(ctx->op_work_mutex);
     const int DP = plan->dim <= 32 ? 32 : plan->dim <= 64 ? 64 : 128;
-    const size_t part_bytes = (size_t)plan->n_key_slots * plan->kv_heads * 2 * GRAD_WAVES * 32 * DP * sizeof(float);
+    const size_t part_bytes = (size_t)sides.n_slots * plan->kv_heads * 2 * GRAD_WAVES * 32 * DP * sizeof(float);
     LEANN_TRY(ctx->reserve(ctx->op_work, stats_bytes + part_bytes + (dbias_dev ? row_bytes * (n + groups) : 0)));
     float2 *stats = (float2 *)ctx->op_work.p;
     float *parts = (float *)((char *)ctx->op_work.p + stats_bytes), *by_position = dbias_dev ? (float *)((char *)parts + part_bytes) : nullptr;
@@ -663,18 +940,31 @@ extern "C" int leann_attention_backward(leann_ctx *ctx, const leann_attention_pl
         typedef GradCfg<DP> Cfg;
         const int table = BIAS ? ((positions + 2 * ATT_EXT + 3) & ~3) * 4 : 0;
         const int query_smem = Cfg::QUERY_TILES + (by_position ? table * (1 + GRAD_WAVES) + Cfg::DIAGONALS : table);
-        if (plan->n_grad_items)
-            hipLaunchKernelGGL((query_grad_kernel<T, DP, BIAS>), dim3(plan->n_grad_items), dim3(GRAD_WAVES * 64),
-                               query_smem, ctx->stream, plan->grad_items, plan->grad_tiles, a, (const T *)dout_dev, ldd,
-                               (const T *)q_dev, ldq, (const T *)k_dev, ldk, (const T *)v_dev, ldv, (const T *)out_dev, ldo, lse_dev, plan->Tq, bias_dev, plan->bucket_of,
-                               (T *)dq_dev, lddq, stats, by_position);
-        if (plan->n_key_items)
-            hipLaunchKernelGGL((key_grad_kernel<T, DP, BIAS>), dim3(plan->n_key_items), dim3(GRAD_WAVES * 64), Cfg::KEY_TILES + Cfg::KEY_STAGES * Cfg::STATS + table, ctx->stream, plan->key_items,
-                               plan->key_tiles, a, (const T *)dout_dev, ldd, (const T *)q_dev, ldq, (const T *)k_dev, ldk, (const T *)v_dev, ldv, stats, plan->Tq,
+        if (sides.n_query_items)
+            hipLaunchKernelGGL((query_grad_kernel<T, DP, BIAS>), dim3(sides.n_query_items), dim3(GRAD_WAVES * 64), query_smem, ctx->stream, sides.query_items, sides.query_tiles, a,
+                               (const T *)dout_dev, ldd, (const T *)q_dev, ldq, (const T *)k_dev, ldk, (const T *)v_dev, ldv, (const T *)out_dev, ldo, lse_dev, plan->Tq, bias_dev,
+                               plan->bucket_of, (T *)dq_dev, lddq, stats, by_position);
+        if (sides.n_key_items)
+            hipLaunchKernelGGL((key_grad_kernel<T, DP, BIAS>), dim3(sides.n_key_items), dim3(GRAD_WAVES * 64), Cfg::KEY_TILES + Cfg::KEY_STAGES * Cfg::STATS + table, ctx->stream,
+                               sides.key_items, sides.key_tiles, a, (const T *)dout_dev, ldd, (const T *)q_dev, ldq, (const T *)k_dev, ldk, (const T *)v_dev, ldv, stats, plan->Tq,
                                bias_dev, plan->bucket_of, (T *)dk_dev, lddk, (T *)dv_dev, lddv, parts);
-        if (plan->n_key_joins)
-            hipLaunchKernelGGL(key_join_kernel<T>, dim3(plan->n_key_joins, plan->kv_heads, 2), dim3(256), 0, ctx->stream, plan->key_joins, plan->kv_heads, plan->dim, DP, parts,
+        if (sides.n_joins)
+            hipLaunchKernelGGL(key_join_kernel<T>, dim3(sides.n_joins, plan->kv_heads, 2), dim3(256), 0, ctx->stream, sides.joins, plan->kv_heads, plan->dim, DP, parts,
                                (T *)dk_dev, lddk, (T *)dv_dev, lddv);
+        if constexpr (std::is_same_v<T, bf16_t> && DP <= 64) {
+            float *rows = by_position ? by_position + (size_t)sides.n_tiles * plan->heads * positions : nullptr;
+            auto whole = [&](const AttentionWhole &w, auto waves) {
+                constexpr int NW = decltype(waves)::value;
+                typedef WholeCfg<DP, NW> Whole;
+                if (!w.n_items) return;
+                hipLaunchKernelGGL((whole_grad_kernel<T, DP, NW, BIAS>), dim3(w.n_items), dim3(NW * 64), Whole::FIXED + (rows ? table * (1 + NW) + Whole::DIAGONALS : table), ctx->stream,
+                                   w.items, w.tiles, a, (const T *)dout_dev, ldd, (const T *)q_dev, ldq, (const T *)k_dev, ldk, (const T *)v_dev, ldv, (const T *)out_dev, ldo, lse_dev,
+                                   plan->Tq, bias_dev, plan->bucket_of, (T *)dq_dev, lddq, (T *)dk_dev, lddk, (T *)dv_dev, lddv, rows);
+                if (rows) rows += (size_t)w.n_tiles * plan->heads * positions;
+            };
+            whole(plan->whole[0], std::integral_constant<int, 4>());
+            whole(plan->whole[1], std::integral_constant<int, 8>());
+        }
     };
     auto with_type = [&](auto *type) {
         auto with_bias = [&](auto dp) {

@@ -61,16 +61,17 @@ struct AttentionItem {
     int32_t tile, head;  // tile -1: nothing to do
 };
 
-// A side's tiles of `block_rows` rows of every sequence, and the joins.  share: heads per key head.  split > 0: no block has more than `split` tiles of the other side.
+// A side's tiles of `block_rows` rows of every sequence, and the joins.  share: heads per key head.  without: sequences that are left out.  split > 0: no block has more than `split` tiles of the other side.
 inline void att_make_tiles(const AttentionRules &r, int n, const int32_t *q_rows, const int32_t *k_rows, const int32_t *first, bool keys, int share, int block_rows,
-                           int split, std::vector<AttentionTile> &tiles, std::vector<int32_t> &tiles_of, std::vector<AttentionJoin> &joins)
+                           int split, std::vector<AttentionTile> &tiles, std::vector<int32_t> &tiles_of, std::vector<AttentionJoin> &joins,
+                           const std::vector<char> *without = nullptr)
 {
     int64_t q0 = 0, k0 = 0;
     int32_t slots = 0;
     tiles_of.assign(n + 1, 0);
     for (int s = 0; s < n; ++s) {
         const int64_t lq = q_rows[s], lk = k_rows[s], f = first[s];
-        for (int64_t i = 0; i < (keys ? lk : lq); i += block_rows) {
+        for (int64_t i = 0; i < (keys ? lk : lq) && !(without && (*without)[s]); i += block_rows) {
             const int64_t rows = std::min<int64_t>(block_rows, (keys ? lk : lq) - i);
             const AttentionSpan span = keys ? att_queries_seen(r, i, i + rows - 1, lq, f) : att_keys_seen(r, f + i, f + i + rows - 1, lk);
             AttentionTile t = {};
