@@ -7,7 +7,7 @@ constexpr int ATT_MOST_DISTANCE = 1024;
 constexpr float ATT_LEAST_SCALE = 0x1p-20f, ATT_MOST_SCALE = 0x1p20f;
 constexpr int64_t ATT_MOST_LD = (int64_t)1 << 22;  // 256 rows are within a buffer's 2^31 bytes
 constexpr int ATT_WHOLE = 256;                      // keys and queries that one block's gradient kernel takes
-constexpr int ATT_EXT = 96;  // a wavefront's 32 rows and 64 of the other side have relative positions in a range of 95
+constexpr int ATT_EXT = 104;  // a wavefront's 32 rows and 64 of the other side have relative positions in a range of 95; sums of theirs touch nine places more
 
 // What the two gradient kernels go through.
 struct AttentionSides {

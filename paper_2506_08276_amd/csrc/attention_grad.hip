@@ -28,7 +28,6 @@ struct GradCfg {
     static constexpr int QUERY_STAGES = DP == 128 ? 2 : 3, KEY_STAGES = DP == 128 ? 2 : 4;
     static constexpr int QUERY_TILES = QUERY_STAGES * 2 * TILE * 2, KEY_TILES = KEY_STAGES * 2 * TILE * 2;  // bytes
     static constexpr int STATS = ATT_STEP * (int)sizeof(float2);                                             // per stage
-    static constexpr int DIAGONALS = GRAD_WAVES * 16 * 68 * (int)sizeof(float);
 };
 
 // fp16: lowers `factor` and scales `sums` where a value of this step would pass 2^15.
@@ -63,49 +62,78 @@ __device__ inline float lse_in_log2(float lse)  // of rows that see nothing: P i
     return lse == -INFINITY ? INFINITY : lse * LOG2E;
 }
 
-// Sums of a wavefront's dS^T (a query per lane, 64 keys in its registers) by relative position: added to sums[0 .. 94], of which place 31 + key - query, numbers within the tile, is
-// key - query's.  16 queries at a time lie in LDS as rows of 64 keys (and 4 more, so that 16 lanes' writes reach all banks), where lane l walks along its diagonal,
-// query by query from the last: key l - 15 + query until that is below 0, which is from there on lane l's other diagonal, 64 further.
-// Sums in LDS by atomic additions, 32 instead of these 48 accesses, took 160 cycles each.
-__device__ inline void add_diagonals(const f32x16 (&d)[2], bool valid, float *rows, float *sums, int lane)
+// Sums of dS along its diagonals, by relative position, without leaving the registers: a register is one row of the tile, a lane one column of it.  Row n + 16 c (and 4 more in the
+// upper half of the lanes) moves by n lanes within each 16 as it is added, so that a diagonal's elements meet in one lane: what stays within the 16 lanes is added to
+// a[c], what would leave them comes in again at the other end and is added to a[c + 1], 16 diagonals further.  Two additions per register.  (Rows written to LDS and
+// read along the diagonals took 110 us of the training batch's gradient, atomic additions in LDS 1100.)
+template <int N>
+__device__ inline void add_moved(float &stays, float &leaves, float x)
 {
-    const int half = lane >> 5, l32 = lane & 31;
-    float first[2], other[2];
-#pragma unroll
-    for (int part = 0; part < 2; ++part) {
-        wave_fence();
-        if ((l32 >> 4) == part) {
-#pragma unroll
-            for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    f32x4 x;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) x[e] = valid ? d[kt][4 * c + e] : 0.f;
-                    *reinterpret_cast<f32x4 *>(rows + (l32 & 15) * 68 + kt * 32 + 8 * c + 4 * half) = x;
-                }
-        }
-        wave_fence();
-        const float *near = rows + lane, *far = rows + lane + 64;
-        float sum = 0.f, until = 0.f;
-#pragma unroll
-        for (int step = 0; step < 16; ++step) {  // query 15 - step, key lane - step or lane - step + 64
-            // masks of low lanes only: one with its upper half set became a scalar move whose literal the hardware extends with zeros
-            const bool over = __builtin_amdgcn_inverse_ballot_w64((1ull << step) - 1);  // lanes below step
-            sum += (over ? far : near)[(15 - step) * 68 - step];
-            if (step < 15) until = __builtin_amdgcn_inverse_ballot_w64(1ull << step) ? sum : until;
-        }
-        first[part] = lane < 15 ? until : sum;
-        other[part] = sum - until;
+    if constexpr (N == 0) {
+        stays += x;
+    } else {
+        stays += __uint_as_float(dpp_mov<0x100 + N>(__float_as_uint(x)));        // lane i has lane i + N's, or 0
+        leaves += __uint_as_float(dpp_mov<0x110 + 16 - N>(__float_as_uint(x)));  // lane i has lane i + N - 16's, or 0
     }
-    // lane l of part 0 stands for key - query = l - 15, of part 1 for l - 31: places l + 16 and l
-    wave_fence();
-    sums[lane + 16] += first[0];
-    if (lane < 15) sums[lane + 80] += other[0];
-    wave_fence();
-    sums[lane] += first[1];
-    if (lane < 15) sums[lane + 64] += other[1];
-    wave_fence();
+}
+template <int R, int NA, int NV>
+__device__ inline void add_rows(float (&a)[NA], const f32x16 (&d)[NV])
+{
+    if constexpr (R < NV * 16) {
+        constexpr int row = R / 16 * 32 + acc_row(R % 16);
+        add_moved<row % 16>(a[row / 16], a[row / 16 + 1], d[R / 16][R % 16]);
+        add_rows<R + 1>(a, d);
+    }
+}
+// In p[0] the even 16 lanes of a pair have their own, the odd ones the even ones'; in p[1] the other way round.
+__device__ inline float2 both_rows(float v)
+{
+    const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return make_float2(__uint_as_float(p[0]), __uint_as_float(p[1]));
+}
+
+// dS^T with a query per lane and 64 keys in registers; sums[0] is relative position 0 within the tile.  Lane 16 b + i (of either half) holds in a[c] position 16 (c - b) - i + 4 half.
+__device__ inline void add_diagonals(const f32x16 (&d)[2], float *sums, int lane)
+{
+    float a[5] = {0.f, 0.f, 0.f, 0.f, 0.f};
+    add_rows<0>(a, d);
+    const bool odd = lane & 16;
+    const float2 one = both_rows(a[1]), three = both_rows(a[3]);
+    a[0] += odd ? 0.f : one.y;
+    a[2] += odd ? one.x : three.y;
+    a[4] += odd ? three.x : 0.f;
+    float *at = sums - (lane & 15) - (lane & 16) + 4 * (lane >> 5);
+    at[0] += a[0];
+    at[32] += a[2];
+    at[64] += a[4];
+}
+
+// A block's sums by relative position, its wavefronts' [NW][2][room] in order; the ends have what lies beyond, `behind` and `ahead` what a lane has added to none of them.  far:
+// LDS that is free behind the first barrier.
+template <int NW>
+__device__ inline void sums_by_position(const float *sums, int room, int distance, float behind, float ahead, float *far, float factor, float *to)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, positions = 2 * distance + 1, entries = bias_entries(distance);
+    const float *mine = sums + 2 * wave * room, *other = mine + room;
+    __syncthreads();
+    for (int e = lane; e < ATT_EXT; e += 64) {
+        behind += mine[e] + other[e];
+        ahead += mine[entries - 1 - e] + other[entries - 1 - e];
+    }
+    behind = wave_sum(behind);
+    ahead = wave_sum(ahead);
+    if (lane == 0) far[wave * 2] = behind, far[wave * 2 + 1] = ahead;
+    __syncthreads();
+    for (int i = threadIdx.x; i < positions; i += NW * 64) {
+        float sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            sum += sums[2 * w * room + i + ATT_EXT] + sums[(2 * w + 1) * room + i + ATT_EXT];
+            if (i == 0) sum += far[w * 2];
+            if (i == positions - 1) sum += far[w * 2 + 1];
+        }
+        to[i] = sum * factor;
+    }
 }
 
 // A block takes 128 queries of one head through their keys, as the forward pass does.  S^T and dP^T = V dO^T have a query per lane; dS^T, rounded, is the other operand of
@@ -127,7 +155,7 @@ __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void query_grad
     T *Ks = reinterpret_cast<T *>(smem), *Vs = Ks + STAGES * TILE;
     float *table = reinterpret_cast<float *>(smem + Cfg::QUERY_TILES);
     const int entries = bias_entries(a.distance), room = (entries + 3) & ~3;
-    float *sums = table + room, *rows = sums + GRAD_WAVES * room;  // per wavefront: sums by position, 16 rows of dS
+    float *sums = table + room;  // [4 wavefronts][2 halves][room]
 
     const AttentionItem item = items[blockIdx.x];
     if (item.tile < 0) return;
@@ -159,7 +187,7 @@ __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void query_grad
     if (BIAS) {
         make_bias(table, bias, bucket_of, a, h);
         if (by_position)
-            for (int i = tid; i < GRAD_WAVES * room; i += NT) sums[i] = 0.f;
+            for (int i = tid; i < 2 * GRAD_WAVES * room; i += NT) sums[i] = 0.f;
     }
     float my_delta = 0.f;
 #pragma unroll
@@ -253,15 +281,20 @@ __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void query_grad
                 }
         }
         if (BIAS && by_position) {
+            if (my_rows < 32) {
+#pragma unroll
+                for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) d[kt][r] = valid ? d[kt][r] : 0.f;
+            }
             if (near) {
-                add_diagonals(d, valid, rows + wave * 16 * 68, sums + wave * room + (j0 - p0 - 31 + a.distance + ATT_EXT), lane);
+                add_diagonals(d, sums + (2 * wave + half) * room + (j0 - p0 + a.distance + ATT_EXT), lane);
             } else {
                 float sum = 0.f;
 #pragma unroll
                 for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
                     for (int r = 0; r < 16; ++r) sum += d[kt][r];
-                if (!valid) sum = 0.f;
                 if (most <= -a.distance) behind += sum;
                 else ahead += sum;
             }
@@ -299,31 +332,9 @@ __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void query_grad
     store_columns<T, ND>(acc, a.scale / factor * (F16 ? 0x1p-15f : 1.f), dq + my_row * lddq + h * a.dim, valid, a.dim, lane);
 
     if (BIAS && by_position) {
-        // the ends have what lies beyond: each wavefront's, lane by lane, then over the lanes
-        const int positions = 2 * a.distance + 1;
-        const float *mine = sums + wave * room;
         if (t.begin == t.end) block_barrier();  // the sums are cleared
-        for (int e = lane; e < ATT_EXT; e += 64) {
-            behind += mine[e];
-            ahead += mine[entries - 1 - e];
-        }
-        behind = wave_sum(behind);
-        ahead = wave_sum(ahead);
-        float *far_sums = rows;
-        __syncthreads();
-        if (lane == 0) far_sums[wave * 2] = behind, far_sums[wave * 2 + 1] = ahead;
-        __syncthreads();
-        float *to = by_position + ((int64_t)item.tile * a.heads + h) * positions;
-        for (int i = tid; i < positions; i += NT) {
-            float sum = 0.f;
-#pragma unroll
-            for (int w = 0; w < GRAD_WAVES; ++w) {
-                sum += sums[w * room + i + ATT_EXT];
-                if (i == 0) sum += far_sums[w * 2];
-                if (i == positions - 1) sum += far_sums[w * 2 + 1];
-            }
-            to[i] = sum * (F16 ? 0x1p-15f : 1.f);
-        }
+        sums_by_position<GRAD_WAVES>(sums, room, a.distance, behind, ahead, reinterpret_cast<float *>(smem), F16 ? 0x1p-15f : 1.f,
+                                     by_position + ((int64_t)item.tile * a.heads + h) * (2 * a.distance + 1));
     }
 }
 
@@ -573,39 +584,35 @@ struct WholeCfg {
     static constexpr int KEYS = 32 * NW, STAGE = 32 * DP;  // elements of a stage's Q, or dO
     static constexpr int K_BYTES = KEYS * DP * 2, STAGES_BYTES = 2 * 2 * STAGE * 2, DS_BYTES = 32 * KEYS * 2, NUMBERS_BYTES = KEYS * 2 * (int)sizeof(float);
     static constexpr int FIXED = K_BYTES + STAGES_BYTES + DS_BYTES + NUMBERS_BYTES;
-    static constexpr int DIAGONALS = NW * 32 * 36 * (int)sizeof(float);
 };
 
-// dS in LDS: rows of queries, 16-byte chunks of keys XORed with the row.
-template <int NW>
-__device__ inline int whole_swizzle(int row) { return NW == 4 ? row & 15 : row & 31; }
-
-// As add_diagonals, of 32 keys (one per lane) and 32 queries (in its registers): sums[31 + key - query].  Rows of keys in LDS; lane l and lane l + 32 walk along diagonal l, or l + 32,
-// for the queries 0 .. 15 and 16 .. 31.
-__device__ inline void add_diagonals_of_keys(const f32x16 &d, float *rows, float *sums, int lane)
+// As add_diagonals, of dS with a key per lane and 32 queries in registers: lane 16 b + i holds in a[c] position 16 (b - c) + i - 4 half.
+__device__ inline void add_diagonals_of_keys(const f32x16 (&d)[1], float *sums, int lane)
 {
-    const int half = lane >> 5, l32 = lane & 31;
-    wave_fence();
+    float a[3] = {0.f, 0.f, 0.f};
+    add_rows<0>(a, d);
+    const bool odd = lane & 16;
+    const float2 one = both_rows(a[1]);
+    a[0] += odd ? 0.f : one.y;
+    a[2] += odd ? one.x : 0.f;
+    float *at = sums + (lane & 31) - 4 * (lane >> 5);
+    at[0] += a[0];
+    at[-32] += a[2];
+}
+
+// Operand A of dQ^T for four groups of 32 keys from group FROM on.
+template <class T, int DP, int FROM>
+__device__ inline void groups_of_keys(const uint32_t (&at)[2], typename Half8<T>::type (&x)[4])
+{
+    constexpr int GROUP = 32 * DP * 2;
+    s16x4 o[8];
+    asm volatile("ds_read_b64_tr_b16 %0, %8 offset:%10\n\tds_read_b64_tr_b16 %1, %9 offset:%10\n\tds_read_b64_tr_b16 %2, %8 offset:%11\n\t"
+                 "ds_read_b64_tr_b16 %3, %9 offset:%11\n\tds_read_b64_tr_b16 %4, %8 offset:%12\n\tds_read_b64_tr_b16 %5, %9 offset:%12\n\t"
+                 "ds_read_b64_tr_b16 %6, %8 offset:%13\n\tds_read_b64_tr_b16 %7, %9 offset:%13\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(o[0]), "=&v"(o[1]), "=&v"(o[2]), "=&v"(o[3]), "=&v"(o[4]), "=&v"(o[5]), "=&v"(o[6]), "=&v"(o[7])
+                 : "v"(at[0]), "v"(at[1]), "n"(FROM * GROUP), "n"((FROM + 1) * GROUP), "n"((FROM + 2) * GROUP), "n"((FROM + 3) * GROUP));
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-        const f32x4 x = {d[4 * c], d[4 * c + 1], d[4 * c + 2], d[4 * c + 3]};
-        *reinterpret_cast<f32x4 *>(rows + l32 * 36 + 8 * c + 4 * half) = x;
-    }
-    wave_fence();
-    // query 16 half + 15 - step, key l32 - 31 + query, or 32 more
-    const float *near = rows + (l32 - 16 + 16 * half) * 36 + 16 * half + 15, *far = near + 32 * 36;
-    float sum = 0.f, until = 0.f;
-#pragma unroll
-    for (int step = 0; step < 16; ++step) {
-        const bool over = __builtin_amdgcn_inverse_ballot_w64(((1ull << (step + 16)) - 1) | ((1ull << step) - 1) << 32);
-        sum += (over ? far : near)[-step * 37];
-        until = __builtin_amdgcn_inverse_ballot_w64(1ull << (step + 16) | 1ull << (32 + step)) ? sum : until;
-    }
-    const float first = lane < 48 ? until : sum, other = sum - first;
-    const float a = both_halves_sum(first), b = both_halves_sum(other);
-    wave_fence();
-    sums[lane] += half ? b : a;
-    wave_fence();
+    for (int u = 0; u < 4; ++u) x[u] = Columns<T, DP>::join(o[2 * u], o[2 * u + 1]);
 }
 
 template <class T, int DP, int NW, bool BIAS>
@@ -624,7 +631,7 @@ __global__ __launch_bounds__(NW * 64, 2) void whole_grad_kernel(const AttentionI
     float *numbers = reinterpret_cast<float *>(smem + Cfg::K_BYTES + Cfg::STAGES_BYTES + Cfg::DS_BYTES);   // [-lse, -delta][KEYS]
     float *table = reinterpret_cast<float *>(smem + Cfg::FIXED);
     const int entries = bias_entries(a.distance), room = (entries + 3) & ~3;
-    float *sums = table + room, *diagonals = sums + NW * room;
+    float *sums = table + room;  // [NW wavefronts][2 halves][room]
 
     const AttentionItem item = items[blockIdx.x];
     if (item.tile < 0) return;
@@ -664,7 +671,7 @@ __global__ __launch_bounds__(NW * 64, 2) void whole_grad_kernel(const AttentionI
     if (BIAS) {
         make_bias(table, bias, bucket_of, a, h);
         if (by_position)
-            for (int i = tid; i < NW * room; i += NW * 64) sums[i] = 0.f;
+            for (int i = tid; i < 2 * NW * room; i += NW * 64) sums[i] = 0.f;
     }
     float my_delta = 0.f;
 #pragma unroll
@@ -696,6 +703,14 @@ __global__ __launch_bounds__(NW * 64, 2) void whole_grad_kernel(const AttentionI
         }
     }
     const int key_groups = (lk + 31) / 32;
+    // dS in LDS: rows of queries, 16-byte chunks of keys XORed with the row's last three bits.  The lane's place in rows 4 half + {0..3}; columns of no keys are zeros.
+    int ds_at[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) ds_at[e] = (4 * half + e) * KEYS + (((j >> 3) ^ (4 * half + e)) << 3) + (j & 7);
+    if (my_keys <= 0)
+        for (int row = 0; row < 32; row += 8)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) Ds[ds_at[e] + row * KEYS] = (T)0.f;
     arrived(vf);
     V8 kf[NS];
     f32x4 dq_acc[MINE];
@@ -724,7 +739,7 @@ __global__ __launch_bounds__(NW * 64, 2) void whole_grad_kernel(const AttentionI
         }
         if (step + 1 < steps) request(step + 1, stage ^ 1);
         if (my_keys > 0) {
-            f32x16 s, d;
+            f32x16 s, d[1];
             const int i0 = step * 32, pw = t.first + i0;
             const int least = wave * 32 - (pw + 31), most = wave * 32 + 31 - pw;  // relative positions
             const bool near = most > -a.distance && least < a.distance;
@@ -733,7 +748,7 @@ __global__ __launch_bounds__(NW * 64, 2) void whole_grad_kernel(const AttentionI
             for (int c = 0; c < 4; ++c) {
                 const f32x4 x = *reinterpret_cast<const f32x4 *>(numbers + i0 + 4 * half + 8 * c), y = *reinterpret_cast<const f32x4 *>(numbers + KEYS + i0 + 4 * half + 8 * c);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) ls[4 * c + e] = x[e], d[4 * c + e] = y[e];
+                for (int e = 0; e < 4; ++e) ls[4 * c + e] = x[e], d[0][4 * c + e] = y[e];
             }
             if (BIAS && near) {
                 const int at = one_register(Cfg::FIXED / 4 + j - pw - 4 * half - 27 + a.distance + ATT_EXT);
@@ -747,21 +762,21 @@ __global__ __launch_bounds__(NW * 64, 2) void whole_grad_kernel(const AttentionI
 #pragma unroll
             for (int i = 0; i < NS; ++i) {
                 s = att_mfma(row_operand<T, DP>(Qt, 0, i, lane), kf[i], s);
-                d = att_mfma(row_operand<T, DP>(Gt, 0, i, lane), vf[i], d);
+                d[0] = att_mfma(row_operand<T, DP>(Gt, 0, i, lane), vf[i], d[0]);
             }
             V8 gc[ND], qc[ND];
             columns.template both<0>(Gt, Qt, gc, qc);
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], scale2, ls[r]));
-                d[r] *= s[r];
+                d[0][r] *= s[r];
             }
             if (!valid)  // keys behind the last one
 #pragma unroll
-                for (int r = 0; r < 16; ++r) d[r] = 0.f;
+                for (int r = 0; r < 16; ++r) d[0][r] = 0.f;
 #pragma unroll
             for (int w = 0; w < 2; ++w) {
-                const V8 pf = rounded<T>(s, w), df = rounded<T>(d, w);
+                const V8 pf = rounded<T>(s, w), df = rounded<T>(d[0], w);
 #pragma unroll
                 for (int dt = 0; dt < ND; ++dt) {
                     dv_acc[dt] = att_mfma(gc[dt], pf, dv_acc[dt]);
@@ -769,14 +784,14 @@ __global__ __launch_bounds__(NW * 64, 2) void whole_grad_kernel(const AttentionI
                 }
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {  // dS to its rows
-                    const int row = acc_row(8 * w + i) + 4 * half;
-                    Ds[row * KEYS + (((j >> 3) ^ whole_swizzle<NW>(row)) << 3) + (j & 7)] = df[i];
+                    const int row = acc_row(8 * w + i);  // less 4 half
+                    Ds[ds_at[row & 3] + (row & ~7) * KEYS] = df[i];
                 }
                 if (w == 0) columns.template both<16>(Gt, Qt, gc, qc);
             }
-            if (BIAS && by_position) {
-                // register r of a lane: query i0 + 4 half + acc_row(r), as add_diagonals_of_keys takes them
-                add_diagonals_of_keys(d, diagonals + wave * 32 * 36, sums + wave * room + min(max(wave * 32 - pw - 31, -a.distance - 62), a.distance) + a.distance + ATT_EXT, lane);
+            if (BIAS && by_position) {  // a tile that is all behind `distance`, to either side, adds to places there
+                const int first = min(max(wave * 32 - pw, -a.distance - 31), a.distance + 31);
+                add_diagonals_of_keys(d, sums + (2 * wave + half) * room + first + a.distance + ATT_EXT, lane);
             }
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -785,11 +800,16 @@ __global__ __launch_bounds__(NW * 64, 2) void whole_grad_kernel(const AttentionI
         for (int m = 0; m < MINE; ++m) {
             const int tile = (wave + m * NW) % TILES, row = tile / (DP / 16) * 16 + l16;
             f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-            for (int u = 0; u < key_groups; ++u) {
-                const V8 b = *reinterpret_cast<const V8 *>(Ds + row * KEYS + (((u * 4 + g16) ^ whole_swizzle<NW>(row)) << 3));
-                s16x4 x[2];
-                transposed2(k_at[m][0] + u * 32 * DP * 2, k_at[m][1] + u * 32 * DP * 2, x);
-                acc = att_mfma16(Columns<T, DP>::join(x[0], x[1]), b, acc);
+#pragma unroll
+            for (int part = 0; part < NW / 4; ++part) {  // 128 keys at a time
+                if (part * 4 >= key_groups) continue;
+                V8 b[4], x[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) b[u] = *reinterpret_cast<const V8 *>(Ds + row * KEYS + ((((part * 4 + u) * 4 + g16) ^ (row & 7)) << 3));
+                if (part == 0) groups_of_keys<T, DP, 0>(k_at[m], x);
+                else groups_of_keys<T, DP, 4>(k_at[m], x);
+#pragma unroll
+                for (int u = 0; u < 4; ++u) acc = att_mfma16(x[u], b[u], acc);
             }
             dq_acc[m] = acc;
         }
@@ -799,31 +819,8 @@ __global__ __launch_bounds__(NW * 64, 2) void whole_grad_kernel(const AttentionI
     store_columns<T, ND>(dk_acc, a.scale, dk + my_row * lddk + h * a.dim, valid, a.dim, lane);
     store_columns<T, ND>(dv_acc, 1.f, dv + my_row * lddv + h * a.dim, valid, a.dim, lane);
 
-    if (BIAS && by_position) {
-        const int positions = 2 * a.distance + 1;
-        const float *mine = sums + wave * room;
-        float behind = 0.f, ahead = 0.f;
-        __syncthreads();
-        for (int e = lane; e < ATT_EXT; e += 64) {
-            behind += mine[e];
-            ahead += mine[entries - 1 - e];
-        }
-        behind = wave_sum(behind);
-        ahead = wave_sum(ahead);
-        if (lane == 0) diagonals[wave * 2] = behind, diagonals[wave * 2 + 1] = ahead;
-        __syncthreads();
-        float *to = by_position + ((int64_t)item.tile * a.heads + h) * positions;
-        for (int i = tid; i < positions; i += NW * 64) {
-            float sum = 0.f;
-#pragma unroll
-            for (int w = 0; w < NW; ++w) {
-                sum += sums[w * room + i + ATT_EXT];
-                if (i == 0) sum += diagonals[w * 2];
-                if (i == positions - 1) sum += diagonals[w * 2 + 1];
-            }
-            to[i] = sum;
-        }
-    }
+    if (BIAS && by_position)
+        sums_by_position<NW>(sums, room, a.distance, 0.f, 0.f, reinterpret_cast<float *>(Ds), 1.f, by_position + ((int64_t)item.tile * a.heads + h) * (2 * a.distance + 1));
 }
 
 // Sums of the bias's gradient by relative position over up to POSITION_ROWS tiles each, in their order.
@@ -939,7 +936,7 @@ extern "C" int leann_attention_backward(leann_ctx *ctx, const leann_attention_pl
         constexpr bool BIAS = decltype(with_bias)::value;
         typedef GradCfg<DP> Cfg;
         const int table = BIAS ? ((positions + 2 * ATT_EXT + 3) & ~3) * 4 : 0;
-        const int query_smem = Cfg::QUERY_TILES + (by_position ? table * (1 + GRAD_WAVES) + Cfg::DIAGONALS : table);
+        const int query_smem = Cfg::QUERY_TILES + table * (by_position ? 1 + 2 * GRAD_WAVES : 1);
         if (sides.n_query_items)
             hipLaunchKernelGGL((query_grad_kernel<T, DP, BIAS>), dim3(sides.n_query_items), dim3(GRAD_WAVES * 64), query_smem, ctx->stream, sides.query_items, sides.query_tiles, a,
                                (const T *)dout_dev, ldd, (const T *)q_dev, ldq, (const T *)k_dev, ldk, (const T *)v_dev, ldv, (const T *)out_dev, ldo, lse_dev, plan->Tq, bias_dev,
@@ -957,7 +954,7 @@ extern "C" int leann_attention_backward(leann_ctx *ctx, const leann_attention_pl
                 constexpr int NW = decltype(waves)::value;
                 typedef WholeCfg<DP, NW> Whole;
                 if (!w.n_items) return;
-                hipLaunchKernelGGL((whole_grad_kernel<T, DP, NW, BIAS>), dim3(w.n_items), dim3(NW * 64), Whole::FIXED + (rows ? table * (1 + NW) + Whole::DIAGONALS : table), ctx->stream,
+                hipLaunchKernelGGL((whole_grad_kernel<T, DP, NW, BIAS>), dim3(w.n_items), dim3(NW * 64), Whole::FIXED + table * (rows ? 1 + 2 * NW : 1), ctx->stream,
                                    w.items, w.tiles, a, (const T *)dout_dev, ldd, (const T *)q_dev, ldq, (const T *)k_dev, ldk, (const T *)v_dev, ldv, (const T *)out_dev, ldo, lse_dev,
                                    plan->Tq, bias_dev, plan->bucket_of, (T *)dq_dev, lddq, (T *)dk_dev, lddk, (T *)dv_dev, lddv, rows);
                 if (rows) rows += (size_t)w.n_tiles * plan->heads * positions;
