@@ -12,6 +12,7 @@ constexpr int ATT_EXT = 104;  // a wavefront's 32 rows and 64 of the other side 
 // What the two gradient kernels go through.
 struct AttentionSides {
     int32_t n_tiles = 0, n_query_items = 0, n_key_items = 0, n_joins = 0, n_slots = 0;  // tiles: of queries
+    int32_t key_waves = 4;  // wavefronts of 32 keys of their own in a block for keys: 4 or 2
     const AttentionTile *query_tiles = nullptr, *key_tiles = nullptr;
     const AttentionItem *query_items = nullptr, *key_items = nullptr;
     const AttentionJoin *joins = nullptr;

@@ -132,7 +132,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : 1) void at
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const int key = kt * 32 + acc_row(r);
-                    s[kt][r] = (key < least) & (key >= sinks) ? -INFINITY : s[kt][r];
+                    s[kt][r] = ((key < least) & (key >= sinks)) ? -INFINITY : s[kt][r];
                 }
         }
         float top = s[0][0];
@@ -340,11 +340,17 @@ int make_plan(leann_ctx *ctx, const int32_t *q_rows, const int32_t *k_rows, cons
         std::vector<int32_t> query_of, key_of;
         std::vector<AttentionJoin> key_joins, none;
         att_make_tiles(r, n, q_rows, k_rows, first, false, share, 128, 0, query_tiles, query_of, none, taken);
-        // Keys that many queries see, as a sequence's first ones, have their queries split, so that no block has much more than a compute unit's share of the work.
+        // 64 keys per block where 128 would make fewer than two blocks per compute unit.
         att_make_tiles(r, n, q_rows, k_rows, first, true, share, 128, 0, key_tiles, key_of, key_joins, taken);
+        if ((int64_t)key_tiles.size() * p->kv_heads < 2 * cus) {
+            sides->key_waves = 2;
+            key_tiles.clear();
+            att_make_tiles(r, n, q_rows, k_rows, first, true, share, 64, 0, key_tiles, key_of, key_joins, taken);
+        }
+        // Keys that many queries see, as a sequence's first ones, have their queries split, so that no block has much more than a compute unit's share of the work.
         if (const int split = att_split(key_tiles, p->kv_heads, cus, 1, 16)) {
             key_tiles.clear();
-            att_make_tiles(r, n, q_rows, k_rows, first, true, share, 128, split, key_tiles, key_of, key_joins, taken);
+            att_make_tiles(r, n, q_rows, k_rows, first, true, share, sides->key_waves * 32, split, key_tiles, key_of, key_joins, taken);
         }
         for (const AttentionJoin &j : key_joins) sides->n_slots += j.slots;
         sides->n_tiles = (int32_t)query_tiles.size();

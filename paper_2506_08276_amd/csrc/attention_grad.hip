@@ -277,7 +277,7 @@ __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void query_grad
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const int key = kt * 32 + acc_row(r);
-                    d[kt][r] = (key < from) & (key >= sinks) ? 0.f : d[kt][r];
+                    d[kt][r] = ((key < from) & (key >= sinks)) ? 0.f : d[kt][r];
                 }
         }
         if (BIAS && by_position) {
@@ -338,9 +338,10 @@ __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void query_grad
     }
 }
 
-// A block takes 128 keys of one key head through the queries that see them, of every head that shares it: S = Q K^T and dP = dO V^T have a key per lane; P and dS, rounded, are the
+// A block takes 32 KW keys of one key head through the queries that see them, of every head that shares it: S = Q K^T and dP = dO V^T have a key per lane; P and dS, rounded, are the
 // other operands of dV^T = dO^T P and dK^T = Q^T dS.  K and V stay in registers; Q, dO and the queries' numbers come from memory to LDS, STAGES - 1 tiles ahead.
-template <class T, int DP, bool BIAS>
+// KW = 4: a wavefront has 32 keys.  KW = 2, for few keys: two wavefronts share them, each with 32 of a step's 64 queries, and their sums meet in LDS at the end.
+template <class T, int DP, int KW, bool BIAS>
 __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void key_grad_kernel(
     const AttentionItem *__restrict__ items, const AttentionTile *__restrict__ tiles, AttentionShape a, const T *__restrict__ dout, int64_t ldd, const T *__restrict__ q,
     int64_t ldq, const T *__restrict__ k, int64_t ldk, const T *__restrict__ v, int64_t ldv, const float2 *__restrict__ stats, int64_t Tq, const float *__restrict__ bias,
@@ -361,12 +362,13 @@ __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void key_grad_k
     const AttentionTile t = tiles[item.tile];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, l32 = lane & 31;
     const int g = item.head;
-    const int my_rows = min(32, t.rows - wave * 32), jw = t.at + wave * 32, j = jw + l32;
-    const int64_t my_row = t.row0 + wave * 32 + l32;
+    const int own = wave % KW * 32, share = wave / KW;  // first of the wavefront's keys in the block, which of the sharing wavefronts it is
+    const int my_rows = min(32, t.rows - own), jw = t.at + own, j = jw + l32;
+    const int64_t my_row = t.row0 + own + l32;
     const bool valid = l32 < my_rows;
     V8 kf[NS], vf[NS];
-    load_rows<T, DP>(k + (int64_t)(t.row0 + wave * 32) * ldk + g * a.dim, ldk, my_rows, a.dim, lane, kf);
-    load_rows<T, DP>(v + (int64_t)(t.row0 + wave * 32) * ldv + g * a.dim, ldv, my_rows, a.dim, lane, vf);
+    load_rows<T, DP>(k + (int64_t)(t.row0 + own) * ldk + g * a.dim, ldk, my_rows, a.dim, lane, kf);
+    load_rows<T, DP>(v + (int64_t)(t.row0 + own) * ldv + g * a.dim, ldv, my_rows, a.dim, lane, vf);
 
     Requests qr, gr;
     qr.init(ldq, a.dim, wave, lane);
@@ -436,7 +438,8 @@ __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void key_grad_k
 
         bool taken_out = false;
 #pragma unroll
-        for (int qs = 0; qs < 2; ++qs) {
+        for (int turn = 0; turn < KW / 2; ++turn) {
+            const int qs = KW == 4 ? turn : share;  // which 32 of the 64 queries
             f32x16 s[1], d[1];
             // register r is query i0 + 32 qs + 4 half + acc_row(r); queries behind the last one have rows of zeros and any numbers
             const int from = i0 + qs * 32 + 4 * half, p = t.first + from;
@@ -464,8 +467,8 @@ __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void key_grad_k
                 d[0] = att_mfma(row_operand<T, DP>(Gt, qs * 32, i, lane), vf[i], d[0]);
             }
             V8 qc[ND], gc[ND];  // of the first 16 queries
-            if (qs == 0) columns.template both<0>(Gt, Qt, gc, qc);
-            else columns.template both<32>(Gt, Qt, gc, qc);
+            const T *Gh = Gt + qs * 32 * DP, *Qh = Qt + qs * 32 * DP;
+            columns.template both<0>(Gh, Qh, gc, qc);
             if (BIAS && !near) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) ls[r] += c;
@@ -517,10 +520,7 @@ __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void key_grad_k
                     dv_acc[dt] = att_mfma(gc[dt], pf, dv_acc[dt]);
                     dk_acc[dt] = att_mfma(qc[dt], df, dk_acc[dt]);
                 }
-                if (w == 0) {
-                    if (qs == 0) columns.template both<16>(Gt, Qt, gc, qc);
-                    else columns.template both<48>(Gt, Qt, gc, qc);
-                }
+                if (w == 0) columns.template both<16>(Gh, Qh, gc, qc);
             }
         }
         if (taken_out) {
@@ -530,9 +530,39 @@ __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void key_grad_k
         }
     }
     if (hurt) factor = __builtin_nanf("");
-    const float dk_factor = a.scale / factor * (F16 ? 0x1p-15f : 1.f), dv_factor = F16 ? 0x1p-15f : 1.f;
+    float dk_factor = a.scale / factor * (F16 ? 0x1p-15f : 1.f), dv_factor = F16 ? 0x1p-15f : 1.f;
+    if constexpr (KW == 2) {  // the second wavefront's sums, made alike, go to the first one's
+        f32x4 *meet = reinterpret_cast<f32x4 *>(smem) + (wave % KW) * (2 * ND * 4 * 64) + lane;
+        __syncthreads();
+        if (share) {
+#pragma unroll
+            for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    f32x4 x, y;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[e] = dk_acc[dt][4 * c + e] * dk_factor, y[e] = dv_acc[dt][4 * c + e] * dv_factor;
+                    meet[(dt * 4 + c) * 64] = x;
+                    meet[((ND + dt) * 4 + c) * 64] = y;
+                }
+        }
+        __syncthreads();
+        if (share) return;
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const f32x4 x = meet[(dt * 4 + c) * 64], y = meet[((ND + dt) * 4 + c) * 64];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    dk_acc[dt][4 * c + e] = fmaf(dk_acc[dt][4 * c + e], dk_factor, x[e]);
+                    dv_acc[dt][4 * c + e] = fmaf(dv_acc[dt][4 * c + e], dv_factor, y[e]);
+                }
+            }
+        dk_factor = dv_factor = 1.f;
+    }
     if (t.slot >= 0) {  // a part of the queries: [slot][key head][dK, dV][128][DP]
-        float *to = parts + ((((int64_t)t.slot * (a.heads / a.share) + g) * 2) * GRAD_WAVES * 32 + wave * 32 + l32) * DP + 4 * half;
+        float *to = parts + ((((int64_t)t.slot * (a.heads / a.share) + g) * 2) * GRAD_WAVES * 32 + own + l32) * DP + 4 * half;
         if (valid)
 #pragma unroll
             for (int dt = 0; dt < ND; ++dt)
@@ -869,8 +899,8 @@ int allow_whole()
 template <class T, int DP>
 int allow_grad()
 {
-    for (const void *f : {(const void *)query_grad_kernel<T, DP, false>, (const void *)query_grad_kernel<T, DP, true>, (const void *)key_grad_kernel<T, DP, false>,
-                          (const void *)key_grad_kernel<T, DP, true>})
+    for (const void *f : {(const void *)query_grad_kernel<T, DP, false>, (const void *)query_grad_kernel<T, DP, true>, (const void *)key_grad_kernel<T, DP, 4, false>,
+                          (const void *)key_grad_kernel<T, DP, 4, true>, (const void *)key_grad_kernel<T, DP, 2, false>, (const void *)key_grad_kernel<T, DP, 2, true>})
         LEANN_HIP(hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024));
     return LEANN_OK;
 }
@@ -941,10 +971,12 @@ extern "C" int leann_attention_backward(leann_ctx *ctx, const leann_attention_pl
             hipLaunchKernelGGL((query_grad_kernel<T, DP, BIAS>), dim3(sides.n_query_items), dim3(GRAD_WAVES * 64), query_smem, ctx->stream, sides.query_items, sides.query_tiles, a,
                                (const T *)dout_dev, ldd, (const T *)q_dev, ldq, (const T *)k_dev, ldk, (const T *)v_dev, ldv, (const T *)out_dev, ldo, lse_dev, plan->Tq, bias_dev,
                                plan->bucket_of, (T *)dq_dev, lddq, stats, by_position);
-        if (sides.n_key_items)
-            hipLaunchKernelGGL((key_grad_kernel<T, DP, BIAS>), dim3(sides.n_key_items), dim3(GRAD_WAVES * 64), Cfg::KEY_TILES + Cfg::KEY_STAGES * Cfg::STATS + table, ctx->stream,
-                               sides.key_items, sides.key_tiles, a, (const T *)dout_dev, ldd, (const T *)q_dev, ldq, (const T *)k_dev, ldk, (const T *)v_dev, ldv, stats, plan->Tq,
-                               bias_dev, plan->bucket_of, (T *)dk_dev, lddk, (T *)dv_dev, lddv, parts);
+        auto keys = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, dim3(sides.n_key_items), dim3(GRAD_WAVES * 64), Cfg::KEY_TILES + Cfg::KEY_STAGES * Cfg::STATS + table, ctx->stream, sides.key_items,
+                               sides.key_tiles, a, (const T *)dout_dev, ldd, (const T *)q_dev, ldq, (const T *)k_dev, ldk, (const T *)v_dev, ldv, stats, plan->Tq, bias_dev,
+                               plan->bucket_of, (T *)dk_dev, lddk, (T *)dv_dev, lddv, parts);
+        };
+        if (sides.n_key_items) sides.key_waves == 4 ? keys(key_grad_kernel<T, DP, 4, BIAS>) : keys(key_grad_kernel<T, DP, 2, BIAS>);
         if (sides.n_joins)
             hipLaunchKernelGGL(key_join_kernel<T>, dim3(sides.n_joins, plan->kv_heads, 2), dim3(256), 0, ctx->stream, sides.joins, plan->kv_heads, plan->dim, DP, parts,
                                (T *)dk_dev, lddk, (T *)dv_dev, lddv);
