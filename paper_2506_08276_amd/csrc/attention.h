@@ -6,6 +6,7 @@
 constexpr int ATT_MOST_DISTANCE = 1024;
 constexpr float ATT_LEAST_SCALE = 0x1p-20f, ATT_MOST_SCALE = 0x1p20f;
 constexpr int64_t ATT_MOST_LD = (int64_t)1 << 22;  // 256 rows are within a buffer's 2^31 bytes
+constexpr int ATT_LDS = 160 * 1024;                  // of a compute unit
 constexpr int ATT_WHOLE = 256;                      // keys and queries that one block's gradient kernel takes
 constexpr int ATT_EXT = 104;  // a wavefront's 32 rows and 64 of the other side have relative positions in a range of 95; sums of theirs touch nine places more
 
@@ -413,10 +414,21 @@ __device__ inline void add_nonfinite(f32x16 (&o)[ND], const T *base, int64_t ld,
     });
 }
 
+__host__ __device__ inline int bias_entries(int distance) { return 2 * distance + 1 + 2 * ATT_EXT; }
+
+// LDS of a block that takes a sequence whole (whole_grad_kernel): NW wavefronts, rows of DP.
+template <int DP, int NW>
+struct WholeCfg {
+    static constexpr int KEYS = 32 * NW, STAGE = 32 * DP;  // elements of a stage's Q, or dO
+    static constexpr int K_BYTES = KEYS * DP * 2, STAGES_BYTES = 2 * 2 * STAGE * 2, DS_BYTES = 32 * KEYS * 2, NUMBERS_BYTES = KEYS * 2 * (int)sizeof(float);
+    static constexpr int FIXED = K_BYTES + STAGES_BYTES + DS_BYTES + NUMBERS_BYTES;
+    // With a bias one table, with its gradient two more per wavefront.
+    static int bytes(int distance, bool bias, bool dbias) { return FIXED + (bias ? ((bias_entries(distance) + 3) & ~3) * 4 * (dbias ? 1 + 2 * NW : 1) : 0); }
+};
+
 // The bias of one head by relative position, in units of the scores before they are scaled, so that the products of queries and keys add to it:
 // [2 distance + 1 + 2 ATT_EXT], the ends repeated.  A finite bias beyond 2^100 counts as 2^100, which scores of any size are lost against: a row of them is
 // even, as it would be in numbers without end, and no difference is one of infinities.
-__device__ inline int bias_entries(int distance) { return 2 * distance + 1 + 2 * ATT_EXT; }
 __device__ inline void make_bias(float *table, const float *bias, const int32_t *bucket_of, const AttentionShape &a, int head)
 {
     const float inverse = 1.f / __builtin_fabsf(a.scale);

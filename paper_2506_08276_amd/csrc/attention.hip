@@ -302,6 +302,11 @@ int make_plan(leann_ctx *ctx, const int32_t *q_rows, const int32_t *k_rows, cons
         p->Tk += k_rows[s];
         if (q_rows[s] && k_rows[s]) furthest = std::max<int64_t>({furthest, (int64_t)first[s] + q_rows[s] - 1, (int64_t)k_rows[s] - 1 - first[s]});
     }
+    std::vector<int32_t> buckets;
+    if (bucket_of) {  // no longer than the sequences
+        p->distance = (int32_t)std::min<int64_t>(distance, furthest);
+        buckets.assign(bucket_of + distance - p->distance, bucket_of + distance + p->distance + 1);
+    }
     // 32 queries per block where no sequence has more: the other wavefronts would only load.  128 where they share the keys' tiles.
     p->query_waves = longest <= 32 ? 1 : 4;
     std::vector<AttentionTile> tiles;
@@ -367,14 +372,19 @@ int make_plan(leann_ctx *ctx, const int32_t *q_rows, const int32_t *k_rows, cons
     std::vector<char> taken(n, 0);
     const bool sees_all = r.left >= (1 << 30) && r.right >= (1 << 30);
     int n_taken = 0;
-    for (int s = 0; s < n; ++s) n_taken += taken[s] = sees_all && share == 1 && p->dim <= 64 && q_rows[s] <= ATT_WHOLE && k_rows[s] <= ATT_WHOLE;
+    auto in_class = [&](int s) { return q_rows[s] > ATT_WHOLE / 2 || k_rows[s] > ATT_WHOLE / 2 ? 1 : 0; };
+    // The tables of biases and their sums go by the distance that the plan's longest sequence has: beyond about 600 they leave a block of 8 wavefronts too little LDS.
+    const bool fits[2] = {(p->dim <= 32 ? WholeCfg<32, 4>::bytes(p->distance, bucket_of, true) : WholeCfg<64, 4>::bytes(p->distance, bucket_of, true)) <= ATT_LDS,
+                          (p->dim <= 32 ? WholeCfg<32, 8>::bytes(p->distance, bucket_of, true) : WholeCfg<64, 8>::bytes(p->distance, bucket_of, true)) <= ATT_LDS};
+    for (int s = 0; s < n; ++s)
+        n_taken += taken[s] = sees_all && share == 1 && p->dim <= 64 && q_rows[s] <= ATT_WHOLE && k_rows[s] <= ATT_WHOLE && fits[in_class(s)];
     if (n_taken) make_sides(&taken, &p->others, others_at);
     for (int c = 0; n_taken && c < 2; ++c) {
         std::vector<AttentionTile> whole;
         std::vector<int32_t> whole_of(1, 0);
         int64_t q0 = 0, k0 = 0;
         for (int s = 0; s < n; q0 += q_rows[s], k0 += k_rows[s], ++s) {
-            if (!taken[s] || (q_rows[s] > ATT_WHOLE / 2 || k_rows[s] > ATT_WHOLE / 2) != (c == 1) || (!q_rows[s] && !k_rows[s])) continue;
+            if (!taken[s] || in_class(s) != c || (!q_rows[s] && !k_rows[s])) continue;
             AttentionTile t = {};
             t.row0 = (int32_t)k0;
             t.rows = k_rows[s];
@@ -393,11 +403,6 @@ int make_plan(leann_ctx *ctx, const int32_t *q_rows, const int32_t *k_rows, cons
     if (most_blocks > ((size_t)1 << 24) - 1) {
         leann_set_error("leann_attention_create: sequences of this number and length are not covered (more than 2^24 - 1 workgroups in a launch)");
         return LEANN_ESHAPE;
-    }
-    std::vector<int32_t> buckets;
-    if (bucket_of) {  // no longer than the sequences
-        p->distance = (int32_t)std::min<int64_t>(distance, furthest);
-        buckets.assign(bucket_of + distance - p->distance, bucket_of + distance + p->distance + 1);
     }
     const size_t buckets_at = put(buckets);
     LEANN_TRY(ctx->reserve(p->mem, std::max<size_t>(image.size(), 1)));

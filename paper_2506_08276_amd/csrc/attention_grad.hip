@@ -609,12 +609,6 @@ __global__ __launch_bounds__(256) void key_join_kernel(const AttentionJoin *__re
 // the two kernels above read all but O twice, which bounds them there.  A wavefront has 32 keys in registers, K in LDS as well; the queries go by, 32 at a time: S = Q K^T and
 // dP = dO V^T with a key per lane, P and dS from registers into dV^T and dK^T as in key_grad_kernel; dS, rounded, through LDS into dQ^T = K^T dS^T, of which each
 // wavefront has tiles of 16 x 16, all keys of them.  The stores of a step's dQ are issued behind the next step's wait, which else would be for them.
-template <int DP, int NW>
-struct WholeCfg {
-    static constexpr int KEYS = 32 * NW, STAGE = 32 * DP;  // elements of a stage's Q, or dO
-    static constexpr int K_BYTES = KEYS * DP * 2, STAGES_BYTES = 2 * 2 * STAGE * 2, DS_BYTES = 32 * KEYS * 2, NUMBERS_BYTES = KEYS * 2 * (int)sizeof(float);
-    static constexpr int FIXED = K_BYTES + STAGES_BYTES + DS_BYTES + NUMBERS_BYTES;
-};
 
 // As add_diagonals, of dS with a key per lane and 32 queries in registers: lane 16 b + i holds in a[c] position 16 (b - c) + i - 4 half.
 __device__ inline void add_diagonals_of_keys(const f32x16 (&d)[1], float *sums, int lane)
@@ -892,7 +886,7 @@ int allow_whole()
 {
     for (const void *f : {(const void *)whole_grad_kernel<bf16_t, DP, 4, false>, (const void *)whole_grad_kernel<bf16_t, DP, 4, true>,
                           (const void *)whole_grad_kernel<bf16_t, DP, 8, false>, (const void *)whole_grad_kernel<bf16_t, DP, 8, true>})
-        LEANN_HIP(hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024));
+        LEANN_HIP(hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, ATT_LDS));
     return LEANN_OK;
 }
 
@@ -901,7 +895,7 @@ int allow_grad()
 {
     for (const void *f : {(const void *)query_grad_kernel<T, DP, false>, (const void *)query_grad_kernel<T, DP, true>, (const void *)key_grad_kernel<T, DP, 4, false>,
                           (const void *)key_grad_kernel<T, DP, 4, true>, (const void *)key_grad_kernel<T, DP, 2, false>, (const void *)key_grad_kernel<T, DP, 2, true>})
-        LEANN_HIP(hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024));
+        LEANN_HIP(hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, ATT_LDS));
     return LEANN_OK;
 }
 
@@ -986,7 +980,7 @@ extern "C" int leann_attention_backward(leann_ctx *ctx, const leann_attention_pl
                 constexpr int NW = decltype(waves)::value;
                 typedef WholeCfg<DP, NW> Whole;
                 if (!w.n_items) return;
-                hipLaunchKernelGGL((whole_grad_kernel<T, DP, NW, BIAS>), dim3(w.n_items), dim3(NW * 64), Whole::FIXED + table * (rows ? 1 + 2 * NW : 1), ctx->stream,
+                hipLaunchKernelGGL((whole_grad_kernel<T, DP, NW, BIAS>), dim3(w.n_items), dim3(NW * 64), Whole::bytes(plan->distance, BIAS, rows != nullptr), ctx->stream,
                                    w.items, w.tiles, a, (const T *)dout_dev, ldd, (const T *)q_dev, ldq, (const T *)k_dev, ldk, (const T *)v_dev, ldv, (const T *)out_dev, ldo, lse_dev,
                                    plan->Tq, bias_dev, plan->bucket_of, (T *)dq_dev, lddq, (T *)dk_dev, lddk, (T *)dv_dev, lddv, rows);
                 if (rows) rows += (size_t)w.n_tiles * plan->heads * positions;

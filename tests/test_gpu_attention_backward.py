@@ -32,6 +32,17 @@ def test_against_the_definition(ctx, name):  # noqa: F811
         check(c)
 
 
+@pytest.mark.parametrize("distance", [1024, 603, 604])
+@pytest.mark.parametrize("dim", [32, 64])
+def test_long_tables_of_biases_beside_short_sequences(ctx, dim, distance):  # noqa: F811
+    """Tables go by the longest sequence, or the last position; a block that takes a whole short one has less room the more wavefronts it has."""
+    say("attention backward, tables", dim, distance)
+    with Case(ctx, [1100, 200, 100, 1], heads=2, dim=dim, buckets=64, distance=distance) as c:
+        check(c)
+    with Case(ctx, [200, 100], heads=2, dim=dim, buckets=64, distance=distance, first=[3000, 0]) as c:
+        check(c)
+
+
 @pytest.mark.parametrize("size", [1e-4, 300.0])
 @pytest.mark.parametrize("dim", [32, 128])
 def test_fp16_of_any_size(ctx, size, dim):  # noqa: F811
