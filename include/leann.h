@@ -352,6 +352,8 @@ int leann_bench_l1pull(leann_ctx *ctx, int64_t panel_rows, int32_t launches, dou
  *   - The workspace stays with the context, as large as the largest call needed.  For every 16 of max_rank a projection takes 64 bytes per row and 64 n_out per adapter that has
  *     rows; its gradient 128 per row and, per adapter, 64 n_in + 32 n_out and 64 (n_in + n_out) for each of its chunks of up to 2048 rows.  It is freed when another
  *     allocation of the context finds no memory, and by leann_destroy.
+ *   - Calls may be captured into a graph once a call of that size has made the workspace large enough.  The context keeps what a capture met, also when a later call needs
+ *     more, until leann_destroy; handles have to live as long.  Graphs and calls of a context share a workspace: they run one after another, in the order of its stream.
  *   - Sums and statistics are fp32; every output is rounded once, to nearest.  No atomics: the bits repeat from call to call.
  *   - Zero rows are no error.  leann_profile_begin does not bracket their kernels.
  */
@@ -450,21 +452,22 @@ typedef struct {
 int leann_position_buckets(int32_t buckets, int32_t distance, int both, int32_t *bucket_of_host);
 
 /* The sequences of a batch, one plan for the layers and directions that it goes through.  k_rows_host NULL: as q_rows (self-attention); first_host NULL: 0.  Host arrays, copied;
- * lengths of 0 are allowed.  Synchronises the stream.  Errors: negative lengths or positions, windows below -1, buckets outside the table -> LEANN_EINVAL; sizes beyond those above,
- * positions of 2^30, 2^31 - 256 rows, 2^24 workgroups -> LEANN_ESHAPE. */
+ * lengths of 0 are allowed.  Synchronises the stream, so not while it is captured.  Errors: negative lengths or positions, windows below -1, buckets outside the table -> LEANN_EINVAL; sizes beyond those above,
+ * positions of 2^30, 2^31 - 256 rows, 2^24 workgroups of 256 -> LEANN_ESHAPE. */
 int leann_attention_create(leann_ctx *ctx, const int32_t *q_rows_host, const int32_t *k_rows_host, const int32_t *first_host, int32_t n_sequences,
                            const leann_attention_desc *desc, leann_attention_plan **out);
 void leann_attention_free(leann_attention_plan *plan);
 
 /* out[Tq][heads * dim] from q[Tq][heads * dim], k and v[Tk][kv_heads * dim]: bf16 or f16, 16-byte alignment, rows a multiple of 8 elements apart and at most 2^22 (slices of one
  * projection's output are fine).  bias: fp32[buckets][heads].  lse (NULL, or fp32[heads][Tq]): what the backward pass needs.  out must not overlap q, k or v (LEANN_EINVAL).
- * Where there are few queries, their keys are split over blocks whose sums are joined: a row's bits may depend on the other sequences' lengths, its value does not. */
+ * Where there are few queries, their keys are split over blocks whose sums are joined: a row's bits may depend on the other sequences' lengths, not on what they hold.
+ * Workspace: where keys are split (a plan with fewer blocks than two per compute unit), 32 or 128 rows of 34, 66 or 130 floats per part and head. */
 int leann_attention(leann_ctx *ctx, const leann_attention_plan *plan, const void *q_dev, int64_t ldq, const void *k_dev, int64_t ldk, const void *v_dev, int64_t ldv, int dtype,
                     float scale, const float *bias_dev, void *out_dev, int64_t ldo, float *lse_dev);
 
 /* Gradients from dout, the gradient of out, and what the forward call left in out and lse, under the same scale and bias: dq[Tq][heads * dim], dk and dv[Tk][kv_heads * dim] (the sums
  * over the heads that share a key head), dbias fp32[buckets][heads] (NULL: not wanted).  Written, not added to; dq, dk and dv may be slices of one matrix, and must not overlap
- * each other or an input (LEANN_EINVAL).  No atomics in memory: the bits repeat, and a sequence's dq, dk and dv do not depend on the others.
+ * each other or an input (LEANN_EINVAL).  No atomics in memory: the bits repeat; a sequence's dq, dk and dv may differ in bits with the other sequences' lengths, not with what they hold.
  * A query or key that is infinite or NaN makes NaN of the gradients of the keys or queries that it meets and of no others.
  * Workspace: 8 bytes per query and head; with dbias 4 (2 distance + 1) more per head and 128 queries (of every sequence), distance no more than the sequences' longest;
  * where keys have their queries split (a few that all of a long sequence see), 256 * 32, 64 or 128 floats per part and key head. */

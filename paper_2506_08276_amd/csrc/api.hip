@@ -42,6 +42,16 @@ void DevBuf::release()
 
 int leann_ctx::reserve(DevBuf &buf, size_t need)
 {
+    if (&buf == &op_work) {
+        if (op_work_captured && need > op_work.bytes) {
+            op_work_kept.push_back(op_work);
+            op_work = DevBuf();
+            op_work_captured = false;
+        }
+        hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+        if (stream) LEANN_HIP(hipStreamIsCapturing(stream, &status));  // the null stream is never captured
+        op_work_captured |= status != hipStreamCaptureStatusNone;
+    }
     int rc = buf.reserve(need);
     if (rc == LEANN_OK) return rc;
     {
@@ -58,7 +68,7 @@ int leann_ctx::reserve(DevBuf &buf, size_t need)
 bool leann_ctx::give_back_op_work()
 {
     std::unique_lock<std::mutex> turn(op_work_mutex, std::try_to_lock);
-    if (!turn.owns_lock() || !op_work.p) return false;  // an operator on another thread needs it now
+    if (!turn.owns_lock() || !op_work.p || op_work_captured) return false;  // an operator on another thread, or a captured graph, needs it
     op_work.release();
     return true;
 }
@@ -292,6 +302,7 @@ void leann_destroy(leann_ctx *ctx)
                       &ctx->len, &ctx->meta, &ctx->enc_ids, &ctx->s_state, &ctx->s_emb, &ctx->s_lut, &ctx->s_seen,
                       &ctx->s_misc, &ctx->s_owner, &ctx->s_buf, &ctx->s_memo_slot, &ctx->s_memo_emb, &ctx->pq_work, &ctx->op_work};
     for (DevBuf *b : bufs) b->release();
+    for (DevBuf &b : ctx->op_work_kept) b.release();
     ctx->prof_tokens.release();
     if (ctx->host_counters) (void)hipHostFree(ctx->host_counters);
     if (ctx->host_flags) (void)hipHostFree(ctx->host_flags);

@@ -329,14 +329,14 @@ int make_plan(leann_ctx *ctx, const int32_t *q_rows, const int32_t *k_rows, cons
         if (bytes) memcpy(image.data() + at, v.data(), bytes);
         return at;
     };
-    size_t most_blocks = joins.size();
-    auto order = [&](const std::vector<AttentionTile> &t, const std::vector<int32_t> &t_of, int heads, int s, int32_t *count) {
+    size_t most_blocks = joins.size();  // of 256 threads, of which a launch has fewer than 2^32
+    auto order = [&](const std::vector<AttentionTile> &t, const std::vector<int32_t> &t_of, int heads, int s, int threads, int32_t *count) {
         const std::vector<AttentionItem> items = att_order(t, t_of, heads, s);
         *count = (int32_t)items.size();
-        most_blocks = std::max(most_blocks, items.size());
+        most_blocks = std::max(most_blocks, items.size() * (threads / 256));
         return put(items);
     };
-    const size_t tiles_at = put(tiles), items_at = order(tiles, of, p->heads, share, &p->n_items), joins_at = put(joins);
+    const size_t tiles_at = put(tiles), items_at = order(tiles, of, p->heads, share, 256, &p->n_items), joins_at = put(joins);
     p->n_joins = (int32_t)joins.size();
 
     // The gradient's two sides, of all sequences or of those that are not taken whole.
@@ -362,9 +362,9 @@ int make_plan(leann_ctx *ctx, const int32_t *q_rows, const int32_t *k_rows, cons
         sides->n_joins = (int32_t)key_joins.size();
         most_blocks = std::max(most_blocks, key_joins.size());
         at[0] = put(query_tiles);
-        at[1] = order(query_tiles, query_of, p->heads, share, &sides->n_query_items);
+        at[1] = order(query_tiles, query_of, p->heads, share, 256, &sides->n_query_items);
         at[2] = put(key_tiles);
-        at[3] = order(key_tiles, key_of, p->kv_heads, 1, &sides->n_key_items);
+        at[3] = order(key_tiles, key_of, p->kv_heads, 1, 256, &sides->n_key_items);
         at[4] = put(key_joins);
     };
     size_t all_at[5], others_at[5], whole_at[2][2] = {};
@@ -398,10 +398,10 @@ int make_plan(leann_ctx *ctx, const int32_t *q_rows, const int32_t *k_rows, cons
         }
         p->whole[c].n_tiles = (int32_t)whole.size();
         whole_at[c][0] = put(whole);
-        whole_at[c][1] = order(whole, whole_of, p->heads, 1, &p->whole[c].n_items);
+        whole_at[c][1] = order(whole, whole_of, p->heads, 1, c ? 512 : 256, &p->whole[c].n_items);
     }
     if (most_blocks > ((size_t)1 << 24) - 1) {
-        leann_set_error("leann_attention_create: sequences of this number and length are not covered (more than 2^24 - 1 workgroups in a launch)");
+        leann_set_error("leann_attention_create: sequences of this number and length are not covered (more than 2^24 - 1 workgroups of 256 in a launch)");
         return LEANN_ESHAPE;
     }
     const size_t buckets_at = put(buckets);

@@ -85,6 +85,9 @@ struct leann_ctx {
     // allocation of the context finds no memory.  A call holds the mutex from where it reserves to its last launch; what is launched is waited for by hipFree.
     DevBuf op_work;
     std::mutex op_work_mutex;
+    // A captured graph has the addresses of the workspace that its capture met: that one is neither given back nor freed when a larger one replaces it.
+    bool op_work_captured = false;
+    std::vector<DevBuf> op_work_kept;
     int64_t memo_rows = 0;  // rows of the per-call embedding memo (leann_set_call_memo), 0 = off
     // optional per-kernel timing (leann_profile_begin / leann_profile_end)
     bool prof_on = false;
@@ -96,7 +99,7 @@ struct leann_ctx {
     std::vector<ProfSpan> prof_spans;
     std::vector<hipEvent_t> prof_pool;
 
-    int reserve(DevBuf &buf, size_t need);  // all device memory of a call: as buf.reserve, with pq_work given back if that fails, then op_work
+    int reserve(DevBuf &buf, size_t need);  // all device memory of a call: as buf.reserve (see op_work_captured), with pq_work given back if that fails, then op_work
     bool give_back_op_work();  // whether there is memory to be had by it
     int reserve_for_pass(DevBuf &buf, size_t need);  // for calls that run the encoder: then the packed matrices, too
 };

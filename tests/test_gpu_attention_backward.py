@@ -33,7 +33,7 @@ def test_against_the_definition(ctx, name):  # noqa: F811
 
 
 @pytest.mark.parametrize("distance", [1024, 603, 604])
-@pytest.mark.parametrize("dim", [32, 64])
+@pytest.mark.parametrize("dim", [32, 64, 128])
 def test_long_tables_of_biases_beside_short_sequences(ctx, dim, distance):  # noqa: F811
     """Tables go by the longest sequence, or the last position; a block that takes a whole short one has less room the more wavefronts it has."""
     say("attention backward, tables", dim, distance)
@@ -82,7 +82,7 @@ def test_bits_repeat_and_sequences_are_apart(ctx):  # noqa: F811
             assert torch.equal(x[:150], y[:150]) and torch.equal(x[190:], y[190:])
 
 
-@pytest.mark.parametrize("window,sinks", [((30, 30), 0), ((64, 0), 3), ((-1, 0), 0)])
+@pytest.mark.parametrize("window,sinks", [((30, 30), 0), ((64, 0), 3), ((-1, 0), 0), (None, 0)])
 @pytest.mark.parametrize("what", ["q", "k", "v", "dout"])
 def test_what_is_hidden_does_not_reach_a_row(ctx, window, sinks, what):  # noqa: F811
     import torch
@@ -179,6 +179,39 @@ def test_captured_and_replayed():
                     assert torch.equal(a, b), i
                 torch.zeros(1000, device="cuda:0").sum().item()
             assert eager[0].shape == captured[0].shape
+            del graph
+        stream.synchronize()
+        L.leann_destroy(own)
+
+
+def test_a_workspace_that_grows_behind_a_capture():
+    """A graph keeps the workspace that its capture met: a larger call, and what is allocated then, changes nothing in its replays."""
+    import torch
+    import paper_2506_08276_amd as L
+    say("attention backward, a workspace that grows")
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        own = L.leann_create(CTX, torch.zeros(640, device="cuda:0"), stream=stream.cuda_stream)
+        args = dict(buckets=32, distance=128)
+        with Case(own, [3, 9], k_rows=[2500, 700], **args) as c, Case(own, [4000, 300], packed=True, **args) as large:
+            def step(of):
+                out, lse = of.run()
+                return (out, lse, *backward(of, out, lse))
+            eager = step(c)
+            stream.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=stream):
+                captured = step(c)
+            for i in range(3):
+                other = step(large)
+                rest = [torch.full((1 << 22,), float("nan"), device="cuda:0") for _ in range(4)]
+                graph.replay()
+                stream.synchronize()
+                for a, b in zip(captured, eager):
+                    assert torch.equal(a, b), i
+                for a, b in zip(step(large), other):
+                    assert torch.equal(a, b), i
+                del rest
             del graph
         stream.synchronize()
         L.leann_destroy(own)
