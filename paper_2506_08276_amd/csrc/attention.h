@@ -34,6 +34,7 @@ struct leann_attention_plan {
     int32_t distance = 0, buckets = 0;         // distance: of the table below, no longer than the sequences make it
     int32_t query_waves = 0;                   // wavefronts of a forward block, 32 queries each
     int32_t n_items = 0, n_joins = 0, n_slots = 0;
+    int32_t join_rows = 0;                     // of a join, the most
     DevBuf mem;
     const AttentionTile *tiles = nullptr;
     const AttentionItem *items = nullptr;

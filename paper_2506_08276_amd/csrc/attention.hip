@@ -212,6 +212,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : 1) void at
 
 // The parts of split rows: m the largest, l and O summed under it.  A wavefront has one row of one head; its lanes have the parts in turn for m and l, and for O the row's
 // pieces of eight elements of every 8th part (of DP 32: 16th, 128: 4th), added up over the lanes at the end: the order is the same in every call.
+constexpr int JOIN_ROWS = 8;  // of a block
 template <class T, int DP>
 __global__ __launch_bounds__(256) void join_kernel(const AttentionJoin *__restrict__ joins, int heads, int dim, int block_rows, const float *__restrict__ part_o,
                                                    const float2 *__restrict__ part_ml, T *__restrict__ out, int64_t ldo, float *__restrict__ lse, int64_t Tq)
@@ -219,7 +220,7 @@ __global__ __launch_bounds__(256) void join_kernel(const AttentionJoin *__restri
     constexpr int CH = DP / 8, GROUPS = 64 / CH;
     const AttentionJoin jn = joins[blockIdx.x];
     const int h = blockIdx.y, lane = threadIdx.x & 63, c = lane % CH, group = lane / CH;
-    for (int row = threadIdx.x >> 6; row < jn.rows; row += 4) {
+    for (int row = blockIdx.z * JOIN_ROWS + (threadIdx.x >> 6); row < min(jn.rows, (int)(blockIdx.z + 1) * JOIN_ROWS); row += 4) {
         auto at = [&](int s) { return ((int64_t)(jn.slot0 + s) * heads + h) * block_rows + row; };
         float m = -INFINITY;
         for (int s = lane; s < jn.slots; s += 64) m = __builtin_fmaxf(m, part_ml[at(s)].x);
@@ -282,7 +283,7 @@ int launch_attend(leann_ctx *ctx, const leann_attention_plan *p, const Attention
     hipLaunchKernelGGL((attend_kernel<T, DP, NW, BIAS>), dim3(p->n_items), dim3(NW * 64), smem, ctx->stream, p->items, p->tiles, a, q, ldq, k, ldk, v, ldv, bias,
                        p->bucket_of, out, ldo, lse, p->Tq, part_o, part_ml);
     if (p->n_joins)
-        hipLaunchKernelGGL((join_kernel<T, DP>), dim3(p->n_joins, p->heads), dim3(256), 0, ctx->stream, p->joins, p->heads, p->dim, NW * 32, part_o, part_ml, out, ldo, lse,
+        hipLaunchKernelGGL((join_kernel<T, DP>), dim3(p->n_joins, p->heads, (p->join_rows + JOIN_ROWS - 1) / JOIN_ROWS), dim3(256), 0, ctx->stream, p->joins, p->heads, p->dim, NW * 32, part_o, part_ml, out, ldo, lse,
                            p->Tq);
     return att_launched("leann_attention");
 }
@@ -314,14 +315,18 @@ int make_plan(leann_ctx *ctx, const int32_t *q_rows, const int32_t *k_rows, cons
     std::vector<AttentionJoin> joins;
     const int share = p->heads / p->kv_heads, cus = ctx->num_cus;
     att_make_tiles(r, n, q_rows, k_rows, first, false, share, p->query_waves * 32, 0, tiles, of, joins);
-    // Keys are split where there are fewer than two blocks per compute unit, into parts that make four, of four tiles at least: each costs a block's start and its
-    // sums' way through memory.
+    // Keys are split where there are fewer than two blocks per compute unit.  Of few queries the parts make four blocks per unit, of four tiles at least; of 128 queries,
+    // whose sums are a part's way through memory of 128 rows, one, of 16 tiles (8 sequences of 512 tokens, 12 heads: 42 us in parts of four, 19 whole; one of 2048, 8 heads of
+    // 128 elements: 44 us in two parts, 51 whole).
     if ((int64_t)tiles.size() * p->heads < 2 * cus)
-        if (const int split = att_split(tiles, p->heads, cus, 4, 4)) {
+        if (const int split = p->query_waves == 1 ? att_split(tiles, p->heads, cus, 4, 4) : att_split(tiles, p->heads, cus, 1, 16)) {
             tiles.clear();
             att_make_tiles(r, n, q_rows, k_rows, first, false, share, p->query_waves * 32, split, tiles, of, joins);
         }
-    for (const AttentionJoin &j : joins) p->n_slots += j.slots;
+    for (const AttentionJoin &j : joins) {
+        p->n_slots += j.slots;
+        p->join_rows = std::max(p->join_rows, j.rows);
+    }
     std::vector<char> image;
     auto put = [&](const auto &v) {
         const size_t at = att_up256(image.size()), bytes = v.size() * sizeof(v[0]);
@@ -352,8 +357,9 @@ int make_plan(leann_ctx *ctx, const int32_t *q_rows, const int32_t *k_rows, cons
             key_tiles.clear();
             att_make_tiles(r, n, q_rows, k_rows, first, true, share, 64, 0, key_tiles, key_of, key_joins, taken);
         }
-        // Keys that many queries see, as a sequence's first ones, have their queries split, so that no block has much more than a compute unit's share of the work.
-        if (const int split = att_split(key_tiles, p->kv_heads, cus, 1, 16)) {
+        // Keys that many queries see, as a sequence's first ones, have their queries split, so that no block has much more than half of a compute unit's share, of which it has
+        // two (two documents with a window: 79 us, with parts of a unit's share 102).
+        if (const int split = att_split(key_tiles, p->kv_heads, cus, 2, 8)) {
             key_tiles.clear();
             att_make_tiles(r, n, q_rows, k_rows, first, true, share, sides->key_waves * 32, split, key_tiles, key_of, key_joins, taken);
         }
