@@ -82,17 +82,6 @@ struct Half8<f16_t> {
     static constexpr uint32_t EXPONENT = 0x7c00;
 };
 
-template <class T>
-struct Half4;
-template <>
-struct Half4<bf16_t> {
-    typedef bf16x4 type;
-};
-template <>
-struct Half4<f16_t> {
-    typedef f16x4 type;
-};
-
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 
@@ -100,7 +89,6 @@ __device__ inline f32x16 att_mfma(const bf16x8 &a, const bf16x8 &b, const f32x16
 __device__ inline f32x16 att_mfma(const f16x8 &a, const f16x8 &b, const f32x16 &c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 
 __device__ inline f32x4 att_mfma16(const bf16x8 &a, const bf16x8 &b, const f32x4 &c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
-__device__ inline f32x4 att_mfma16(const f16x8 &a, const f16x8 &b, const f32x4 &c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
 // Tiles of 64 rows of DP elements (the head's size, zeros up to 32, 64 or 128) lie in LDS as rows of 16-byte chunks, chunk c of row r at c ^ att_swizzle(r): 16 rows' reads
 // of one chunk, and the reads of four adjacent rows' 64 bytes that transpose, reach all banks.
@@ -160,12 +148,6 @@ __device__ inline void block_barrier()
     asm volatile("" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
 }
-// What the lanes of a wavefront wrote to LDS, its other lanes read behind this: the accesses are served in their order.
-__device__ inline void wave_fence()
-{
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-}
 
 // Infinities and NaN of an operand.  Where a tile is partly hidden they have to be taken out: a row of the other side that does not see them would get NaN from a product with
 // zero.
@@ -203,10 +185,6 @@ __device__ inline typename Half8<T>::type row_operand(const T *lds, int row0, in
 // get a column of four each.
 // The reads are written out, each group with its wait behind it: before the builtin's, the compiler waits for every request from memory to LDS that is on its way, the tiles ahead
 // among them (LDS arrays and requests look alike to it).
-__device__ inline void transposed2(uint32_t a, uint32_t b, s16x4 (&o)[2])
-{
-    asm volatile("ds_read_b64_tr_b16 %0, %2\n\tds_read_b64_tr_b16 %1, %3\n\ts_waitcnt lgkmcnt(0)" : "=&v"(o[0]), "=&v"(o[1]) : "v"(a), "v"(b));
-}
 template <int FROM>
 __device__ inline void transposed4(const uint32_t (&a)[4], s16x4 (&o)[4])
 {

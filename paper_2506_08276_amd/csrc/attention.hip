@@ -16,6 +16,10 @@ namespace {
 // weights 2^(scale log2 e (s - m)), O = sum of weights times v, l and O scaled when m grows.  P^T, rounded to the inputs' type (an error of half a step in each term, as the inputs themselves have), is the
 // other operand of O^T = V^T P^T without leaving its registers, see Columns.
 // K and V tiles go from memory to LDS without registers, one tile ahead (two ahead, with a third stage, took the same time).
+// What bounds it: over few keys memory (12 heads of 64, single queries over 8 sequences of 500 to 16384 keys: 39 us, 222 MB, 5.6 TB/s); else vector instructions, some
+// ten per score and lane beside its products (256 sequences of up to 512 tokens: 140 us, vector units 56 %, matrix cores 25 % busy; 4 wavefronts per SIMD spill registers: 200 us
+// and more).  Three documents of 3001 to 4096 tokens with a window of 256: 38 us, 960 blocks in two rounds; of 64 queries, with two wavefronts at each 32 and their sums joined in
+// LDS, 37 to 40, and 40 sequences of 256 tokens 26 instead of 23.
 template <int DP, int NW>
 struct AttendCfg {
     static constexpr int STAGES = 2, TILE = ATT_STEP * DP;
@@ -211,7 +215,8 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : 1) void at
 }
 
 // The parts of split rows: m the largest, l and O summed under it.  A wavefront has one row of one head; its lanes have the parts in turn for m and l, and for O the row's
-// pieces of eight elements of every 8th part (of DP 32: 16th, 128: 4th), added up over the lanes at the end: the order is the same in every call.
+// pieces of eight elements of every 8th part (of DP 32: 16th, 128: 4th), added up over the lanes at the end: the order is the same in every call.  4 us, latency of dependent loads;
+// a block takes 8 rows, as 128 rows of a join in four wavefronts took 26 us more (8 sequences of 512 tokens, split).
 constexpr int JOIN_ROWS = 8;  // of a block
 template <class T, int DP>
 __global__ __launch_bounds__(256) void join_kernel(const AttentionJoin *__restrict__ joins, int heads, int dim, int block_rows, const float *__restrict__ part_o,

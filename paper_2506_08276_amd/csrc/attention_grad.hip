@@ -140,6 +140,8 @@ __device__ inline void sums_by_position(const float *sums, int room, int distanc
 // dQ^T = K^T dS^T.  It leaves what the other kernel needs of each query: the log-sum in units of log 2 and delta, both negative.
 // The bias's gradient is summed by relative position, each wavefront into an array of its own in LDS, so that the order of the additions is the program's.  Tiles
 // behind `distance` add to one place, in a register.
+// Bound by the latency of its chains with two wavefronts per SIMD (200 registers): two documents of 3001 and more tokens, window 256, 12 heads of 64: 56 us, vector units 35 %,
+// matrix cores 19 % busy.  64 queries per block, with two wavefronts at each 32, took 57 to 67.
 template <class T, int DP, bool BIAS>
 __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void query_grad_kernel(
     const AttentionItem *__restrict__ items, const AttentionTile *__restrict__ tiles, AttentionShape a, const T *__restrict__ dout, int64_t ldd, const T *__restrict__ q,
@@ -341,6 +343,7 @@ __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void query_grad
 // A block takes 32 KW keys of one key head through the queries that see them, of every head that shares it: S = Q K^T and dP = dO V^T have a key per lane; P and dS, rounded, are the
 // other operands of dV^T = dO^T P and dK^T = Q^T dS.  K and V stay in registers; Q, dO and the queries' numbers come from memory to LDS, STAGES - 1 tiles ahead.
 // KW = 4: a wavefront has 32 keys.  KW = 2, for few keys: two wavefronts share them, each with 32 of a step's 64 queries, and their sums meet in LDS at the end.
+// Bound as the other kernel: the same documents 79 us with KW = 2, 520 blocks; 95 with KW = 4 and splits to match (25 to 31 steps in a row instead of twice as many half as dear).
 template <class T, int DP, int KW, bool BIAS>
 __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void key_grad_kernel(
     const AttentionItem *__restrict__ items, const AttentionTile *__restrict__ tiles, AttentionShape a, const T *__restrict__ dout, int64_t ldd, const T *__restrict__ q,
@@ -609,6 +612,10 @@ __global__ __launch_bounds__(256) void key_join_kernel(const AttentionJoin *__re
 // the two kernels above read all but O twice, which bounds them there.  A wavefront has 32 keys in registers, K in LDS as well; the queries go by, 32 at a time: S = Q K^T and
 // dP = dO V^T with a key per lane, P and dS from registers into dV^T and dK^T as in key_grad_kernel; dS, rounded, through LDS into dQ^T = K^T dS^T, of which each
 // wavefront has tiles of 16 x 16, all keys of them.  The stores of a step's dQ are issued behind the next step's wait, which else would be for them.
+// 512 sequences of 64 to 256 tokens, 12 heads of 64, with the bias's gradient: 73 us for those up to 128 and 416 for the others, 1.03 GB (the two kernels took 659 where this one took 553, both with
+// an earlier form of the bias's sums).  Bound by latency: wavefronts
+// wait 41 % of their time, two per SIMD at 212 registers, vector units 30 %, LDS 26 % and matrix cores 14 % busy.  dQ is some 13 % of it.  One barrier per step instead of two, dQ a step
+// later, took 5 % more (registers spill), four stages of Q and dO 3 % more.
 
 // As add_diagonals, of dS with a key per lane and 32 queries in registers: lane 16 b + i holds in a[c] position 16 (b - c) + i - 4 half.
 __device__ inline void add_diagonals_of_keys(const f32x16 (&d)[1], float *sums, int lane)
@@ -743,7 +750,7 @@ __global__ __launch_bounds__(NW * 64, 2) void whole_grad_kernel(const AttentionI
         for (int m = 0; m < MINE; ++m) {
             const int tile = wave + m * NW, d = tile % (DP / 16) * 16 + 4 * g16, row = step * 32 + tile / (DP / 16) * 16 + l16;
             if (tile < TILES && row < lq && d < a.dim) {
-                typedef typename Half4<T>::type V4;
+                typedef T V4 __attribute__((ext_vector_type(4)));
                 const f32x4 x = dq_acc[m] * a.scale;
                 *reinterpret_cast<V4 *>(dq + (int64_t)(t.other0 + row) * lddq + h * a.dim + d) = __builtin_convertvector(x, V4);
             }
