@@ -388,6 +388,14 @@ def _rows(t, what, like=None):
     return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1]  # a single row's stride is none
 
 
+def _rows_or_new(t, what, like):
+    """(t, pointer, distance of rows) of an output like a tensor that _rows has looked at; None: a new one, whose rows lie side by side."""
+    if t is None:
+        t = torch.empty_like(like)
+        return t, t.data_ptr(), like.shape[1]
+    return t, *_rows(t, what, like)
+
+
 def _drop(drop):
     return None if drop is None else C.byref(DropoutDesc(*drop))
 
@@ -573,11 +581,8 @@ def leann_attention(ctx, plan, q, k, v, scale=None, bias=None, keep=False, out=N
     """softmax(scale q k^T + bias) v for every sequence and head of the plan; q [Tq][heads * head_dim], k and v [Tk][kv_heads * head_dim], bias float32
     [buckets][heads]; scale None: head_dim ** -0.5.  keep: returns (out, lse), what the backward pass needs; else out."""
     (qp, ldq, kp, ldk, vp, ldv), bp = _attention_inputs(plan, q, k, v, bias)
-    if out is None:
-        out = torch.empty((plan.Tq, plan.heads * plan.dim), dtype=q.dtype, device=q.device)
-    assert out.shape == q.shape and out.dtype == q.dtype, "out: shape or type differs"
-    lse = torch.empty((plan.heads, plan.Tq), dtype=torch.float32, device=q.device) if keep else None
-    op, ldo = _rows(out, "out")
+    out, op, ldo = _rows_or_new(out, "out", q)
+    lse = q.new_empty((plan.heads, plan.Tq), dtype=torch.float32) if keep else None
     scale = plan.dim ** -0.5 if scale is None else scale
     _check(load_library().leann_attention(ctx, plan, qp, ldq, kp, ldk, vp, ldv, _dtype(q), scale, bp, op, ldo, lse.data_ptr() if keep else None))
     return (out, lse) if keep else out
@@ -589,13 +594,11 @@ def leann_attention_backward(ctx, plan, dout, q, k, v, out, lse, scale=None, bia
     (qp, ldq, kp, ldk, vp, ldv), bp = _attention_inputs(plan, q, k, v, bias)
     assert dout.shape == out.shape == q.shape and dout.dtype == out.dtype == q.dtype, "dout, out: shape or type differs"
     assert lse.is_cuda and lse.is_contiguous() and lse.shape == (plan.heads, plan.Tq) and lse.dtype == torch.float32, "lse: need float32 [heads][Tq]"
-    dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) if d is None else d for d, t in ((dq, q), (dk, k), (dv, v)))
-    for d, t in ((dq, q), (dk, k), (dv, v)):
-        assert d.shape == t.shape and d.dtype == t.dtype, "dq, dk, dv: shape or type differs"
+    (dq, dqp, lddq), (dk, dkp, lddk), (dv, dvp, lddv) = _rows_or_new(dq, "dq", q), _rows_or_new(dk, "dk", k), _rows_or_new(dv, "dv", v)
     dbias = None
     if bias is not None and need_bias:  # rows that no relative position has stay zero
         dbias = torch.empty_like(bias) if bias.shape[0] == plan.buckets else torch.zeros_like(bias)
-    (gp, ldd), (op, ldo), (dqp, lddq), (dkp, lddk), (dvp, lddv) = _rows(dout, "dout"), _rows(out, "out"), _rows(dq, "dq"), _rows(dk, "dk"), _rows(dv, "dv")
+    (gp, ldd), (op, ldo) = _rows(dout, "dout"), _rows(out, "out")
     scale = plan.dim ** -0.5 if scale is None else scale
     _check(load_library().leann_attention_backward(ctx, plan, gp, ldd, qp, ldq, kp, ldk, vp, ldv, op, ldo, lse.data_ptr(), _dtype(q), scale, bp, dqp, lddq,
                                                    dkp, lddk, dvp, lddv, None if dbias is None else dbias.data_ptr()))
@@ -612,9 +615,10 @@ def _kind(kind):
 
 
 def _checkpoint_like(x):
-    assert x.dim() == 2, "x: need a 2-D CUDA tensor with unit column stride"
-    return (torch.empty(x.shape, dtype=torch.int8, device=x.device),
-            torch.empty((x.shape[0], (x.shape[1] + 127) // 128), dtype=torch.float32, device=x.device))
+    """A new checkpoint for x, which _rows has looked at, and what _checkpoint gives of it."""
+    rows, cols = x.shape
+    codes, scales = torch.empty_like(x, dtype=torch.int8), x.new_empty((rows, (cols + 127) // 128), dtype=torch.float32)
+    return (codes, scales), (codes.data_ptr(), cols, scales.data_ptr())
 
 
 def _checkpoint(kept):
@@ -626,42 +630,43 @@ def _checkpoint(kept):
 
 def leann_checkpoint(ctx, x):
     """A 2-D tensor in 8 bits: (codes int8 [rows][cols], scales float32 [rows][ceil(cols / 128)]), the largest of 128 columns being 127 steps."""
-    kept = _checkpoint_like(x)
-    (xp, ldx), (cp, ldc, sp) = _rows(x, "x"), _checkpoint(kept)
-    _check(load_library().leann_checkpoint(ctx, xp, ldx, x.shape[0], x.shape[1], _dtype(x), cp, ldc, sp))
+    xp, ldx = _rows(x, "x")
+    kept, to = _checkpoint_like(x)
+    _check(load_library().leann_checkpoint(ctx, xp, ldx, *x.shape, _dtype(x), *to))
     return kept
 
 
 def leann_checkpoint_restore(ctx, kept, dtype=None, out=None):
     """The tensor that a checkpoint stands for, in `dtype` (or into `out`)."""
+    cp, ldc, sp = _checkpoint(kept)
     rows, cols = kept[0].shape
     if out is None:
         assert dtype in _DTYPES, "need float32, bfloat16 or float16"
-        out = torch.empty((rows, cols), dtype=dtype, device=kept[0].device)
-    assert out.shape == kept[0].shape and dtype in (None, out.dtype), "out: shape or type differs"
-    (cp, ldc, sp), (op, ldo) = _checkpoint(kept), _rows(out, "out")
+        out = torch.empty_like(kept[0], dtype=dtype)
+        op, ldo = out.data_ptr(), cols
+    else:
+        assert out.shape == kept[0].shape and dtype in (None, out.dtype), "out: shape or type differs"
+        op, ldo = _rows(out, "out")
     _check(load_library().leann_checkpoint_restore(ctx, cp, ldc, sp, rows, cols, _dtype(out), op, ldo))
     return out
 
 
 def leann_activation(ctx, x, kind="gelu", keep=False, out=None):
     """GELU of a 2-D tensor ("gelu", or "gelu_tanh" for its approximation); keep: returns (out, checkpoint of x), what the backward pass needs; else out."""
-    if out is None:
-        out = torch.empty_like(x)
-    kept = _checkpoint_like(x) if keep else None
-    (xp, ldx), (op, ldo), (cp, ldc, sp) = _rows(x, "x"), _rows(out, "out", x), _checkpoint(kept) if keep else (None, 0, None)
-    _check(load_library().leann_activation(ctx, xp, ldx, x.shape[0], x.shape[1], _dtype(x), _kind(kind), op, ldo, cp, ldc, sp))
+    xp, ldx = _rows(x, "x")
+    out, op, ldo = _rows_or_new(out, "out", x)
+    kept, to = _checkpoint_like(x) if keep else (None, (None, 0, None))
+    _check(load_library().leann_activation(ctx, xp, ldx, *x.shape, _dtype(x), _kind(kind), op, ldo, *to))
     return (out, kept) if keep else out
 
 
 def leann_activation_backward(ctx, dout, kept, kind="gelu", again=False, dx=None):
     """The gradient of leann_activation's input from that of its output and the input, a checkpoint or the tensor itself; again: (dx, output once more)."""
-    if dx is None:
-        dx = torch.empty_like(dout)
-    y = torch.empty_like(dout) if again else None
     plain = isinstance(kept, torch.Tensor)
     assert plain or kept[0].shape == dout.shape, "checkpoint: shape differs"
-    (gp, ldd), (dp, lddx), (yp, lda) = _rows(dout, "dout"), _rows(dx, "dx", dout), _rows(y, "again")
+    gp, ldd = _rows(dout, "dout")
+    dx, dp, lddx = _rows_or_new(dx, "dx", dout)
+    y, yp, lda = _rows_or_new(None, "again", dout) if again else (None, None, 0)
     (xp, ldx), (cp, ldc, sp) = (_rows(kept, "x", dout), (None, 0, None)) if plain else ((None, 0), _checkpoint(kept))
     _check(load_library().leann_activation_backward(ctx, gp, ldd, xp, ldx, cp, ldc, sp, dout.shape[0], dout.shape[1], _dtype(dout), _kind(kind), dp, lddx, yp, lda))
     return (dx, y) if again else dx
