@@ -123,41 +123,49 @@ inline std::vector<AttentionItem> att_order(const std::vector<AttentionTile> &ti
 {
     struct Piece {
         int64_t cost;
-        int32_t from, to, head;  // tiles [from, to), heads head .. head + share - 1
+        int32_t from, to;  // tiles [from, to)
     };
     auto cost = [&](int t) { return (int64_t)(tiles[t].end - tiles[t].begin) * ((tiles[t].rows + 31) / 32) + 8; };  // of a wavefront's tiles; 8: what a block takes besides
+    const int groups = own_heads / share;
     int64_t total = 0;
     for (size_t t = 0; t < tiles.size(); ++t) total += cost((int)t);
-    total *= own_heads / share;
+    total *= groups;
     std::vector<Piece> pieces;
+    pieces.reserve(tiles_of.size());
     for (size_t s = 0; s + 1 < tiles_of.size(); ++s) {
-        Piece p = {0, tiles_of[s], tiles_of[s], 0};
+        Piece p = {0, tiles_of[s], tiles_of[s]};
         for (int t = tiles_of[s]; t < tiles_of[s + 1]; ++t) {
             p.cost += cost(t);
             p.to = t + 1;
             if (t + 1 == tiles_of[s + 1] || p.cost * (8 * ATT_XCDS) >= total) {
-                for (int h = 0; h < own_heads; h += share) {
-                    p.head = h;
-                    pieces.push_back(p);
-                }
-                p = {0, t + 1, t + 1, 0};
+                pieces.push_back(p);
+                p = {0, t + 1, t + 1};
             }
         }
     }
     std::stable_sort(pieces.begin(), pieces.end(), [](const Piece &a, const Piece &b) { return a.cost > b.cost; });
-    std::vector<AttentionItem> of[ATT_XCDS];
+    // to the XCD that has the least so far; first how many items each gets, then where they lie
+    std::vector<uint8_t> xcds(pieces.size() * groups);
     int64_t load[ATT_XCDS] = {};
-    for (const Piece &p : pieces) {
-        const int x = (int)(std::min_element(load, load + ATT_XCDS) - load);
-        load[x] += p.cost;
-        for (int t = p.from; t < p.to; ++t)
-            for (int h = 0; h < share; ++h) of[x].push_back({t, p.head + h});
-    }
-    size_t most = 0;
-    for (const auto &v : of) most = std::max(most, v.size());
-    std::vector<AttentionItem> items(most * ATT_XCDS, AttentionItem{-1, 0});
-    for (int x = 0; x < ATT_XCDS; ++x)
-        for (size_t i = 0; i < of[x].size(); ++i) items[i * ATT_XCDS + x] = of[x][i];
+    size_t count[ATT_XCDS] = {}, at = 0;
+    for (const Piece &p : pieces)
+        for (int g = 0; g < groups; ++g) {
+            int x = 0;
+            for (int i = 1; i < ATT_XCDS; ++i) x = load[i] < load[x] ? i : x;
+            load[x] += p.cost;
+            count[x] += (size_t)(p.to - p.from) * share;
+            xcds[at++] = (uint8_t)x;
+        }
+    std::vector<AttentionItem> items(*std::max_element(count, count + ATT_XCDS) * ATT_XCDS, AttentionItem{-1, 0});
+    AttentionItem *next[ATT_XCDS];
+    for (int x = 0; x < ATT_XCDS; ++x) next[x] = items.data() + x;
+    at = 0;
+    for (const Piece &p : pieces)
+        for (int g = 0; g < groups; ++g) {
+            AttentionItem *&to = next[xcds[at++]];
+            for (int t = p.from; t < p.to; ++t)
+                for (int h = 0; h < share; ++h, to += ATT_XCDS) *to = {t, g * share + h};
+        }
     return items;
 }
 
