@@ -91,6 +91,9 @@ CASES = {
     "few queries, long keys": dict(q_rows=[1, 3, 1, 16], k_rows=[5000, 1, 0, 777], heads=2, buckets=32, distance=128),
     "last queries": dict(q_rows=[1, 4, 1], k_rows=[3000, 4, 1], first=[2999, 0, 0], window=(100, 0), sinks=2, heads=2),
     "last queries, long": dict(q_rows=[1, 9], k_rows=[9000, 20000], first=[8999, 19991], heads=3, kv_heads=1, dim=128, dtype="float16"),
+    "128 queries, keys in parts": dict(q_rows=[40, 130, 1], k_rows=[3000, 2100, 5], heads=2, buckets=32, distance=128),
+    "keys in parts, some hidden": dict(q_rows=[200, 33], k_rows=[2500, 1700], first=[1500, 1667], window=(-1, 0), heads=4, kv_heads=2, dim=128, dtype="float16"),
+    "keys in parts behind first ones": dict(q_rows=[150], k_rows=[4000], first=[3800], window=(2000, 0), sinks=70, heads=2, dim=32),
     "queries that see nothing": dict(q_rows=[40, 100], k_rows=[10, 0], first=[5, 0], window=(3, 3)),
     "long, split": dict(q_rows=[2000], heads=1),
     "long, first tokens, shared heads": dict(q_rows=[2500, 1300], heads=6, kv_heads=1, dim=32, window=(40, 40), sinks=3, dtype="float16", packed=True),
