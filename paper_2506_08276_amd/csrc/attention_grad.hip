@@ -263,9 +263,10 @@ __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void query_grad
         for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
             for (int r = 0; r < 16; ++r) d[kt][r] *= __builtin_amdgcn_exp2f(fmaf(s[kt][r], scale2, c));
-        // what is hidden is a choice, not a product; keys behind the last one are zeros, which add nothing to dQ
+        // What is hidden is a choice, not a product.  So are keys behind the last one: their rows are zeros, but their weight exp(0 - lse) has no bound, is infinite from a log-sum of
+        // -88 (fp16: -78) on, and would long before take fp16's range from the others.
         const Edges e = edges(a, p0, my_rows, j0, keys);
-        if (e.behind && (BIAS || !see.all)) {
+        if (e.behind) {
             const int last = min(t.others - 1, p + a.right) - j;
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt)
