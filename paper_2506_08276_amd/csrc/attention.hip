@@ -91,7 +91,6 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : 1) void at
         if (see.none) continue;
 
         f32x16 s[2];
-        float c = 0.f;  // added to all of the tile's scores
         if (BIAS) {
             const int least = j0 - (p0 + 31), most = j0 + ATT_STEP - 1 - p0;  // relative positions
             const bool near = most > -a.distance && least < a.distance;
@@ -101,12 +100,12 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : 1) void at
                 for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
                     for (int r = 0; r < 16; ++r) s[kt][r] = reinterpret_cast<const float *>(smem)[at + kt * 32 + acc_row(r)];
-            } else {
-                c = table[most <= -a.distance ? 0 : bias_entries(a.distance) - 1];
+            } else {  // one bias for all, a part of the scores as any other: it may be -inf, or all of a row's lowest
+                const float c = table[most <= -a.distance ? 0 : bias_entries(a.distance) - 1];
 #pragma unroll
                 for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) s[kt][r] = 0.f;
+                    for (int r = 0; r < 16; ++r) s[kt][r] = c;
             }
         } else {
 #pragma unroll
@@ -145,7 +144,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : 1) void at
         for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
             for (int r = 0; r < 16; ++r) top = __builtin_fmaxf(top, s[kt][r]);
-        top = __builtin_fmaxf(m, both_halves_max(top) + c);
+        top = __builtin_fmaxf(m, both_halves_max(top));
         // m follows the largest score only where that is more than 2^8 times m's weight: sums and fp16's weights have room for it.  Lane by lane: a row's bits are its own.
         const bool grown = (top - m) * scale2 > 8.f;
         if (__ballot(grown)) {
@@ -157,7 +156,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : 1) void at
 #pragma unroll
                 for (int r = 0; r < 16; ++r) o[dt][r] *= alpha;
         }
-        const float base = m == -INFINITY ? 0.f : (c - m) * scale2;
+        const float base = m == -INFINITY ? 0.f : -m * scale2;
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
