@@ -406,14 +406,16 @@ struct WholeCfg {
 };
 
 // The bias of one head by relative position, in units of the scores before they are scaled, so that the products of queries and keys add to it:
-// [2 distance + 1 + 2 ATT_EXT], the ends repeated.  A finite bias beyond 2^100 counts as 2^100, which scores of any size are lost against: a row of them is
-// even, as it would be in numbers without end, and no difference is one of infinities.
-__device__ inline void make_bias(float *table, const float *bias, const int32_t *bucket_of, const AttentionShape &a, int head)
+// [2 distance + 1 + 2 ATT_EXT], the ends repeated, which stand for all beyond; 0 where no position is from `least` to `most`.  A finite bias beyond 2^100 counts as 2^100, which scores of any size are
+// lost against: a row of them is even, as it would be in numbers without end, and no difference is one of infinities.
+__device__ inline void make_bias(float *table, const float *bias, const int32_t *bucket_of, const AttentionShape &a, int head, int least = INT32_MIN, int most = INT32_MAX)
 {
     const float inverse = 1.f / __builtin_fabsf(a.scale);
+    least = min(max(least, -a.distance), a.distance), most = min(max(most, -a.distance), a.distance);
     for (int i = threadIdx.x; i < bias_entries(a.distance); i += blockDim.x) {
         const int d = min(max(i - ATT_EXT, 0), 2 * a.distance);
-        const float b = bias[(int64_t)bucket_of[d] * a.heads + head];
+        float b = bias[(int64_t)bucket_of[d] * a.heads + head];
+        if (d - a.distance < least || d - a.distance > most) b = 0.f;
         table[i] = (__builtin_fabsf(b) < INFINITY ? __builtin_fmaxf(__builtin_fminf(b, 0x1p100f), -0x1p100f) : b) * inverse;
     }
 }

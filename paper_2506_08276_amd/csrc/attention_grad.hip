@@ -701,7 +701,9 @@ __global__ __launch_bounds__(NW * 64, 2) void whole_grad_kernel(const AttentionI
     load_rows<T, DP>(o + (int64_t)(t.other0 + wave * 32) * ldo + h * a.dim, ldo, lq - wave * 32, a.dim, lane, of);
     const float my_lse = j < lq ? lse_in_log2(lse[(int64_t)h * Tq + t.other0 + j]) : INFINITY;
     if (BIAS) {
-        make_bias(table, bias, bucket_of, a, h);
+        // Behind the last query P is 0 times whatever the bias makes of it, so that has to be finite: positions that no pair of this sequence has are 0.  Of those that a pair has an
+        // infinity or NaN is in that query's log-sum, and so in the gradients of all its keys, which are all of the sequence's.
+        make_bias(table, bias, bucket_of, a, h, 1 - t.first - lq, lk - 1 - t.first);
         if (by_position)
             for (int i = tid; i < 2 * NW * room; i += NW * 64) sums[i] = 0.f;
     }
