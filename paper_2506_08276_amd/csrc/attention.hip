@@ -156,7 +156,15 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : 1) void at
 #pragma unroll
                 for (int r = 0; r < 16; ++r) o[dt][r] *= alpha;
         }
-        const float base = m == -INFINITY ? 0.f : -m * scale2;
+        float base = m == -INFINITY ? 0.f : -m * scale2;
+        const bool large = __builtin_fabsf(base) > 0x1p24f;
+        if (__ballot(large)) {  // base is off by more than a half: weights under it would leave fp16's range, then fp32's.  The maximum is taken from the scores first.
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[kt][r] -= large ? m : 0.f;
+            base = large ? 0.f : base;
+        }
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
