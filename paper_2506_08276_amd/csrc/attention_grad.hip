@@ -57,9 +57,11 @@ __device__ inline void stay_in_range(f32x16 (&ds)[NV], f32x16 (&sums)[ND], float
         for (int r = 0; r < 16; ++r) ds[i][r] *= factor;
 }
 
-__device__ inline float lse_in_log2(float lse)  // of rows that see nothing: P is 0
+// P is 0 for rows that see nothing, and for those whose log-sum is so large that a step of it is 1 or more: it cannot hold the logarithm of a number of keys, and under a row of
+// biases of -1e9, say, P would be 2^-64 to 2^64 by its rounding alone.
+__device__ inline float lse_in_log2(float lse)
 {
-    return lse == -INFINITY ? INFINITY : lse * LOG2E;
+    return __builtin_fabsf(lse) >= 0x1p23f ? INFINITY : lse * LOG2E;
 }
 
 // Sums of dS along its diagonals, by relative position, without leaving the registers: a register is one row of the tile, a lane one column of it.  Row n + 16 c (and 4 more in the
