@@ -323,6 +323,19 @@ int make_plan(leann_ctx *ctx, const int32_t *q_rows, const int32_t *k_rows, cons
     }
     // 32 queries per block where no sequence has more: the other wavefronts would only load.  128 where they share the keys' tiles.
     p->query_waves = longest <= 32 ? 1 : 4;
+    // Too many blocks are refused before there are tables of them: 2^30 queries of 1024 heads would have 69 GB.  The tables themselves may have a few more, see `order`.
+    constexpr int64_t MOST_BLOCKS = (1 << 24) - 1;  // of 256 threads, of which a launch has fewer than 2^32
+    auto refused = [&](int64_t blocks) {
+        if (blocks <= MOST_BLOCKS) return LEANN_OK;
+        leann_set_error("leann_attention_create: sequences of this number and length are not covered (more than 2^24 - 1 workgroups of 256 in a launch)");
+        return LEANN_ESHAPE;
+    };
+    int64_t query_blocks = 0, key_blocks = 0;
+    for (int s = 0; s < n; ++s) {
+        query_blocks += ((int64_t)q_rows[s] + 127) / 128;
+        key_blocks += ((int64_t)k_rows[s] + 127) / 128;
+    }
+    LEANN_TRY(refused(std::max(query_blocks * p->heads, key_blocks * p->kv_heads)));
     std::vector<AttentionTile> tiles;
     std::vector<int32_t> of;
     std::vector<AttentionJoin> joins;
@@ -347,7 +360,7 @@ int make_plan(leann_ctx *ctx, const int32_t *q_rows, const int32_t *k_rows, cons
         if (bytes) memcpy(image.data() + at, v.data(), bytes);
         return at;
     };
-    size_t most_blocks = joins.size();  // of 256 threads, of which a launch has fewer than 2^32
+    size_t most_blocks = joins.size();
     auto order = [&](const std::vector<AttentionTile> &t, const std::vector<int32_t> &t_of, int heads, int s, int threads, int32_t *count) {
         const std::vector<AttentionItem> items = att_order(t, t_of, heads, s);
         *count = (int32_t)items.size();
@@ -419,10 +432,7 @@ int make_plan(leann_ctx *ctx, const int32_t *q_rows, const int32_t *k_rows, cons
         whole_at[c][0] = put(whole);
         whole_at[c][1] = order(whole, whole_of, p->heads, 1, c ? 512 : 256, &p->whole[c].n_items);
     }
-    if (most_blocks > ((size_t)1 << 24) - 1) {
-        leann_set_error("leann_attention_create: sequences of this number and length are not covered (more than 2^24 - 1 workgroups of 256 in a launch)");
-        return LEANN_ESHAPE;
-    }
+    LEANN_TRY(refused((int64_t)most_blocks));
     const size_t buckets_at = put(buckets);
     LEANN_TRY(ctx->reserve(p->mem, std::max<size_t>(image.size(), 1)));
     if (!image.empty()) LEANN_HIP(hipMemcpyAsync(p->mem.p, image.data(), image.size(), hipMemcpyHostToDevice, ctx->stream));
