@@ -57,6 +57,9 @@ __device__ inline void stay_in_range(f32x16 (&ds)[NV], f32x16 (&sums)[ND], float
         for (int r = 0; r < 16; ++r) ds[i][r] *= factor;
 }
 
+// dS of a sequence's only key is 0, not what the roundings of dO V^T and delta leave of it: a factor of its sums, so that infinities and NaN stay.
+__device__ inline float unless_only(int keys) { return keys == 1 ? 0.f : 1.f; }
+
 // P is 0 for rows that see nothing, and for those whose log-sum is so large that a step of it is 1 or more: it cannot hold the logarithm of a number of keys, and under a row of
 // biases of -1e9, say, P would be 2^-64 to 2^64 by its rounding alone.
 __device__ inline float lse_in_log2(float lse)
@@ -334,11 +337,12 @@ __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void query_grad
             for_nonfinite_rows<T>(kb, ldk, j0, keys, a.dim, lane, [&](int at, const T *) { hurt |= at <= p + a.right && (at >= p - a.left || at < a.sinks); });
     }
     if (hurt) factor = __builtin_nanf("");
-    store_columns<T, ND>(acc, a.scale / factor * (F16 ? 0x1p-15f : 1.f), dq + my_row * lddq + h * a.dim, valid, a.dim, lane);
+    const float some = unless_only(t.others) * (F16 ? 0x1p-15f : 1.f);
+    store_columns<T, ND>(acc, a.scale / factor * some, dq + my_row * lddq + h * a.dim, valid, a.dim, lane);
 
     if (BIAS && by_position) {
         if (t.begin == t.end) block_barrier();  // the sums are cleared
-        sums_by_position<GRAD_WAVES>(sums, room, a.distance, behind, ahead, reinterpret_cast<float *>(smem), F16 ? 0x1p-15f : 1.f,
+        sums_by_position<GRAD_WAVES>(sums, room, a.distance, behind, ahead, reinterpret_cast<float *>(smem), some,
                                      by_position + ((int64_t)item.tile * a.heads + h) * (2 * a.distance + 1));
     }
 }
@@ -536,7 +540,7 @@ __global__ __launch_bounds__(GRAD_WAVES * 64, DP == 128 ? 1 : 2) void key_grad_k
         }
     }
     if (hurt) factor = __builtin_nanf("");
-    float dk_factor = a.scale / factor * (F16 ? 0x1p-15f : 1.f), dv_factor = F16 ? 0x1p-15f : 1.f;
+    float dk_factor = a.scale * (jw == 0 ? unless_only(my_rows) : 1.f) / factor * (F16 ? 0x1p-15f : 1.f), dv_factor = F16 ? 0x1p-15f : 1.f;
     if constexpr (KW == 2) {  // the second wavefront's sums, made alike, go to the first one's
         f32x4 *meet = reinterpret_cast<f32x4 *>(smem) + (wave % KW) * (2 * ND * 4 * 64) + lane;
         __syncthreads();
@@ -750,13 +754,14 @@ __global__ __launch_bounds__(NW * 64, 2) void whole_grad_kernel(const AttentionI
     arrived(vf);
     V8 kf[NS];
     f32x4 dq_acc[MINE];
+    const float some = unless_only(lk), ds_scale = a.scale * some;
     auto store_dq = [&](int step) {
 #pragma unroll
         for (int m = 0; m < MINE; ++m) {
             const int tile = wave + m * NW, d = tile % (DP / 16) * 16 + 4 * g16, row = step * 32 + tile / (DP / 16) * 16 + l16;
             if (tile < TILES && row < lq && d < a.dim) {
                 typedef T V4 __attribute__((ext_vector_type(4)));
-                const f32x4 x = dq_acc[m] * a.scale;
+                const f32x4 x = dq_acc[m] * ds_scale;
                 *reinterpret_cast<V4 *>(dq + (int64_t)(t.other0 + row) * lddq + h * a.dim + d) = __builtin_convertvector(x, V4);
             }
         }
@@ -852,11 +857,11 @@ __global__ __launch_bounds__(NW * 64, 2) void whole_grad_kernel(const AttentionI
     }
     if (steps) store_dq(steps - 1);
     const int64_t my_row = t.row0 + j;
-    store_columns<T, ND>(dk_acc, a.scale, dk + my_row * lddk + h * a.dim, valid, a.dim, lane);
+    store_columns<T, ND>(dk_acc, ds_scale, dk + my_row * lddk + h * a.dim, valid, a.dim, lane);
     store_columns<T, ND>(dv_acc, 1.f, dv + my_row * lddv + h * a.dim, valid, a.dim, lane);
 
     if (BIAS && by_position)
-        sums_by_position<NW>(sums, room, a.distance, 0.f, 0.f, reinterpret_cast<float *>(Ds), 1.f, by_position + ((int64_t)item.tile * a.heads + h) * (2 * a.distance + 1));
+        sums_by_position<NW>(sums, room, a.distance, 0.f, 0.f, reinterpret_cast<float *>(Ds), some, by_position + ((int64_t)item.tile * a.heads + h) * (2 * a.distance + 1));
 }
 
 // Sums of the bias's gradient by relative position over `each` tiles, in their order: 16, and of more than 1024 tiles half of their number's root, so that the next kernel
