@@ -469,7 +469,7 @@ int leann_attention(leann_ctx *ctx, const leann_attention_plan *plan, const void
  * over the heads that share a key head), dbias fp32[buckets][heads] (NULL: not wanted).  Written, not added to; dq, dk and dv may be slices of one matrix, and must not overlap
  * each other or an input (LEANN_EINVAL).  No atomics in memory: the bits repeat; a sequence's dq, dk and dv may differ in bits with the other sequences' lengths, not with what they hold.
  * A query or key that is infinite or NaN makes NaN of the gradients of the keys or queries that it meets and of no others.
- * exp(s - lse) is off by up to 2^-22 |lse| of itself; from |lse| = 2^23 on, as of a row that biases of -1e9 or fp32's lowest hide altogether, a row counts as one that sees nothing.
+ * exp(s - lse) is off by up to 2^-22 |lse| of itself; from |lse| = 2^21 on, as of a row that biases of -1e9 or fp32's lowest hide altogether, a row counts as one that sees nothing.
  * Workspace: 8 bytes per query and head; with dbias 4 (2 distance + 1) more per head and 128 queries (of every sequence), distance no more than the sequences' longest;
  * where keys have their queries split (a few that all of a long sequence see), 256 * 32, 64 or 128 floats per part and key head. */
 int leann_attention_backward(leann_ctx *ctx, const leann_attention_plan *plan, const void *dout_dev, int64_t ldd, const void *q_dev, int64_t ldq, const void *k_dev, int64_t ldk,

@@ -60,11 +60,11 @@ __device__ inline void stay_in_range(f32x16 (&ds)[NV], f32x16 (&sums)[ND], float
 // dS of a sequence's only key is 0, not what the roundings of dO V^T and delta leave of it: a factor of its sums, so that infinities and NaN stay.
 __device__ inline float unless_only(int keys) { return keys == 1 ? 0.f : 1.f; }
 
-// P is 0 for rows that see nothing, and for those whose log-sum is so large that a step of it is 1 or more: it cannot hold the logarithm of a number of keys, and under a row of
-// biases of -1e9, say, P would be 2^-64 to 2^64 by its rounding alone.
+// P is 0 for rows that see nothing, and for those whose log-sum is so large that P is its rounding's: three of 2^-24 of it, of which each makes 0.18 of the exponent at 2^21, where
+// 2^15 P still is within fp16's range; under a row of biases of -1e9 P would be 2^-64 to 2^64.
 __device__ inline float lse_in_log2(float lse)
 {
-    return __builtin_fabsf(lse) >= 0x1p23f ? INFINITY : lse * LOG2E;
+    return __builtin_fabsf(lse) >= 0x1p21f ? INFINITY : lse * LOG2E;
 }
 
 // Sums of dS along its diagonals, by relative position, without leaving the registers: a register is one row of the tile, a lane one column of it.  Row n + 16 c (and 4 more in the

@@ -1,4 +1,4 @@
-"""The gradient of rows that large finite biases hide altogether, as 1e9 and fp32's lowest value: their log-sum cannot hold the number of keys, and they have none."""
+"""The gradient of rows of large log-sums, as biases of -1e9 and fp32's lowest value make them that hide a row altogether: exp(s - lse) is all rounding there, and they have none."""
 import pytest
 
 from gpu_util import say
@@ -35,3 +35,34 @@ def test_some_rows(ctx, dim, heads, dtype, value):  # noqa: F811
         for a, b in zip(*got):
             assert bool(torch.isfinite(a).all()) and torch.equal(a, b)
         assert not any(t[90:130].any() for t in got[0][:3]) and all(t[:90].any() for t in got[0][:3])
+
+
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("dim", [32, 64, 128])
+def test_up_to_the_border(ctx, dim, dtype, sign):  # noqa: F811
+    """Scores of queries and keys alone: below 2^21 weights are off by less than a half and within fp16's range, from there on there are none."""
+    import torch
+    say("attention backward, large log-sums", dim, dtype, sign)
+    g = torch.Generator("cuda:0").manual_seed(1)
+    for log in [14, 17] + [20 + i / 8 for i in range(25)]:
+        with Case(ctx, [3, 90, 300], heads=2, dim=dim, dtype=dtype) as c:
+            c.q[:], c.k[:] = 0, 0
+            # the sequence's best key has steps of 128 (or 256, the other way round), its score is 2^log in magnitude, up to the rounding of q
+            c.q[:, ::dim] = 2.0 ** (log - 14) / c.scale / (1 if sign < 0 else 2)
+            steps = torch.randint(129, 255, (393, 2), generator=g, device="cuda:0")
+            for at in (0, 3, 93):
+                steps[at] = 128 if sign < 0 else 256
+            c.k[:, ::dim] = (sign * steps * 128).to(c.k.dtype)
+            out, lse = c.run()
+            top = lse.abs().max()
+            assert float(lse.abs().min()) == float(top) and abs(float(top.log2()) - log) < 2.0 ** -7
+            if float(top) < 2.0 ** 21:
+                got = backward(c, out, lse)
+                want = c.sequences().backward(c.dout, out, lse, c.step)
+                for at in (0, 3, 93):  # the best key's weights
+                    size = want[2][0][at].abs()
+                    assert bool(((got[2][at].double() - want[2][0][at]).abs() <= (0.5 + 2 * c.step) * size + 1e-6).all())
+                assert all(bool(torch.isfinite(x).all()) for x in got[:3])
+            else:
+                assert not any(x.any() for x in backward(c, out, lse)[:3])
