@@ -7,8 +7,8 @@
 namespace {
 
 // A checkpoint: of each row's 128 columns, a = max |x|, scale = a / 127, code = 127 x / a to the nearest whole number, ties to even; it stands for code * scale, off by at most
-// half a scale.  16 lanes have 128 columns, eight elements each, and find a by register moves.  An infinity or NaN makes the scale infinite or NaN and the codes 0: all 128 come
-// back as NaN.
+// half a scale.  16 lanes have 128 columns, eight elements each, and find a by register moves.  An infinity makes the scale infinite and all codes 0, a NaN makes the scale NaN,
+// whatever the codes: all 128 come back as NaN.
 // All kernels here are one pass, bound by memory; a thread has UNITS accesses on their way.  131072 x 768 bf16: kept in 55 us, back in 46 (5.6 TB/s); x 1536: GELU with its input kept
 // 222 us (4.6 TB/s, as much as a copy), the gradient with the output once more 303 (4.6).
 constexpr int BLOCK = 128;
@@ -63,7 +63,7 @@ __device__ inline uint32_t max16(uint32_t v)  // over the 16 lanes of a row of l
 }
 
 // Phi(x), or its tanh form, and where GRAD is the derivative of x Phi(x).  Phi by 7.1.26 of Abramowitz and Stegun (Handbook of Mathematical Functions), whose erfc is off by at most
-// 1.5e-7 and whose exponential is the derivative's, too; the other by (1 + tanh u) / 2 = 1 / (1 + e^(-2u)).
+// 1.5e-7 and whose exponential is the derivative's, too: of Phi itself 0.16 % at -5, 0.4 % (a half step of bf16) at -6, 3 % at -12; the other by (1 + tanh u) / 2 = 1 / (1 + e^(-2u)).
 template <int KIND, bool GRAD>
 __device__ inline float distribution(float x, float &slope)
 {

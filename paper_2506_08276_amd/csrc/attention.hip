@@ -17,9 +17,9 @@ namespace {
 // other operand of O^T = V^T P^T without leaving its registers, see Columns.
 // K and V tiles go from memory to LDS without registers, one tile ahead (two ahead, with a third stage, took the same time).
 // What bounds it: over few queries memory (12 heads of 64, single queries over 8 sequences of 500 to 16384 keys: 39 us, 222 MB, 5.6 TB/s).  Else a block's loads and stores, and its
-// steps, overlap in part only with three wavefronts per SIMD: 256 sequences of up to 512 tokens 140 to 147 us, of which memory needs 80 and the steps some 95; vector units 56 %,
+// steps, overlap in part only with three wavefronts per SIMD: 256 sequences of up to 512 tokens 146 to 151 us, of which memory needs 80 and the steps some 95; vector units 56 %,
 // matrix cores 25 % busy (ten vector instructions per score and lane; a sixth of them less gave 0.8 %; four wavefronts per SIMD spill registers, 200 us and more).
-// Three documents of 3001 to 4096 tokens with a window of 256: 38 us, 960 blocks in two rounds; of 64 queries, with two wavefronts at each 32 and their sums joined in
+// Three documents of 3001 to 4096 tokens with a window of 256: 38 to 39 us, 960 blocks in two rounds; of 64 queries, with two wavefronts at each 32 and their sums joined in
 // LDS, 37 to 40, and 40 sequences of 256 tokens 26 instead of 23.
 template <int DP, int NW>
 struct AttendCfg {

@@ -619,8 +619,8 @@ __global__ __launch_bounds__(256) void key_join_kernel(const AttentionJoin *__re
 // the two kernels above read all but O twice, which bounds them there.  A wavefront has 32 keys in registers, K in LDS as well; the queries go by, 32 at a time: S = Q K^T and
 // dP = dO V^T with a key per lane, P and dS from registers into dV^T and dK^T as in key_grad_kernel; dS, rounded, through LDS into dQ^T = K^T dS^T, of which each
 // wavefront has tiles of 16 x 16, all keys of them.  The stores of a step's dQ are issued behind the next step's wait, which else would be for them.
-// 512 sequences of 64 to 256 tokens, 12 heads of 64, with the bias's gradient: 73 us for those up to 128 and 416 for the others, 1.03 GB (the two kernels took 659 where this one took 553, both with
-// an earlier form of the bias's sums).  Bound by latency: wavefronts
+// 512 sequences of 64 to 256 tokens, 12 heads of 64, with the bias's gradient: 73 us for those up to 128 and 416 for the others, 1.03 GB (the two kernels take 622 for
+// all of it where this one takes 467).  Bound by latency: wavefronts
 // wait 41 % of their time, two per SIMD at 212 registers, vector units 30 %, LDS 26 % and matrix cores 14 % busy.  dQ is some 13 % of it.  One barrier per step instead of two, dQ a step
 // later, took 5 % more (registers spill), four stages of Q and dO 3 % more.
 
