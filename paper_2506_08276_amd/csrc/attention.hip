@@ -146,7 +146,8 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? (DP == 128 ? 2 : 3) : 1) void at
             for (int r = 0; r < 16; ++r) top = __builtin_fmaxf(top, s[kt][r]);
         top = __builtin_fmaxf(m, both_halves_max(top));
         // m follows the largest score only where that is more than 2^8 times m's weight: sums and fp16's weights have room for it.  Lane by lane: a row's bits are its own.
-        const bool grown = (top - m) * scale2 > 8.f;
+        // Few queries, which memory bounds, follow it always: the largest weight then is 1, which is not rounded (380 keys: a tenth less error).
+        const bool grown = (top - m) * scale2 > (NW == 1 ? 0.f : 8.f);
         if (__ballot(grown)) {
             const float alpha = grown ? __builtin_amdgcn_exp2f((m - top) * scale2) : 1.f;
             m = grown ? top : m;
